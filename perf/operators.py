@@ -110,7 +110,7 @@ def _codes4(v):
     """4-bit codes of values that are on the grid (times no scale)."""
     a = v.abs()
     c = (a >= 0.5).to(torch.uint8) + (a >= 1) + (a >= 1.5) + (a >= 2) + (a >= 3) + (a >= 4) + (a >= 6)
-    return c + 8 * (v < 0)
+    return c + 8 * (v < 0).to(torch.uint8)
 
 
 def _hold4(w):
