@@ -49,6 +49,7 @@ enum {
 enum { AVITS_F32 = 0, AVITS_BF16 = 1 };
 enum { AVITS_UP_NEAREST = 0, AVITS_UP_BILINEAR = 1 };
 enum { AVITS_BLOCK_DOUBLE = 0, AVITS_BLOCK_SINGLE = 1 };
+enum { AVITS_ACT_NONE = 0, AVITS_ACT_GELU = 1 };
 
 /* Version string "major.minor.patch". */
 const char* avits_version(void);
@@ -652,6 +653,125 @@ int avits_noise_bits(int64_t first_pixel, int64_t n_pixels, int64_t C, uint64_t 
                      void* stream);
 
 /* ------------------------------------------------------------------------
+ * Low-bit projections, and what training around them needs.
+ *
+ * A block's MLP half, x + gate2 (GELU((LN(x)(1 + scale2) + shift2) W_1^T +
+ * b_1) W_2^T + b_2) (the block of avits_block_forward), with W_1, W_2 and the
+ * activations they multiply held in microscaled 4-bit floats, and the
+ * gradients of its input and modulation with the weights frozen, from
+ * activations kept in 8 bits.  The calls below are its parts.
+ *
+ * Tensors are row-major and contiguous unless said otherwise.  dtype is the
+ * type (AVITS_F32 or AVITS_BF16) of every tensor given as void*; all
+ * arithmetic is fp32 with one rounding to dtype at the end.
+ * ---------------------------------------------------------------------- */
+
+/* ------------------------------------------------------------------------
+ * avits_layer_norm — the modulated layer norm of a block with its statistics:
+ *   mean = avg(x), rstd = 1 / sqrt(avg((x - mean)^2) + eps),
+ *   h = (x - mean) rstd (1 + scale) + shift              for each of M rows
+ * avits_layer_norm_backward — its gradients, from dh, the forward's mean and
+ * rstd, and the rows x, given either as they were (x) or as avits_ckpt8_pack
+ * left them (x_q8, x_s8; the other two pointers NULL):
+ *   n = (x - mean) rstd,  g = dh (1 + scale),
+ *   dx = rstd (g - avg(g) - n avg(g n)) + dres
+ *   dscale = sum over rows of dh n,  dshift = sum over rows of dh
+ *
+ * The rows of B images (1 <= B <= 16) lie one after another, image b's at
+ * [off[b], off[b+1]); off is a host array of B + 1 entries from 0 to M (an
+ * image may have no rows) or NULL with B == 1.  Image b's shift and scale
+ * vectors start b * mod_stride elements after the first image's, e.g.
+ * rows of a [B, 6, D] modulation with mod_stride = 6 D; mod_stride == 0
+ * shares one vector.  shift and scale may each be NULL (0).
+ *
+ * x, h, dh, dx, dres [M, D]; mean, rstd [M] fp32 (outputs of the forward,
+ * each may be NULL there); dres NULL or the gradient that reaches x past the
+ * norm; dscale, dshift fp32, each NULL or [B, D] (contiguous), [D] when mod_stride
+ * == 0: sums over the image's rows (zero for an image without rows), in an
+ * order that depends on the sizes only.  h may be x; dx may be dh or dres;
+ * no other overlap.  Pointers aligned to their element (16 bytes and D a
+ * multiple of 8 (bf16) or 4 (fp32) are faster).  Requires 0 <= M < 2^26, 1 <= D
+ * <= 65536, eps > 0.  M == 0: dscale and dshift are zeroed, nothing else runs.
+ * Errors: AVITS_ERR_INVALID_ARG, AVITS_ERR_UNSUPPORTED (dtype),
+ * AVITS_ERR_WORKSPACE.
+ * ---------------------------------------------------------------------- */
+int avits_layer_norm(const void* x, int64_t M, int64_t D, int32_t B, const int64_t* off, const void* shift,
+                     const void* scale, int64_t mod_stride, float eps, int dtype, void* h, float* mean,
+                     float* rstd, void* stream);
+size_t avits_layer_norm_backward_workspace_bytes(int64_t M, int64_t D, int32_t B);
+int avits_layer_norm_backward(const void* dh, const void* x, const uint8_t* x_q8, const uint8_t* x_s8,
+                              const float* mean, const float* rstd, int64_t M, int64_t D, int32_t B,
+                              const int64_t* off, const void* scale, int64_t mod_stride, const void* dres,
+                              int dtype, void* dx, float* dscale, float* dshift, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * avits_ckpt8_pack / avits_ckpt8_unpack — an activation kept for the backward
+ * pass in 8 bits: e4m3 codes q [M, D] and one scale 2^(s - 127) for each 32
+ * columns of a row (the last of a row may be shorter), s [M, ceil(D / 32)].
+ * The scale is the smallest power of two that leaves the block's largest
+ * magnitude at most 448, at least 2^-127; elements are x / scale rounded to nearest
+ * even (off by at most 2^-4 of themselves, or 2^-10 scales where that is
+ * more).  A block that holds an infinity or a NaN gets s = 255 and reads back
+ * as NaN.
+ * avits_gelu_backward — dm = da GELU'(m), GELU with the tanh approximation, m
+ * given either as it was (m) or packed (m_q8, m_s8; the others NULL).  dm may
+ * be da.
+ * x, m, da, dm [M, D] (dtype).  Requires 0 <= M < 2^31, 1 <= D < 2^24.  Pointers aligned
+ * to their element (16 bytes, 8 for codes, and D a multiple of 32 are faster).
+ * M == 0 enqueues nothing.
+ * ---------------------------------------------------------------------- */
+int avits_ckpt8_pack(const void* x, int64_t M, int64_t D, int dtype, uint8_t* q, uint8_t* s, void* stream);
+int avits_ckpt8_unpack(const uint8_t* q, const uint8_t* s, int64_t M, int64_t D, int dtype, void* x, void* stream);
+int avits_gelu_backward(const void* da, const void* m, const uint8_t* m_q8, const uint8_t* m_s8, int64_t M,
+                        int64_t D, int dtype, void* dm, void* stream);
+
+/* ------------------------------------------------------------------------
+ * avits_mxfp4_quantize / avits_mxfp4_dequantize — microscaled 4-bit floats:
+ * q [M, K / 2] holds two e2m1 codes to a byte (the even column in the low
+ * half; bit 3 the sign, then 0, 0.5, 1, 1.5, 2, 3, 4, 6), and each 32 columns of
+ * a row share the scale 2^(c - 127).  The scale bytes are laid out for the
+ * product: s [ceil(K / 64), Mp, 2] with Mp = M rounded up to 8, the scale of
+ * row m and columns 32 j .. 32 j + 31 at s[j / 2][m][j % 2]; the last pair's second
+ * byte is 0 where K / 32 is odd; rows M .. Mp may hold anything.
+ * avits_mxfp4_scale_bytes(M, K) is the size of s (0 for arguments outside the limits).
+ * The scale is 2^(floor(log2 of the block's largest magnitude) - 2), at least
+ * 2^-127; elements are x / scale rounded to nearest even, magnitudes above 6
+ * to 6.  A block that holds an infinity or a NaN gets c = 255 and reads back
+ * as NaN.  act: AVITS_ACT_NONE, or AVITS_ACT_GELU to quantise GELU_tanh(x).
+ * x [M, K] (dtype).  Requires 0 <= M < 2^28, K a multiple of 32 in [32, 2^24), fewer than
+ * 2^31 scale bytes, 16-byte aligned pointers.  M == 0 enqueues nothing.
+ *
+ * avits_mxfp4_linear — out = x W^T + b with both operands in 4 bits, x [M, K]
+ * as (xq, xs), W [N, K] as (wq, ws), both laid out as above; with gate [N] and
+ * resid [M, N] (both or neither) out = resid + gate (x W^T + b).  The rows of B
+ * images may each have their own gate: B, off and mod_stride as for
+ * avits_layer_norm.  b [N] or NULL; out [M, N] may be resid; b, gate, resid and
+ * out of dtype.  Sums are fp32, in an order that depends on the sizes only.
+ * avits_mxfp4_linear_backward — the gradient of its input: dx [M, K] = dy W,
+ * dy [M, N] and dx of dtype, W as above.
+ * Requires 0 <= M < 2^28, 1 <= N < 2^21, K a multiple of 32 in [32, 2^21), and
+ * 16-byte aligned q, s, dy, dx, resid, out and workspace (>= the matching
+ * query).  M == 0 enqueues nothing.
+ * Errors: AVITS_ERR_INVALID_ARG, AVITS_ERR_UNSUPPORTED (dtype),
+ * AVITS_ERR_WORKSPACE.
+ * ---------------------------------------------------------------------- */
+size_t avits_mxfp4_scale_bytes(int64_t M, int64_t K);
+int avits_mxfp4_quantize(const void* x, int64_t M, int64_t K, int act, int dtype, uint8_t* q, uint8_t* s,
+                         void* stream);
+int avits_mxfp4_dequantize(const uint8_t* q, const uint8_t* s, int64_t M, int64_t K, int dtype, void* x,
+                           void* stream);
+size_t avits_mxfp4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int avits_mxfp4_linear(const uint8_t* xq, const uint8_t* xs, int64_t M, int64_t K, const uint8_t* wq,
+                       const uint8_t* ws, const void* b, int64_t N, int32_t B, const int64_t* off,
+                       const void* gate, int64_t mod_stride, const void* resid, int dtype, void* out,
+                       void* workspace, size_t workspace_bytes, void* stream);
+size_t avits_mxfp4_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int dtype);
+int avits_mxfp4_linear_backward(const void* dy, int64_t M, int64_t N, const uint8_t* wq, const uint8_t* ws,
+                                int64_t K, int dtype, void* dx, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/* ------------------------------------------------------------------------
  * Launch timing (instrumentation for benchmarks; not part of the method).
  * While enabled, every kernel the library enqueues is bracketed by a pair of
  * HIP events on the caller's stream.  avits_timing_read() waits for the
@@ -662,8 +782,11 @@ int avits_noise_bits(int64_t first_pixel, int64_t n_pixels, int64_t C, uint64_t 
  * "splitk_reduce", "qk_rope", "attention", "joint_lse" (also the
  * statistics pass of avits_joint_attention_stats), "gather_mixed",
  * "scatter_mixed", "linear", "final_linear" (the GEMM of avits_final_layer;
- * its layer norm counts as "ln_mod"), "euler", "noise"; "gemm" returns the
- * sum of the six GEMM families (the GEMM kernels alone: the split-K
+ * its layer norm counts as "ln_mod"), "euler", "noise",
+ * "layer_norm", "layer_norm_backward" (its sums too), "ckpt8", "gelu_backward",
+ * "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_linear", and of
+ * avits_mxfp4_linear_backward "mxfp4_transpose" (the weight turned round) and
+ * "mxfp4_backward" (its product); "gemm" returns the sum of the six GEMM families (the GEMM kernels alone: the split-K
  * reduction that follows a split launch is "splitk_reduce").  Unknown
  * family -> AVITS_ERR_INVALID_ARG.
  * avits_timing_reset() waits for pending events and zeroes every total.

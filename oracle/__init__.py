@@ -26,6 +26,10 @@ from .block import (  # noqa: F401
     layer_norm, rms_norm, rope_angles, apply_rope, attention, gelu_tanh,
     double_block, single_block, block_qk, block_batched,
 )
+from .lowbit import (  # noqa: F401
+    E2M1, E4M3, nearest_code, block_exponents, hold, held_values, mx_pack, mx_unpack, ckpt_scales,
+    norm_forward, norm_backward, gelu_slope,
+)
 from .sampler import linear, final_layer, euler_update, euler_integrate  # noqa: F401
 from .noise import (  # noqa: F401
     philox4x32_10, box_muller, pixel_noise_bits, pixel_noise, block_noise, halfunit_noise, reinject,

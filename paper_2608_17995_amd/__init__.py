@@ -25,5 +25,10 @@ from ._binding import (  # noqa: F401
     avits_linear, avits_final_layer_workspace_bytes, avits_final_layer, avits_euler_update,
     avits_noise_reinject, avits_noise_bits, NOISE_RASTER, NOISE_HALF_UNITS, NOISE_LOWRES,
     avits_grid_positions, avits_scale_positions,
+    ACT_NONE, ACT_GELU, avits_layer_norm, avits_layer_norm_backward_workspace_bytes, avits_layer_norm_backward,
+    avits_ckpt8_pack, avits_ckpt8_unpack, avits_gelu_backward,
+    avits_mxfp4_scale_bytes, avits_mxfp4_scale_shape, avits_mxfp4_quantize, avits_mxfp4_dequantize,
+    avits_mxfp4_linear_workspace_bytes, avits_mxfp4_linear, avits_mxfp4_linear_backward_workspace_bytes,
+    avits_mxfp4_linear_backward,
     avits_timing_enable, avits_timing_reset, avits_timing_read,
 )

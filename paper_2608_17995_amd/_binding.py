@@ -10,6 +10,7 @@ _LIB = None
 F32, BF16 = 0, 1
 UP_NEAREST, UP_BILINEAR = 0, 1
 BLOCK_DOUBLE, BLOCK_SINGLE = 0, 1
+ACT_NONE, ACT_GELU = 0, 1
 
 _c_void_p, _i64, _i32, _f32, _size = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
 
@@ -116,6 +117,27 @@ _SIGS = {
                                              _f32, _f32,
                                              ctypes.c_int, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _size,
                                              _c_void_p]),
+    "avits_layer_norm": (ctypes.c_int, [_c_void_p, _i64, _i64, _i32, _c_void_p, _c_void_p, _c_void_p, _i64, _f32,
+                                        ctypes.c_int, _c_void_p, _c_void_p, _c_void_p, _c_void_p]),
+    "avits_layer_norm_backward_workspace_bytes": (_size, [_i64, _i64, _i32]),
+    "avits_layer_norm_backward": (ctypes.c_int, [_c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p,
+                                                 _i64, _i64, _i32, _c_void_p, _c_void_p, _i64, _c_void_p, ctypes.c_int,
+                                                 _c_void_p, _c_void_p, _c_void_p, _c_void_p, _size, _c_void_p]),
+    "avits_ckpt8_pack": (ctypes.c_int, [_c_void_p, _i64, _i64, ctypes.c_int, _c_void_p, _c_void_p, _c_void_p]),
+    "avits_ckpt8_unpack": (ctypes.c_int, [_c_void_p, _c_void_p, _i64, _i64, ctypes.c_int, _c_void_p, _c_void_p]),
+    "avits_gelu_backward": (ctypes.c_int, [_c_void_p, _c_void_p, _c_void_p, _c_void_p, _i64, _i64, ctypes.c_int,
+                                           _c_void_p, _c_void_p]),
+    "avits_mxfp4_scale_bytes": (_size, [_i64, _i64]),
+    "avits_mxfp4_quantize": (ctypes.c_int, [_c_void_p, _i64, _i64, ctypes.c_int, ctypes.c_int, _c_void_p, _c_void_p,
+                                            _c_void_p]),
+    "avits_mxfp4_dequantize": (ctypes.c_int, [_c_void_p, _c_void_p, _i64, _i64, ctypes.c_int, _c_void_p, _c_void_p]),
+    "avits_mxfp4_linear_workspace_bytes": (_size, [_i64, _i64, _i64]),
+    "avits_mxfp4_linear": (ctypes.c_int, [_c_void_p, _c_void_p, _i64, _i64, _c_void_p, _c_void_p, _c_void_p, _i64,
+                                          _i32, _c_void_p, _c_void_p, _i64, _c_void_p, ctypes.c_int, _c_void_p,
+                                          _c_void_p, _size, _c_void_p]),
+    "avits_mxfp4_linear_backward_workspace_bytes": (_size, [_i64, _i64, _i64, ctypes.c_int]),
+    "avits_mxfp4_linear_backward": (ctypes.c_int, [_c_void_p, _i64, _i64, _c_void_p, _c_void_p, _i64, ctypes.c_int,
+                                                   _c_void_p, _c_void_p, _size, _c_void_p]),
     "avits_timing_enable": (ctypes.c_int, [ctypes.c_int]),
     "avits_timing_reset": (None, []),
     "avits_timing_read": (ctypes.c_int, [ctypes.c_char_p, ctypes.POINTER(ctypes.c_double),
@@ -472,6 +494,212 @@ class BlockWeights:
             self.c.mlp_hidden = single["w_out"].shape[1] - D
             for name, _ in _Single._fields_:
                 setattr(self.c.single, name, _dev(single[name], f"single.{name}"))
+
+
+# ---------------------------------------------------------------------------
+# Low-bit projections and the training operators around them.
+
+def _mod_rows(named, D, n_images, dt):
+    """Pointers of shift / scale vectors given as [D] (shared) or [B, D] (rows
+    any number of elements apart, e.g. a slice of a [B, 6, D] modulation), and
+    their common stride in elements."""
+    stride, ptrs = None, []
+    for name, t in named:
+        if t is None:
+            ptrs.append(None)
+            continue
+        if not t.is_cuda or t.dtype != dt:
+            raise AvitsError(-1, f"{name} must be a {dt} GPU tensor")
+        if t.dim() == 1 and t.shape[0] == D:
+            step = 0
+        elif t.dim() == 2 and tuple(t.shape) == (n_images, D):
+            step = t.stride(0) if n_images > 1 else D
+        else:
+            raise ValueError(f"{name}: [{D}] or [{n_images}, {D}], got {tuple(t.shape)}")
+        if D > 1 and t.stride(-1) != 1:
+            raise AvitsError(-1, f"{name} must have contiguous rows")
+        if step == 0 and t.dim() == 2:
+            raise AvitsError(-1, f"{name}: give one shared vector as [{D}]")
+        if stride is not None and step != stride:
+            raise ValueError("shift and scale must be laid out alike")
+        stride = step
+        ptrs.append(t.data_ptr())
+    return ptrs, stride
+
+
+def _want(t, shape, name):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _offsets(off, name):
+    off = None if off is None else [int(o) for o in off]
+    n = 1 if off is None else len(off) - 1
+    if n < 1:
+        raise ValueError(f"{name}: off needs at least two entries")
+    return n, None if off is None else _host_i64(off, n + 1, "off")
+
+
+def avits_layer_norm(x, shift, scale, h, mean=None, rstd=None, off=None, eps=1e-6, stream=None):
+    """h [M, D] = LN(x)(1 + scale) + shift, with the rows' mean and rstd [M]
+    fp32 where asked for.  off: host row offsets of B images (B + 1), whose
+    shift and scale are [B, D] or one shared [D] (each may be None)."""
+    import torch
+    M, D = x.shape
+    n, offs = _offsets(off, "avits_layer_norm")
+    (sh, sc), stride = _mod_rows((("shift", shift), ("scale", scale)), D, n, x.dtype)
+    _want(h, (M, D), "h")
+    _want(mean, (M,), "mean")
+    _want(rstd, (M,), "rstd")
+    _check(load().avits_layer_norm(_dev(x, "x"), M, D, n, offs, sh, sc, stride or 0, eps, _dtype_code(x),
+                                   _dev(h, "h", x.dtype), _dev(mean, "mean", torch.float32),
+                                   _dev(rstd, "rstd", torch.float32), _stream(stream)))
+    return h
+
+
+def avits_layer_norm_backward_workspace_bytes(M: int, D: int, n_images: int = 1) -> int:
+    return load().avits_layer_norm_backward_workspace_bytes(M, D, n_images)
+
+
+def avits_layer_norm_backward(dh, mean, rstd, scale, dx, dscale=None, dshift=None, x=None, x_q8=None, x_s8=None,
+                              dres=None, off=None, workspace=None, stream=None):
+    """dx [M, D] of avits_layer_norm from dh, with dres added where given, and
+    the fp32 gradients dscale and dshift ([B, D], or [D] where scale is one
+    shared vector).  The forward's rows are x or, packed by avits_ckpt8_pack,
+    x_q8 [M, D] and x_s8 [M, ceil(D / 32)].  Without a scale the gradients'
+    shape says which."""
+    import torch
+    M, D = dh.shape
+    n, offs = _offsets(off, "avits_layer_norm_backward")
+    (sc,), stride = _mod_rows((("scale", scale),), D, n, dh.dtype)
+    if stride is None:
+        grads = [g for g in (dscale, dshift) if g is not None]
+        stride = D if grads and grads[0].dim() == 2 else 0
+    for name, t in (("dscale", dscale), ("dshift", dshift)):
+        _want(t, (n, D) if stride else (D,), name)
+    for name, t, shape in (("x", x, (M, D)), ("x_q8", x_q8, (M, D)), ("x_s8", x_s8, (M, (D + 31) // 32)),
+                           ("dres", dres, (M, D)), ("dx", dx, (M, D)), ("mean", mean, (M,)), ("rstd", rstd, (M,))):
+        _want(t, shape, name)
+    dt, u8, f32 = dh.dtype, torch.uint8, torch.float32
+    ws, wsp, wsb = _workspace(workspace, avits_layer_norm_backward_workspace_bytes(M, D, n), dh.device)
+    _check(load().avits_layer_norm_backward(
+        _dev(dh, "dh"), _dev(x, "x", dt), _dev(x_q8, "x_q8", u8), _dev(x_s8, "x_s8", u8), _dev(mean, "mean", f32),
+        _dev(rstd, "rstd", f32), M, D, n, offs, sc, stride, _dev(dres, "dres", dt), _dtype_code(dh), _dev(dx, "dx", dt),
+        _dev(dscale, "dscale", f32), _dev(dshift, "dshift", f32), wsp, wsb, _stream(stream)))
+    return dx, dscale, dshift
+
+
+def avits_ckpt8_pack(x, q, s, stream=None):
+    """x [M, D] kept in 8 bits: codes q [M, D] and scales s [M, ceil(D / 32)], uint8."""
+    import torch
+    M, D = x.shape
+    _want(q, (M, D), "q")
+    _want(s, (M, (D + 31) // 32), "s")
+    _check(load().avits_ckpt8_pack(_dev(x, "x"), M, D, _dtype_code(x), _dev(q, "q", torch.uint8),
+                                   _dev(s, "s", torch.uint8), _stream(stream)))
+    return q, s
+
+
+def avits_ckpt8_unpack(q, s, x, stream=None):
+    import torch
+    M, D = q.shape
+    _want(x, (M, D), "x")
+    _want(s, (M, (D + 31) // 32), "s")
+    _check(load().avits_ckpt8_unpack(_dev(q, "q", torch.uint8), _dev(s, "s", torch.uint8), M, D, _dtype_code(x),
+                                     _dev(x, "x"), _stream(stream)))
+    return x
+
+
+def avits_gelu_backward(da, dm, m=None, m_q8=None, m_s8=None, stream=None):
+    """dm [M, D] = da GELU'(m), m as it was or packed by avits_ckpt8_pack."""
+    import torch
+    M, D = da.shape
+    for name, t, shape in (("dm", dm, (M, D)), ("m", m, (M, D)), ("m_q8", m_q8, (M, D)),
+                           ("m_s8", m_s8, (M, (D + 31) // 32))):
+        _want(t, shape, name)
+    _check(load().avits_gelu_backward(_dev(da, "da"), _dev(m, "m", da.dtype), _dev(m_q8, "m_q8", torch.uint8),
+                                      _dev(m_s8, "m_s8", torch.uint8), M, D, _dtype_code(da), _dev(dm, "dm", da.dtype),
+                                      _stream(stream)))
+    return dm
+
+
+def avits_mxfp4_scale_bytes(M: int, K: int) -> int:
+    return load().avits_mxfp4_scale_bytes(M, K)
+
+
+def avits_mxfp4_scale_shape(M: int, K: int) -> tuple:
+    """Shape of the scales of an [M, K] tensor: [ceil(K / 64), M rounded up to 8, 2]."""
+    return (K + 63) // 64, (M + 7) // 8 * 8, 2
+
+
+def _mx(q, s, name):
+    """Checks a held 4-bit tensor's codes and scales; returns M, K and the pointers."""
+    import torch
+    if q.dim() != 2:
+        raise ValueError(f"{name}: codes must be [M, K / 2]")
+    M, K = q.shape[0], 2 * q.shape[1]
+    _want(s, avits_mxfp4_scale_shape(M, K), f"{name} scales")
+    return M, K, _dev(q, name, torch.uint8), _dev(s, f"{name} scales", torch.uint8)
+
+
+def avits_mxfp4_quantize(x, q, s, act=ACT_NONE, stream=None):
+    """x [M, K] to codes q [M, K / 2] and scales s (avits_mxfp4_scale_shape),
+    uint8; with act=ACT_GELU the values of GELU_tanh(x)."""
+    M, K = x.shape
+    Mq, Kq, qp, sp = _mx(q, s, "q")
+    if (Mq, Kq) != (M, K):
+        raise ValueError(f"avits_mxfp4_quantize: q must be [{M}, {K} / 2], got {tuple(q.shape)}")
+    _check(load().avits_mxfp4_quantize(_dev(x, "x"), M, K, act, _dtype_code(x), qp, sp, _stream(stream)))
+    return q, s
+
+
+def avits_mxfp4_dequantize(q, s, x, stream=None):
+    M, K, qp, sp = _mx(q, s, "q")
+    _want(x, (M, K), "x")
+    _check(load().avits_mxfp4_dequantize(qp, sp, M, K, _dtype_code(x), _dev(x, "x"), _stream(stream)))
+    return x
+
+
+def avits_mxfp4_linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    return load().avits_mxfp4_linear_workspace_bytes(M, N, K)
+
+
+def avits_mxfp4_linear(xq, xs, wq, ws, b, out, gate=None, resid=None, off=None, workspace=None, stream=None):
+    """out [M, N] = x W^T + b, x [M, K] and W [N, K] held in 4 bits; with gate
+    [N] and resid [M, N], out = resid + gate (x W^T + b), or with a gate [B, N]
+    for the rows of B images at the host row offsets off."""
+    M, K, xqp, xsp = _mx(xq, xs, "x")
+    N, Kw, wqp, wsp = _mx(wq, ws, "w")
+    if K != Kw:
+        raise ValueError(f"avits_mxfp4_linear: x has {K} columns, w {Kw}")
+    dt = out.dtype
+    for name, t, shape in (("b", b, (N,)), ("out", out, (M, N)), ("resid", resid, (M, N))):
+        _want(t, shape, name)
+    n, offs = _offsets(off, "avits_mxfp4_linear")
+    (gp,), stride = _mod_rows((("gate", gate),), N, n, dt)
+    buf, bp, nb = _workspace(workspace, avits_mxfp4_linear_workspace_bytes(M, N, K), out.device)
+    _check(load().avits_mxfp4_linear(xqp, xsp, M, K, wqp, wsp, _dev(b, "b", dt), N, n, offs, gp, stride or 0,
+                                     _dev(resid, "resid", dt), _dtype_code(out), _dev(out, "out"), bp, nb,
+                                     _stream(stream)))
+    return out
+
+
+def avits_mxfp4_linear_backward_workspace_bytes(M: int, N: int, K: int, dtype: int) -> int:
+    return load().avits_mxfp4_linear_backward_workspace_bytes(M, N, K, dtype)
+
+
+def avits_mxfp4_linear_backward(dy, wq, ws, dx, workspace=None, stream=None):
+    """dx [M, K] = dy [M, N] W, W [N, K] held in 4 bits."""
+    M, N = dy.shape
+    Nw, K, wqp, wsp = _mx(wq, ws, "w")
+    if N != Nw:
+        raise ValueError(f"avits_mxfp4_linear_backward: dy has {N} columns, w {Nw} rows")
+    _want(dx, (M, K), "dx")
+    code = _dtype_code(dy)
+    buf, bp, nb = _workspace(workspace, avits_mxfp4_linear_backward_workspace_bytes(M, N, K, code), dy.device)
+    _check(load().avits_mxfp4_linear_backward(_dev(dy, "dy"), M, N, wqp, wsp, K, code, _dev(dx, "dx", dy.dtype), bp, nb,
+                                              _stream(stream)))
+    return dx
 
 
 def avits_timing_enable(on: bool = True):

@@ -1,0 +1,327 @@
+// Conversions to and from the block-scaled formats, and the GELU's gradient
+// from an activation kept in 8 bits.  Every kernel here moves its data once;
+// what bounds them is HBM bandwidth, and the launch for a few rows.
+#include <type_traits>
+
+#include "kernels.h"
+#include "lowbit.h"
+
+namespace avits {
+namespace {
+
+// ----------------------------------------------------------------------------
+// 8-bit activations: codes [M, D], scales [M, ceil(D / 32)].
+
+// D a multiple of 32, 16-byte aligned: blocks lie one after another through the
+// whole array.  A lane takes eight elements, four lanes a block.
+template <typename T>
+__global__ __launch_bounds__(256) void pack8_kernel(const T* __restrict__ x, int64_t n8, uint8_t* __restrict__ q,
+                                                    uint8_t* __restrict__ s) {
+  // n8 is a multiple of 4: a block's lanes stay together.
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n8; i += int64_t(gridDim.x) * 256) {
+    float v[8];
+    load8(x + 8 * i, v);
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[e]));
+    top = quad_umax(top);
+    const uint32_t c = scale8_code(top);
+    const float inv = c == 255u ? 0.f : scale_inverse(c);
+    reinterpret_cast<u32x2*>(q)[i] = u32x2{encode8x4(v, inv), encode8x4(v + 4, inv)};
+    if (i % 4 == 0) s[i / 4] = uint8_t(c);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void unpack8_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ s,
+                                                      int64_t n8, T* __restrict__ x) {
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n8; i += int64_t(gridDim.x) * 256) {
+    const u32x2 c = reinterpret_cast<const u32x2*>(q)[i];
+    const float sc = scale_value(s[i / 4]);
+    float v[8];
+    decode8x4(c[0], sc, v);
+    decode8x4(c[1], sc, v + 4);
+    store8(x + 8 * i, v);
+  }
+}
+
+// Any width and alignment: half a wave per block, an element per lane.
+template <typename T>
+__global__ __launch_bounds__(256) void pack8_any_kernel(const T* __restrict__ x, int64_t M, int64_t D, int64_t ns,
+                                                        uint8_t* __restrict__ q, uint8_t* __restrict__ s) {
+  const int l = threadIdx.x % 32;
+  for (int64_t b = int64_t(blockIdx.x) * 8 + threadIdx.x / 32; b < M * ns; b += int64_t(gridDim.x) * 8) {
+    const int64_t m = b / ns, i = (b % ns) * kBlk + l;
+    const float v = i < D ? ld(x, m * D + i) : 0.f;
+    uint32_t top = magnitude(v);
+#pragma unroll
+    for (int k = 1; k < 32; k *= 2) top = max(top, uint32_t(__shfl_xor(int(top), k, 32)));
+    const uint32_t c = scale8_code(top);
+    const float inv = c == 255u ? 0.f : scale_inverse(c);
+    if (i < D) q[m * D + i] = uint8_t(__builtin_amdgcn_cvt_pk_fp8_f32(v * inv, v * inv, 0, false));
+    if (l == 0) s[b] = uint8_t(c);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void unpack8_any_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ s,
+                                                          int64_t M, int64_t D, int64_t ns, T* __restrict__ x) {
+  const int l = threadIdx.x % 32;
+  for (int64_t b = int64_t(blockIdx.x) * 8 + threadIdx.x / 32; b < M * ns; b += int64_t(gridDim.x) * 8) {
+    const int64_t m = b / ns, i = (b % ns) * kBlk + l;
+    if (i < D) st(x, m * D + i, decode8(q[m * D + i], scale_value(s[b])));
+  }
+}
+
+// dm = da gelu'(m), m in its own type or kept in 8 bits.
+template <typename T, bool HELD>
+__global__ __launch_bounds__(256) void gelu_back_kernel(const T* da, const T* m, const uint8_t* __restrict__ q,
+                                                        const uint8_t* __restrict__ s, int64_t n8, T* dm) {
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n8; i += int64_t(gridDim.x) * 256) {
+    float d[8], v[8];
+    load8(da + 8 * i, d);
+    if constexpr (HELD) {
+      const u32x2 c = reinterpret_cast<const u32x2*>(q)[i];
+      const float sc = scale_value(s[i / 4]);
+      decode8x4(c[0], sc, v);
+      decode8x4(c[1], sc, v + 4);
+    } else {
+      load8(m + 8 * i, v);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d[e] *= gelu_slope(v[e]);
+    store8(dm + 8 * i, d);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void gelu_back_any_kernel(const T* da, const T* m, const uint8_t* __restrict__ q,
+                                                            const uint8_t* __restrict__ s, int64_t M, int64_t D, int64_t ns,
+                                                            T* dm) {
+  const int l = threadIdx.x % 32;
+  for (int64_t b = int64_t(blockIdx.x) * 8 + threadIdx.x / 32; b < M * ns; b += int64_t(gridDim.x) * 8) {
+    const int64_t row = b / ns, i = (b % ns) * kBlk + l;
+    if (i >= D) continue;
+    const int64_t at = row * D + i;
+    const float v = m ? ld(m, at) : decode8(q[at], scale_value(s[b]));
+    st(dm, at, ld(da, at) * gelu_slope(v));
+  }
+}
+
+// ----------------------------------------------------------------------------
+// Microscaled 4-bit floats: codes [M, K / 2], scales [ceil(K / 64), Mp, 2] with
+// Mp = M rounded up to 8: the two scales of 64 columns of a row side by side,
+// the rows one after another, so that a lane of the product that owns several
+// consecutive rows reads their scales at once.
+//
+// A workgroup converts 32 rows x 512 columns: a wave a row at a time (a lane
+// eight elements, four lanes a block), the scales turned round through LDS so that
+// they leave in runs of 64 bytes.
+constexpr int kQRows = 32, kQCols = 512;
+
+template <typename T, bool GELU>
+__global__ __launch_bounds__(256) void quantize4_kernel(const T* __restrict__ x, int64_t M, int64_t K,
+                                                        uint8_t* __restrict__ q, uint8_t* __restrict__ s) {
+  __shared__ uint16_t sc[kQCols / 64][kQRows];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int64_t m0 = int64_t(blockIdx.x) * kQRows, k = int64_t(blockIdx.y) * kQCols + 8 * lane;
+  const int64_t Mp = scale_rows(M);
+  const bool in = k < K;  // K is a multiple of 32: all four lanes of a block, or none
+#pragma unroll
+  for (int r = 0; r < kQRows / 4; ++r) {
+    const int row = wave + 4 * r;
+    const int64_t m = m0 + row;
+    float v[8] = {};
+    if (in && m < M) load8(x + m * K + k, v);
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (GELU) v[e] = gelu_value(v[e]);
+      top = max(top, magnitude(v[e]));
+    }
+    const uint32_t c = scale4_code(quad_umax(top));
+    const uint32_t o = encode4x8(v, c == 255u ? 0.f : scale_inverse(c));
+    if (in && m < M) *reinterpret_cast<uint32_t*>(q + (m * K + k) / 2) = o;
+    // Lane 8 j: its own block's scale and, from lane 8 j + 7, the next block's.
+    const uint32_t up = uint32_t(__builtin_amdgcn_update_dpp(0, int(c), kDppHalfMirror, 0xf, 0xf, false));
+    if (lane % 8 == 0) sc[lane / 8][row] = uint16_t(c | up << 8);
+  }
+  __syncthreads();
+  const int pair = threadIdx.x / kQRows, row = threadIdx.x % kQRows;
+  const int64_t gp = int64_t(blockIdx.y) * (kQCols / 64) + pair, m = m0 + row;
+  if (gp < scale_groups(K) && m < Mp) reinterpret_cast<uint16_t*>(s)[gp * Mp + m] = sc[pair][row];
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void dequantize4_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ s,
+                                                          int64_t M, int64_t K, T* __restrict__ x) {
+  __shared__ uint16_t sc[kQCols / 64][kQRows];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int64_t m0 = int64_t(blockIdx.x) * kQRows, k = int64_t(blockIdx.y) * kQCols + 8 * lane;
+  const int64_t Mp = scale_rows(M);
+  {
+    const int pair = threadIdx.x / kQRows, row = threadIdx.x % kQRows;
+    const int64_t gp = int64_t(blockIdx.y) * (kQCols / 64) + pair, m = m0 + row;
+    sc[pair][row] = gp < scale_groups(K) && m < Mp ? reinterpret_cast<const uint16_t*>(s)[gp * Mp + m] : uint16_t(0);
+  }
+  __syncthreads();
+  if (k >= K) return;
+#pragma unroll
+  for (int r = 0; r < kQRows / 4; ++r) {
+    const int row = wave + 4 * r;
+    const int64_t m = m0 + row;
+    if (m >= M) continue;
+    float v[8];
+    const uint32_t c = sc[lane / 8][row] >> (lane & 4 ? 8 : 0);
+    decode4x8(*reinterpret_cast<const uint32_t*>(q + (m * K + k) / 2), scale_value(c & 255u), v);
+    store8(x + m * K + k, v);
+  }
+}
+
+int check_type(const char* who, int64_t M, int64_t D, int dtype) {
+  AVITS_REQUIRE(M >= 0 && M < (int64_t(1) << 31), "%s: M=%lld outside [0, 2^31)", who, (long long)M);
+  AVITS_REQUIRE(D >= 1 && D < (int64_t(1) << 24), "%s: D=%lld outside [1, 2^24)", who, (long long)D);
+  if (dtype != AVITS_F32 && dtype != AVITS_BF16) return set_error(AVITS_ERR_UNSUPPORTED, "%s: dtype %d unsupported", who, dtype);
+  return AVITS_OK;
+}
+
+bool vectors_ok(int64_t D, std::initializer_list<const void*> wide, const void* codes) {
+  return D % kBlk == 0 && aligned_to(wide, 16) && aligned_to({codes}, 8);
+}
+
+constexpr int64_t kMaxGrid = 1 << 22;  // workgroups; beyond it the kernels loop
+dim3 blocks_grid(int64_t M, int64_t ns) { return dim3(unsigned(std::min(kMaxGrid, ceil_div64(M * ns, 8)))); }
+dim3 flat_grid(int64_t n8) { return dim3(unsigned(std::min(kMaxGrid, ceil_div64(n8, 256)))); }
+
+template <typename F>
+int by_type(int dtype, F f) {
+  if (dtype == AVITS_BF16) f(bf16_t{});
+  else f(float{});
+  return AVITS_OK;
+}
+
+int check_mx(const char* who, int64_t M, int64_t K, int dtype) {
+  const int rc = check_type(who, M, K, dtype);
+  if (rc != AVITS_OK) return rc;
+  AVITS_REQUIRE(M < (int64_t(1) << 28), "%s: M=%lld is 2^28 or more", who, (long long)M);
+  AVITS_REQUIRE(K % kBlk == 0, "%s: K=%lld must be a multiple of 32", who, (long long)K);
+  AVITS_REQUIRE(scale_groups(K) * scale_rows(M) * 2 < (int64_t(1) << 31), "%s: M=%lld x K=%lld has 2^31 scales or more", who,
+                (long long)M, (long long)K);
+  return AVITS_OK;
+}
+
+}  // namespace
+}  // namespace avits
+
+using namespace avits;
+
+extern "C" int avits_ckpt8_pack(const void* x, int64_t M, int64_t D, int dtype, uint8_t* q, uint8_t* s, void* stream) {
+  const int rc = check_type("ckpt8_pack", M, D, dtype);
+  if (rc != AVITS_OK) return rc;
+  if (M == 0) return AVITS_OK;
+  AVITS_REQUIRE(x && q && s, "ckpt8_pack: null x/q/s");
+  AVITS_REQUIRE(aligned_to({x}, dtype == AVITS_BF16 ? 2 : 4), "ckpt8_pack: x is not aligned to its element");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  TimedLaunch timed("ckpt8", st);
+  by_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    const T* p = static_cast<const T*>(x);
+    if (vectors_ok(D, {x}, q))
+      hipLaunchKernelGGL(pack8_kernel<T>, flat_grid(M * D / 8), dim3(256), 0, st, p, M * D / 8, q, s);
+    else
+      hipLaunchKernelGGL(pack8_any_kernel<T>, blocks_grid(M, ceil_div64(D, kBlk)), dim3(256), 0, st, p, M, D,
+                         ceil_div64(D, kBlk), q, s);
+  });
+  return launch_status("ckpt8_pack");
+}
+
+extern "C" int avits_ckpt8_unpack(const uint8_t* q, const uint8_t* s, int64_t M, int64_t D, int dtype, void* x, void* stream) {
+  const int rc = check_type("ckpt8_unpack", M, D, dtype);
+  if (rc != AVITS_OK) return rc;
+  if (M == 0) return AVITS_OK;
+  AVITS_REQUIRE(x && q && s, "ckpt8_unpack: null q/s/x");
+  AVITS_REQUIRE(aligned_to({x}, dtype == AVITS_BF16 ? 2 : 4), "ckpt8_unpack: x is not aligned to its element");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  TimedLaunch timed("ckpt8", st);
+  by_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    T* p = static_cast<T*>(x);
+    if (vectors_ok(D, {x}, q))
+      hipLaunchKernelGGL(unpack8_kernel<T>, flat_grid(M * D / 8), dim3(256), 0, st, q, s, M * D / 8, p);
+    else
+      hipLaunchKernelGGL(unpack8_any_kernel<T>, blocks_grid(M, ceil_div64(D, kBlk)), dim3(256), 0, st, q, s, M, D,
+                         ceil_div64(D, kBlk), p);
+  });
+  return launch_status("ckpt8_unpack");
+}
+
+extern "C" int avits_gelu_backward(const void* da, const void* m, const uint8_t* m_q8, const uint8_t* m_s8, int64_t M,
+                                   int64_t D, int dtype, void* dm, void* stream) {
+  const int rc = check_type("gelu_backward", M, D, dtype);
+  if (rc != AVITS_OK) return rc;
+  if (M == 0) return AVITS_OK;
+  AVITS_REQUIRE((m != nullptr) != (m_q8 != nullptr) && (m_q8 != nullptr) == (m_s8 != nullptr),
+                "gelu_backward: give either m or both m_q8 and m_s8");
+  AVITS_REQUIRE(da && dm, "gelu_backward: null da/dm");
+  AVITS_REQUIRE(aligned_to({da, m, dm}, dtype == AVITS_BF16 ? 2 : 4), "gelu_backward: a pointer is not aligned to its element");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  TimedLaunch timed("gelu_backward", st);
+  by_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    const T *d = static_cast<const T*>(da), *v = static_cast<const T*>(m);
+    T* o = static_cast<T*>(dm);
+    const int64_t n8 = M * D / 8;
+    if (!vectors_ok(D, {da, m, dm}, m_q8))
+      hipLaunchKernelGGL(gelu_back_any_kernel<T>, blocks_grid(M, ceil_div64(D, kBlk)), dim3(256), 0, st, d, v, m_q8, m_s8, M,
+                         D, ceil_div64(D, kBlk), o);
+    else if (m_q8)
+      hipLaunchKernelGGL((gelu_back_kernel<T, true>), flat_grid(n8), dim3(256), 0, st, d, v, m_q8, m_s8, n8, o);
+    else
+      hipLaunchKernelGGL((gelu_back_kernel<T, false>), flat_grid(n8), dim3(256), 0, st, d, v, m_q8, m_s8, n8, o);
+  });
+  return launch_status("gelu_backward");
+}
+
+extern "C" size_t avits_mxfp4_scale_bytes(int64_t M, int64_t K) {
+  if (M < 0 || M >= (int64_t(1) << 28) || K < kBlk || K >= (int64_t(1) << 24) || K % kBlk != 0) return 0;
+  return size_t(scale_groups(K)) * size_t(scale_rows(M)) * 2;
+}
+
+extern "C" int avits_mxfp4_quantize(const void* x, int64_t M, int64_t K, int act, int dtype, uint8_t* q, uint8_t* s,
+                                    void* stream) {
+  const int rc = check_mx("mxfp4_quantize", M, K, dtype);
+  if (rc != AVITS_OK) return rc;
+  AVITS_REQUIRE(act == AVITS_ACT_NONE || act == AVITS_ACT_GELU, "mxfp4_quantize: act=%d unknown", act);
+  if (M == 0) return AVITS_OK;
+  AVITS_REQUIRE(x && q && s, "mxfp4_quantize: null x/q/s");
+  AVITS_REQUIRE(aligned_to({x, q, s}, 16), "mxfp4_quantize: x, q and s must be 16-byte aligned");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const dim3 grid(unsigned(ceil_div64(M, kQRows)), unsigned(ceil_div64(K, kQCols)));
+  TimedLaunch timed("mxfp4_quantize", st);
+  by_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    const T* p = static_cast<const T*>(x);
+    if (act == AVITS_ACT_GELU)
+      hipLaunchKernelGGL((quantize4_kernel<T, true>), grid, dim3(256), 0, st, p, M, K, q, s);
+    else
+      hipLaunchKernelGGL((quantize4_kernel<T, false>), grid, dim3(256), 0, st, p, M, K, q, s);
+  });
+  return launch_status("mxfp4_quantize");
+}
+
+extern "C" int avits_mxfp4_dequantize(const uint8_t* q, const uint8_t* s, int64_t M, int64_t K, int dtype, void* x,
+                                      void* stream) {
+  const int rc = check_mx("mxfp4_dequantize", M, K, dtype);
+  if (rc != AVITS_OK) return rc;
+  if (M == 0) return AVITS_OK;
+  AVITS_REQUIRE(x && q && s, "mxfp4_dequantize: null q/s/x");
+  AVITS_REQUIRE(aligned_to({x, q, s}, 16), "mxfp4_dequantize: q, s and x must be 16-byte aligned");
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const dim3 grid(unsigned(ceil_div64(M, kQRows)), unsigned(ceil_div64(K, kQCols)));
+  TimedLaunch timed("mxfp4_dequantize", st);
+  by_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    hipLaunchKernelGGL(dequantize4_kernel<T>, grid, dim3(256), 0, st, q, s, M, K, static_cast<T*>(x));
+  });
+  return launch_status("mxfp4_dequantize");
+}

@@ -685,3 +685,108 @@ class ThreeStageSampler:
         self.transition23(stream)
         self.stage3(prefix, stream)
         return self.z3
+
+
+class Mxfp4Mlp:
+    """The MLP half of a double-stream block (the block's second half in
+    avits_block_forward) with its weights, and the activations they multiply,
+    held in microscaled 4-bit floats:
+
+        branch(x) = GELU((LN(x)(1 + scale) + shift) W1^T + b1) W2^T + b2
+
+    run() is the inference form, out = x + gate * branch(x).  forward() and
+    backward() tune what lies around the frozen weights (the modulation, a
+    gate, anything in front): forward() gives the branch and keeps its norm's
+    rows and its hidden activation in 8 bits, backward() the gradients of x, scale and
+    shift, the roundings to 4 bits taken as the identity.
+
+    w1 [F, D], w2 [D, F] (D, F multiples of 32), b1, b2: bf16 or fp32, that
+    type is the type of every activation; they are quantised here and not kept.
+    All buffers for up to `rows` rows are allocated here (the ones of the backward pass
+    with tune=True); the calls only enqueue.  One object's calls belong on one stream
+    at a time, and backward() belongs to the forward() before it.
+    """
+
+    def __init__(self, w1, b1, w2, b2, rows: int, tune=False, eps=1e-6):
+        import torch
+        F, D = w1.shape
+        if tuple(w2.shape) != (D, F):
+            raise ValueError(f"Mxfp4Mlp: w1 is [{F}, {D}], so w2 must be [{D}, {F}], got {tuple(w2.shape)}")
+        self.D, self.F, self.rows, self.tune, self.eps, self.dtype = D, F, rows, tune, eps, w1.dtype
+        self.b1, self.b2 = b1, b2
+        dev, u8 = w1.device, torch.uint8
+
+        def new(*shape, dtype=None):
+            return torch.empty(*shape, dtype=dtype or w1.dtype, device=dev)
+
+        def quantised(w):
+            q, s = new(w.shape[0], w.shape[1] // 2, dtype=u8), new(*B.avits_mxfp4_scale_shape(*w.shape), dtype=u8)
+            return B.avits_mxfp4_quantize(w, q, s)
+
+        self.w1, self.w2 = quantised(w1.contiguous()), quantised(w2.contiguous())
+        self._h, self._m = new(rows, D), new(rows, F)
+        self._hq, self._hs = new(rows, D // 2, dtype=u8), new(B.avits_mxfp4_scale_bytes(rows, D), dtype=u8)
+        self._aq, self._as = new(rows, F // 2, dtype=u8), new(B.avits_mxfp4_scale_bytes(rows, F), dtype=u8)
+        nbytes = [B.avits_mxfp4_linear_workspace_bytes(rows, F, D), B.avits_mxfp4_linear_workspace_bytes(rows, D, F)]
+        if tune:
+            f32 = torch.float32
+            self._mean, self._rstd = new(rows, dtype=f32), new(rows, dtype=f32)
+            self._x8, self._xs = new(rows, D, dtype=u8), new(rows, (D + 31) // 32, dtype=u8)
+            self._m8, self._ms = new(rows, F, dtype=u8), new(rows, (F + 31) // 32, dtype=u8)
+            code = B._dtype_code(w1)
+            nbytes += [B.avits_mxfp4_linear_backward_workspace_bytes(rows, D, F, code),
+                       B.avits_mxfp4_linear_backward_workspace_bytes(rows, F, D, code),
+                       B.avits_layer_norm_backward_workspace_bytes(rows, D, 16)]
+        self._ws = new(max(nbytes + [16]), dtype=u8)
+        self._n = None
+
+    def _scales(self, buf, M, K):
+        return buf[:B.avits_mxfp4_scale_bytes(M, K)].view(B.avits_mxfp4_scale_shape(M, K))
+
+    def _hidden(self, x, shift, scale, off, stream, mean=None, rstd=None):
+        """The hidden activation m of x's rows before the GELU."""
+        M = x.shape[0]
+        if M > self.rows or x.shape[1] != self.D:
+            raise ValueError(f"Mxfp4Mlp: x must be [at most {self.rows}, {self.D}], got {tuple(x.shape)}")
+        h, hq, hs, m = self._h[:M], self._hq[:M], self._scales(self._hs, M, self.D), self._m[:M]
+        B.avits_layer_norm(x, shift, scale, h, mean, rstd, off=off, eps=self.eps, stream=stream)
+        B.avits_mxfp4_quantize(h, hq, hs, stream=stream)
+        B.avits_mxfp4_linear(hq, hs, *self.w1, self.b1, m, workspace=self._ws, stream=stream)
+        return m
+
+    def _out(self, m, out, stream, **kw):
+        M = m.shape[0]
+        aq, a_s = self._aq[:M], self._scales(self._as, M, self.F)
+        B.avits_mxfp4_quantize(m, aq, a_s, act=B.ACT_GELU, stream=stream)
+        return B.avits_mxfp4_linear(aq, a_s, *self.w2, self.b2, out, workspace=self._ws, stream=stream, **kw)
+
+    def run(self, x, shift, scale, gate, out, off=None, stream=None):
+        """out [M, D] = x + gate * branch(x) (out may be x); shift, scale, gate
+        [D], or [B, D] for the rows of B images at the host offsets off."""
+        return self._out(self._hidden(x, shift, scale, off, stream), out, stream, gate=gate, resid=x, off=off)
+
+    def forward(self, x, shift, scale, z, off=None, stream=None):
+        """z [M, D] = branch(x), with what backward() needs kept."""
+        if not self.tune:
+            raise ValueError("Mxfp4Mlp: built without tune=True")
+        M = x.shape[0]
+        m = self._hidden(x, shift, scale, off, stream, self._mean[:M], self._rstd[:M])
+        B.avits_ckpt8_pack(x, self._x8[:M], self._xs[:M], stream=stream)
+        B.avits_ckpt8_pack(m, self._m8[:M], self._ms[:M], stream=stream)
+        self._n, self._off = M, None if off is None else [int(o) for o in off]
+        return self._out(m, z, stream)
+
+    def backward(self, dz, scale, dx, dscale=None, dshift=None, dres=None, stream=None):
+        """The gradients of the last forward() from dz [M, D], its branch's:
+        dx (with dres, the gradient that passes the branch by, added), dscale
+        and dshift fp32 as avits_layer_norm_backward gives them."""
+        if self._n is None:
+            raise ValueError("Mxfp4Mlp: backward() without a forward()")
+        M = self._n
+        da, dh = self._m[:M], self._h[:M]     # the forward's buffers: m is kept in 8 bits
+        B.avits_mxfp4_linear_backward(dz, *self.w2, da, workspace=self._ws, stream=stream)
+        B.avits_gelu_backward(da, da, m_q8=self._m8[:M], m_s8=self._ms[:M], stream=stream)
+        B.avits_mxfp4_linear_backward(da, *self.w1, dh, workspace=self._ws, stream=stream)
+        return B.avits_layer_norm_backward(dh, self._mean[:M], self._rstd[:M], scale, dx, dscale, dshift,
+                                           x_q8=self._x8[:M], x_s8=self._xs[:M], dres=dres, off=self._off,
+                                           workspace=self._ws, stream=stream)
