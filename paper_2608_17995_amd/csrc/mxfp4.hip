@@ -17,6 +17,7 @@
 
 #include "kernels.h"
 #include "lowbit.h"
+#include "tiles.h"
 
 namespace avits {
 namespace {
@@ -153,6 +154,363 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args a) {
   }
 }
 
+// Sixteen consecutive elements from element `at` of an array of `n` (zeros
+// past its end), whatever its alignment.
+template <typename T>
+__device__ __forceinline__ void load16(const void* base, int64_t n, int64_t at, float (&v)[16]) {
+  const __amdgpu_buffer_rsrc_t r = range_of(base, base ? n * int64_t(sizeof(T)) : 0);
+#pragma unroll
+  for (int c = 0; c < 16; ++c) {
+    if constexpr (sizeof(T) == 2)
+      v[c] = bf2f(bf16_t(__builtin_amdgcn_raw_buffer_load_b16(r, int((at + c) * 2), 0, 0)));
+    else
+      v[c] = __uint_as_float(uint32_t(__builtin_amdgcn_raw_buffer_load_b32(r, int((at + c) * 4), 0, 0)));
+  }
+}
+
+// Stores a wave's block: lane (l, g) holds rows
+// mb + TM l + i and, of each, the columns nb + 16 g .. + 15 (register r of
+// accumulator j is column 4 r + j).  Buffer accesses drop what lies outside;
+// where rows do not start on 16 bytes the columns go one by one.
+typedef const __attribute__((address_space(4))) Mx4Args* Mx4ArgsPtr;
+
+// lds_load16 to LDS byte dst + OFF + 16 lane, the sum made in m0 itself.
+template <int OFF>
+__device__ __forceinline__ void lds_load16_at(uint32_t dst, uint32_t voff, const u32x4& rsrc, uint32_t soff) {
+  asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               ::"s"(dst), "v"(voff), "s"(rsrc), "s"(soff), "n"(OFF) : "memory", "m0", "scc");
+}
+template <int TM, int TN, typename T, bool GATED, bool VEC>
+__device__ __forceinline__ void tile_epilogue(Mx4ArgsPtr a, int64_t mb, int64_t nb, int l, int g,
+                                              const f32x4 (&acc)[TM][TN], const T* bias_lds) {
+  static_assert(TN == 4, "sixteen columns per lane");
+  constexpr int Z = sizeof(T), E = 16 / Z, V = 16 / E;   // elements of a vector, vectors of a lane's columns
+  const int64_t N = a->N;
+  const int rows = int(std::min<int64_t>(16 * TM, a->M - mb)), cols = int(std::min<int64_t>(64, N - nb));
+  const uint32_t ld = uint32_t(N * Z), span = uint32_t((rows - 1) * N * Z + cols * Z);
+  const bool one = a->im.B == 1 || a->im.stride == 0;
+  float gate[16], bias[16];
+  if constexpr (VEC) {
+#pragma unroll
+    for (int c = 0; c < 16; ++c) bias[c] = a->bias ? Elem<T>::load(bias_lds, 16 * g + c) : 0.f;
+  } else {
+    load16<T>(a->bias, N, nb + 16 * g, bias);
+  }
+  if (GATED && one) load16<T>(a->gate, N, nb + 16 * g, gate);
+  const __amdgpu_buffer_rsrc_t ro = range_of(static_cast<T*>(a->out) + mb * N + nb, span);
+  const __amdgpu_buffer_rsrc_t rr = range_of(static_cast<const T*>(GATED ? a->resid : a->out) + mb * N + nb, span);
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int row = TM * l + i;
+    const uint32_t at = uint32_t(row) * ld + uint32_t(16 * g * Z);
+    float v[16];
+#pragma unroll
+    for (int c = 0; c < 16; ++c) v[c] = acc[i][c % 4][c / 4] + bias[c];
+    if constexpr (GATED) {
+      if (!one) {
+        int64_t skip = 0;
+        const int64_t stride = a->im.stride, at_row = mb + std::min(row, rows - 1);
+#pragma unroll 1
+        for (int b = 0; b < a->im.B - 1; ++b) skip += at_row >= a->im.end[b] ? stride : 0;  // scalars are short: rolled
+        const T* p = static_cast<const T*>(a->gate) + skip + nb;
+#pragma unroll
+        for (int c = 0; c < 16; ++c) gate[c] = Elem<T>::load(p, std::min(16 * g + c, cols - 1));
+      }
+      float res[16];
+      if constexpr (VEC) {
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+          const u32x4 w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                              rr, int(16 * g + E * q < cols ? at + 16 * q : kNowhere), 0, 0));
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            res[E * q + e] = Z == 4 ? __uint_as_float(w[e % 4])
+                                    : __uint_as_float(e % 2 ? w[e / 2 % 4] & 0xffff0000u : w[e / 2 % 4] << 16);
+        }
+      } else {
+        const T* p = static_cast<const T*>(a->resid) + (mb + std::min(row, rows - 1)) * N + nb;
+#pragma unroll
+        for (int c = 0; c < 16; ++c) res[c] = Elem<T>::load(p, std::min(16 * g + c, cols - 1));
+      }
+#pragma unroll
+      for (int c = 0; c < 16; ++c) v[c] = res[c] + gate[c] * v[c];
+    }
+    if constexpr (VEC) {
+#pragma unroll
+      for (int q = 0; q < V; ++q) {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          w[e] = Z == 4 ? __float_as_uint(v[4 * q % 16 + e]) : pack_bf2(v[(8 * q + 2 * e) % 16], v[(8 * q + 2 * e + 1) % 16]);
+        __builtin_amdgcn_raw_buffer_store_b128(w, ro, int(16 * g + E * q < cols ? at + 16 * q : kNowhere), 0, 0);
+      }
+    } else if (row < rows) {
+      T* p = static_cast<T*>(a->out) + (mb + row) * N + nb;
+#pragma unroll
+      for (int c = 0; c < 16; ++c)
+        if (16 * g + c < cols) st(p, 16 * g + c, v[c]);
+    }
+  }
+}
+
+// Many rows: 256 x 256 outputs to a workgroup of eight waves, a step of 256
+// elements (128 bytes of every row) at a time.  In bytes and matrix cycles this
+// is the bf16 product of a quarter of the contraction, and it runs in the same
+// ping-pong form: two groups of four waves (one of each per SIMD), group g the
+// output rows 128 g .. + 127, alternate a memory phase (read the fragments of a
+// whole step from LDS, issue loads) with a compute phase (its 64 matrix
+// instructions), one barrier per phase, the groups one phase apart:
+//   phase 2t:     group 0 reads step t;        group 1 multiplies t - 1;
+//   phase 2t + 1: group 0 multiplies step t;   group 1 reads t.
+// Loads go to LDS directly.  Group 0 issues in phase 2t the first half of W and
+// the second half of A (rows 128 .., which only group 1 reads) of step t + 1;
+// group 1 in phase 2t + 1 the first half of A (read by group 0 only), the second
+// half of W and the scales of step t + 2.  So two slots hold A, two the first half
+// of W, three its second half and the scales, two the tile's
+// biases: 158 KB.  LDS rows are 128 bytes;
+// LDS row 16 i + l of a strip holds its row T l + i, block 2 g + k of a row lies
+// in chunk (4 k + g) ^ (row / 2 mod 8): the 16 lanes that a read serves at once,
+// of two lane groups, then meet every bank once (with the blocks in their own order
+// half of them collided: 8192 x 8192 x 8192 294 us instead of 271).
+// The contraction is short (8 steps for K = 2048), so a tile's head and tail
+// are hidden too: a workgroup keeps taking tiles, the next tile's first loads go out before
+// the stores of the last, and the waits for them leave those stores in flight.
+template <typename T, bool GATED, bool VEC>
+__global__ __launch_bounds__(512) void mx4_tile_kernel(const Mx4Args args, uint32_t units) {
+  constexpr int TM = 8, TN = 4;
+  // LDS in bytes: half a step of one operand is 16 KB.
+  constexpr uint32_t kHalf = 0x4000, kA = 0, kWf = 4 * kHalf, kWs = 6 * kHalf, kS = 9 * kHalf, kSc = 0x1000, kB = kS + 3 * kSc;
+  constexpr int kStores = TM * int(sizeof(T));       // store instructions of an epilogue of vectors
+  __shared__ __attribute__((aligned(16))) char lds[kB + 2 * 1024];
+  Mx4ArgsPtr a = (Mx4ArgsPtr)__builtin_amdgcn_kernarg_segment_ptr();  // scalar loads where needed
+  const int tid = threadIdx.x;
+  auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  auto uniform = [](u32x4 r) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = __builtin_amdgcn_readfirstlane(r[e]);
+    return r;
+  };
+  auto bar = [&]() {
+    __builtin_amdgcn_sched_barrier(0);
+    lds_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  const int wave = scalar(tid / kWave);
+  const int grp = wave / 4, sub = wave % 4;
+  const uint32_t lds0 = uint32_t(scalar(int(uint32_t(reinterpret_cast<uintptr_t>(
+      (__attribute__((address_space(3))) char*)(&lds[0]))))));
+  const uint32_t rowb = uint32_t(a->K / 2), tn_all = uint32_t((a->N + 255) / 256), tm_all = uint32_t((a->M + 255) / 256);
+  const int n_t = int((rowb + 127) / 128), n_whole = int(rowb / 128);
+
+  // What a step needs per lane is made once: beside the matrix instructions of
+  // the other group's wave every instruction of a memory phase costs its time.
+  // One load instruction moves 8 LDS rows of 128 bytes; wave `sub` of a group
+  // those from 8 sub + 32 j of a half (j = 0 .. 3).  LDS row r holds row T (r % 16)
+  // + r / 16 of its strip; its chunk position p holds the block of slot p ^ (r / 2
+  // mod 8), slot 4 k + g that of lane group g, k.
+  uint32_t x_off[4], w_off[4];
+  auto chunk_byte = [&](int lane) {   // byte of the row that the lane fetches
+    const int slot = (lane % 8) ^ ((4 * sub + lane / 16) & 7);
+    return uint32_t(16 * (2 * (slot & 3) + (slot >> 2)));
+  };
+  // LDS byte of a fragment within its strip's first tile, for k = 0 and 1, and
+  // of the lane's scales.
+  uint32_t f_at[2], s_at;
+  {
+    const int lane = tid % kWave, l = lane % 16, g = lane / 16;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = sub * 8 + lane / 8 + 32 * j;
+      x_off[j] = uint32_t(128 * (1 - grp) + TM * (r % 16) + r / 16) * rowb + chunk_byte(lane);
+      w_off[j] = uint32_t(128 * grp + 64 * (r / 64) + TN * (r % 16) + r / 16 % 4) * rowb + chunk_byte(lane);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) f_at[k] = 16 * (8 * l + ((4 * k + g) ^ ((l >> 1) & 7)));
+    s_at = 512 * g + 16 * l;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(x_off[j]), "+v"(w_off[j]));
+    asm volatile("" : "+v"(f_at[0]), "+v"(f_at[1]), "+v"(s_at));
+  }
+  auto lane_id = []() { return int(__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u))); };
+  // Scales: waves 0, 1 of group 1 load the rows' pairs (4 t + 2 sub, + 1), waves 2, 3 the columns'.
+  const bool sc_w = sub >= 2;
+  const uint32_t srow = uint32_t(scale_rows(sc_w ? a->N : a->M) * 2);
+
+  // The tile in work: its place and where its loads start.
+  int tm = 0, tn = 0;
+  u32x4 xr = {}, wr = {}, sr = {};
+  uint32_t unit0 = 0;
+  auto take = [&]() {   // the next tile of this workgroup; false: none
+    while (unit0 < units) {
+      const uint32_t here = unit0, n = std::min(units - here, uint32_t(gridDim.x));
+      unit0 = here + n;
+      if (blockIdx.x >= n) continue;
+      int prob;
+      pp_place(here + xcd_logical_id32(blockIdx.x, n), tn_all, tm_all, 0, prob, tm, tn);
+      tm = scalar(tm);
+      tn = scalar(tn);
+      const int64_t m0 = int64_t(tm) * 256, n0 = int64_t(tn) * 256;
+      xr = uniform(buffer_rsrc(a->xq + m0 * rowb, uint32_t(std::min<int64_t>((a->M - m0) * rowb, kNowhere))));
+      wr = uniform(buffer_rsrc(a->wq + n0 * rowb, uint32_t(std::min<int64_t>((a->N - n0) * rowb, kNowhere))));
+      const int64_t skip = (sc_w ? n0 : m0) * 2;
+      sr = uniform(buffer_rsrc((sc_w ? a->ws : a->xs) + skip, uint32_t(scale_groups(a->K) * srow - skip)));
+      return true;
+    }
+    return false;
+  };
+
+  // The loads of step t (past the end: none of memory, but counted).
+  auto load_half = [&](const u32x4& r, const uint32_t (&off)[4], uint32_t dst, int t) {
+    const bool live = t < n_t;
+    const u32x4 rr = {r[0], r[1], live ? r[2] : 0u, r[3]};
+    const uint32_t k = live ? uint32_t(t) * 128 : 0u;
+    if (t < n_whole) {
+      lds_load16_at<0>(dst, off[0], rr, k);
+      lds_load16_at<0x1000>(dst, off[1], rr, k);
+      lds_load16_at<0x2000>(dst, off[2], rr, k);
+      lds_load16_at<0x3000>(dst, off[3], rr, k);
+    } else {   // the last step may end within a row's 128 bytes: what lies past them reads as 0
+      const uint32_t far = k + chunk_byte(lane_id()) >= rowb ? kNowhere : 0u;
+      lds_load16_at<0>(dst, off[0] | far, rr, k);
+      lds_load16_at<0x1000>(dst, off[1] | far, rr, k);
+      lds_load16_at<0x2000>(dst, off[2] | far, rr, k);
+      lds_load16_at<0x3000>(dst, off[3] | far, rr, k);
+    }
+  };
+  const uint32_t own = lds0 + sub * 1024;   // where this wave's rows of a half land
+  auto load_a = [&](int t) { load_half(xr, x_off, own + kA + ((t & 1) * 2 + 1 - grp) * kHalf, t); };
+  auto load_w = [&](int t, int slot3) {
+    load_half(wr, w_off, own + (grp ? kWs + slot3 * kHalf : kWf + (t & 1) * kHalf), t);
+  };
+  auto load_s = [&](int t, int slot3) {
+    const bool live = t < n_t;
+    const u32x4 rr = {sr[0], sr[1], live ? sr[2] : 0u, sr[3]};
+    const int lane = lane_id();
+    const uint32_t off = (4 * uint32_t(t) + 2 * (sub & 1) + lane / 32) * srow + 16 * (lane % 32);
+    lds_load16_at<0>(own + kS + slot3 * kSc, live ? off : kNowhere, rr, 0u);
+  };
+
+  f32x4 acc[TM][TN];
+  u32x4 af[2][TM], wf[2][TN], as;
+  u32x2 ws;
+  const uint32_t w_first = (sub < 2 ? kWf : kWs) + (sub & 1) * 0x2000;
+  auto read = [&](int t, int slot3) {
+    const uint32_t A = kA + ((t & 1) * 2 + grp) * kHalf, W = w_first + (sub < 2 ? t & 1 : slot3) * kHalf, S = kS + slot3 * kSc;
+    as = *reinterpret_cast<const u32x4*>(lds + S + grp * 256 + s_at);
+    // (512 g + 8 l: four rows of a column pair array, s_at has eight.)
+    ws = *reinterpret_cast<const u32x2*>(lds + S + 2048 + sub * 128 + (s_at & ~511u) + (s_at & 511u) / 2);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) wf[k][j] = *reinterpret_cast<const u32x4*>(lds + W + f_at[k] + 2048 * j);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) af[k][i] = *reinterpret_cast<const u32x4*>(lds + A + f_at[k] + 2048 * i);
+    }
+  };
+  auto mul = [&]() {
+    __builtin_amdgcn_s_setprio(1);
+    __builtin_amdgcn_sched_barrier(0);
+    unrolled<2>([&](auto k) {
+      unrolled<TM>([&](auto i) {
+        unrolled<TN>([&](auto j) {
+          acc[i][j] = mfma4<2 * (j % 2) + k, 2 * (i % 2) + k>(wf[k][j], af[k][i], acc[i][j], ws[j / 2], as[i / 2]);
+        });
+      });
+    });
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(0);
+  };
+
+  int par = 0;               // which of two places the loads' tile has its biases in
+  int64_t mb = -1, nb = 0;   // the finished tile's block of this wave
+  for (;;) {
+    // Every fragment of the finished tile has been read (group 0 is a barrier
+    // past group 1's last read): the slots are free.  A wave's own late loads
+    // past the end come before its next ones to the same place.
+    asm volatile("" : "+s"(a));
+    const bool more = take();
+    if (more) {
+      if (grp == 0) {
+        // The tile's 256 biases (and what follows them), zeros past the end.
+        if (VEC && a->bias)
+          lds_load16_at<0>(lds0 + kB + 1024 * par, 16 * lane_id(),
+                           uniform(buffer_rsrc(static_cast<const T*>(a->bias) + int64_t(tn) * 256,
+                                               uint32_t((a->N - int64_t(tn) * 256) * int64_t(sizeof(T))))), 0u);
+        load_w(0, 0);
+        load_a(0);
+      } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          load_a(t);
+          load_w(t, t);
+          load_s(t, t);
+        }
+      }
+    }
+    // acc[i][j][r] = out[mb + 8 l + i][nb + 16 g + 4 r + j].
+    const bool out = mb >= 0 && mb < a->M && nb < a->N;
+    if (out) {
+      const int lane = lane_id();
+      tile_epilogue<TM, TN, T, GATED, VEC>(a, mb, nb, lane % 16, lane / 16, acc,
+                                           reinterpret_cast<const T*>(lds + kB + 1024 * (par ^ 1)) + 64 * sub);
+    }
+    if (!more) break;
+    par ^= 1;
+    // Whether kStores stores at least are younger than the tile's first loads.
+    int young = scalar(out && VEC ? 1 : 0);
+    mb = int64_t(tm) * 256 + 128 * grp;
+    nb = int64_t(tn) * 256 + 64 * sub;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // (The step number and `young` are opaque: the loops would be peeled.)
+    if (grp == 0) {
+      if (young) vm_wait<4 + kStores>(); else vm_wait<4>();   // the first half of W(0)
+      bar();
+      int s3 = 0;
+      for (int u = 0; u < n_t; ++u) {
+        int t = u;
+        asm volatile("" : "+s"(young), "+s"(t));
+        read(t, s3);
+        __builtin_amdgcn_sched_barrier(0);
+        load_w(t + 1, 0);
+        load_a(t + 1);
+        // The second half of A(t), which phase 2t + 1 reads.
+        if (young) vm_wait<8 + kStores>(); else vm_wait<8>();
+        young >>= 1;
+        bar();
+        mul();
+        vm_wait<4>();                 // the first half of W(t + 1), which phase 2t + 2 reads
+        bar();
+        s3 = s3 == 2 ? 0 : s3 + 1;
+      }
+    } else {
+      if (young) vm_wait<9 + kStores>(); else vm_wait<9>();   // step 0
+      bar();
+      int s3 = 0;
+      for (int u = 0; u < n_t; ++u) {
+        int t = u;
+        bar();
+        asm volatile("" : "+s"(young), "+s"(t));
+        const int s2 = s3 == 0 ? 2 : s3 - 1;   // the slot of t - 1 and t + 2
+        read(t, s3);
+        __builtin_amdgcn_sched_barrier(0);
+        load_a(t + 2);
+        load_w(t + 2, s2);
+        load_s(t + 2, s2);
+        // Step t + 1, which phase 2t + 2 reads.
+        if (young) vm_wait<9 + kStores>(); else vm_wait<9>();
+        young >>= 1;
+        bar();
+        mul();
+        s3 = s3 == 2 ? 0 : s3 + 1;
+      }
+    }
+  }
+  vm_wait<0>();   // loads to LDS end before the workgroup does
+}
+
 // The weight as T values, transposed: wt [K, ld] with zeros in columns N .. ld.
 // A workgroup turns 64 rows x 64 columns round in LDS.
 template <typename T>
@@ -209,7 +567,16 @@ void run_product(const Mx4Args& a, hipStream_t s) {
   auto grid = [&](int tm, int tn) {
     return dim3(unsigned(std::min<int64_t>(ceil_div64(a.M, 16 * tm) * ceil_div64(a.N, 16 * tn), 1 << 22)));
   };
+  const int64_t units = ceil_div64(a.M, 256) * ceil_div64(a.N, 256);
   if (a.M <= 16) hipLaunchKernelGGL((mx4_rows_kernel<1, 2, T>), grid(1, 2), dim3(256), 0, s, a);
+  else if (units >= 128) {
+    const dim3 grid(unsigned(ceil_div64(units, ceil_div64(units, 256)))), wg(512);
+    const bool vec = a.N % (16 / int64_t(sizeof(T))) == 0 && aligned_to({a.bias}, 16);
+    if (a.gate && vec) hipLaunchKernelGGL((mx4_tile_kernel<T, true, true>), grid, wg, 0, s, a, uint32_t(units));
+    else if (a.gate) hipLaunchKernelGGL((mx4_tile_kernel<T, true, false>), grid, wg, 0, s, a, uint32_t(units));
+    else if (vec) hipLaunchKernelGGL((mx4_tile_kernel<T, false, true>), grid, wg, 0, s, a, uint32_t(units));
+    else hipLaunchKernelGGL((mx4_tile_kernel<T, false, false>), grid, wg, 0, s, a, uint32_t(units));
+  }
   else hipLaunchKernelGGL((mx4_rows_kernel<4, 4, T>), grid(4, 4), dim3(256), 0, s, a);
 }
 
