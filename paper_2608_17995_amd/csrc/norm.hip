@@ -7,6 +7,7 @@
 // Rows of several images lie one after another; image b's rows take the
 // vectors b * mod_stride elements after the first image's.
 #include <cmath>
+#include <type_traits>
 
 #include "kernels.h"
 #include "lowbit.h"
@@ -42,6 +43,121 @@ __global__ __launch_bounds__(256) void norm_any_kernel(const T* x, int64_t M, in
   if (lane == 0) {
     if (mean) mean[row] = mu;
     if (rstd) rstd[row] = rs;
+  }
+}
+
+// 16 bytes of a row as floats, and back.
+template <typename T> constexpr int kVec = 16 / int(sizeof(T));
+template <typename T>
+__device__ __forceinline__ void widen(const u32x4& w, float (&v)[kVec<T>]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (sizeof(T) == 2) {
+      v[2 * e] = __uint_as_float(w[e] << 16);
+      v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    } else {
+      v[e] = __uint_as_float(w[e]);
+    }
+  }
+}
+template <typename T>
+__device__ __forceinline__ u32x4 narrow(const float (&v)[kVec<T>]) {
+  u32x4 w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (sizeof(T) == 2) w[e] = pack_bf2(v[2 * e], v[2 * e + 1]);
+    else w[e] = __float_as_uint(v[e]);
+  }
+  return w;
+}
+
+// Rows of whole 16-byte chunks: WAVES waves hold a row in registers, NC chunks
+// in a lane (chunk l + 64 WAVES c), so memory is read once and written once,
+// which is the bound.  A workgroup takes `per` consecutive rows, keeps the modulation
+// of an image as long as its rows last, and loads the next row while it reduces one.
+template <typename T, int NC, int WAVES>
+__global__ __launch_bounds__(256) void norm_rows_kernel(const T* x, int64_t M, int64_t D, const Images im,
+                                                        const T* __restrict__ shift, const T* __restrict__ scale, float eps,
+                                                        T* h, float* __restrict__ mean, float* __restrict__ rstd, int per) {
+  constexpr int E = kVec<T>, kTeams = 4 / WAVES;
+  __shared__ float red[2][4];
+  const int lane = threadIdx.x % (kWave * WAVES), team = threadIdx.x / (kWave * WAVES);
+  const int64_t nchunk = D / E;
+  const int64_t first = (int64_t(blockIdx.x) * kTeams + team) * per, last = std::min<int64_t>(first + per, M);
+  const float inv = 1.f / float(D);
+  auto load = [&](int64_t row, u32x4 (&v)[NC]) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int64_t at = lane + kWave * WAVES * c;
+      v[c] = at < nchunk ? reinterpret_cast<const u32x4*>(x + row * D)[at] : u32x4{0u, 0u, 0u, 0u};
+    }
+  };
+  auto total = [&](float s, int slot) {
+    s = wave_sum(s);
+    if constexpr (WAVES > 1) {
+      if (threadIdx.x % kWave == 0) red[slot][threadIdx.x / kWave] = s;
+      __syncthreads();
+      s = (red[slot][0] + red[slot][1]) + (red[slot][2] + red[slot][3]);
+    }
+    return s;
+  };
+  u32x4 cur[NC], nxt[NC], g[NC], t[NC];
+  int image = -1;
+  if (first < last) load(first, cur);
+  for (int64_t row = first; row < last; ++row) {
+    if (row + 1 < last) load(row + 1, nxt);
+    const int b = image_of(im, row);
+    if (b != image) {
+      image = b;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int64_t at = lane + kWave * WAVES * c;
+        const T* none = nullptr;
+        const T *sc = scale ? scale + b * im.stride : none, *sh = shift ? shift + b * im.stride : none;
+        g[c] = sc && at < nchunk ? reinterpret_cast<const u32x4*>(sc)[at] : u32x4{0u, 0u, 0u, 0u};
+        t[c] = sh && at < nchunk ? reinterpret_cast<const u32x4*>(sh)[at] : u32x4{0u, 0u, 0u, 0u};
+      }
+    }
+    float s = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float v[E];
+      widen<T>(cur[c], v);
+#pragma unroll
+      for (int e = 0; e < E; e += 2) s += v[e] + v[e + 1];
+    }
+    const float mu = total(s, 0) * inv;
+    float q = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float v[E];
+      widen<T>(cur[c], v);
+      if (lane + kWave * WAVES * c < nchunk) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) q = fmaf(v[e] - mu, v[e] - mu, q);
+      }
+    }
+    const float rs = rsqrtf(total(q, 1) * inv + eps);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int64_t at = lane + kWave * WAVES * c;
+      if (at < nchunk) {
+        float v[E], w[E], z[E];
+        widen<T>(cur[c], v);
+        widen<T>(g[c], w);
+        widen<T>(t[c], z);
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = (v[e] - mu) * rs * (1.f + w[e]) + z[e];
+        reinterpret_cast<u32x4*>(h + row * D)[at] = narrow<T>(v);
+      }
+    }
+    if (lane == 0) {
+      if (mean) mean[row] = mu;
+      if (rstd) rstd[row] = rs;
+    }
+    if constexpr (WAVES > 1) __syncthreads();   // before the next row's sums
+#pragma unroll
+    for (int c = 0; c < NC; ++c) cur[c] = nxt[c];
   }
 }
 
@@ -137,15 +253,168 @@ __global__ __launch_bounds__(256) void norm_back_any_kernel(const T* dh, const R
   }
 }
 
-// Sums of the chunks' parts, in chunk order within each of 16 strands: 16
-// columns of a workgroup, blockIdx.y the image (or all of them together),
-// blockIdx.z scale or shift.
+// Backward of rows of whole 16-byte chunks: a workgroup takes a chunk of rows, R
+// at a time; a thread owns NC vectors of columns for all of them, holds their
+// weight and their column sums in registers, and the rows' two averages meet
+// in LDS with one barrier for R rows.  Everything is read once and written once.
+template <typename T, bool HELD, int NC, int R>
+__global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const Rows<T> xr, const float* __restrict__ mean,
+                                                             const float* __restrict__ rstd, int64_t D, const Images im,
+                                                             const Chunks ch, const T* __restrict__ scale, const T* dres,
+                                                             T* dx, float* __restrict__ part, int parts) {
+  constexpr int E = kVec<T>;
+  __shared__ float red[2][8][2 * R];
+  const int waves = blockDim.x / kWave, wave = threadIdx.x / kWave;
+  const int nchunk = int(D / E);
+  const float inv = 1.f / float(D);
+  int b;
+  int64_t lo, hi;
+  chunk_rows(im, ch, blockIdx.x, b, lo, hi);
+  int at[NC];
+  float w[NC][E], sc[NC][E], sh[NC][E];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    at[c] = threadIdx.x + blockDim.x * c;
+    u32x4 g = {0u, 0u, 0u, 0u};
+    if (scale && at[c] < nchunk) g = reinterpret_cast<const u32x4*>(scale + b * im.stride)[at[c]];
+    widen<T>(g, w[c]);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      w[c][e] = at[c] < nchunk ? 1.f + w[c][e] : 0.f;
+      sc[c][e] = sh[c][e] = 0.f;
+    }
+  }
+  // The rows' data as loaded; rows past the chunk and columns past D as zeros.
+  struct Batch {
+    u32x4 d[R][NC], x[R][NC], r[R][NC];
+    uint32_t s[R][NC];
+    float mu[R], rs[R];
+  };
+  auto load = [&](int64_t row, Batch& t) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool in = row + r < hi;
+      const int64_t m = in ? row + r : hi - 1;
+      t.mu[r] = mean[m];
+      t.rs[r] = rstd[m];
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const u32x4 zero = {0u, 0u, 0u, 0u};
+        const bool here = in && at[c] < nchunk;
+        t.d[r][c] = here ? reinterpret_cast<const u32x4*>(dh + m * D)[at[c]] : zero;
+        t.x[r][c] = zero;
+        if constexpr (HELD) {
+          const uint8_t* q = xr.q + m * D + at[c] * E;
+          if (here) {
+            if constexpr (E == 8) {
+              const u32x2 v = *reinterpret_cast<const u32x2*>(q);
+              t.x[r][c][0] = v[0];
+              t.x[r][c][1] = v[1];
+            } else {
+              t.x[r][c][0] = *reinterpret_cast<const uint32_t*>(q);
+            }
+          }
+          t.s[r][c] = here ? xr.s[m * xr.ns + at[c] * E / kBlk] : 0u;
+        } else if (here) {
+          t.x[r][c] = reinterpret_cast<const u32x4*>(xr.x + m * D)[at[c]];
+        }
+        t.r[r][c] = here && dres ? reinterpret_cast<const u32x4*>(dres + m * D)[at[c]] : zero;
+      }
+    }
+  };
+  Batch t, next;
+  if (lo < hi) load(lo, t);
+  int turn = 0;
+  for (int64_t row = lo; row < hi; row += R, turn ^= 1) {
+    if (row + R < hi) load(row + R, next);
+    auto normed = [&](int r, int c, float (&n)[E]) {
+      if constexpr (HELD) {
+        const float scale8 = scale_value(t.s[r][c]);
+        decode8x4(t.x[r][c][0], scale8, n);
+        if constexpr (E == 8) decode8x4(t.x[r][c][1], scale8, n + 4);
+      } else {
+        widen<T>(t.x[r][c], n);
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) n[e] = (n[e] - t.mu[r]) * t.rs[r];
+    };
+    float sum[2 * R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      sum[2 * r] = sum[2 * r + 1] = 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        float dv[E], n[E];
+        widen<T>(t.d[r][c], dv);
+        normed(r, c, n);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float g = dv[e] * w[c][e];
+          sum[2 * r] += g;
+          sum[2 * r + 1] = fmaf(g, n[e], sum[2 * r + 1]);
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 2 * R; ++k) sum[k] = wave_sum(sum[k]);
+    if (waves > 1) {
+      if (threadIdx.x % kWave == 0)
+#pragma unroll
+        for (int k = 0; k < 2 * R; ++k) red[turn][wave][k] = sum[k];
+      __syncthreads();   // the other half of red is read before the next one's barrier
+#pragma unroll
+      for (int k = 0; k < 2 * R; ++k) sum[k] = red[turn][0][k];
+      for (int v = 1; v < waves; ++v)
+#pragma unroll
+        for (int k = 0; k < 2 * R; ++k) sum[k] += red[turn][v][k];
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (row + r >= hi) continue;
+      const float ag = sum[2 * r] * inv, an = sum[2 * r + 1] * inv;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        if (at[c] >= nchunk) continue;
+        float dv[E], n[E], o[E];
+        widen<T>(t.d[r][c], dv);
+        normed(r, c, n);
+        widen<T>(t.r[r][c], o);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          sc[c][e] = fmaf(dv[e], n[e], sc[c][e]);
+          sh[c][e] += dv[e];
+          o[e] += t.rs[r] * (dv[e] * w[c][e] - ag - n[e] * an);
+        }
+        reinterpret_cast<u32x4*>(dx + (row + r) * D)[at[c]] = narrow<T>(o);
+      }
+    }
+    t = next;
+  }
+  if (parts) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      if (at[c] >= nchunk) continue;
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        float* p = part + int64_t(2 * blockIdx.x) * D + at[c] * E + e;
+        *reinterpret_cast<f32x4*>(p) = f32x4{sc[c][e], sc[c][e + 1], sc[c][e + 2], sc[c][e + 3]};
+        *reinterpret_cast<f32x4*>(p + D) = f32x4{sh[c][e], sh[c][e + 1], sh[c][e + 2], sh[c][e + 3]};
+      }
+    }
+  }
+}
+
+// Sums of the chunks' parts, in chunk order within each of 16 strands: 16 V
+// columns of a workgroup (V = 4 where rows of D floats are aligned), blockIdx.y
+// the image (or all of them together), blockIdx.z scale or shift.
+template <int V>
 __global__ __launch_bounds__(256) void norm_back_sum_kernel(const float* __restrict__ part, int64_t D, const Chunks ch,
                                                             int together, float* __restrict__ dscale,
                                                             float* __restrict__ dshift) {
-  __shared__ float red[16][17];
+  typedef float vec __attribute__((ext_vector_type(V)));
+  __shared__ vec red[16][17];
   const int col = threadIdx.x % 16, strand = threadIdx.x / 16;
-  const int64_t i = int64_t(blockIdx.x) * 16 + col;
+  const int64_t i = (int64_t(blockIdx.x) * 16 + col) * V;
   float* out = blockIdx.z ? dshift : dscale;
   if (!out) return;
   int c0 = 0, c1 = ch.first[kMaxSeqs];
@@ -157,15 +426,27 @@ __global__ __launch_bounds__(256) void norm_back_sum_kernel(const float* __restr
         c1 = ch.first[b + 1];
       }
   }
-  float v = 0.f;
-  if (i < D)
-    for (int c = c0 + strand; c < c1; c += 16) v += part[int64_t(2 * c + blockIdx.z) * D + i];
+  vec v = 0.f;
+  if (i < D) {
+    const float* p = part + blockIdx.z * D + i;
+    int c = c0 + strand;
+    for (; c + 16 * 7 < c1; c += 16 * 8) {   // eight loads in flight
+      vec t[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) t[k] = *reinterpret_cast<const vec*>(p + 2 * D * (c + 16 * k));
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v += t[k];
+    }
+    for (; c < c1; c += 16) v += *reinterpret_cast<const vec*>(p + 2 * D * c);
+  }
   red[strand][col] = v;
   __syncthreads();
   if (strand == 0 && i < D) {
 #pragma unroll
     for (int k = 1; k < 16; ++k) v += red[k][col];
-    out[int64_t(blockIdx.y) * D + i] = v;
+    float* o = out + int64_t(blockIdx.y) * D + i;
+#pragma unroll
+    for (int e = 0; e < V; ++e) o[e] = v[e];
   }
 }
 
@@ -193,12 +474,41 @@ Chunks make_chunks(int64_t M, const Images& im) {
   return ch;
 }
 
+// Whether rows and vectors come in whole, aligned 16-byte chunks.
+bool chunked(int64_t D, int64_t stride, size_t z, std::initializer_list<const void*> ps) {
+  const int64_t e = int64_t(16 / z);
+  return D % e == 0 && stride % e == 0 && aligned_to(ps, 16);
+}
+
 template <typename T>
 void run_norm(const void* x, int64_t M, int64_t D, const Images& im, const void* shift, const void* scale, float eps,
               void* h, float* mean, float* rstd, hipStream_t s) {
   TimedLaunch timed("layer_norm", s);
-  hipLaunchKernelGGL(norm_any_kernel<T>, dim3(unsigned(ceil_div64(M, 4))), dim3(256), 0, s, static_cast<const T*>(x), M, D,
-                     im, static_cast<const T*>(shift), static_cast<const T*>(scale), eps, static_cast<T*>(h), mean, rstd);
+  const T *px = static_cast<const T*>(x), *sh = static_cast<const T*>(shift), *sc = static_cast<const T*>(scale);
+  T* ph = static_cast<T*>(h);
+  const int64_t chunks = ceil_div64(D * int64_t(sizeof(T)), 16 * kWave);   // a wave's chunks per lane
+  if (!chunked(D, im.stride, sizeof(T), {x, h, shift, scale}) || chunks > 32) {
+    hipLaunchKernelGGL(norm_any_kernel<T>, dim3(unsigned(ceil_div64(M, 4))), dim3(256), 0, s, px, M, D, im, sh, sc, eps, ph,
+                       mean, rstd);
+    return;
+  }
+  auto go = [&](auto nc, auto waves) {
+    constexpr int kNC = decltype(nc)::value, kW = decltype(waves)::value;
+    const int64_t teams = 4 / kW;
+    // A few rows to a team, once there are enough for every SIMD.
+    const int per = int(std::min<int64_t>(8, std::max<int64_t>(1, M / (teams * 2048))));
+    hipLaunchKernelGGL((norm_rows_kernel<T, kNC, kW>), dim3(unsigned(ceil_div64(M, teams * per))), dim3(256), 0, s, px, M, D, im,
+                       sh, sc, eps, ph, mean, rstd, per);
+  };
+  using std::integral_constant;
+  const integral_constant<int, 1> one;
+  const integral_constant<int, 4> four;
+  if (chunks <= 1) go(one, one);
+  else if (chunks <= 2) go(integral_constant<int, 2>(), one);
+  else if (chunks <= 4) go(four, one);
+  else if (chunks <= 8) go(integral_constant<int, 8>(), one);
+  else if (chunks <= 16) go(four, four);
+  else go(integral_constant<int, 8>(), four);
 }
 
 template <typename T>
@@ -210,17 +520,40 @@ void run_norm_back(const void* dh, const Rows<T>& rows, const float* mean, const
   const int n = ch.first[kMaxSeqs];
   float* avg = ws;
   float* part = ws + align_up(size_t(2 * M), 64);
-  const T *d = static_cast<const T*>(dh), *sc = static_cast<const T*>(scale);
-  if (M > 0)
-    hipLaunchKernelGGL(norm_back_avg_kernel<T>, dim3(unsigned(ceil_div64(M, 4))), dim3(256), 0, s, d, rows, mean, rstd, M, D,
-                       im, sc, avg);
-  hipLaunchKernelGGL(norm_back_any_kernel<T>, dim3(unsigned(n), unsigned(ceil_div64(D, 256))), dim3(256), 0, s, d, rows, mean,
-                     rstd, D, im, ch, sc, static_cast<const T*>(dres), (const float*)avg, static_cast<T*>(dx), part,
-                     dscale || dshift ? 1 : 0);
-  if (dscale || dshift) {
+  const T *d = static_cast<const T*>(dh), *sc = static_cast<const T*>(scale), *res = static_cast<const T*>(dres);
+  T* o = static_cast<T*>(dx);
+  const int parts = dscale || dshift ? 1 : 0;
+  const int64_t chunks = ceil_div64(D * int64_t(sizeof(T)), 16);
+  if (chunked(D, im.stride, sizeof(T), {dh, rows.x, scale, dres, dx, ws}) && (!rows.q || aligned_to({rows.q}, 8)) &&
+      chunks <= 1024) {
+    auto go = [&](auto nc) {
+      constexpr int kNC = decltype(nc)::value, kR = kNC == 1 ? 2 : 1;
+      const dim3 wg(unsigned(ceil_div64(ceil_div64(chunks, kNC), kWave) * kWave));
+      if (rows.q)
+        hipLaunchKernelGGL((norm_back_rows_kernel<T, true, kNC, kR>), dim3(unsigned(n)), wg, 0, s, d, rows, mean, rstd, D, im, ch,
+                           sc, res, o, part, parts);
+      else
+        hipLaunchKernelGGL((norm_back_rows_kernel<T, false, kNC, kR>), dim3(unsigned(n)), wg, 0, s, d, rows, mean, rstd, D, im, ch,
+                           sc, res, o, part, parts);
+    };
+    if (chunks <= 512) go(std::integral_constant<int, 1>());
+    else go(std::integral_constant<int, 2>());
+  } else {
+    if (M > 0)
+      hipLaunchKernelGGL(norm_back_avg_kernel<T>, dim3(unsigned(ceil_div64(M, 4))), dim3(256), 0, s, d, rows, mean, rstd, M, D,
+                         im, sc, avg);
+    hipLaunchKernelGGL(norm_back_any_kernel<T>, dim3(unsigned(n), unsigned(ceil_div64(D, 256))), dim3(256), 0, s, d, rows,
+                       mean, rstd, D, im, ch, sc, res, (const float*)avg, o, part, parts);
+  }
+  if (parts) {
     const int together = im.stride == 0 ? 1 : 0;
-    hipLaunchKernelGGL(norm_back_sum_kernel, dim3(unsigned(ceil_div64(D, 16)), unsigned(together ? 1 : im.B), 2), dim3(256), 0,
-                       s, (const float*)part, D, ch, together, dscale, dshift);
+    auto sum = [&](auto v) {
+      constexpr int kV = decltype(v)::value;
+      hipLaunchKernelGGL(norm_back_sum_kernel<kV>, dim3(unsigned(ceil_div64(D, 16 * kV)), unsigned(together ? 1 : im.B), 2),
+                         dim3(256), 0, s, (const float*)part, D, ch, together, dscale, dshift);
+    };
+    if (D % 4 == 0 && aligned_to({part}, 16)) sum(std::integral_constant<int, 4>());
+    else sum(std::integral_constant<int, 1>());
   }
 }
 
