@@ -114,25 +114,26 @@ __global__ __launch_bounds__(256) void gelu_back_any_kernel(const T* da, const T
 // the rows one after another, so that a lane of the product that owns several
 // consecutive rows reads their scales at once.
 //
-// A workgroup converts 32 rows x 512 columns: a wave a row at a time (a lane
-// eight elements, four lanes a block), the scales turned round through LDS so that
-// they leave in runs of 64 bytes.
-constexpr int kQRows = 32, kQCols = 512;
+// A workgroup converts kQRows x kQCols elements: a wave 512 columns of a row at a
+// time (a lane eight elements, four lanes a block), the scales turned round
+// through LDS so that each pair's rows leave in one run.
+constexpr int kQRows = 16, kQCols = 1024, kQSegs = kQCols / 512, kQItems = kQRows * kQSegs / 4;
+static_assert(kQRows * (kQCols / 64) == 256, "one scale pair per thread");
 
 template <typename T, bool GELU>
 __global__ __launch_bounds__(256) void quantize4_kernel(const T* __restrict__ x, int64_t M, int64_t K,
                                                         uint8_t* __restrict__ q, uint8_t* __restrict__ s) {
   __shared__ uint16_t sc[kQCols / 64][kQRows];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int64_t m0 = int64_t(blockIdx.x) * kQRows, k = int64_t(blockIdx.y) * kQCols + 8 * lane;
+  const int64_t m0 = int64_t(blockIdx.x) * kQRows, k0 = int64_t(blockIdx.y) * kQCols + 8 * lane;
   const int64_t Mp = scale_rows(M);
-  const bool in = k < K;  // K is a multiple of 32: all four lanes of a block, or none
 #pragma unroll
-  for (int r = 0; r < kQRows / 4; ++r) {
-    const int row = wave + 4 * r;
-    const int64_t m = m0 + row;
+  for (int r = 0; r < kQItems; ++r) {
+    const int row = (wave * kQItems + r) / kQSegs, seg = r % kQSegs;
+    const int64_t m = m0 + row, k = k0 + 512 * seg;
+    const bool in = k < K && m < M;  // K is a multiple of 32: all four lanes of a block, or none
     float v[8] = {};
-    if (in && m < M) load8(x + m * K + k, v);
+    if (in) load8(x + m * K + k, v);
     uint32_t top = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -141,10 +142,10 @@ __global__ __launch_bounds__(256) void quantize4_kernel(const T* __restrict__ x,
     }
     const uint32_t c = scale4_code(quad_umax(top));
     const uint32_t o = encode4x8(v, c == 255u ? 0.f : scale_inverse(c));
-    if (in && m < M) *reinterpret_cast<uint32_t*>(q + (m * K + k) / 2) = o;
+    if (in) *reinterpret_cast<uint32_t*>(q + (m * K + k) / 2) = o;
     // Lane 8 j: its own block's scale and, from lane 8 j + 7, the next block's.
     const uint32_t up = uint32_t(__builtin_amdgcn_update_dpp(0, int(c), kDppHalfMirror, 0xf, 0xf, false));
-    if (lane % 8 == 0) sc[lane / 8][row] = uint16_t(c | up << 8);
+    if (lane % 8 == 0) sc[seg * 8 + lane / 8][row] = uint16_t(c | up << 8);
   }
   __syncthreads();
   const int pair = threadIdx.x / kQRows, row = threadIdx.x % kQRows;
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(256) void dequantize4_kernel(const uint8_t* __restr
                                                           int64_t M, int64_t K, T* __restrict__ x) {
   __shared__ uint16_t sc[kQCols / 64][kQRows];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int64_t m0 = int64_t(blockIdx.x) * kQRows, k = int64_t(blockIdx.y) * kQCols + 8 * lane;
+  const int64_t m0 = int64_t(blockIdx.x) * kQRows, k0 = int64_t(blockIdx.y) * kQCols + 8 * lane;
   const int64_t Mp = scale_rows(M);
   {
     const int pair = threadIdx.x / kQRows, row = threadIdx.x % kQRows;
@@ -165,14 +166,13 @@ __global__ __launch_bounds__(256) void dequantize4_kernel(const uint8_t* __restr
     sc[pair][row] = gp < scale_groups(K) && m < Mp ? reinterpret_cast<const uint16_t*>(s)[gp * Mp + m] : uint16_t(0);
   }
   __syncthreads();
-  if (k >= K) return;
 #pragma unroll
-  for (int r = 0; r < kQRows / 4; ++r) {
-    const int row = wave + 4 * r;
-    const int64_t m = m0 + row;
-    if (m >= M) continue;
+  for (int r = 0; r < kQItems; ++r) {
+    const int row = (wave * kQItems + r) / kQSegs, seg = r % kQSegs;
+    const int64_t m = m0 + row, k = k0 + 512 * seg;
+    if (m >= M || k >= K) continue;
     float v[8];
-    const uint32_t c = sc[lane / 8][row] >> (lane & 4 ? 8 : 0);
+    const uint32_t c = sc[seg * 8 + lane / 8][row] >> (lane & 4 ? 8 : 0);
     decode4x8(*reinterpret_cast<const uint32_t*>(q + (m * K + k) / 2), scale_value(c & 255u), v);
     store8(x + m * K + k, v);
   }
