@@ -199,10 +199,21 @@ def _dev(t, name, dtype=None):
 
 
 def _stream(stream):
-    import torch
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     return getattr(stream, "cuda_stream", stream)
+
+
+def _current_stream():
+    """Handle of the current device's current stream."""
+    import torch
+    raw, device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+    # The handle without a Stream object around it, where this torch has it (2.7 us less per call).
+    if raw is None or device is None or not torch.cuda.is_initialized():
+        return torch.cuda.current_stream().cuda_stream
+    global _current_stream
+    _current_stream = lambda: raw(device())  # noqa: E731
+    return _current_stream()
 
 
 def _workspace(ws, nbytes, device):
@@ -497,63 +508,95 @@ class BlockWeights:
 
 
 # ---------------------------------------------------------------------------
-# Low-bit projections and the training operators around them.
+# Low-bit projections and the training operators around them.  These calls can
+# be shorter than a microsecond's worth of checks on the host, so each tensor
+# is looked at once (_arg).
 
-def _mod_rows(named, D, n_images, dt):
-    """Pointers of shift / scale vectors given as [D] (shared) or [B, D] (rows
-    any number of elements apart, e.g. a slice of a [B, 6, D] modulation), and
-    their common stride in elements."""
-    stride, ptrs = None, []
-    for name, t in named:
-        if t is None:
-            ptrs.append(None)
-            continue
-        if not t.is_cuda or t.dtype != dt:
-            raise AvitsError(-1, f"{name} must be a {dt} GPU tensor")
-        if t.dim() == 1 and t.shape[0] == D:
-            step = 0
-        elif t.dim() == 2 and tuple(t.shape) == (n_images, D):
-            step = t.stride(0) if n_images > 1 else D
-        else:
-            raise ValueError(f"{name}: [{D}] or [{n_images}, {D}], got {tuple(t.shape)}")
-        if D > 1 and t.stride(-1) != 1:
-            raise AvitsError(-1, f"{name} must have contiguous rows")
-        if step == 0 and t.dim() == 2:
-            raise AvitsError(-1, f"{name}: give one shared vector as [{D}]")
-        if stride is not None and step != stride:
-            raise ValueError("shift and scale must be laid out alike")
-        stride = step
-        ptrs.append(t.data_ptr())
-    return ptrs, stride
+def _arg(t, name, dtype, *shape):
+    """Device pointer of a contiguous GPU tensor of a type and shape (None passes NULL)."""
+    if t is None:
+        return None
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected {shape}, got {tuple(t.shape)}")
+    if not t.is_cuda or t.dtype is not dtype or not t.is_contiguous():
+        raise AvitsError(-1, f"{name} must be a contiguous {dtype} GPU tensor, got {t.dtype} on {t.device}"
+                             f"{'' if t.is_contiguous() else ', not contiguous'}")
+    return t.data_ptr()
 
 
-def _want(t, shape, name):
-    if t is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: expected {tuple(shape)}, got {tuple(t.shape)}")
+def _mod_rows(name, t, dtype, D, n_images):
+    """Pointer of a vector given as [D] (shared) or [B, D] (rows any number of
+    elements apart, e.g. a slice of a [B, 6, D] modulation), and the
+    distance of the images' rows in elements."""
+    if t is None:
+        return None, None
+    if t.dim() == 1:
+        return _arg(t, name, dtype, D), 0
+    if t.shape != (n_images, D):
+        raise ValueError(f"{name}: [{D}] or [{n_images}, {D}], got {tuple(t.shape)}")
+    step, unit = t.stride()
+    if not t.is_cuda or t.dtype is not dtype or (unit != 1 and D > 1):
+        raise AvitsError(-1, f"{name} must be a {dtype} GPU tensor with contiguous rows")
+    if n_images == 1:
+        step = D
+    elif step == 0:
+        raise AvitsError(-1, f"{name}: give one shared vector as [{D}]")
+    return t.data_ptr(), step
 
 
 def _offsets(off, name):
-    off = None if off is None else [int(o) for o in off]
-    n = 1 if off is None else len(off) - 1
+    if off is None:
+        return 1, None
+    n = len(off) - 1
     if n < 1:
         raise ValueError(f"{name}: off needs at least two entries")
-    return n, None if off is None else _host_i64(off, n + 1, "off")
+    return n, (ctypes.c_int64 * (n + 1))(*off)
+
+
+_TYPES = {}
+
+
+def _types():
+    """torch's types by the library's codes, filled on first use (torch is imported then)."""
+    import torch
+    _TYPES.update({torch.float32: F32, torch.bfloat16: BF16})
+    _TYPES["u8"], _TYPES["f32"] = torch.uint8, torch.float32
+    return _TYPES
+
+
+def _code(t):
+    code = (_TYPES or _types()).get(t.dtype)
+    if code is None:
+        raise AvitsError(-2, f"unsupported dtype {t.dtype}")
+    return code
+
+
+def _scratch(ws, need, device):
+    """Pointer and size of the workspace, made here (need() bytes) where none is given."""
+    if ws is None:
+        nbytes = need()
+        if not nbytes:
+            return None, None, 0
+        ws, _, _ = _workspace(None, nbytes, device)
+    return ws, _dev(ws, "workspace"), ws.numel() * ws.element_size()
 
 
 def avits_layer_norm(x, shift, scale, h, mean=None, rstd=None, off=None, eps=1e-6, stream=None):
     """h [M, D] = LN(x)(1 + scale) + shift, with the rows' mean and rstd [M]
     fp32 where asked for.  off: host row offsets of B images (B + 1), whose
     shift and scale are [B, D] or one shared [D] (each may be None)."""
-    import torch
     M, D = x.shape
+    code, dt, f32 = _code(x), x.dtype, _TYPES["f32"]
     n, offs = _offsets(off, "avits_layer_norm")
-    (sh, sc), stride = _mod_rows((("shift", shift), ("scale", scale)), D, n, x.dtype)
-    _want(h, (M, D), "h")
-    _want(mean, (M,), "mean")
-    _want(rstd, (M,), "rstd")
-    _check(load().avits_layer_norm(_dev(x, "x"), M, D, n, offs, sh, sc, stride or 0, eps, _dtype_code(x),
-                                   _dev(h, "h", x.dtype), _dev(mean, "mean", torch.float32),
-                                   _dev(rstd, "rstd", torch.float32), _stream(stream)))
+    sh, step = _mod_rows("shift", shift, dt, D, n)
+    sc, step2 = _mod_rows("scale", scale, dt, D, n)
+    if step is not None and step2 is not None and step != step2:
+        raise ValueError("avits_layer_norm: shift and scale must be laid out alike")
+    rc = load().avits_layer_norm(_arg(x, "x", dt, M, D), M, D, n, offs, sh, sc, step or step2 or 0, eps, code,
+                                 _arg(h, "h", dt, M, D), _arg(mean, "mean", f32, M), _arg(rstd, "rstd", f32, M),
+                                 _stream(stream))
+    if rc:
+        _check(rc)
     return h
 
 
@@ -568,58 +611,56 @@ def avits_layer_norm_backward(dh, mean, rstd, scale, dx, dscale=None, dshift=Non
     shared vector).  The forward's rows are x or, packed by avits_ckpt8_pack,
     x_q8 [M, D] and x_s8 [M, ceil(D / 32)].  Without a scale the gradients'
     shape says which."""
-    import torch
     M, D = dh.shape
+    code, dt = _code(dh), dh.dtype
+    f32, u8 = _TYPES["f32"], _TYPES["u8"]
     n, offs = _offsets(off, "avits_layer_norm_backward")
-    (sc,), stride = _mod_rows((("scale", scale),), D, n, dh.dtype)
-    if stride is None:
-        grads = [g for g in (dscale, dshift) if g is not None]
-        stride = D if grads and grads[0].dim() == 2 else 0
-    for name, t in (("dscale", dscale), ("dshift", dshift)):
-        _want(t, (n, D) if stride else (D,), name)
-    for name, t, shape in (("x", x, (M, D)), ("x_q8", x_q8, (M, D)), ("x_s8", x_s8, (M, (D + 31) // 32)),
-                           ("dres", dres, (M, D)), ("dx", dx, (M, D)), ("mean", mean, (M,)), ("rstd", rstd, (M,))):
-        _want(t, shape, name)
-    dt, u8, f32 = dh.dtype, torch.uint8, torch.float32
-    ws, wsp, wsb = _workspace(workspace, avits_layer_norm_backward_workspace_bytes(M, D, n), dh.device)
-    _check(load().avits_layer_norm_backward(
-        _dev(dh, "dh"), _dev(x, "x", dt), _dev(x_q8, "x_q8", u8), _dev(x_s8, "x_s8", u8), _dev(mean, "mean", f32),
-        _dev(rstd, "rstd", f32), M, D, n, offs, sc, stride, _dev(dres, "dres", dt), _dtype_code(dh), _dev(dx, "dx", dt),
-        _dev(dscale, "dscale", f32), _dev(dshift, "dshift", f32), wsp, wsb, _stream(stream)))
+    sc, step = _mod_rows("scale", scale, dt, D, n)
+    if step is None:
+        grad = dscale if dscale is not None else dshift
+        step = D if grad is not None and grad.dim() == 2 else 0
+    shape = (n, D) if step else (D,)
+    ws, wsp, wsb = _scratch(workspace, lambda: avits_layer_norm_backward_workspace_bytes(M, D, n), dh.device)
+    rc = load().avits_layer_norm_backward(
+        _arg(dh, "dh", dt, M, D), _arg(x, "x", dt, M, D), _arg(x_q8, "x_q8", u8, M, D),
+        _arg(x_s8, "x_s8", u8, M, (D + 31) // 32), _arg(mean, "mean", f32, M), _arg(rstd, "rstd", f32, M), M, D, n, offs,
+        sc, step, _arg(dres, "dres", dt, M, D), code, _arg(dx, "dx", dt, M, D), _arg(dscale, "dscale", f32, *shape),
+        _arg(dshift, "dshift", f32, *shape), wsp, wsb, _stream(stream))
+    if rc:
+        _check(rc)
     return dx, dscale, dshift
 
 
 def avits_ckpt8_pack(x, q, s, stream=None):
     """x [M, D] kept in 8 bits: codes q [M, D] and scales s [M, ceil(D / 32)], uint8."""
-    import torch
     M, D = x.shape
-    _want(q, (M, D), "q")
-    _want(s, (M, (D + 31) // 32), "s")
-    _check(load().avits_ckpt8_pack(_dev(x, "x"), M, D, _dtype_code(x), _dev(q, "q", torch.uint8),
-                                   _dev(s, "s", torch.uint8), _stream(stream)))
+    code, u8 = _code(x), _TYPES["u8"]
+    rc = load().avits_ckpt8_pack(_arg(x, "x", x.dtype, M, D), M, D, code, _arg(q, "q", u8, M, D),
+                                 _arg(s, "s", u8, M, (D + 31) // 32), _stream(stream))
+    if rc:
+        _check(rc)
     return q, s
 
 
 def avits_ckpt8_unpack(q, s, x, stream=None):
-    import torch
-    M, D = q.shape
-    _want(x, (M, D), "x")
-    _want(s, (M, (D + 31) // 32), "s")
-    _check(load().avits_ckpt8_unpack(_dev(q, "q", torch.uint8), _dev(s, "s", torch.uint8), M, D, _dtype_code(x),
-                                     _dev(x, "x"), _stream(stream)))
+    M, D = x.shape
+    code, u8 = _code(x), _TYPES["u8"]
+    rc = load().avits_ckpt8_unpack(_arg(q, "q", u8, M, D), _arg(s, "s", u8, M, (D + 31) // 32), M, D, code,
+                                   _arg(x, "x", x.dtype, M, D), _stream(stream))
+    if rc:
+        _check(rc)
     return x
 
 
 def avits_gelu_backward(da, dm, m=None, m_q8=None, m_s8=None, stream=None):
     """dm [M, D] = da GELU'(m), m as it was or packed by avits_ckpt8_pack."""
-    import torch
     M, D = da.shape
-    for name, t, shape in (("dm", dm, (M, D)), ("m", m, (M, D)), ("m_q8", m_q8, (M, D)),
-                           ("m_s8", m_s8, (M, (D + 31) // 32))):
-        _want(t, shape, name)
-    _check(load().avits_gelu_backward(_dev(da, "da"), _dev(m, "m", da.dtype), _dev(m_q8, "m_q8", torch.uint8),
-                                      _dev(m_s8, "m_s8", torch.uint8), M, D, _dtype_code(da), _dev(dm, "dm", da.dtype),
-                                      _stream(stream)))
+    code, dt, u8 = _code(da), da.dtype, _TYPES["u8"]
+    rc = load().avits_gelu_backward(_arg(da, "da", dt, M, D), _arg(m, "m", dt, M, D), _arg(m_q8, "m_q8", u8, M, D),
+                                    _arg(m_s8, "m_s8", u8, M, (D + 31) // 32), M, D, code, _arg(dm, "dm", dt, M, D),
+                                    _stream(stream))
+    if rc:
+        _check(rc)
     return dm
 
 
@@ -632,31 +673,34 @@ def avits_mxfp4_scale_shape(M: int, K: int) -> tuple:
     return (K + 63) // 64, (M + 7) // 8 * 8, 2
 
 
-def _mx(q, s, name):
-    """Checks a held 4-bit tensor's codes and scales; returns M, K and the pointers."""
-    import torch
-    if q.dim() != 2:
-        raise ValueError(f"{name}: codes must be [M, K / 2]")
-    M, K = q.shape[0], 2 * q.shape[1]
-    _want(s, avits_mxfp4_scale_shape(M, K), f"{name} scales")
-    return M, K, _dev(q, name, torch.uint8), _dev(s, f"{name} scales", torch.uint8)
+def _mx(q, s, name, M, K):
+    """Pointers of an [M, K] tensor held in 4 bits: codes [M, K / 2] and scales."""
+    if K % 2:
+        raise ValueError(f"{name}: {K} columns cannot be held in 4 bits")
+    u8 = (_TYPES or _types())["u8"]
+    return _arg(q, name, u8, M, K // 2), _arg(s, f"{name} scales", u8, (K + 63) // 64, (M + 7) // 8 * 8, 2)
 
 
 def avits_mxfp4_quantize(x, q, s, act=ACT_NONE, stream=None):
     """x [M, K] to codes q [M, K / 2] and scales s (avits_mxfp4_scale_shape),
     uint8; with act=ACT_GELU the values of GELU_tanh(x)."""
     M, K = x.shape
-    Mq, Kq, qp, sp = _mx(q, s, "q")
-    if (Mq, Kq) != (M, K):
-        raise ValueError(f"avits_mxfp4_quantize: q must be [{M}, {K} / 2], got {tuple(q.shape)}")
-    _check(load().avits_mxfp4_quantize(_dev(x, "x"), M, K, act, _dtype_code(x), qp, sp, _stream(stream)))
+    code = _code(x)
+    qp, sp = _mx(q, s, "q", M, K)
+    rc = load().avits_mxfp4_quantize(_arg(x, "x", x.dtype, M, K), M, K, act, code, qp, sp, _stream(stream))
+    if rc:
+        _check(rc)
     return q, s
 
 
 def avits_mxfp4_dequantize(q, s, x, stream=None):
-    M, K, qp, sp = _mx(q, s, "q")
-    _want(x, (M, K), "x")
-    _check(load().avits_mxfp4_dequantize(qp, sp, M, K, _dtype_code(x), _dev(x, "x"), _stream(stream)))
+    """The values that codes q and scales s stand for, to x [M, K]."""
+    M, K = x.shape
+    code = _code(x)
+    qp, sp = _mx(q, s, "q", M, K)
+    rc = load().avits_mxfp4_dequantize(qp, sp, M, K, code, _arg(x, "x", x.dtype, M, K), _stream(stream))
+    if rc:
+        _check(rc)
     return x
 
 
@@ -668,19 +712,19 @@ def avits_mxfp4_linear(xq, xs, wq, ws, b, out, gate=None, resid=None, off=None, 
     """out [M, N] = x W^T + b, x [M, K] and W [N, K] held in 4 bits; with gate
     [N] and resid [M, N], out = resid + gate (x W^T + b), or with a gate [B, N]
     for the rows of B images at the host row offsets off."""
-    M, K, xqp, xsp = _mx(xq, xs, "x")
-    N, Kw, wqp, wsp = _mx(wq, ws, "w")
-    if K != Kw:
-        raise ValueError(f"avits_mxfp4_linear: x has {K} columns, w {Kw}")
-    dt = out.dtype
-    for name, t, shape in (("b", b, (N,)), ("out", out, (M, N)), ("resid", resid, (M, N))):
-        _want(t, shape, name)
+    M, N = out.shape
+    K = 2 * xq.shape[-1]
+    code, dt = _code(out), out.dtype
+    xqp, xsp = _mx(xq, xs, "x", M, K)
+    wqp, wsp = _mx(wq, ws, "w", N, K)
     n, offs = _offsets(off, "avits_mxfp4_linear")
-    (gp,), stride = _mod_rows((("gate", gate),), N, n, dt)
-    buf, bp, nb = _workspace(workspace, avits_mxfp4_linear_workspace_bytes(M, N, K), out.device)
-    _check(load().avits_mxfp4_linear(xqp, xsp, M, K, wqp, wsp, _dev(b, "b", dt), N, n, offs, gp, stride or 0,
-                                     _dev(resid, "resid", dt), _dtype_code(out), _dev(out, "out"), bp, nb,
-                                     _stream(stream)))
+    gp, step = _mod_rows("gate", gate, dt, N, n)
+    buf, bp, nb = _scratch(workspace, lambda: avits_mxfp4_linear_workspace_bytes(M, N, K), out.device)
+    rc = load().avits_mxfp4_linear(xqp, xsp, M, K, wqp, wsp, _arg(b, "b", dt, N), N, n, offs, gp, step or 0,
+                                   _arg(resid, "resid", dt, M, N), code, _arg(out, "out", dt, M, N), bp, nb,
+                                   _stream(stream))
+    if rc:
+        _check(rc)
     return out
 
 
@@ -691,14 +735,14 @@ def avits_mxfp4_linear_backward_workspace_bytes(M: int, N: int, K: int, dtype: i
 def avits_mxfp4_linear_backward(dy, wq, ws, dx, workspace=None, stream=None):
     """dx [M, K] = dy [M, N] W, W [N, K] held in 4 bits."""
     M, N = dy.shape
-    Nw, K, wqp, wsp = _mx(wq, ws, "w")
-    if N != Nw:
-        raise ValueError(f"avits_mxfp4_linear_backward: dy has {N} columns, w {Nw} rows")
-    _want(dx, (M, K), "dx")
-    code = _dtype_code(dy)
-    buf, bp, nb = _workspace(workspace, avits_mxfp4_linear_backward_workspace_bytes(M, N, K, code), dy.device)
-    _check(load().avits_mxfp4_linear_backward(_dev(dy, "dy"), M, N, wqp, wsp, K, code, _dev(dx, "dx", dy.dtype), bp, nb,
-                                              _stream(stream)))
+    K = dx.shape[-1]
+    code, dt = _code(dy), dy.dtype
+    wqp, wsp = _mx(wq, ws, "w", N, K)
+    buf, bp, nb = _scratch(workspace, lambda: avits_mxfp4_linear_backward_workspace_bytes(M, N, K, code), dy.device)
+    rc = load().avits_mxfp4_linear_backward(_arg(dy, "dy", dt, M, N), M, N, wqp, wsp, K, code, _arg(dx, "dx", dt, M, K),
+                                            bp, nb, _stream(stream))
+    if rc:
+        _check(rc)
     return dx
 
 
