@@ -748,6 +748,8 @@ int avits_gelu_backward(const void* da, const void* m, const uint8_t* m_q8, cons
  * images may each have their own gate: B, off and mod_stride as for
  * avits_layer_norm.  b [N] or NULL; out [M, N] may be resid; b, gate, resid and
  * out of dtype.  Sums are fp32, in an order that depends on the sizes only.
+ * avits_mxfp4_linear_workspace_bytes(M, N, K) suffices for any number of rows
+ * up to M; a call that does not split its contraction needs none.
  * avits_mxfp4_linear_backward — the gradient of its input: dx [M, K] = dy W,
  * dy [M, N] and dx of dtype, W as above.
  * Requires 0 <= M < 2^28, 1 <= N < 2^21, K a multiple of 32 in [32, 2^21), and

@@ -51,7 +51,7 @@ def _run(cmd):
 # than half their speed; the selections keep their keys in registers.
 NO_SCRATCH = {"gemm.hip": ("gemm_bf16",), "attention.hip": ("attn_bf16_kernel",),
               "score.hip": ("spatial_temporal_bf16", "finalize_select"), "select.hip": ("radix_select",), 
-              "mxfp4.hip": ("mx4_tile_kernelItLb0ELb1", "mx4_tile_kernelItLb1ELb1", "mx4_tile_kernelIfLb0ELb1")}
+              "mxfp4.hip": ("mx4_tile_kernelItLb0ELb1", "mx4_tile_kernelIfLb0ELb1")}
 _USAGE = ["-Rpass-analysis=kernel-resource-usage"]
 
 

@@ -40,10 +40,14 @@ __device__ __forceinline__ f32x4 mfma4(const u32x4& a, const u32x4& b, const f32
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(va, vb, c, 4, 4, OA, int(sa), OB, int(sb));
 }
 
+// f(0) .. f(N - 1) with compile-time arguments.
+template <typename F, int... I>
+__device__ __forceinline__ void unrolled_over(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>()), ...);
+}
 template <int N, typename F>
 __device__ __forceinline__ void unrolled(F&& f) {
-  [&]<int... I>(std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>()), ...); }
-  (std::make_integer_sequence<int, N>());
+  unrolled_over(f, std::make_integer_sequence<int, N>());
 }
 
 // The scale pairs of T consecutive rows: row i's bytes (block 2 g, 2 g + 1) are
@@ -88,12 +92,12 @@ __device__ __forceinline__ void finish(const Mx4Args& a, int64_t m, int64_t n, f
   st(static_cast<T*>(a.out), m * a.N + n, v);
 }
 
-// Few rows: a workgroup of four waves owns 16 TM x 16 TN outputs, the waves
-// take every fourth step of the contraction straight from memory into
-// registers, and their sums meet in LDS.
-template <int TM, int TN, typename T>
-__global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args a) {
-  __shared__ float red[4][TM * TN * 4][kWave];
+// Few rows: a workgroup of NW waves owns 16 TM x 16 TN outputs, the waves take
+// every NW-th step of the contraction straight from memory into registers (the next
+// one while one is multiplied), and their sums meet in LDS.
+template <int TM, int TN, int NW, typename T>
+__global__ __launch_bounds__(64 * NW) void mx4_rows_kernel(const Mx4Args a) {
+  __shared__ float red[NW][TM * TN * 4][kWave];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int l = lane % 16, g = lane / 16;
   const int64_t tn = (a.N + 16 * TN - 1) / (16 * TN), tiles = tn * ((a.M + 16 * TM - 1) / (16 * TM));
@@ -105,30 +109,42 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args a) {
     const __amdgpu_buffer_rsrc_t rxs = range_of(a.xs, groups * Mp * 2), rws = range_of(a.ws, groups * Np * 2);
     const uint32_t rowb = uint32_t(a.K / 2);
     const int steps = int((a.K + kStepK - 1) / kStepK);
-    f32x4 acc[TM][TN] = {};
-    for (int t = wave; t < steps; t += 4) {
+    struct Step {
       u32x4 x[TM][2], w[TN][2];
+      Pairs<TM> sx;
+      Pairs<TN> sw;
+    };
+    auto load = [&](int t, Step& v) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const uint32_t c = uint32_t(t) * 128 + 32 * g + 16 * k;  // byte of the row; past its end nothing is read
 #pragma unroll
         for (int j = 0; j < TN; ++j)
-          w[j][k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                                  rw, int(c < rowb ? (TN * l + j) * rowb + c : kNowhere), 0, 0));
+          v.w[j][k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                    rw, int(c < rowb ? (TN * l + j) * rowb + c : kNowhere), 0, 0));
 #pragma unroll
         for (int i = 0; i < TM; ++i)
-          x[i][k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                                  rx, int(c < rowb ? (TM * l + i) * rowb + c : kNowhere), 0, 0));
+          v.x[i][k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                    rx, int(c < rowb ? (TM * l + i) * rowb + c : kNowhere), 0, 0));
       }
-      const Pairs<TN> sw = load_pairs<TN>(rws, uint32_t(((4 * t + g) * Np + n0 + TN * l) * 2));
-      const Pairs<TM> sx = load_pairs<TM>(rxs, uint32_t(((4 * t + g) * Mp + m0 + TM * l) * 2));
+      const bool in = t < steps;
+      v.sw = load_pairs<TN>(rws, in ? uint32_t(((4 * t + g) * Np + n0 + TN * l) * 2) : kNowhere);
+      v.sx = load_pairs<TM>(rxs, in ? uint32_t(((4 * t + g) * Mp + m0 + TM * l) * 2) : kNowhere);
+    };
+    f32x4 acc[TM][TN] = {};
+    Step cur, next;
+    load(wave, cur);
+    for (int t = wave; t < steps; t += NW) {
+      load(t + NW, next);
       unrolled<2>([&](auto k) {
         unrolled<TM>([&](auto i) {
           unrolled<TN>([&](auto j) {
-            acc[i][j] = mfma4<2 * (j % 2) + k, 2 * (i % 2) + k>(w[j][k], x[i][k], acc[i][j], sw.v[j / 2], sx.v[i / 2]);
+            acc[i][j] =
+                mfma4<2 * (j % 2) + k, 2 * (i % 2) + k>(cur.w[j][k], cur.x[i][k], acc[i][j], cur.sw.v[j / 2], cur.sx.v[i / 2]);
           });
         });
       });
+      cur = next;
     }
     // acc[i][j][r] = out[m0 + TM l + i][n0 + TN (4 g + r) + j].
 #pragma unroll
@@ -138,40 +154,45 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args a) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) red[wave][(i * TN + j) * 4 + r][lane] = acc[i][j][r];
     __syncthreads();
-    // Wave w finishes register w of every accumulator.
+    // The values of the tile, dealt over the waves.
+    constexpr int kAll = TM * TN * 4;
+    for (int v = wave; v < kAll; v += NW) {
+      const int i = v / (TN * 4), j = v / 4 % TN, r = v % 4;
+      float s = red[0][v][lane];
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int64_t m = m0 + TM * l + i;
-#pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int at = (i * TN + j) * 4 + wave;
-        const float v = (red[0][at][lane] + red[1][at][lane]) + (red[2][at][lane] + red[3][at][lane]);
-        const int64_t n = n0 + TN * (4 * g + wave) + j;
-        if (m < a.M && n < a.N) finish<T>(a, m, n, v);
-      }
+      for (int k = 1; k < NW; ++k) s += red[k][v][lane];
+      const int64_t m = m0 + TM * l + i, n = n0 + TN * (4 * g + r) + j;
+      if (m < a.M && n < a.N) finish<T>(a, m, n, s);
     }
     __syncthreads();  // before the next tile's sums
   }
 }
 
-// Sixteen consecutive elements from element `at` of an array of `n` (zeros
-// past its end), whatever its alignment.
+// Sixteen consecutive elements, held as they lie in memory.
 template <typename T>
-__device__ __forceinline__ void load16(const void* base, int64_t n, int64_t at, float (&v)[16]) {
-  const __amdgpu_buffer_rsrc_t r = range_of(base, base ? n * int64_t(sizeof(T)) : 0);
-#pragma unroll
-  for (int c = 0; c < 16; ++c) {
-    if constexpr (sizeof(T) == 2)
-      v[c] = bf2f(bf16_t(__builtin_amdgcn_raw_buffer_load_b16(r, int((at + c) * 2), 0, 0)));
-    else
-      v[c] = __uint_as_float(uint32_t(__builtin_amdgcn_raw_buffer_load_b32(r, int((at + c) * 4), 0, 0)));
+struct Sixteen {
+  static constexpr int V = int(sizeof(T));  // 16-byte words
+  u32x4 w[V];
+  __device__ __forceinline__ float at(int c) const {
+    const uint32_t x = w[c * V / 16][c * V / 4 % 4];
+    return V == 4 ? __uint_as_float(x) : __uint_as_float(c % 2 ? x & 0xffff0000u : x << 16);
   }
-}
+  // From element `first` of an array of `n` (zeros past its end), whatever its alignment.
+  __device__ __forceinline__ void load(const void* base, int64_t n, int64_t first) {
+    const __amdgpu_buffer_rsrc_t r = range_of(base, base ? n * int64_t(sizeof(T)) : 0);
+#pragma unroll
+    for (int c = 0; c < 4 * V; ++c) {
+      if constexpr (sizeof(T) == 2) {
+        const uint32_t lo = uint16_t(__builtin_amdgcn_raw_buffer_load_b16(r, int((first + 2 * c) * 2), 0, 0));
+        const uint32_t hi = uint16_t(__builtin_amdgcn_raw_buffer_load_b16(r, int((first + 2 * c + 1) * 2), 0, 0));
+        w[c / 4][c % 4] = lo | hi << 16;
+      } else {
+        w[c / 4][c % 4] = uint32_t(__builtin_amdgcn_raw_buffer_load_b32(r, int((first + c) * 4), 0, 0));
+      }
+    }
+  }
+};
 
-// Stores a wave's block: lane (l, g) holds rows
-// mb + TM l + i and, of each, the columns nb + 16 g .. + 15 (register r of
-// accumulator j is column 4 r + j).  Buffer accesses drop what lies outside;
-// where rows do not start on 16 bytes the columns go one by one.
 typedef const __attribute__((address_space(4))) Mx4Args* Mx4ArgsPtr;
 
 // lds_load16 to LDS byte dst + OFF + 16 lane, the sum made in m0 itself.
@@ -180,78 +201,119 @@ __device__ __forceinline__ void lds_load16_at(uint32_t dst, uint32_t voff, const
   asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                ::"s"(dst), "v"(voff), "s"(rsrc), "s"(soff), "n"(OFF) : "memory", "m0", "scc");
 }
-template <int TM, int TN, typename T, bool GATED, bool VEC>
-__device__ __forceinline__ void tile_epilogue(Mx4ArgsPtr a, int64_t mb, int64_t nb, int l, int g,
-                                              const f32x4 (&acc)[TM][TN], const T* bias_lds) {
-  static_assert(TN == 4, "sixteen columns per lane");
-  constexpr int Z = sizeof(T), E = 16 / Z, V = 16 / E;   // elements of a vector, vectors of a lane's columns
-  const int64_t N = a->N;
-  const int rows = int(std::min<int64_t>(16 * TM, a->M - mb)), cols = int(std::min<int64_t>(64, N - nb));
-  const uint32_t ld = uint32_t(N * Z), span = uint32_t((rows - 1) * N * Z + cols * Z);
-  const bool one = a->im.B == 1 || a->im.stride == 0;
-  float gate[16], bias[16];
-  if constexpr (VEC) {
+// Where 2 (bf16) or 4 (fp32) neighbouring lanes hold that many 16-byte chunks each
+// of their own row, chunk q of lane p goes to lane q and comes back as its p:
+// afterwards the lanes hold the chunks of one row side by side. (Its own inverse.)
+template <int CTRL>
+__device__ __forceinline__ void swap_chunks(u32x4& lower, u32x4& upper, bool is_upper) {
 #pragma unroll
-    for (int c = 0; c < 16; ++c) bias[c] = a->bias ? Elem<T>::load(bias_lds, 16 * g + c) : 0.f;
-  } else {
-    load16<T>(a->bias, N, nb + 16 * g, bias);
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t send = is_upper ? lower[e] : upper[e];
+    const uint32_t got = uint32_t(__builtin_amdgcn_update_dpp(0, int(send), CTRL, 0xf, 0xf, false));
+    lower[e] = is_upper ? got : lower[e];
+    upper[e] = is_upper ? upper[e] : got;
   }
-  if (GATED && one) load16<T>(a->gate, N, nb + 16 * g, gate);
-  const __amdgpu_buffer_rsrc_t ro = range_of(static_cast<T*>(a->out) + mb * N + nb, span);
-  const __amdgpu_buffer_rsrc_t rr = range_of(static_cast<const T*>(GATED ? a->resid : a->out) + mb * N + nb, span);
+}
+template <int V>
+__device__ __forceinline__ void turn_chunks(u32x4 (&c)[V], int l) {
+  if constexpr (V == 2) {
+    swap_chunks<kDppXor1>(c[0], c[1], l & 1);
+  } else {
+    swap_chunks<kDppXor1>(c[0], c[1], l & 1);
+    swap_chunks<kDppXor1>(c[2], c[3], l & 1);
+    swap_chunks<kDppXor2>(c[0], c[2], l & 2);
+    swap_chunks<kDppXor2>(c[1], c[3], l & 2);
+  }
+}
+
+// The end of a 128 x 64 block that a wave holds as the tile kernel's sums: lane
+// (l, g) has rows mb + 8 l + i and, of each, the columns nb + 16 g .. + 15.
+// Whole 16-byte chunks of a row are turned over between neighbouring lanes, so
+// that a store instruction covers whole rows of the block (16-byte pieces
+// of 64 bytes each took four times as long), by buffer accesses that drop what lies
+// outside; where rows (or the bias) do not start on 16 bytes the columns go one by one.
+template <typename T, bool GATED, bool VEC>
+struct BlockEnd {
+  static constexpr int Z = sizeof(T), E = 16 / Z, V = 16 / E;   // elements of a chunk, chunks of a lane's columns
+  Mx4ArgsPtr a;
+  int64_t mb, nb, N;
+  int l, g, rows, cols;
+  bool one;
+  Sixteen<T> gate, bias;
+  __amdgpu_buffer_rsrc_t ro, rr;
+
+  // bias_lds: the block's biases (VEC), or null to read them from memory.
+  __device__ __forceinline__ BlockEnd(Mx4ArgsPtr args, int64_t mb_, int64_t nb_, int lane, const T* bias_lds)
+      : a(args), mb(mb_), nb(nb_), N(args->N), l(lane % 16), g(lane / 16),
+        rows(int(std::min<int64_t>(128, args->M - mb_))), cols(int(std::min<int64_t>(64, args->N - nb_))),
+        one(args->im.B == 1 || args->im.stride == 0) {
+    if (VEC && bias_lds) {
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int row = TM * l + i;
-    const uint32_t at = uint32_t(row) * ld + uint32_t(16 * g * Z);
-    float v[16];
+      for (int q = 0; q < V; ++q)
+        bias.w[q] = a->bias ? *reinterpret_cast<const u32x4*>(bias_lds + 16 * g + E * q) : u32x4{0u, 0u, 0u, 0u};
+    } else {
+      bias.load(a->bias, N, nb + 16 * g);
+    }
+    if (GATED && one) gate.load(a->gate, N, nb + 16 * g);
+    const int64_t span = ((rows - 1) * N + cols) * Z;
+    ro = range_of(static_cast<T*>(a->out) + mb * N + nb, span);
+    if (GATED) rr = range_of(static_cast<const T*>(a->resid) + mb * N + nb, span);
+  }
+  // Offset of chunk q after the turn: row 8 (l with its low bits q) + i, chunk V g + (l's low bits).
+  __device__ __forceinline__ uint32_t at(int i, int q) const {
+    const int chunk = V * g + (l & (V - 1)), row = 8 * ((l & ~(V - 1)) + q) + i;
+    return E * chunk < cols ? uint32_t(row) * uint32_t(N * Z) + 16 * chunk : kNowhere;
+  }
+  __device__ __forceinline__ void row(int i, float (&v)[16]) {
 #pragma unroll
-    for (int c = 0; c < 16; ++c) v[c] = acc[i][c % 4][c / 4] + bias[c];
+    for (int c = 0; c < 16; ++c) v[c] += bias.at(c);
+    const int r = 8 * l + i;
     if constexpr (GATED) {
       if (!one) {
         int64_t skip = 0;
-        const int64_t stride = a->im.stride, at_row = mb + std::min(row, rows - 1);
+        const int64_t stride = a->im.stride, at_row = mb + std::min(r, rows - 1);
 #pragma unroll 1
         for (int b = 0; b < a->im.B - 1; ++b) skip += at_row >= a->im.end[b] ? stride : 0;  // scalars are short: rolled
+        // (No uniform base: element loads; columns past N repeat the last one, unused.)
         const T* p = static_cast<const T*>(a->gate) + skip + nb;
 #pragma unroll
-        for (int c = 0; c < 16; ++c) gate[c] = Elem<T>::load(p, std::min(16 * g + c, cols - 1));
+        for (int c = 0; c < 16; ++c) {
+          const int at_c = std::min(16 * g + c, cols - 1);
+          if constexpr (Z == 4) gate.w[c / 4][c % 4] = __float_as_uint(p[at_c]);
+          else if (c % 2 == 0) gate.w[c / 8][c / 2 % 4] = p[at_c];
+          else gate.w[c / 8][c / 2 % 4] |= uint32_t(p[at_c]) << 16;
+        }
       }
-      float res[16];
+      Sixteen<T> res;
       if constexpr (VEC) {
 #pragma unroll
-        for (int q = 0; q < V; ++q) {
-          const u32x4 w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                              rr, int(16 * g + E * q < cols ? at + 16 * q : kNowhere), 0, 0));
-#pragma unroll
-          for (int e = 0; e < E; ++e)
-            res[E * q + e] = Z == 4 ? __uint_as_float(w[e % 4])
-                                    : __uint_as_float(e % 2 ? w[e / 2 % 4] & 0xffff0000u : w[e / 2 % 4] << 16);
-        }
+        for (int q = 0; q < V; ++q)
+          res.w[q] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, int(at(i, q)), 0, 0));
+        turn_chunks<V>(res.w, l);
       } else {
-        const T* p = static_cast<const T*>(a->resid) + (mb + std::min(row, rows - 1)) * N + nb;
-#pragma unroll
-        for (int c = 0; c < 16; ++c) res[c] = Elem<T>::load(p, std::min(16 * g + c, cols - 1));
+        res.load(static_cast<const T*>(a->resid) + mb * N, int64_t(rows) * N, int64_t(std::min(r, rows - 1)) * N + nb + 16 * g);
       }
 #pragma unroll
-      for (int c = 0; c < 16; ++c) v[c] = res[c] + gate[c] * v[c];
+      for (int c = 0; c < 16; ++c) v[c] = res.at(c) + gate.at(c) * v[c];
     }
     if constexpr (VEC) {
+      u32x4 w[V];
 #pragma unroll
-      for (int q = 0; q < V; ++q) {
-        u32x4 w;
+      for (int q = 0; q < V; ++q)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          w[e] = Z == 4 ? __float_as_uint(v[4 * q % 16 + e]) : pack_bf2(v[(8 * q + 2 * e) % 16], v[(8 * q + 2 * e + 1) % 16]);
-        __builtin_amdgcn_raw_buffer_store_b128(w, ro, int(16 * g + E * q < cols ? at + 16 * q : kNowhere), 0, 0);
-      }
-    } else if (row < rows) {
-      T* p = static_cast<T*>(a->out) + (mb + row) * N + nb;
+          w[q][e] = Z == 4 ? __float_as_uint(v[4 * q % 16 + e]) : pack_bf2(v[(8 * q + 2 * e) % 16], v[(8 * q + 2 * e + 1) % 16]);
+      turn_chunks<V>(w, l);
+#pragma unroll
+      for (int q = 0; q < V; ++q) __builtin_amdgcn_raw_buffer_store_b128(w[q], ro, int(at(i, q)), 0, 0);
+    } else if (r < rows) {
+      T* p = static_cast<T*>(a->out) + (mb + r) * N + nb;
 #pragma unroll
       for (int c = 0; c < 16; ++c)
         if (16 * g + c < cols) st(p, 16 * g + c, v[c]);
     }
   }
-}
+};
 
 // Many rows: 256 x 256 outputs to a workgroup of eight waves, a step of 256
 // elements (128 bytes of every row) at a time.  In bytes and matrix cycles this
@@ -275,12 +337,14 @@ __device__ __forceinline__ void tile_epilogue(Mx4ArgsPtr a, int64_t mb, int64_t 
 // The contraction is short (8 steps for K = 2048), so a tile's head and tail
 // are hidden too: a workgroup keeps taking tiles, the next tile's first loads go out before
 // the stores of the last, and the waits for them leave those stores in flight.
-template <typename T, bool GATED, bool VEC>
-__global__ __launch_bounds__(512) void mx4_tile_kernel(const Mx4Args args, uint32_t units) {
+// PARTS: a tile is `splits` units, each a part of the contraction, and a unit's sums go
+// to out as the registers lie: 16 bytes of every lane side by side, 256 KB a unit.
+template <typename T, bool GATED, bool VEC, bool PARTS>
+__global__ __launch_bounds__(512) void mx4_tile_kernel(const Mx4Args args, uint32_t units, uint32_t splits) {
   constexpr int TM = 8, TN = 4;
   // LDS in bytes: half a step of one operand is 16 KB.
   constexpr uint32_t kHalf = 0x4000, kA = 0, kWf = 4 * kHalf, kWs = 6 * kHalf, kS = 9 * kHalf, kSc = 0x1000, kB = kS + 3 * kSc;
-  constexpr int kStores = TM * int(sizeof(T));       // store instructions of an epilogue of vectors
+  constexpr int kStores = PARTS ? 32 : TM * int(sizeof(T));   // store instructions of an epilogue of vectors
   __shared__ __attribute__((aligned(16))) char lds[kB + 2 * 1024];
   Mx4ArgsPtr a = (Mx4ArgsPtr)__builtin_amdgcn_kernarg_segment_ptr();  // scalar loads where needed
   const int tid = threadIdx.x;
@@ -300,7 +364,7 @@ __global__ __launch_bounds__(512) void mx4_tile_kernel(const Mx4Args args, uint3
   const uint32_t lds0 = uint32_t(scalar(int(uint32_t(reinterpret_cast<uintptr_t>(
       (__attribute__((address_space(3))) char*)(&lds[0]))))));
   const uint32_t rowb = uint32_t(a->K / 2), tn_all = uint32_t((a->N + 255) / 256), tm_all = uint32_t((a->M + 255) / 256);
-  const int n_t = int((rowb + 127) / 128), n_whole = int(rowb / 128);
+  const int n_all = int((rowb + 127) / 128), n_whole = int(rowb / 128);
 
   // What a step needs per lane is made once: beside the matrix instructions of
   // the other group's wave every instruction of a memory phase costs its time.
@@ -337,7 +401,8 @@ __global__ __launch_bounds__(512) void mx4_tile_kernel(const Mx4Args args, uint3
   const uint32_t srow = uint32_t(scale_rows(sc_w ? a->N : a->M) * 2);
 
   // The tile in work: its place and where its loads start.
-  int tm = 0, tn = 0;
+  int tm = 0, tn = 0, part = 0;
+  int t0 = 0, n_t = 0;       // its first step, and how many it has
   u32x4 xr = {}, wr = {}, sr = {};
   uint32_t unit0 = 0;
   auto take = [&]() {   // the next tile of this workgroup; false: none
@@ -346,9 +411,13 @@ __global__ __launch_bounds__(512) void mx4_tile_kernel(const Mx4Args args, uint3
       unit0 = here + n;
       if (blockIdx.x >= n) continue;
       int prob;
-      pp_place(here + xcd_logical_id32(blockIdx.x, n), tn_all, tm_all, 0, prob, tm, tn);
+      const uint32_t unit = here + xcd_logical_id32(blockIdx.x, n);
+      if (PARTS) part = scalar(int(unit));
+      pp_place(unit / splits, tn_all, tm_all, 0, prob, tm, tn);
       tm = scalar(tm);
       tn = scalar(tn);
+      t0 = scalar(int(uint32_t(n_all) * (unit % splits) / splits));
+      n_t = scalar(int(uint32_t(n_all) * (unit % splits + 1) / splits)) - t0;
       const int64_t m0 = int64_t(tm) * 256, n0 = int64_t(tn) * 256;
       xr = uniform(buffer_rsrc(a->xq + m0 * rowb, uint32_t(std::min<int64_t>((a->M - m0) * rowb, kNowhere))));
       wr = uniform(buffer_rsrc(a->wq + n0 * rowb, uint32_t(std::min<int64_t>((a->N - n0) * rowb, kNowhere))));
@@ -363,8 +432,8 @@ __global__ __launch_bounds__(512) void mx4_tile_kernel(const Mx4Args args, uint3
   auto load_half = [&](const u32x4& r, const uint32_t (&off)[4], uint32_t dst, int t) {
     const bool live = t < n_t;
     const u32x4 rr = {r[0], r[1], live ? r[2] : 0u, r[3]};
-    const uint32_t k = live ? uint32_t(t) * 128 : 0u;
-    if (t < n_whole) {
+    const uint32_t k = live ? uint32_t(t0 + t) * 128 : 0u;
+    if (t0 + t < n_whole) {
       lds_load16_at<0>(dst, off[0], rr, k);
       lds_load16_at<0x1000>(dst, off[1], rr, k);
       lds_load16_at<0x2000>(dst, off[2], rr, k);
@@ -386,7 +455,7 @@ __global__ __launch_bounds__(512) void mx4_tile_kernel(const Mx4Args args, uint3
     const bool live = t < n_t;
     const u32x4 rr = {sr[0], sr[1], live ? sr[2] : 0u, sr[3]};
     const int lane = lane_id();
-    const uint32_t off = (4 * uint32_t(t) + 2 * (sub & 1) + lane / 32) * srow + 16 * (lane % 32);
+    const uint32_t off = (4 * uint32_t(t0 + t) + 2 * (sub & 1) + lane / 32) * srow + 16 * (lane % 32);
     lds_load16_at<0>(own + kS + slot3 * kSc, live ? off : kNowhere, rr, 0u);
   };
 
@@ -423,6 +492,7 @@ __global__ __launch_bounds__(512) void mx4_tile_kernel(const Mx4Args args, uint3
 
   int par = 0;               // which of two places the loads' tile has its biases in
   int64_t mb = -1, nb = 0;   // the finished tile's block of this wave
+  int done = 0;              // and its unit
   for (;;) {
     // Every fragment of the finished tile has been read (group 0 is a barrier
     // past group 1's last read): the slots are free.  A wave's own late loads
@@ -450,9 +520,22 @@ __global__ __launch_bounds__(512) void mx4_tile_kernel(const Mx4Args args, uint3
     // acc[i][j][r] = out[mb + 8 l + i][nb + 16 g + 4 r + j].
     const bool out = mb >= 0 && mb < a->M && nb < a->N;
     if (out) {
-      const int lane = lane_id();
-      tile_epilogue<TM, TN, T, GATED, VEC>(a, mb, nb, lane % 16, lane / 16, acc,
-                                           reinterpret_cast<const T*>(lds + kB + 1024 * (par ^ 1)) + 64 * sub);
+      if constexpr (PARTS) {
+        f32x4* p = static_cast<f32x4*>(a->out) + (int64_t(done) * 8 + wave) * (TM * TN * kWave) + lane_id();
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) p[(i * TN + j) * kWave] = acc[i][j];
+      } else {
+        BlockEnd<T, GATED, VEC> end(a, mb, nb, lane_id(), reinterpret_cast<const T*>(lds + kB + 1024 * (par ^ 1)) + 64 * sub);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          float v[16];
+#pragma unroll
+          for (int c = 0; c < 16; ++c) v[c] = acc[i][c % 4][c / 4];
+          end.row(i, v);
+        }
+      }
     }
     if (!more) break;
     par ^= 1;
@@ -460,6 +543,7 @@ __global__ __launch_bounds__(512) void mx4_tile_kernel(const Mx4Args args, uint3
     int young = scalar(out && VEC ? 1 : 0);
     mb = int64_t(tm) * 256 + 128 * grp;
     nb = int64_t(tn) * 256 + 64 * sub;
+    done = part;
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -509,6 +593,137 @@ __global__ __launch_bounds__(512) void mx4_tile_kernel(const Mx4Args args, uint3
     }
   }
   vm_wait<0>();   // loads to LDS end before the workgroup does
+}
+
+// Joins the parts of a split product in their order: a workgroup a 128 x 64 block,
+// a wave two of its eight row groups.
+template <typename T, bool GATED, bool VEC>
+__global__ __launch_bounds__(256) void mx4_join_kernel(const Mx4Args args, const float* __restrict__ parts, uint32_t splits) {
+  const Mx4ArgsPtr a = (Mx4ArgsPtr)__builtin_amdgcn_kernarg_segment_ptr();
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const uint32_t tile = blockIdx.x / 8, block = blockIdx.x % 8;
+  int prob, tm, tn;
+  pp_place(tile, uint32_t((a->N + 255) / 256), uint32_t((a->M + 255) / 256), 0, prob, tm, tn);
+  const int64_t mb = int64_t(tm) * 256 + 128 * (block / 4), nb = int64_t(tn) * 256 + 64 * (block % 4);
+  if (mb >= a->M || nb >= a->N) return;
+  BlockEnd<T, GATED, VEC> end(a, mb, nb, lane, nullptr);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int i = 2 * wave + h;
+    f32x4 sum[4] = {};
+    for (uint32_t k = 0; k < splits; ++k) {
+      const f32x4* p = reinterpret_cast<const f32x4*>(parts) + ((int64_t(tile) * splits + k) * 8 + block) * (32 * kWave) +
+                       i * 4 * kWave + lane;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum[j] += p[j * kWave];
+    }
+    float v[16];
+#pragma unroll
+    for (int c = 0; c < 16; ++c) v[c] = sum[c % 4][c / 4];
+    end.row(i, v);
+  }
+}
+
+// The input gradient for few rows, straight from the held weight: a workgroup
+// of NW waves owns 16 TM rows x 128 columns of dx, the waves take every NW-th 32
+// rows n of W (the contraction) and their sums meet in LDS.  A lane loads 8 rows n =
+// 8 g + e of W, 8 columns k = 8 l + t of each (one dword, one scale; the eight rows'
+// scales lie side by side), turns them into bf16 (exact: e2m1 times a power of
+// two) and has, for each t, the operand of one bf16 instruction: 8 n of column k.
+// So the result's lane holds 8 consecutive columns of rows 4 g + r.
+// Bound by the conversions (about 220 vector instructions for 8 TM matrix ones).
+// blockIdx.y: part of the contraction, summed into its own [M, K] where there are several.
+template <int TM, int NW, typename OUT>
+__global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const bf16_t* __restrict__ dy, int64_t M, int64_t N,
+                                                                const uint8_t* __restrict__ wq, const uint8_t* __restrict__ ws,
+                                                                int64_t K, OUT* __restrict__ dx) {
+  __shared__ float red[NW][TM * 32][kWave];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int l = lane % 16, g = lane / 16;
+  const int64_t tk = (K + 127) / 128;
+  const int64_t k0 = int64_t(blockIdx.x) % tk * 128, m0 = int64_t(blockIdx.x) / tk * (16 * TM);
+  const int64_t Np = scale_rows(N), rowb = K / 2, k = k0 + 8 * l;
+  const __amdgpu_buffer_rsrc_t rs = range_of(ws, scale_groups(K) * Np * 2);
+  const __amdgpu_buffer_rsrc_t ry = range_of(dy + m0 * N, (M - m0) * N * 2);
+  const int shift = 8 * int(k / 32 % 2);
+  const int steps = int((N + 31) / 32);
+  f32x4 acc[TM][8] = {};
+  struct Step {
+    uint32_t w[8];
+    u32x4 sc, y[TM];
+  };
+  // (Past the last step everything is out of range: zeros, no memory.)
+  auto load = [&](int t, Step& v) {
+    const int64_t n = int64_t(t) * 32 + 8 * g;   // N is a multiple of 8: the lane's eight rows are there or not
+    const __amdgpu_buffer_rsrc_t rw = range_of(wq + int64_t(t) * 32 * rowb, (N - int64_t(t) * 32) * rowb);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      v.w[e] = uint32_t(__builtin_amdgcn_raw_buffer_load_b32(
+          rw, int(k < K ? uint32_t((8 * g + e) * rowb + k / 2) : kNowhere), 0, 0));
+    v.sc = __builtin_bit_cast(
+        u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, int(k < K && n < N ? uint32_t((k / 64 * Np + n) * 2) : kNowhere), 0, 0));
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+      v.y[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                             ry, int(n < N ? uint32_t(((16 * i + l) * N + n) * 2) : kNowhere), 0, 0));
+  };
+  const int stride = NW * int(gridDim.y);
+  int t = int(blockIdx.y) * NW + wave;
+  Step cur, next;
+  load(t, cur);
+  for (; t < steps; t += stride) {
+    load(t + stride, next);
+    u32x4 f[8];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      float a[8], b[8];
+      const uint32_t pair = cur.sc[e / 2] >> shift;
+      decode4x8(cur.w[e], scale_value(pair & 255u), a);
+      decode4x8(cur.w[e + 1], scale_value(pair >> 16 & 255u), b);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) f[c][e / 2] = pack_bf2(a[c], b[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+#pragma unroll
+      for (int i = 0; i < TM; ++i) acc[i][c] = mfma16x16x32(as_bf16x8(cur.y[i]), as_bf16x8(f[c]), acc[i][c]);
+    cur = next;
+  }
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) red[wave][(i * 4 + r) * 8 + c][lane] = acc[i][c][r];
+  __syncthreads();
+  dx += int64_t(blockIdx.y) * M * K;
+  // The 4 TM groups of eight columns of a lane, dealt over the waves.
+  for (int v = wave; v < 4 * TM; v += NW) {
+    float o[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      o[c] = red[0][v * 8 + c][lane];
+#pragma unroll
+      for (int u = 1; u < NW; ++u) o[c] += red[u][v * 8 + c][lane];
+    }
+    const int64_t m = m0 + 16 * (v / 4) + 4 * g + v % 4;
+    if (m < M && k < K) store8(dx + m * K + k, o);
+  }
+}
+
+// Sums of `parts` [n] arrays, in their order, as bf16 (n a multiple of 8).
+__global__ __launch_bounds__(256) void mx4_back_join_kernel(const float* __restrict__ part, int64_t n, int parts,
+                                                            bf16_t* __restrict__ dx) {
+  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 8;
+  if (i >= n) return;
+  float v[8], t[8];
+  load8(part + i, v);
+  for (int k = 1; k < parts; ++k) {
+    load8(part + k * n + i, t);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += t[e];
+  }
+  store8(dx + i, v);
 }
 
 // The weight as T values, transposed: wt [K, ld] with zeros in columns N .. ld.
@@ -561,23 +776,103 @@ int check_product(const char* who, int64_t M, int64_t N, int64_t K, int dtype) {
   return AVITS_OK;
 }
 
-template <typename T>
-void run_product(const Mx4Args& a, hipStream_t s) {
-  TimedLaunch timed("mxfp4_linear", s);
-  auto grid = [&](int tm, int tn) {
-    return dim3(unsigned(std::min<int64_t>(ceil_div64(a.M, 16 * tm) * ceil_div64(a.N, 16 * tn), 1 << 22)));
-  };
-  const int64_t units = ceil_div64(a.M, 256) * ceil_div64(a.N, 256);
-  if (a.M <= 16) hipLaunchKernelGGL((mx4_rows_kernel<1, 2, T>), grid(1, 2), dim3(256), 0, s, a);
-  else if (units >= 128) {
-    const dim3 grid(unsigned(ceil_div64(units, ceil_div64(units, 256)))), wg(512);
-    const bool vec = a.N % (16 / int64_t(sizeof(T))) == 0 && aligned_to({a.bias}, 16);
-    if (a.gate && vec) hipLaunchKernelGGL((mx4_tile_kernel<T, true, true>), grid, wg, 0, s, a, uint32_t(units));
-    else if (a.gate) hipLaunchKernelGGL((mx4_tile_kernel<T, true, false>), grid, wg, 0, s, a, uint32_t(units));
-    else if (vec) hipLaunchKernelGGL((mx4_tile_kernel<T, false, true>), grid, wg, 0, s, a, uint32_t(units));
-    else hipLaunchKernelGGL((mx4_tile_kernel<T, false, false>), grid, wg, 0, s, a, uint32_t(units));
+
+// How a product runs: 256 x 256 tiles, each in `splits` parts of the contraction,
+// or (splits == 0) form `rows` of the kernel for few rows.  The least predicted
+// time (us), from what was measured:
+//  - few rows: the larger of the operands' bytes, which each workgroup reads for
+//    itself, at the rate its form reaches, and its chain of steps over its waves;
+//  - tiles, in equal rounds of at most one unit per CU: 1.2 (few CUs busy) to 1.5 a
+//    step and 6.5 a unit; parts are written and read at 7 TB/s by a second launch.
+// Measured (bf16 out; forms 1 x 1, 2 x 2, 4 x 2, 4 x 4 strips of 16, tiles whole, in 4 parts):
+//   16 x 8192 x 2048    5.5   5.0   6.2  10.3  15.6  21.5     32 x 2048 x 8192     7.0  11.8  13.7  21.1  45.5  23.1
+//   64 x 8192 x 2048   14.6   8.7   8.2  12.5  15.7  21.6     300 x 4096 x 4096   42.5  25.8  28.5  24.6  26.7  26.9
+//   512 x 8192 x 2048  93.1  49.4  51.5  35.1  17.9  32.1     1741 x 2048 x 8192   214   112   103  75.5  47.5  36.9
+constexpr struct {
+  int tm, tn, waves;
+  double fixed, rate, step;   // us beside, TB/s from the caches, us a step of the chain
+} kForms[4] = {{1, 1, 8, 2.5, 7.0, 1.1}, {2, 2, 8, 2.5, 7.0, 2.3}, {4, 2, 8, 3.5, 6.0, 2.6}, {4, 4, 4, 6.0, 4.8, 2.0}};
+struct ProductPlan {
+  int splits = 0, form = 0;
+};
+constexpr size_t kMaxPartBytes = size_t(64) << 20;
+constexpr int kCUs = 256, kMaxSplits = 4;
+size_t part_bytes(int splits, int64_t M, int64_t N) {
+  return size_t(splits) * size_t(ceil_div64(M, 256)) * size_t(ceil_div64(N, 256)) * (256 * 256 * sizeof(float));
+}
+ProductPlan plan_product(int64_t M, int64_t N, int64_t K) {
+  ProductPlan p;
+  const double steps = double(ceil_div64(K, kStepK));
+  double best = 1e30;
+  for (int f = 0; f < 4; ++f) {
+    const auto& form = kForms[f];
+    const double wgs = double(ceil_div64(M, 16 * form.tm)) * double(ceil_div64(N, 16 * form.tn));
+    const double bytes = wgs * 16.0 * (form.tm + form.tn) * double(K) * 0.53e-6;
+    const double us = form.fixed + std::max(bytes / form.rate, std::ceil(steps / form.waves) * form.step);
+    if (us >= best) continue;
+    best = us;
+    p.form = f;
   }
-  else hipLaunchKernelGGL((mx4_rows_kernel<4, 4, T>), grid(4, 4), dim3(256), 0, s, a);
+  const double tiles = double(ceil_div64(M, 256)) * double(ceil_div64(N, 256));
+  for (int sp = 1; sp <= kMaxSplits && sp <= int(steps); ++sp) {
+    if (sp > 1 && part_bytes(sp, M, N) > kMaxPartBytes) break;
+    const double units = tiles * sp, rounds = std::ceil(units / kCUs), per = std::ceil(units / rounds);
+    const double us = rounds * (std::ceil(steps / sp) * (1.2 + 0.3 * per / kCUs) + 6.5) +
+                      (sp > 1 ? 3.0 + 2e-6 * double(part_bytes(sp, M, N)) / 7.0 : 0.0);
+    if (us >= best) continue;
+    best = us;
+    p.splits = sp;
+  }
+  return p;
+}
+
+template <typename T>
+void run_product(const Mx4Args& a, const ProductPlan& p, float* part, hipStream_t s) {
+  TimedLaunch timed("mxfp4_linear", s);
+  auto rows = [&](auto tm, auto tn, auto nw) {
+    constexpr int kTM = decltype(tm)::value, kTN = decltype(tn)::value, kNW = decltype(nw)::value;
+    const int64_t tiles = ceil_div64(a.M, 16 * kTM) * ceil_div64(a.N, 16 * kTN);
+    hipLaunchKernelGGL((mx4_rows_kernel<kTM, kTN, kNW, T>), dim3(unsigned(std::min<int64_t>(tiles, 1 << 22))), dim3(64 * kNW), 0,
+                       s, a);
+  };
+  using std::integral_constant;
+  const integral_constant<int, 1> one;
+  const integral_constant<int, 2> two;
+  const integral_constant<int, 4> four;
+  const integral_constant<int, 8> eight;
+  if (p.splits == 0) {
+    if (p.form == 0) rows(one, one, eight);
+    else if (p.form == 1) rows(two, two, eight);
+    else if (p.form == 2) rows(four, two, eight);
+    else rows(four, four, four);
+    return;
+  }
+  const int64_t units = ceil_div64(a.M, 256) * ceil_div64(a.N, 256) * p.splits;
+  const dim3 grid(unsigned(ceil_div64(units, ceil_div64(units, kCUs)))), wg(512);
+  const bool vec = a.N % (16 / int64_t(sizeof(T))) == 0 && aligned_to({a.bias}, 16);
+  auto by_form = [&](auto go) {
+    const std::true_type yes;
+    const std::false_type no;
+    if (a.gate && vec) go(yes, yes);
+    else if (a.gate) go(yes, no);
+    else if (vec) go(no, yes);
+    else go(no, no);
+  };
+  if (p.splits == 1) {
+    by_form([&](auto gated, auto vectors) {
+      hipLaunchKernelGGL((mx4_tile_kernel<T, decltype(gated)::value, decltype(vectors)::value, false>), grid, wg, 0, s, a,
+                         uint32_t(units), 1u);
+    });
+    return;
+  }
+  Mx4Args g = a;
+  g.bias = nullptr;
+  g.out = part;
+  hipLaunchKernelGGL((mx4_tile_kernel<float, false, true, true>), grid, wg, 0, s, g, uint32_t(units), uint32_t(p.splits));
+  by_form([&](auto gated, auto vectors) {
+    hipLaunchKernelGGL((mx4_join_kernel<T, decltype(gated)::value, decltype(vectors)::value>),
+                       dim3(unsigned(units / p.splits * 8)), dim3(256), 0, s, a, (const float*)part, uint32_t(p.splits));
+  });
 }
 
 // Scratch of the input gradient: the weight transposed in dtype, dy widened where
@@ -585,7 +880,17 @@ void run_product(const Mx4Args& a, hipStream_t s) {
 struct BackPlan {
   int64_t ld;
   size_t wt, dy, part;
+  int rows = 0, parts = 1;   // rows > 0: the kernel for few rows with 16 `rows` rows to a workgroup
 };
+// Few rows (bf16, rows of dy whole 16-byte chunks) go straight from the held
+// weight, 16 of them to a workgroup of eight waves (two of which fit a CU) or 64 to
+// one of four, the contraction whole or in parts; the other way is to turn the
+// weight round and run the bf16 product.  The least predicted time (us).  A chain
+// step takes 1.0 us (1.7 with two workgroups on a CU; 1.2 with 64 rows), parts a
+// launch and their bytes.  Measured (16 rows whole, in 4; 64 rows in 4; turned round):
+//   16 x 8192 x 2048   33.3  13.6  24.4  45.9     512 x 8192 x 2048  56.6  59.6  48.0  46.9
+//   128 x 8192 x 2048  33.0  21.0  25.6  44.1     67 x 1024 x 256     6.6   6.5   9.1  13.4
+//   256 x 8192 x 2048  33.6  34.3  26.8  44.3     64 x 2048 x 8192   10.7  17.9  16.0  32.3
 BackPlan plan_back(int64_t M, int64_t N, int64_t K, int dtype) {
   const size_t z = dtype == AVITS_BF16 ? 2 : 4;
   BackPlan p;
@@ -593,6 +898,23 @@ BackPlan plan_back(int64_t M, int64_t N, int64_t K, int dtype) {
   p.wt = align_up(size_t(K) * size_t(p.ld) * z, 256);
   p.dy = p.ld != N ? align_up(size_t(M) * size_t(p.ld) * z, 256) : 0;
   p.part = dtype == AVITS_BF16 ? std::min<size_t>(gemm_partial_reserve(M, K), size_t(64) << 20) : 0;
+  if (dtype == AVITS_BF16 && N % 8 == 0) {
+    const double weights = double(N) * double(K) * 1e-6;
+    double best = 16.0 + weights * 4.5 / 4.0 + 2.0 * double(M) * weights / 1.1e6;
+    for (int rows : {1, 4})
+      for (int parts = 1; parts <= 8; parts *= 2) {
+        const int waves = rows == 1 ? 8 : 4;
+        const int64_t steps = ceil_div64(N, 32), wgs = ceil_div64(M, 16 * rows) * ceil_div64(K, 128) * parts;
+        if (parts > 1 && (steps < parts * waves || size_t(parts) * size_t(M) * size_t(K) * sizeof(float) > kMaxPartBytes)) break;
+        const double step = rows == 4 ? 1.2 : wgs <= kCUs ? 1.0 : 1.7;
+        const double us = 2.5 + double(ceil_div64(steps, waves * parts)) * step * double(ceil_div64(wgs, rows == 4 ? kCUs : 2 * kCUs)) +
+                          (parts > 1 ? 2.5 + double(parts) * double(M) * double(K) * 8e-6 / 4.0 : 0.0);
+        if (us >= best) continue;
+        best = us;
+        p.rows = rows;
+        p.parts = parts;
+      }
+  }
   return p;
 }
 
@@ -600,6 +922,31 @@ template <typename T>
 int run_back(const void* dy, int64_t M, int64_t N, const uint8_t* wq, const uint8_t* ws, int64_t K, int dtype, void* dx,
              char* scratch, hipStream_t s) {
   const BackPlan p = plan_back(M, N, K, dtype);
+  if constexpr (sizeof(T) == 2) {
+    if (p.rows) {
+      TimedLaunch timed("mxfp4_backward", s);
+      const bf16_t* y = static_cast<const bf16_t*>(dy);
+      auto go = [&](auto tm, auto nw, auto* out) {
+        constexpr int kTM = decltype(tm)::value, kNW = decltype(nw)::value;
+        const dim3 grid(unsigned(ceil_div64(M, 16 * kTM) * ceil_div64(K, 128)), unsigned(p.parts));
+        hipLaunchKernelGGL((mx4_back_rows_kernel<kTM, kNW, std::remove_pointer_t<decltype(out)>>), grid, dim3(64 * kNW), 0, s, y, M,
+                           N, wq, ws, K, out);
+      };
+      using std::integral_constant;
+      auto by_rows = [&](auto* out) {
+        if (p.rows == 1) go(integral_constant<int, 1>(), integral_constant<int, 8>(), out);
+        else go(integral_constant<int, 4>(), integral_constant<int, 4>(), out);
+      };
+      if (p.parts == 1) {
+        by_rows(static_cast<bf16_t*>(dx));
+        return launch_status("mxfp4_linear_backward");
+      }
+      by_rows(reinterpret_cast<float*>(scratch));
+      hipLaunchKernelGGL(mx4_back_join_kernel, dim3(unsigned(ceil_div64(M * K / 8, 256))), dim3(256), 0, s,
+                         reinterpret_cast<const float*>(scratch), M * K, p.parts, static_cast<bf16_t*>(dx));
+      return launch_status("mxfp4_linear_backward");
+    }
+  }
   T* wt = reinterpret_cast<T*>(scratch);
   {
     TimedLaunch timed("mxfp4_transpose", s);
@@ -630,8 +977,9 @@ int run_back(const void* dy, int64_t M, int64_t N, const uint8_t* wq, const uint
 using namespace avits;
 
 extern "C" size_t avits_mxfp4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-  if (check_product("mxfp4_linear_workspace_bytes", M, N, K, AVITS_BF16) != AVITS_OK) return 0;
-  return 0;
+  if (check_product("mxfp4_linear_workspace_bytes", M, N, K, AVITS_BF16) != AVITS_OK || M == 0) return 0;
+  const int64_t steps = ceil_div64(K, kStepK);
+  return steps < 2 ? 0 : std::min(kMaxPartBytes, part_bytes(int(std::min<int64_t>(steps, kMaxSplits)), M, N));
 }
 
 extern "C" int avits_mxfp4_linear(const uint8_t* xq, const uint8_t* xs, int64_t M, int64_t K, const uint8_t* wq,
@@ -646,19 +994,23 @@ extern "C" int avits_mxfp4_linear(const uint8_t* xq, const uint8_t* xs, int64_t 
   AVITS_REQUIRE(xq && xs && wq && ws && out, "mxfp4_linear: null xq/xs/wq/ws/out");
   AVITS_REQUIRE(aligned_to({xq, xs, wq, ws, out, resid}, 16), "mxfp4_linear: xq, xs, wq, ws, resid and out must be 16-byte aligned");
   AVITS_REQUIRE(aligned_to({b, gate}, dtype == AVITS_BF16 ? 2 : 4), "mxfp4_linear: b or gate is not aligned to its element");
-  const size_t need = avits_mxfp4_linear_workspace_bytes(M, N, K);
+  const ProductPlan p = plan_product(M, N, K);
+  const size_t need = p.splits > 1 ? part_bytes(p.splits, M, N) : 0;
   if (need && (!workspace || workspace_bytes < need))
     return set_error(AVITS_ERR_WORKSPACE, "mxfp4_linear: workspace of %zu bytes, need %zu", workspace_bytes, need);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (dtype == AVITS_BF16) run_product<bf16_t>(a, s);
-  else run_product<float>(a, s);
+  AVITS_REQUIRE(!need || aligned_to({workspace}, 16), "mxfp4_linear: workspace must be 16-byte aligned");
+  if (dtype == AVITS_BF16) run_product<bf16_t>(a, p, static_cast<float*>(workspace), s);
+  else run_product<float>(a, p, static_cast<float*>(workspace), s);
   return launch_status("mxfp4_linear");
 }
 
 extern "C" size_t avits_mxfp4_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, int dtype) {
   if (check_product("mxfp4_linear_backward_workspace_bytes", M, N, K, dtype) != AVITS_OK) return 0;
   const BackPlan p = plan_back(M, N, K, dtype);
-  return p.wt + p.dy + p.part;
+  // Any smaller M too, which may run as parts of [M, K] (at most 64 MiB of them).
+  const size_t few = std::min<size_t>(kMaxPartBytes, size_t(8) * size_t(M) * size_t(K) * sizeof(float));
+  return std::max(p.wt + p.dy + p.part, few);
 }
 
 extern "C" int avits_mxfp4_linear_backward(const void* dy, int64_t M, int64_t N, const uint8_t* wq, const uint8_t* ws,

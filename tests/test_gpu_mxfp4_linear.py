@@ -37,7 +37,8 @@ def _np(t):
 
 SIZES = [(1, 1, 32), (1, 8, 64), (1, 300, 2048), (3, 33, 96), (16, 64, 256), (17, 65, 288), (64, 128, 544), (65, 63, 32),
          (100, 257, 1056), (255, 256, 512), (257, 520, 768), (600, 1000, 160), (513, 771, 2080), (2, 4096, 5120), (40, 2048, 2048),
-         (1030, 2056, 320), (300, 1024, 4096), (4099, 2056, 288), (3000, 3001, 1056)]
+         (1030, 2056, 320), (300, 1024, 4096), (4099, 2056, 288), (3000, 3001, 1056),
+         (900, 771, 8224), (1030, 1032, 4128)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
