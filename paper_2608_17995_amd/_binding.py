@@ -516,12 +516,12 @@ def _arg(t, name, dtype, *shape):
     """Device pointer of a contiguous GPU tensor of a type and shape (None passes NULL)."""
     if t is None:
         return None
+    if t.shape == shape and t.dtype is dtype and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
     if t.shape != shape:
         raise ValueError(f"{name}: expected {shape}, got {tuple(t.shape)}")
-    if not t.is_cuda or t.dtype is not dtype or not t.is_contiguous():
-        raise AvitsError(-1, f"{name} must be a contiguous {dtype} GPU tensor, got {t.dtype} on {t.device}"
-                             f"{'' if t.is_contiguous() else ', not contiguous'}")
-    return t.data_ptr()
+    raise AvitsError(-1, f"{name} must be a contiguous {dtype} GPU tensor, got {t.dtype} on {t.device}"
+                         f"{'' if t.is_contiguous() else ', not contiguous'}")
 
 
 def _mod_rows(name, t, dtype, D, n_images):
@@ -535,7 +535,7 @@ def _mod_rows(name, t, dtype, D, n_images):
     if t.shape != (n_images, D):
         raise ValueError(f"{name}: [{D}] or [{n_images}, {D}], got {tuple(t.shape)}")
     step, unit = t.stride()
-    if not t.is_cuda or t.dtype is not dtype or (unit != 1 and D > 1):
+    if t.dtype is not dtype or not t.is_cuda or (unit != 1 and D > 1):
         raise AvitsError(-1, f"{name} must be a {dtype} GPU tensor with contiguous rows")
     if n_images == 1:
         step = D
@@ -544,10 +544,13 @@ def _mod_rows(name, t, dtype, D, n_images):
     return t.data_ptr(), step
 
 
-def _offsets(off, name):
+def _offsets(off, M, name):
+    """Number of images, and the host array of their offsets (None for one image of all rows)."""
     if off is None:
         return 1, None
     n = len(off) - 1
+    if n == 1 and off[0] == 0 and off[1] == M:
+        return 1, None
     if n < 1:
         raise ValueError(f"{name}: off needs at least two entries")
     return n, (ctypes.c_int64 * (n + 1))(*off)
@@ -587,14 +590,14 @@ def avits_layer_norm(x, shift, scale, h, mean=None, rstd=None, off=None, eps=1e-
     shift and scale are [B, D] or one shared [D] (each may be None)."""
     M, D = x.shape
     code, dt, f32 = _code(x), x.dtype, _TYPES["f32"]
-    n, offs = _offsets(off, "avits_layer_norm")
+    n, offs = _offsets(off, M, "avits_layer_norm")
     sh, step = _mod_rows("shift", shift, dt, D, n)
     sc, step2 = _mod_rows("scale", scale, dt, D, n)
     if step is not None and step2 is not None and step != step2:
         raise ValueError("avits_layer_norm: shift and scale must be laid out alike")
-    rc = load().avits_layer_norm(_arg(x, "x", dt, M, D), M, D, n, offs, sh, sc, step or step2 or 0, eps, code,
+    rc = (_LIB or load()).avits_layer_norm(_arg(x, "x", dt, M, D), M, D, n, offs, sh, sc, step or step2 or 0, eps, code,
                                  _arg(h, "h", dt, M, D), _arg(mean, "mean", f32, M), _arg(rstd, "rstd", f32, M),
-                                 _stream(stream))
+                                 _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return h
@@ -614,18 +617,18 @@ def avits_layer_norm_backward(dh, mean, rstd, scale, dx, dscale=None, dshift=Non
     M, D = dh.shape
     code, dt = _code(dh), dh.dtype
     f32, u8 = _TYPES["f32"], _TYPES["u8"]
-    n, offs = _offsets(off, "avits_layer_norm_backward")
+    n, offs = _offsets(off, M, "avits_layer_norm_backward")
     sc, step = _mod_rows("scale", scale, dt, D, n)
     if step is None:
         grad = dscale if dscale is not None else dshift
         step = D if grad is not None and grad.dim() == 2 else 0
     shape = (n, D) if step else (D,)
     ws, wsp, wsb = _scratch(workspace, lambda: avits_layer_norm_backward_workspace_bytes(M, D, n), dh.device)
-    rc = load().avits_layer_norm_backward(
+    rc = (_LIB or load()).avits_layer_norm_backward(
         _arg(dh, "dh", dt, M, D), _arg(x, "x", dt, M, D), _arg(x_q8, "x_q8", u8, M, D),
         _arg(x_s8, "x_s8", u8, M, (D + 31) // 32), _arg(mean, "mean", f32, M), _arg(rstd, "rstd", f32, M), M, D, n, offs,
         sc, step, _arg(dres, "dres", dt, M, D), code, _arg(dx, "dx", dt, M, D), _arg(dscale, "dscale", f32, *shape),
-        _arg(dshift, "dshift", f32, *shape), wsp, wsb, _stream(stream))
+        _arg(dshift, "dshift", f32, *shape), wsp, wsb, _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return dx, dscale, dshift
@@ -635,8 +638,8 @@ def avits_ckpt8_pack(x, q, s, stream=None):
     """x [M, D] kept in 8 bits: codes q [M, D] and scales s [M, ceil(D / 32)], uint8."""
     M, D = x.shape
     code, u8 = _code(x), _TYPES["u8"]
-    rc = load().avits_ckpt8_pack(_arg(x, "x", x.dtype, M, D), M, D, code, _arg(q, "q", u8, M, D),
-                                 _arg(s, "s", u8, M, (D + 31) // 32), _stream(stream))
+    rc = (_LIB or load()).avits_ckpt8_pack(_arg(x, "x", x.dtype, M, D), M, D, code, _arg(q, "q", u8, M, D),
+                                 _arg(s, "s", u8, M, (D + 31) // 32), _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return q, s
@@ -645,8 +648,8 @@ def avits_ckpt8_pack(x, q, s, stream=None):
 def avits_ckpt8_unpack(q, s, x, stream=None):
     M, D = x.shape
     code, u8 = _code(x), _TYPES["u8"]
-    rc = load().avits_ckpt8_unpack(_arg(q, "q", u8, M, D), _arg(s, "s", u8, M, (D + 31) // 32), M, D, code,
-                                   _arg(x, "x", x.dtype, M, D), _stream(stream))
+    rc = (_LIB or load()).avits_ckpt8_unpack(_arg(q, "q", u8, M, D), _arg(s, "s", u8, M, (D + 31) // 32), M, D, code,
+                                   _arg(x, "x", x.dtype, M, D), _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return x
@@ -656,9 +659,9 @@ def avits_gelu_backward(da, dm, m=None, m_q8=None, m_s8=None, stream=None):
     """dm [M, D] = da GELU'(m), m as it was or packed by avits_ckpt8_pack."""
     M, D = da.shape
     code, dt, u8 = _code(da), da.dtype, _TYPES["u8"]
-    rc = load().avits_gelu_backward(_arg(da, "da", dt, M, D), _arg(m, "m", dt, M, D), _arg(m_q8, "m_q8", u8, M, D),
+    rc = (_LIB or load()).avits_gelu_backward(_arg(da, "da", dt, M, D), _arg(m, "m", dt, M, D), _arg(m_q8, "m_q8", u8, M, D),
                                     _arg(m_s8, "m_s8", u8, M, (D + 31) // 32), M, D, code, _arg(dm, "dm", dt, M, D),
-                                    _stream(stream))
+                                    _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return dm
@@ -687,7 +690,7 @@ def avits_mxfp4_quantize(x, q, s, act=ACT_NONE, stream=None):
     M, K = x.shape
     code = _code(x)
     qp, sp = _mx(q, s, "q", M, K)
-    rc = load().avits_mxfp4_quantize(_arg(x, "x", x.dtype, M, K), M, K, act, code, qp, sp, _stream(stream))
+    rc = (_LIB or load()).avits_mxfp4_quantize(_arg(x, "x", x.dtype, M, K), M, K, act, code, qp, sp, _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return q, s
@@ -698,7 +701,7 @@ def avits_mxfp4_dequantize(q, s, x, stream=None):
     M, K = x.shape
     code = _code(x)
     qp, sp = _mx(q, s, "q", M, K)
-    rc = load().avits_mxfp4_dequantize(qp, sp, M, K, code, _arg(x, "x", x.dtype, M, K), _stream(stream))
+    rc = (_LIB or load()).avits_mxfp4_dequantize(qp, sp, M, K, code, _arg(x, "x", x.dtype, M, K), _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return x
@@ -717,12 +720,12 @@ def avits_mxfp4_linear(xq, xs, wq, ws, b, out, gate=None, resid=None, off=None, 
     code, dt = _code(out), out.dtype
     xqp, xsp = _mx(xq, xs, "x", M, K)
     wqp, wsp = _mx(wq, ws, "w", N, K)
-    n, offs = _offsets(off, "avits_mxfp4_linear")
+    n, offs = _offsets(off, M, "avits_mxfp4_linear")
     gp, step = _mod_rows("gate", gate, dt, N, n)
     buf, bp, nb = _scratch(workspace, lambda: avits_mxfp4_linear_workspace_bytes(M, N, K), out.device)
-    rc = load().avits_mxfp4_linear(xqp, xsp, M, K, wqp, wsp, _arg(b, "b", dt, N), N, n, offs, gp, step or 0,
+    rc = (_LIB or load()).avits_mxfp4_linear(xqp, xsp, M, K, wqp, wsp, _arg(b, "b", dt, N), N, n, offs, gp, step or 0,
                                    _arg(resid, "resid", dt, M, N), code, _arg(out, "out", dt, M, N), bp, nb,
-                                   _stream(stream))
+                                   _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return out
@@ -739,8 +742,8 @@ def avits_mxfp4_linear_backward(dy, wq, ws, dx, workspace=None, stream=None):
     code, dt = _code(dy), dy.dtype
     wqp, wsp = _mx(wq, ws, "w", N, K)
     buf, bp, nb = _scratch(workspace, lambda: avits_mxfp4_linear_backward_workspace_bytes(M, N, K, code), dy.device)
-    rc = load().avits_mxfp4_linear_backward(_arg(dy, "dy", dt, M, N), M, N, wqp, wsp, K, code, _arg(dx, "dx", dt, M, K),
-                                            bp, nb, _stream(stream))
+    rc = (_LIB or load()).avits_mxfp4_linear_backward(_arg(dy, "dy", dt, M, N), M, N, wqp, wsp, K, code, _arg(dx, "dx", dt, M, K),
+                                            bp, nb, _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return dx
