@@ -690,7 +690,7 @@ int avits_noise_bits(int64_t first_pixel, int64_t n_pixels, int64_t C, uint64_t 
  * == 0: sums over the image's rows (zero for an image without rows), in an
  * order that depends on the sizes only.  h may be x; dx may be dh or dres;
  * no other overlap.  Pointers aligned to their element (16 bytes and D a
- * multiple of 8 (bf16) or 4 (fp32) are faster).  Requires 0 <= M < 2^26, 1 <= D
+ * multiple of 8 (bf16) or 4 (fp32) are faster).  Requires 0 <= M < 2^25, 1 <= D
  * <= 65536, eps > 0.  M == 0: dscale and dshift are zeroed, nothing else runs.
  * Errors: AVITS_ERR_INVALID_ARG, AVITS_ERR_UNSUPPORTED (dtype),
  * AVITS_ERR_WORKSPACE.
@@ -739,7 +739,7 @@ int avits_gelu_backward(const void* da, const void* m, const uint8_t* m_q8, cons
  * 2^-127; elements are x / scale rounded to nearest even, magnitudes above 6
  * to 6.  A block that holds an infinity or a NaN gets c = 255 and reads back
  * as NaN.  act: AVITS_ACT_NONE, or AVITS_ACT_GELU to quantise GELU_tanh(x).
- * x [M, K] (dtype).  Requires 0 <= M < 2^28, K a multiple of 32 in [32, 2^24), fewer than
+ * x [M, K] (dtype).  Requires 0 <= M < 2^27, K a multiple of 32 in [32, 2^24), fewer than
  * 2^31 scale bytes, 16-byte aligned pointers.  M == 0 enqueues nothing.
  *
  * avits_mxfp4_linear — out = x W^T + b with both operands in 4 bits, x [M, K]
@@ -748,11 +748,11 @@ int avits_gelu_backward(const void* da, const void* m, const uint8_t* m_q8, cons
  * images may each have their own gate: B, off and mod_stride as for
  * avits_layer_norm.  b [N] or NULL; out [M, N] may be resid; b, gate, resid and
  * out of dtype.  Sums are fp32, in an order that depends on the sizes only.
- * avits_mxfp4_linear_workspace_bytes(M, N, K) suffices for any number of rows
- * up to M; a call that does not split its contraction needs none.
+ * A call that does not split its contraction needs no workspace.
  * avits_mxfp4_linear_backward — the gradient of its input: dx [M, K] = dy W,
  * dy [M, N] and dx of dtype, W as above.
- * Requires 0 <= M < 2^28, 1 <= N < 2^21, K a multiple of 32 in [32, 2^21), and
+ * Either's workspace query suffices for any number of rows up to its M.
+ * Requires 0 <= M < 2^27, 1 <= N < 2^21, K a multiple of 32 in [32, 2^21), and
  * 16-byte aligned q, s, dy, dx, resid, out and workspace (>= the matching
  * query).  M == 0 enqueues nothing.
  * Errors: AVITS_ERR_INVALID_ARG, AVITS_ERR_UNSUPPORTED (dtype),
@@ -786,7 +786,8 @@ int avits_mxfp4_linear_backward(const void* dy, int64_t M, int64_t N, const uint
  * "scatter_mixed", "linear", "final_linear" (the GEMM of avits_final_layer;
  * its layer norm counts as "ln_mod"), "euler", "noise",
  * "layer_norm", "layer_norm_backward" (its sums too), "ckpt8", "gelu_backward",
- * "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_linear", and of
+ * "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_linear" (with the join of
+ * split sums), and of
  * avits_mxfp4_linear_backward "mxfp4_transpose" (the weight turned round) and
  * "mxfp4_backward" (its product); "gemm" returns the sum of the six GEMM families (the GEMM kernels alone: the split-K
  * reduction that follows a split launch is "splitk_reduce").  Unknown

@@ -203,7 +203,7 @@ int by_type(int dtype, F f) {
 int check_mx(const char* who, int64_t M, int64_t K, int dtype) {
   const int rc = check_type(who, M, K, dtype);
   if (rc != AVITS_OK) return rc;
-  AVITS_REQUIRE(M < (int64_t(1) << 28), "%s: M=%lld is 2^28 or more", who, (long long)M);
+  AVITS_REQUIRE(M < (int64_t(1) << 27), "%s: M=%lld is 2^27 or more", who, (long long)M);
   AVITS_REQUIRE(K % kBlk == 0, "%s: K=%lld must be a multiple of 32", who, (long long)K);
   AVITS_REQUIRE(scale_groups(K) * scale_rows(M) * 2 < (int64_t(1) << 31), "%s: M=%lld x K=%lld has 2^31 scales or more", who,
                 (long long)M, (long long)K);
@@ -283,7 +283,7 @@ extern "C" int avits_gelu_backward(const void* da, const void* m, const uint8_t*
 }
 
 extern "C" size_t avits_mxfp4_scale_bytes(int64_t M, int64_t K) {
-  if (M < 0 || M >= (int64_t(1) << 28) || K < kBlk || K >= (int64_t(1) << 24) || K % kBlk != 0) return 0;
+  if (M < 0 || M >= (int64_t(1) << 27) || K < kBlk || K >= (int64_t(1) << 24) || K % kBlk != 0) return 0;
   return size_t(scale_groups(K)) * size_t(scale_rows(M)) * 2;
 }
 

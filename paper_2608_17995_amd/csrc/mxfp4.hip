@@ -766,7 +766,7 @@ __global__ __launch_bounds__(256) void widen_kernel(const T* __restrict__ x, int
 }
 
 int check_product(const char* who, int64_t M, int64_t N, int64_t K, int dtype) {
-  AVITS_REQUIRE(M >= 0 && M < (int64_t(1) << 28), "%s: M=%lld outside [0, 2^28)", who, (long long)M);
+  AVITS_REQUIRE(M >= 0 && M < (int64_t(1) << 27), "%s: M=%lld outside [0, 2^27)", who, (long long)M);
   AVITS_REQUIRE(N >= 1 && N < (int64_t(1) << 21), "%s: N=%lld outside [1, 2^21)", who, (long long)N);
   AVITS_REQUIRE(K >= kBlk && K < (int64_t(1) << 21) && K % kBlk == 0, "%s: K=%lld must be a multiple of 32 in [32, 2^21)", who,
                 (long long)K);
@@ -775,7 +775,6 @@ int check_product(const char* who, int64_t M, int64_t N, int64_t K, int dtype) {
   if (dtype != AVITS_F32 && dtype != AVITS_BF16) return set_error(AVITS_ERR_UNSUPPORTED, "%s: dtype %d unsupported", who, dtype);
   return AVITS_OK;
 }
-
 
 // How a product runs: 256 x 256 tiles, each in `splits` parts of the contraction,
 // or (splits == 0) form `rows` of the kernel for few rows.  The least predicted
@@ -984,7 +983,8 @@ extern "C" size_t avits_mxfp4_linear_workspace_bytes(int64_t M, int64_t N, int64
 
 extern "C" int avits_mxfp4_linear(const uint8_t* xq, const uint8_t* xs, int64_t M, int64_t K, const uint8_t* wq,
                                   const uint8_t* ws, const void* b, int64_t N, int32_t B, const int64_t* off,
-                                  const void* gate, int64_t mod_stride, const void* resid, int dtype, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+                                  const void* gate, int64_t mod_stride, const void* resid, int dtype, void* out,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
   int rc = check_product("mxfp4_linear", M, N, K, dtype);
   Mx4Args a = {xq, xs, wq, ws, b, gate, resid, out, M, N, K, {}};
   if (rc == AVITS_OK) rc = fill_images("mxfp4_linear", M, B, off, mod_stride, a.im);
@@ -992,7 +992,8 @@ extern "C" int avits_mxfp4_linear(const uint8_t* xq, const uint8_t* xs, int64_t 
   if (M == 0) return AVITS_OK;
   AVITS_REQUIRE((gate != nullptr) == (resid != nullptr), "mxfp4_linear: gate and resid go together");
   AVITS_REQUIRE(xq && xs && wq && ws && out, "mxfp4_linear: null xq/xs/wq/ws/out");
-  AVITS_REQUIRE(aligned_to({xq, xs, wq, ws, out, resid}, 16), "mxfp4_linear: xq, xs, wq, ws, resid and out must be 16-byte aligned");
+  AVITS_REQUIRE(aligned_to({xq, xs, wq, ws, out, resid}, 16),
+                "mxfp4_linear: xq, xs, wq, ws, resid and out must be 16-byte aligned");
   AVITS_REQUIRE(aligned_to({b, gate}, dtype == AVITS_BF16 ? 2 : 4), "mxfp4_linear: b or gate is not aligned to its element");
   const ProductPlan p = plan_product(M, N, K);
   const size_t need = p.splits > 1 ? part_bytes(p.splits, M, N) : 0;

@@ -452,7 +452,7 @@ __global__ __launch_bounds__(256) void norm_back_sum_kernel(const float* __restr
 
 int check_norm(const char* who, int64_t M, int64_t D, int32_t B, const int64_t* off, int64_t mod_stride, int dtype,
                Images& im) {
-  AVITS_REQUIRE(M >= 0 && M < (int64_t(1) << 26), "%s: M=%lld outside [0, 2^26)", who, (long long)M);
+  AVITS_REQUIRE(M >= 0 && M < (int64_t(1) << 25), "%s: M=%lld outside [0, 2^25)", who, (long long)M);
   AVITS_REQUIRE(D >= 1 && D <= 65536, "%s: D=%lld outside [1, 65536]", who, (long long)D);
   if (dtype != AVITS_F32 && dtype != AVITS_BF16) return set_error(AVITS_ERR_UNSUPPORTED, "%s: dtype %d unsupported", who, dtype);
   return fill_images(who, M, B, off, mod_stride, im);
@@ -581,7 +581,7 @@ extern "C" int avits_layer_norm(const void* x, int64_t M, int64_t D, int32_t B, 
 }
 
 extern "C" size_t avits_layer_norm_backward_workspace_bytes(int64_t M, int64_t D, int32_t B) {
-  if (M < 0 || M >= (int64_t(1) << 26) || D < 1 || D > 65536 || B < 1 || B > kMaxSeqs) return 0;
+  if (M < 0 || M >= (int64_t(1) << 25) || D < 1 || D > 65536 || B < 1 || B > kMaxSeqs) return 0;
   const size_t chunks = size_t(std::min<int64_t>(kMaxChunks, ceil_div64(M, 4))) + size_t(B);
   return (align_up(size_t(2 * M), 64) + 2 * chunks * size_t(D)) * sizeof(float);
 }

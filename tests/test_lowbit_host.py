@@ -164,3 +164,24 @@ def test_the_binding_refuses_shapes_and_types():
         avits.avits_mxfp4_linear(z(4, 32, t=u), z(1, 8, 2, t=u), z(8, 48, t=u), z(2, 8, 2, t=u), None, z(4, 8))
     with pytest.raises((ValueError, avits.AvitsError)):
         avits.avits_mxfp4_linear_backward(z(4, 9), z(8, 32, t=u), z(1, 8, 2, t=u), z(4, 64))
+
+
+def test_the_largest_sizes(lib):
+    """What a launch's 2^32 work-items cannot hold is refused."""
+    assert _norm(lib, M=1 << 25) == INVALID and _back(lib, M=1 << 25) == INVALID
+    assert lib.avits_layer_norm_backward_workspace_bytes((1 << 25) - 1, 1, 1) > 0
+    assert lib.avits_mxfp4_quantize(FAKE, 1 << 27, 32, 0, 1, FAKE, FAKE, None) == INVALID
+    assert lib.avits_mxfp4_dequantize(FAKE, FAKE, 1 << 27, 32, 1, FAKE, None) == INVALID
+    assert lib.avits_mxfp4_scale_bytes(1 << 27, 32) == 0 and lib.avits_mxfp4_scale_bytes((1 << 27) - 1, 32) == 1 << 28
+    assert _linear(lib, M=1 << 27, K=32) == INVALID and _lback(lib, M=1 << 27, K=32) == INVALID
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("N,K", [(8, 32), (9, 64), (256, 1024), (2048, 8192), (4100, 1056)])
+def test_workspaces_cover_fewer_rows(lib, N, K, dtype):
+    sizes = [1, 2, 15, 16, 17, 64, 65, 200, 256, 257, 300, 512, 777, 1024, 1741, 4096, 16896, 70000]
+    for query in (lambda M: lib.avits_mxfp4_linear_workspace_bytes(M, N, K),
+                  lambda M: lib.avits_mxfp4_linear_backward_workspace_bytes(M, N, K, dtype),
+                  lambda M: lib.avits_layer_norm_backward_workspace_bytes(M, K, 4)):
+        need = [query(M) for M in sizes]
+        assert need == sorted(need)
