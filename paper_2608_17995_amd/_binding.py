@@ -216,6 +216,19 @@ def _current_stream():
     return _current_stream()
 
 
+def _current_device():
+    """Index of the current device; None (no tensor's) where there is no GPU."""
+    import torch
+    device = getattr(torch._C, "_cuda_getDevice", None)
+    if not torch.cuda.is_initialized():
+        return None
+    if device is None:
+        return torch.cuda.current_device()
+    global _current_device
+    _current_device = device
+    return device()
+
+
 def _workspace(ws, nbytes, device):
     import torch
     if ws is None:
@@ -512,31 +525,31 @@ class BlockWeights:
 # be shorter than a microsecond's worth of checks on the host, so each tensor
 # is looked at once (_arg).
 
-def _arg(t, name, dtype, *shape):
-    """Device pointer of a contiguous GPU tensor of a type and shape (None passes NULL)."""
+def _arg(t, name, dtype, dev, *shape):
+    """Device pointer of a contiguous GPU tensor of a type, device and shape (None passes NULL)."""
     if t is None:
         return None
-    if t.shape == shape and t.dtype is dtype and t.is_cuda and t.is_contiguous():
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
         return t.data_ptr()
     if t.shape != shape:
         raise ValueError(f"{name}: expected {shape}, got {tuple(t.shape)}")
-    raise AvitsError(-1, f"{name} must be a contiguous {dtype} GPU tensor, got {t.dtype} on {t.device}"
+    raise AvitsError(-1, f"{name} must be a contiguous {dtype} tensor on the current GPU, got {t.dtype} on {t.device}"
                          f"{'' if t.is_contiguous() else ', not contiguous'}")
 
 
-def _mod_rows(name, t, dtype, D, n_images):
+def _mod_rows(name, t, dtype, dev, D, n_images):
     """Pointer of a vector given as [D] (shared) or [B, D] (rows any number of
     elements apart, e.g. a slice of a [B, 6, D] modulation), and the
     distance of the images' rows in elements."""
     if t is None:
         return None, None
     if t.dim() == 1:
-        return _arg(t, name, dtype, D), 0
+        return _arg(t, name, dtype, dev, D), 0
     if t.shape != (n_images, D):
         raise ValueError(f"{name}: [{D}] or [{n_images}, {D}], got {tuple(t.shape)}")
     step, unit = t.stride()
-    if t.dtype is not dtype or not t.is_cuda or (unit != 1 and D > 1):
-        raise AvitsError(-1, f"{name} must be a {dtype} GPU tensor with contiguous rows")
+    if t.dtype is not dtype or t.get_device() != dev or (unit != 1 and D > 1):
+        raise AvitsError(-1, f"{name} must be a {dtype} tensor with contiguous rows on the current GPU, got {t.dtype} on {t.device}")
     if n_images == 1:
         step = D
     elif step == 0:
@@ -568,19 +581,33 @@ def _types():
 
 
 def _code(t):
+    """The library's code of t's type, and the device that every tensor of the
+    call has to be on: the current one, whose stream the work goes to."""
     code = (_TYPES or _types()).get(t.dtype)
     if code is None:
         raise AvitsError(-2, f"unsupported dtype {t.dtype}")
-    return code
+    return code, _current_device()
 
 
-def _scratch(ws, need, device):
-    """Pointer and size of the workspace, made here (need() bytes) where none is given."""
+def _scratch(ws, need, dev, stream):
+    """Pointer and size of the workspace, made here (need() bytes) where none is
+    given: on the stream of the call, after whose work it is free again."""
     if ws is None:
         nbytes = need()
         if not nbytes:
             return None, None, 0
-        ws, _, _ = _workspace(None, nbytes, device)
+        if dev is None:
+            raise AvitsError(-1, "no workspace can be made: no GPU is in use")
+        import torch
+        if stream is None:
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        else:
+            if not isinstance(stream, torch.cuda.Stream):
+                stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+            with torch.cuda.stream(stream):
+                ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    elif ws.get_device() != dev:
+        raise AvitsError(-1, f"workspace must be on the current GPU, got {ws.device}")
     return ws, _dev(ws, "workspace"), ws.numel() * ws.element_size()
 
 
@@ -589,14 +616,14 @@ def avits_layer_norm(x, shift, scale, h, mean=None, rstd=None, off=None, eps=1e-
     fp32 where asked for.  off: host row offsets of B images (B + 1), whose
     shift and scale are [B, D] or one shared [D] (each may be None)."""
     M, D = x.shape
-    code, dt, f32 = _code(x), x.dtype, _TYPES["f32"]
+    (code, dev), dt, f32 = _code(x), x.dtype, _TYPES["f32"]
     n, offs = _offsets(off, M, "avits_layer_norm")
-    sh, step = _mod_rows("shift", shift, dt, D, n)
-    sc, step2 = _mod_rows("scale", scale, dt, D, n)
+    sh, step = _mod_rows("shift", shift, dt, dev, D, n)
+    sc, step2 = _mod_rows("scale", scale, dt, dev, D, n)
     if step is not None and step2 is not None and step != step2:
         raise ValueError("avits_layer_norm: shift and scale must be laid out alike")
-    rc = (_LIB or load()).avits_layer_norm(_arg(x, "x", dt, M, D), M, D, n, offs, sh, sc, step or step2 or 0, eps, code,
-                                 _arg(h, "h", dt, M, D), _arg(mean, "mean", f32, M), _arg(rstd, "rstd", f32, M),
+    rc = (_LIB or load()).avits_layer_norm(_arg(x, "x", dt, dev, M, D), M, D, n, offs, sh, sc, step or step2 or 0, eps, code,
+                                 _arg(h, "h", dt, dev, M, D), _arg(mean, "mean", f32, dev, M), _arg(rstd, "rstd", f32, dev, M),
                                  _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
@@ -615,20 +642,20 @@ def avits_layer_norm_backward(dh, mean, rstd, scale, dx, dscale=None, dshift=Non
     x_q8 [M, D] and x_s8 [M, ceil(D / 32)].  Without a scale the gradients'
     shape says which."""
     M, D = dh.shape
-    code, dt = _code(dh), dh.dtype
+    (code, dev), dt = _code(dh), dh.dtype
     f32, u8 = _TYPES["f32"], _TYPES["u8"]
     n, offs = _offsets(off, M, "avits_layer_norm_backward")
-    sc, step = _mod_rows("scale", scale, dt, D, n)
+    sc, step = _mod_rows("scale", scale, dt, dev, D, n)
     if step is None:
         grad = dscale if dscale is not None else dshift
         step = D if grad is not None and grad.dim() == 2 else 0
     shape = (n, D) if step else (D,)
-    ws, wsp, wsb = _scratch(workspace, lambda: avits_layer_norm_backward_workspace_bytes(M, D, n), dh.device)
+    ws, wsp, wsb = _scratch(workspace, lambda: avits_layer_norm_backward_workspace_bytes(M, D, n), dev, stream)
     rc = (_LIB or load()).avits_layer_norm_backward(
-        _arg(dh, "dh", dt, M, D), _arg(x, "x", dt, M, D), _arg(x_q8, "x_q8", u8, M, D),
-        _arg(x_s8, "x_s8", u8, M, (D + 31) // 32), _arg(mean, "mean", f32, M), _arg(rstd, "rstd", f32, M), M, D, n, offs,
-        sc, step, _arg(dres, "dres", dt, M, D), code, _arg(dx, "dx", dt, M, D), _arg(dscale, "dscale", f32, *shape),
-        _arg(dshift, "dshift", f32, *shape), wsp, wsb, _current_stream() if stream is None else _stream(stream))
+        _arg(dh, "dh", dt, dev, M, D), _arg(x, "x", dt, dev, M, D), _arg(x_q8, "x_q8", u8, dev, M, D),
+        _arg(x_s8, "x_s8", u8, dev, M, (D + 31) // 32), _arg(mean, "mean", f32, dev, M), _arg(rstd, "rstd", f32, dev, M), M, D, n, offs,
+        sc, step, _arg(dres, "dres", dt, dev, M, D), code, _arg(dx, "dx", dt, dev, M, D), _arg(dscale, "dscale", f32, dev, *shape),
+        _arg(dshift, "dshift", f32, dev, *shape), wsp, wsb, _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return dx, dscale, dshift
@@ -637,9 +664,9 @@ def avits_layer_norm_backward(dh, mean, rstd, scale, dx, dscale=None, dshift=Non
 def avits_ckpt8_pack(x, q, s, stream=None):
     """x [M, D] kept in 8 bits: codes q [M, D] and scales s [M, ceil(D / 32)], uint8."""
     M, D = x.shape
-    code, u8 = _code(x), _TYPES["u8"]
-    rc = (_LIB or load()).avits_ckpt8_pack(_arg(x, "x", x.dtype, M, D), M, D, code, _arg(q, "q", u8, M, D),
-                                 _arg(s, "s", u8, M, (D + 31) // 32), _current_stream() if stream is None else _stream(stream))
+    (code, dev), u8 = _code(x), _TYPES["u8"]
+    rc = (_LIB or load()).avits_ckpt8_pack(_arg(x, "x", x.dtype, dev, M, D), M, D, code, _arg(q, "q", u8, dev, M, D),
+                                 _arg(s, "s", u8, dev, M, (D + 31) // 32), _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return q, s
@@ -647,9 +674,9 @@ def avits_ckpt8_pack(x, q, s, stream=None):
 
 def avits_ckpt8_unpack(q, s, x, stream=None):
     M, D = x.shape
-    code, u8 = _code(x), _TYPES["u8"]
-    rc = (_LIB or load()).avits_ckpt8_unpack(_arg(q, "q", u8, M, D), _arg(s, "s", u8, M, (D + 31) // 32), M, D, code,
-                                   _arg(x, "x", x.dtype, M, D), _current_stream() if stream is None else _stream(stream))
+    (code, dev), u8 = _code(x), _TYPES["u8"]
+    rc = (_LIB or load()).avits_ckpt8_unpack(_arg(q, "q", u8, dev, M, D), _arg(s, "s", u8, dev, M, (D + 31) // 32), M, D, code,
+                                   _arg(x, "x", x.dtype, dev, M, D), _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return x
@@ -658,9 +685,9 @@ def avits_ckpt8_unpack(q, s, x, stream=None):
 def avits_gelu_backward(da, dm, m=None, m_q8=None, m_s8=None, stream=None):
     """dm [M, D] = da GELU'(m), m as it was or packed by avits_ckpt8_pack."""
     M, D = da.shape
-    code, dt, u8 = _code(da), da.dtype, _TYPES["u8"]
-    rc = (_LIB or load()).avits_gelu_backward(_arg(da, "da", dt, M, D), _arg(m, "m", dt, M, D), _arg(m_q8, "m_q8", u8, M, D),
-                                    _arg(m_s8, "m_s8", u8, M, (D + 31) // 32), M, D, code, _arg(dm, "dm", dt, M, D),
+    (code, dev), dt, u8 = _code(da), da.dtype, _TYPES["u8"]
+    rc = (_LIB or load()).avits_gelu_backward(_arg(da, "da", dt, dev, M, D), _arg(m, "m", dt, dev, M, D), _arg(m_q8, "m_q8", u8, dev, M, D),
+                                    _arg(m_s8, "m_s8", u8, dev, M, (D + 31) // 32), M, D, code, _arg(dm, "dm", dt, dev, M, D),
                                     _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
@@ -676,21 +703,22 @@ def avits_mxfp4_scale_shape(M: int, K: int) -> tuple:
     return (K + 63) // 64, (M + 7) // 8 * 8, 2
 
 
-def _mx(q, s, name, M, K):
+def _mx(q, s, name, dev, M, K):
     """Pointers of an [M, K] tensor held in 4 bits: codes [M, K / 2] and scales."""
     if K % 2:
         raise ValueError(f"{name}: {K} columns cannot be held in 4 bits")
     u8 = (_TYPES or _types())["u8"]
-    return _arg(q, name, u8, M, K // 2), _arg(s, f"{name} scales", u8, (K + 63) // 64, (M + 7) // 8 * 8, 2)
+    return _arg(q, name, u8, dev, M, K // 2), _arg(s, f"{name} scales", u8, dev, (K + 63) // 64, (M + 7) // 8 * 8, 2)
 
 
 def avits_mxfp4_quantize(x, q, s, act=ACT_NONE, stream=None):
     """x [M, K] to codes q [M, K / 2] and scales s (avits_mxfp4_scale_shape),
     uint8; with act=ACT_GELU the values of GELU_tanh(x)."""
     M, K = x.shape
-    code = _code(x)
-    qp, sp = _mx(q, s, "q", M, K)
-    rc = (_LIB or load()).avits_mxfp4_quantize(_arg(x, "x", x.dtype, M, K), M, K, act, code, qp, sp, _current_stream() if stream is None else _stream(stream))
+    code, dev = _code(x)
+    qp, sp = _mx(q, s, "q", dev, M, K)
+    rc = (_LIB or load()).avits_mxfp4_quantize(_arg(x, "x", x.dtype, dev, M, K), M, K, act, code, qp, sp,
+                                               _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return q, s
@@ -699,9 +727,10 @@ def avits_mxfp4_quantize(x, q, s, act=ACT_NONE, stream=None):
 def avits_mxfp4_dequantize(q, s, x, stream=None):
     """The values that codes q and scales s stand for, to x [M, K]."""
     M, K = x.shape
-    code = _code(x)
-    qp, sp = _mx(q, s, "q", M, K)
-    rc = (_LIB or load()).avits_mxfp4_dequantize(qp, sp, M, K, code, _arg(x, "x", x.dtype, M, K), _current_stream() if stream is None else _stream(stream))
+    code, dev = _code(x)
+    qp, sp = _mx(q, s, "q", dev, M, K)
+    rc = (_LIB or load()).avits_mxfp4_dequantize(qp, sp, M, K, code, _arg(x, "x", x.dtype, dev, M, K),
+                                                 _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return x
@@ -717,14 +746,14 @@ def avits_mxfp4_linear(xq, xs, wq, ws, b, out, gate=None, resid=None, off=None, 
     for the rows of B images at the host row offsets off."""
     M, N = out.shape
     K = 2 * xq.shape[-1]
-    code, dt = _code(out), out.dtype
-    xqp, xsp = _mx(xq, xs, "x", M, K)
-    wqp, wsp = _mx(wq, ws, "w", N, K)
+    (code, dev), dt = _code(out), out.dtype
+    xqp, xsp = _mx(xq, xs, "x", dev, M, K)
+    wqp, wsp = _mx(wq, ws, "w", dev, N, K)
     n, offs = _offsets(off, M, "avits_mxfp4_linear")
-    gp, step = _mod_rows("gate", gate, dt, N, n)
-    buf, bp, nb = _scratch(workspace, lambda: avits_mxfp4_linear_workspace_bytes(M, N, K), out.device)
-    rc = (_LIB or load()).avits_mxfp4_linear(xqp, xsp, M, K, wqp, wsp, _arg(b, "b", dt, N), N, n, offs, gp, step or 0,
-                                   _arg(resid, "resid", dt, M, N), code, _arg(out, "out", dt, M, N), bp, nb,
+    gp, step = _mod_rows("gate", gate, dt, dev, N, n)
+    buf, bp, nb = _scratch(workspace, lambda: avits_mxfp4_linear_workspace_bytes(M, N, K), dev, stream)
+    rc = (_LIB or load()).avits_mxfp4_linear(xqp, xsp, M, K, wqp, wsp, _arg(b, "b", dt, dev, N), N, n, offs, gp, step or 0,
+                                   _arg(resid, "resid", dt, dev, M, N), code, _arg(out, "out", dt, dev, M, N), bp, nb,
                                    _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)
@@ -739,10 +768,10 @@ def avits_mxfp4_linear_backward(dy, wq, ws, dx, workspace=None, stream=None):
     """dx [M, K] = dy [M, N] W, W [N, K] held in 4 bits."""
     M, N = dy.shape
     K = dx.shape[-1]
-    code, dt = _code(dy), dy.dtype
-    wqp, wsp = _mx(wq, ws, "w", N, K)
-    buf, bp, nb = _scratch(workspace, lambda: avits_mxfp4_linear_backward_workspace_bytes(M, N, K, code), dy.device)
-    rc = (_LIB or load()).avits_mxfp4_linear_backward(_arg(dy, "dy", dt, M, N), M, N, wqp, wsp, K, code, _arg(dx, "dx", dt, M, K),
+    (code, dev), dt = _code(dy), dy.dtype
+    wqp, wsp = _mx(wq, ws, "w", dev, N, K)
+    buf, bp, nb = _scratch(workspace, lambda: avits_mxfp4_linear_backward_workspace_bytes(M, N, K, code), dev, stream)
+    rc = (_LIB or load()).avits_mxfp4_linear_backward(_arg(dy, "dy", dt, dev, M, N), M, N, wqp, wsp, K, code, _arg(dx, "dx", dt, dev, M, K),
                                             bp, nb, _current_stream() if stream is None else _stream(stream))
     if rc:
         _check(rc)

@@ -185,3 +185,29 @@ def test_workspaces_cover_fewer_rows(lib, N, K, dtype):
                   lambda M: lib.avits_layer_norm_backward_workspace_bytes(M, K, 4)):
         need = [query(M) for M in sizes]
         assert need == sorted(need)
+
+
+def test_tensors_elsewhere_are_refused():
+    """Everything is on the current device, or nothing is launched: here there is none."""
+    torch = pytest.importorskip("torch")
+    z = lambda *s, t=torch.float32: torch.zeros(*s, dtype=t)  # noqa: E731
+    u, meta = torch.uint8, torch.zeros(4, 64, device="meta")
+    for x in (z(4, 64), meta):
+        with pytest.raises(avits.AvitsError):
+            avits.avits_layer_norm(x, None, None, x)
+        with pytest.raises(avits.AvitsError):
+            avits.avits_layer_norm_backward(x, z(4), z(4), None, x, x=x)
+        with pytest.raises(avits.AvitsError):
+            avits.avits_ckpt8_pack(x, z(4, 64, t=u), z(4, 2, t=u))
+        with pytest.raises(avits.AvitsError):
+            avits.avits_ckpt8_unpack(z(4, 64, t=u), z(4, 2, t=u), x)
+        with pytest.raises(avits.AvitsError):
+            avits.avits_gelu_backward(x, x, m=x)
+        with pytest.raises(avits.AvitsError):
+            avits.avits_mxfp4_quantize(x, z(4, 32, t=u), z(1, 8, 2, t=u))
+        with pytest.raises(avits.AvitsError):
+            avits.avits_mxfp4_dequantize(z(4, 32, t=u), z(1, 8, 2, t=u), x)
+        with pytest.raises(avits.AvitsError):
+            avits.avits_mxfp4_linear(z(8, 16, t=u), z(1, 8, 2, t=u), z(64, 16, t=u), z(1, 64, 2, t=u), None, x[:, :].new_zeros(8, 64))
+        with pytest.raises(avits.AvitsError):
+            avits.avits_mxfp4_linear_backward(x, z(64, 16, t=u), z(1, 64, 2, t=u), x[:, :32], workspace=z(64, t=u))
