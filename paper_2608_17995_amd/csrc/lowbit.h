@@ -85,6 +85,12 @@ __device__ __forceinline__ uint32_t quad_umax(uint32_t v) {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
+// Vectors of memory that need not start on their own size: global accesses of
+// 16 bytes may lie at any element (or byte).
+typedef uint32_t loose4 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t loose2 __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t loose1 __attribute__((aligned(1)));
+
 // Eight elements to eight 4-bit codes (round to nearest even, magnitudes past 6 to 6).
 __device__ __forceinline__ uint32_t encode4x8(const float (&v)[8], float inv) {
   uint32_t o = 0;
@@ -113,33 +119,35 @@ __device__ __forceinline__ float decode8(uint8_t c, float scale) {
   return __builtin_amdgcn_cvt_f32_fp8(int(c), 0) * scale;
 }
 
-// Eight consecutive elements of a 16-byte aligned array as floats, and back.
+// Eight consecutive elements as floats, and back (no alignment but the element's).
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
   if constexpr (sizeof(T) == 2) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+    const loose4 w = *reinterpret_cast<const loose4*>(p);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       v[2 * e] = __uint_as_float(w[e] << 16);
       v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
     }
   } else {
-    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+    const loose4 a = *reinterpret_cast<const loose4*>(p), b = *reinterpret_cast<const loose4*>(p + 4);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      v[e] = a[e];
-      v[4 + e] = b[e];
+      v[e] = __uint_as_float(a[e]);
+      v[4 + e] = __uint_as_float(b[e]);
     }
   }
 }
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
   if constexpr (sizeof(T) == 2) {
-    *reinterpret_cast<u32x4*>(p) =
-        u32x4{pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]), pack_bf2(v[4], v[5]), pack_bf2(v[6], v[7])};
+    *reinterpret_cast<loose4*>(p) =
+        loose4{pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]), pack_bf2(v[4], v[5]), pack_bf2(v[6], v[7])};
   } else {
-    *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-    *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      *reinterpret_cast<loose4*>(p + 4 * h) = loose4{__float_as_uint(v[4 * h]), __float_as_uint(v[4 * h + 1]),
+                                                     __float_as_uint(v[4 * h + 2]), __float_as_uint(v[4 * h + 3])};
   }
 }
 

@@ -45,32 +45,104 @@ __global__ __launch_bounds__(256) void unpack8_kernel(const uint8_t* __restrict_
   }
 }
 
-// Any width and alignment: half a wave per block, an element per lane.
+// Any width and alignment: 2^lg lanes walk a row, eight elements each at a time, so
+// that four lanes hold a block here too.  The eight of a row's last, partial
+// group are the row's last eight: the first `dup` of them belong to the group before
+// it, whose lane gives them the same values, where both are of one block; where
+// they are not (or the row is shorter) the group goes element by element.
+// Bound by HBM like the whole blocks' kernels: 16000 x 3999 of bf16 packed in 43.7 us
+// (its bytes at the copy's rate 37.6), their GELU gradient 74.9 (62.7); a lane
+// per element took 185 and 216.
+struct RowGroup {
+  int64_t at;      // where the eight elements start
+  int own, dup;    // how many are the group's own (0: past the row), and the first of them
+  bool single;     // element by element
+};
+__device__ __forceinline__ RowGroup row_group(int64_t row, int g, int D) {
+  RowGroup r;
+  r.own = max(0, min(8, D - 8 * g));
+  r.single = r.own < 8 && (g % 4 == 0 || D < 8);
+  r.dup = D < 8 ? 0 : 8 - r.own;
+  r.at = row * D + 8 * g - r.dup;
+  return r;
+}
 template <typename T>
-__global__ __launch_bounds__(256) void pack8_any_kernel(const T* __restrict__ x, int64_t M, int64_t D, int64_t ns,
-                                                        uint8_t* __restrict__ q, uint8_t* __restrict__ s) {
-  const int l = threadIdx.x % 32;
-  for (int64_t b = int64_t(blockIdx.x) * 8 + threadIdx.x / 32; b < M * ns; b += int64_t(gridDim.x) * 8) {
-    const int64_t m = b / ns, i = (b % ns) * kBlk + l;
-    const float v = i < D ? ld(x, m * D + i) : 0.f;
-    uint32_t top = magnitude(v);
+__device__ __forceinline__ void load_group(const T* x, const RowGroup& r, int D, float (&v)[8]) {
 #pragma unroll
-    for (int k = 1; k < 32; k *= 2) top = max(top, uint32_t(__shfl_xor(int(top), k, 32)));
-    const uint32_t c = scale8_code(top);
-    const float inv = c == 255u ? 0.f : scale_inverse(c);
-    if (i < D) q[m * D + i] = uint8_t(__builtin_amdgcn_cvt_pk_fp8_f32(v * inv, v * inv, 0, false));
-    if (l == 0) s[b] = uint8_t(c);
+  for (int e = 0; e < 8; ++e) v[e] = 0.f;
+  if (D >= 8) {
+    if (r.own > 0) load8(x + r.at, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < r.own) v[e] = ld(x, r.at + e);
   }
+}
+template <typename T>
+__device__ __forceinline__ void store_group(T* x, const RowGroup& r, const float (&v)[8]) {
+  if (!r.single) {
+    if (r.own > 0) store8(x + r.at, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e >= r.dup && e - r.dup < r.own) st(x, r.at + e, v[e]);
+  }
+}
+// The group's values from its codes and its block's scale (a single group's
+// first `dup` are of another block and not used).
+__device__ __forceinline__ void decode_group(const uint8_t* q, const RowGroup& r, int D, uint32_t c, float (&v)[8]) {
+  loose2 w = {0u, 0u};
+  if (D >= 8) {
+    if (r.own > 0) w = *reinterpret_cast<const loose2*>(q + r.at);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < r.own) w[e / 4] |= uint32_t(q[r.at + e]) << (8 * (e % 4));
+  }
+  const float sc = scale_value(c);
+  decode8x4(w[0], sc, v);
+  decode8x4(w[1], sc, v + 4);
+}
+// f(row, g, group) for the row groups of this thread; where rows are few, gridDim.y
+// walks share one.
+template <typename F>
+__device__ __forceinline__ void each_group(int64_t M, int D, int ns, int lg, F f) {
+  const int lanes = 1 << lg, from = int(blockIdx.y) * lanes + (threadIdx.x & (lanes - 1)), step = int(gridDim.y) * lanes;
+  for (int64_t row = (int64_t(blockIdx.x) * 256 + threadIdx.x) >> lg; row < M; row += int64_t(gridDim.x) * 256 >> lg)
+    for (int g = from; g < 4 * ns; g += step) f(row, g, row_group(row, g, D));
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void unpack8_any_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ s,
-                                                          int64_t M, int64_t D, int64_t ns, T* __restrict__ x) {
-  const int l = threadIdx.x % 32;
-  for (int64_t b = int64_t(blockIdx.x) * 8 + threadIdx.x / 32; b < M * ns; b += int64_t(gridDim.x) * 8) {
-    const int64_t m = b / ns, i = (b % ns) * kBlk + l;
-    if (i < D) st(x, m * D + i, decode8(q[m * D + i], scale_value(s[b])));
-  }
+__global__ __launch_bounds__(256) void pack8_rows_kernel(const T* __restrict__ x, int64_t M, int D, int ns, int lg,
+                                                         uint8_t* __restrict__ q, uint8_t* __restrict__ s) {
+  each_group(M, D, ns, lg, [&](int64_t row, int g, const RowGroup& r) {
+    float v[8];
+    load_group(x, r, D, v);
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, e >= r.dup ? magnitude(v[e]) : 0u);
+    const uint32_t c = scale8_code(quad_umax(top));
+    const float inv = c == 255u ? 0.f : scale_inverse(c);
+    const loose2 o = {encode8x4(v, inv), encode8x4(v + 4, inv)};
+    if (!r.single) {
+      if (r.own > 0) *reinterpret_cast<loose2*>(q + r.at) = o;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e >= r.dup && e - r.dup < r.own) q[r.at + e] = uint8_t(o[e / 4] >> (8 * (e % 4)));
+    }
+    if (g % 4 == 0) s[row * ns + g / 4] = uint8_t(c);
+  });
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void unpack8_rows_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ s,
+                                                           int64_t M, int D, int ns, int lg, T* __restrict__ x) {
+  each_group(M, D, ns, lg, [&](int64_t row, int g, const RowGroup& r) {
+    float v[8];
+    decode_group(q, r, D, s[row * ns + g / 4], v);
+    store_group(x, r, v);
+  });
 }
 
 // dm = da gelu'(m), m in its own type or kept in 8 bits.
@@ -94,18 +166,21 @@ __global__ __launch_bounds__(256) void gelu_back_kernel(const T* da, const T* m,
   }
 }
 
+// (dm may be da: a group's eight and the group's before it are of one block, so
+// they are loaded by one instruction before either's are stored.)
 template <typename T>
-__global__ __launch_bounds__(256) void gelu_back_any_kernel(const T* da, const T* m, const uint8_t* __restrict__ q,
-                                                            const uint8_t* __restrict__ s, int64_t M, int64_t D, int64_t ns,
-                                                            T* dm) {
-  const int l = threadIdx.x % 32;
-  for (int64_t b = int64_t(blockIdx.x) * 8 + threadIdx.x / 32; b < M * ns; b += int64_t(gridDim.x) * 8) {
-    const int64_t row = b / ns, i = (b % ns) * kBlk + l;
-    if (i >= D) continue;
-    const int64_t at = row * D + i;
-    const float v = m ? ld(m, at) : decode8(q[at], scale_value(s[b]));
-    st(dm, at, ld(da, at) * gelu_slope(v));
-  }
+__global__ __launch_bounds__(256) void gelu_back_rows_kernel(const T* da, const T* m, const uint8_t* __restrict__ q,
+                                                             const uint8_t* __restrict__ s, int64_t M, int D, int ns, int lg,
+                                                             T* dm) {
+  each_group(M, D, ns, lg, [&](int64_t row, int g, const RowGroup& r) {
+    float d[8], v[8];
+    load_group(da, r, D, d);
+    if (m) load_group(m, r, D, v);
+    else decode_group(q, r, D, s[row * ns + g / 4], v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d[e] *= gelu_slope(v[e]);
+    store_group(dm, r, d);
+  });
 }
 
 // ----------------------------------------------------------------------------
@@ -190,7 +265,19 @@ bool vectors_ok(int64_t D, std::initializer_list<const void*> wide, const void* 
 }
 
 constexpr int64_t kMaxGrid = 1 << 22;  // workgroups; beyond it the kernels loop
-dim3 blocks_grid(int64_t M, int64_t ns) { return dim3(unsigned(std::min(kMaxGrid, ceil_div64(M * ns, 8)))); }
+// Lanes that walk a row of 4 ns groups: as many of a wave as keep four fifths of
+// them busy.
+int row_lanes_log2(int64_t ns) {
+  int lg = 6;
+  while (lg > 2 && (ceil_div64(4 * ns, int64_t(1) << lg) << lg) * 4 > 4 * ns * 5) --lg;
+  return lg;
+}
+// A thread to each group while there are fewer than 2^19 (1741 x 3999 bf16 values
+// packed: 6.6 us, with one walk to a row 9.1; 300 x 3999: 3.3 and 6.4).
+dim3 rows_grid(int64_t M, int64_t ns, int lg) {
+  const int64_t walks = std::min(ceil_div64(4 * ns, int64_t(1) << lg), std::max<int64_t>(1, (int64_t(1) << 19) / (M << lg)));
+  return dim3(unsigned(std::min(kMaxGrid, ceil_div64(M << lg, 256))), unsigned(walks));
+}
 dim3 flat_grid(int64_t n8) { return dim3(unsigned(std::min(kMaxGrid, ceil_div64(n8, 256)))); }
 
 template <typename F>
@@ -222,6 +309,7 @@ extern "C" int avits_ckpt8_pack(const void* x, int64_t M, int64_t D, int dtype, 
   AVITS_REQUIRE(x && q && s, "ckpt8_pack: null x/q/s");
   AVITS_REQUIRE(aligned_to({x}, dtype == AVITS_BF16 ? 2 : 4), "ckpt8_pack: x is not aligned to its element");
   hipStream_t st = static_cast<hipStream_t>(stream);
+  const int ns = int(ceil_div64(D, kBlk)), lg = row_lanes_log2(ns);
   TimedLaunch timed("ckpt8", st);
   by_type(dtype, [&](auto t) {
     using T = decltype(t);
@@ -229,8 +317,7 @@ extern "C" int avits_ckpt8_pack(const void* x, int64_t M, int64_t D, int dtype, 
     if (vectors_ok(D, {x}, q))
       hipLaunchKernelGGL(pack8_kernel<T>, flat_grid(M * D / 8), dim3(256), 0, st, p, M * D / 8, q, s);
     else
-      hipLaunchKernelGGL(pack8_any_kernel<T>, blocks_grid(M, ceil_div64(D, kBlk)), dim3(256), 0, st, p, M, D,
-                         ceil_div64(D, kBlk), q, s);
+      hipLaunchKernelGGL(pack8_rows_kernel<T>, rows_grid(M, ns, lg), dim3(256), 0, st, p, M, int(D), ns, lg, q, s);
   });
   return launch_status("ckpt8_pack");
 }
@@ -242,6 +329,7 @@ extern "C" int avits_ckpt8_unpack(const uint8_t* q, const uint8_t* s, int64_t M,
   AVITS_REQUIRE(x && q && s, "ckpt8_unpack: null q/s/x");
   AVITS_REQUIRE(aligned_to({x}, dtype == AVITS_BF16 ? 2 : 4), "ckpt8_unpack: x is not aligned to its element");
   hipStream_t st = static_cast<hipStream_t>(stream);
+  const int ns = int(ceil_div64(D, kBlk)), lg = row_lanes_log2(ns);
   TimedLaunch timed("ckpt8", st);
   by_type(dtype, [&](auto t) {
     using T = decltype(t);
@@ -249,8 +337,7 @@ extern "C" int avits_ckpt8_unpack(const uint8_t* q, const uint8_t* s, int64_t M,
     if (vectors_ok(D, {x}, q))
       hipLaunchKernelGGL(unpack8_kernel<T>, flat_grid(M * D / 8), dim3(256), 0, st, q, s, M * D / 8, p);
     else
-      hipLaunchKernelGGL(unpack8_any_kernel<T>, blocks_grid(M, ceil_div64(D, kBlk)), dim3(256), 0, st, q, s, M, D,
-                         ceil_div64(D, kBlk), p);
+      hipLaunchKernelGGL(unpack8_rows_kernel<T>, rows_grid(M, ns, lg), dim3(256), 0, st, q, s, M, int(D), ns, lg, p);
   });
   return launch_status("ckpt8_unpack");
 }
@@ -265,6 +352,7 @@ extern "C" int avits_gelu_backward(const void* da, const void* m, const uint8_t*
   AVITS_REQUIRE(da && dm, "gelu_backward: null da/dm");
   AVITS_REQUIRE(aligned_to({da, m, dm}, dtype == AVITS_BF16 ? 2 : 4), "gelu_backward: a pointer is not aligned to its element");
   hipStream_t st = static_cast<hipStream_t>(stream);
+  const int ns = int(ceil_div64(D, kBlk)), lg = row_lanes_log2(ns);
   TimedLaunch timed("gelu_backward", st);
   by_type(dtype, [&](auto t) {
     using T = decltype(t);
@@ -272,8 +360,7 @@ extern "C" int avits_gelu_backward(const void* da, const void* m, const uint8_t*
     T* o = static_cast<T*>(dm);
     const int64_t n8 = M * D / 8;
     if (!vectors_ok(D, {da, m, dm}, m_q8))
-      hipLaunchKernelGGL(gelu_back_any_kernel<T>, blocks_grid(M, ceil_div64(D, kBlk)), dim3(256), 0, st, d, v, m_q8, m_s8, M,
-                         D, ceil_div64(D, kBlk), o);
+      hipLaunchKernelGGL(gelu_back_rows_kernel<T>, rows_grid(M, ns, lg), dim3(256), 0, st, d, v, m_q8, m_s8, M, int(D), ns, lg, o);
     else if (m_q8)
       hipLaunchKernelGGL((gelu_back_kernel<T, true>), flat_grid(n8), dim3(256), 0, st, d, v, m_q8, m_s8, n8, o);
     else
