@@ -689,9 +689,9 @@ int avits_noise_bits(int64_t first_pixel, int64_t n_pixels, int64_t C, uint64_t 
  * norm; dscale, dshift fp32, each NULL or [B, D] (contiguous), [D] when mod_stride
  * == 0: sums over the image's rows (zero for an image without rows), in an
  * order that depends on the sizes only.  h may be x; dx may be dh or dres;
- * no other overlap.  Pointers aligned to their element (16 bytes and D a
- * multiple of 8 (bf16) or 4 (fp32) are faster).  Requires 0 <= M < 2^25, 1 <= D
- * <= 65536, eps > 0.  M == 0: dscale and dshift are zeroed, nothing else runs.
+ * no other overlap.  Pointers aligned to their element (rows of at most
+ * 32 KB in whole 16-byte chunks are faster).  Requires 0 <= M < 2^25,
+ * 1 <= D <= 65536, eps > 0.  M == 0: dscale and dshift are zeroed, nothing else runs.
  * Errors: AVITS_ERR_INVALID_ARG, AVITS_ERR_UNSUPPORTED (dtype),
  * AVITS_ERR_WORKSPACE.
  * ---------------------------------------------------------------------- */

@@ -18,8 +18,8 @@ namespace {
 template <typename T>
 __device__ __forceinline__ float one_or(const T* p, int64_t i) { return p ? 1.f + ld(p, i) : 1.f; }
 
-// Any width and alignment: a wave per row, elements one by one, the row read
-// three times (it stays in the caches).
+// Rows that are shorter than 16 bytes or longer than registers hold: a wave per
+// row, elements one by one, the row read three times (it stays in the caches).
 template <typename T>
 __global__ __launch_bounds__(256) void norm_any_kernel(const T* x, int64_t M, int64_t D, const Images im,
                                                        const T* __restrict__ shift, const T* __restrict__ scale,
@@ -71,25 +71,57 @@ __device__ __forceinline__ u32x4 narrow(const float (&v)[kVec<T>]) {
   return w;
 }
 
-// Rows of whole 16-byte chunks: WAVES waves hold a row in registers, NC chunks
-// in a lane (chunk l + 64 WAVES c), so memory is read once and written once,
-// which is the bound.  A workgroup takes `per` consecutive rows, keeps the modulation
-// of an image as long as its rows last, and loads the next row while it reduces one.
-template <typename T, int NC, int WAVES>
+// A row's chunks of 16 bytes, at any element.  TAIL: its last chunk is partial and
+// taken from the row's end; its first `dup` elements belong to the chunk before
+// it, whose lane gives them the same bits, and are left out of sums over the row.
+template <int E, bool TAIL>
+struct ChunkAt {
+  int pos, dup;
+  __device__ __forceinline__ ChunkAt(int at, int D) : pos(E * at), dup(0) {
+    if (TAIL && pos + E > D) {
+      dup = pos + E - D;
+      pos = D - E;
+    }
+  }
+};
+// (Under a branch that one wave of a row takes.)
+template <int E>
+__device__ __forceinline__ void zero_first(float (&v)[E], int n) {
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = e < n ? 0.f : v[e];
+}
+template <typename T>
+__device__ __forceinline__ u32x4 chunk_of(const T* p) {
+  const loose4 w = *reinterpret_cast<const loose4*>(p);
+  return u32x4{w[0], w[1], w[2], w[3]};
+}
+template <typename T>
+__device__ __forceinline__ void put_chunk(T* p, const u32x4& w) {
+  *reinterpret_cast<loose4*>(p) = loose4{w[0], w[1], w[2], w[3]};
+}
+
+// WAVES waves hold a row in registers, NC chunks in a lane (chunk l + 64 WAVES c), so
+// memory is read once and written once, which is the bound.  A workgroup takes
+// `per` consecutive rows, keeps the modulation of an image as long as its rows
+// last, and loads the next row while it reduces one.  (h may be x: a row's sums
+// need all of it, so its loads are done before its first store.)  Measured (its bytes
+// at a large copy's rate in brackets): 16000 x 2048 bf16 27.5 us (25.7), x 3999
+// 57.7 (50.2; element by element, reading rows again, 235), x 8192 fp32 212 (206).
+template <typename T, int NC, int WAVES, bool TAIL>
 __global__ __launch_bounds__(256) void norm_rows_kernel(const T* x, int64_t M, int64_t D, const Images im,
                                                         const T* __restrict__ shift, const T* __restrict__ scale, float eps,
                                                         T* h, float* __restrict__ mean, float* __restrict__ rstd, int per) {
   constexpr int E = kVec<T>, kTeams = 4 / WAVES;
   __shared__ float red[2][4];
   const int lane = threadIdx.x % (kWave * WAVES), team = threadIdx.x / (kWave * WAVES);
-  const int64_t nchunk = D / E;
+  const int width = int(D), nchunk = (width + E - 1) / E;
   const int64_t first = (int64_t(blockIdx.x) * kTeams + team) * per, last = std::min<int64_t>(first + per, M);
   const float inv = 1.f / float(D);
   auto load = [&](int64_t row, u32x4 (&v)[NC]) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      const int64_t at = lane + kWave * WAVES * c;
-      v[c] = at < nchunk ? reinterpret_cast<const u32x4*>(x + row * D)[at] : u32x4{0u, 0u, 0u, 0u};
+      const int at = lane + kWave * WAVES * c;
+      v[c] = at < nchunk ? chunk_of(x + row * D + ChunkAt<E, TAIL>(at, width).pos) : u32x4{0u, 0u, 0u, 0u};
     }
   };
   auto total = [&](float s, int slot) {
@@ -111,11 +143,9 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(const T* x, int64_t M, i
       image = b;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const int64_t at = lane + kWave * WAVES * c;
-        const T* none = nullptr;
-        const T *sc = scale ? scale + b * im.stride : none, *sh = shift ? shift + b * im.stride : none;
-        g[c] = sc && at < nchunk ? reinterpret_cast<const u32x4*>(sc)[at] : u32x4{0u, 0u, 0u, 0u};
-        t[c] = sh && at < nchunk ? reinterpret_cast<const u32x4*>(sh)[at] : u32x4{0u, 0u, 0u, 0u};
+        const int at = lane + kWave * WAVES * c, pos = ChunkAt<E, TAIL>(at, width).pos;
+        g[c] = scale && at < nchunk ? chunk_of(scale + b * im.stride + pos) : u32x4{0u, 0u, 0u, 0u};
+        t[c] = shift && at < nchunk ? chunk_of(shift + b * im.stride + pos) : u32x4{0u, 0u, 0u, 0u};
       }
     }
     float s = 0.f;
@@ -123,6 +153,8 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(const T* x, int64_t M, i
     for (int c = 0; c < NC; ++c) {
       float v[E];
       widen<T>(cur[c], v);
+      const ChunkAt<E, TAIL> here(lane + kWave * WAVES * c, width);
+      if (TAIL && here.dup > 0) zero_first(v, here.dup);
 #pragma unroll
       for (int e = 0; e < E; e += 2) s += v[e] + v[e + 1];
     }
@@ -132,15 +164,20 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(const T* x, int64_t M, i
     for (int c = 0; c < NC; ++c) {
       float v[E];
       widen<T>(cur[c], v);
-      if (lane + kWave * WAVES * c < nchunk) {
+      const int at = lane + kWave * WAVES * c;
+      const ChunkAt<E, TAIL> here(at, width);
+      if (at < nchunk) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) q = fmaf(v[e] - mu, v[e] - mu, q);
+        for (int e = 0; e < E; ++e) v[e] -= mu;
+        if (TAIL && here.dup > 0) zero_first(v, here.dup);
+#pragma unroll
+        for (int e = 0; e < E; ++e) q = fmaf(v[e], v[e], q);
       }
     }
     const float rs = rsqrtf(total(q, 1) * inv + eps);
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      const int64_t at = lane + kWave * WAVES * c;
+      const int at = lane + kWave * WAVES * c;
       if (at < nchunk) {
         float v[E], w[E], z[E];
         widen<T>(cur[c], v);
@@ -148,7 +185,7 @@ __global__ __launch_bounds__(256) void norm_rows_kernel(const T* x, int64_t M, i
         widen<T>(t[c], z);
 #pragma unroll
         for (int e = 0; e < E; ++e) v[e] = (v[e] - mu) * rs * (1.f + w[e]) + z[e];
-        reinterpret_cast<u32x4*>(h + row * D)[at] = narrow<T>(v);
+        put_chunk(h + row * D + ChunkAt<E, TAIL>(at, width).pos, narrow<T>(v));
       }
     }
     if (lane == 0) {
@@ -198,7 +235,7 @@ __device__ __forceinline__ void chunk_rows(const Images& im, const Chunks& ch, i
   hi = std::min<int64_t>(lo + ch.rows, end);
 }
 
-// Backward, any width and alignment, in two steps: the two averages of each row
+// Backward of rows that are too short or too long for the kernel below, in two steps: the two averages of each row
 // (a wave per row) ...
 template <typename T>
 __global__ __launch_bounds__(256) void norm_back_avg_kernel(const T* dh, const Rows<T> xr, const float* __restrict__ mean,
@@ -253,11 +290,14 @@ __global__ __launch_bounds__(256) void norm_back_any_kernel(const T* dh, const R
   }
 }
 
-// Backward of rows of whole 16-byte chunks: a workgroup takes a chunk of rows, R
-// at a time; a thread owns NC vectors of columns for all of them, holds their
-// weight and their column sums in registers, and the rows' two averages meet
-// in LDS with one barrier for R rows.  Everything is read once and written once.
-template <typename T, bool HELD, int NC, int R>
+// Backward: a workgroup takes a chunk of rows, R at a time; a thread owns NC
+// vectors of columns for all of them, holds their weight and their column sums
+// in registers, and the rows' two averages meet in LDS with one barrier for R
+// rows.  Everything is read once and written once.  (dx may be dh or dres: rows are
+// loaded whole before the barrier, so also where two lanes store the same elements.)
+// Measured with the sums of the chunks: 16000 x 2048 bf16 48.0 us (38.6 at a copy's
+// rate), from 8 bits 46.5 (32.1), x 3999 90.7 (75.3), x 8192 fp32 311 (308).
+template <typename T, bool HELD, int NC, int R, bool TAIL>
 __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const Rows<T> xr, const float* __restrict__ mean,
                                                              const float* __restrict__ rstd, int64_t D, const Images im,
                                                              const Chunks ch, const T* __restrict__ scale, const T* dres,
@@ -265,18 +305,21 @@ __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const 
   constexpr int E = kVec<T>;
   __shared__ float red[2][8][2 * R];
   const int waves = blockDim.x / kWave, wave = threadIdx.x / kWave;
-  const int nchunk = int(D / E);
+  const int width = int(D), nchunk = (width + E - 1) / E;
   const float inv = 1.f / float(D);
   int b;
   int64_t lo, hi;
   chunk_rows(im, ch, blockIdx.x, b, lo, hi);
-  int at[NC];
+  int at[NC], pos[NC], dup[NC];
   float w[NC][E], sc[NC][E], sh[NC][E];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     at[c] = threadIdx.x + blockDim.x * c;
+    const ChunkAt<E, TAIL> here(at[c], width);
+    pos[c] = here.pos;
+    dup[c] = here.dup;
     u32x4 g = {0u, 0u, 0u, 0u};
-    if (scale && at[c] < nchunk) g = reinterpret_cast<const u32x4*>(scale + b * im.stride)[at[c]];
+    if (scale && at[c] < nchunk) g = chunk_of(scale + b * im.stride + pos[c]);
     widen<T>(g, w[c]);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -287,7 +330,7 @@ __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const 
   // The rows' data as loaded; rows past the chunk and columns past D as zeros.
   struct Batch {
     u32x4 d[R][NC], x[R][NC], r[R][NC];
-    uint32_t s[R][NC];
+    uint32_t s[R][NC], s_first[R][NC];   // (s_first: of a partial chunk's first elements, which may be of the block before)
     float mu[R], rs[R];
   };
   auto load = [&](int64_t row, Batch& t) {
@@ -301,24 +344,25 @@ __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const 
       for (int c = 0; c < NC; ++c) {
         const u32x4 zero = {0u, 0u, 0u, 0u};
         const bool here = in && at[c] < nchunk;
-        t.d[r][c] = here ? reinterpret_cast<const u32x4*>(dh + m * D)[at[c]] : zero;
+        t.d[r][c] = here ? chunk_of(dh + m * D + pos[c]) : zero;
         t.x[r][c] = zero;
         if constexpr (HELD) {
-          const uint8_t* q = xr.q + m * D + at[c] * E;
+          const uint8_t* q = xr.q + m * D + pos[c];
           if (here) {
             if constexpr (E == 8) {
-              const u32x2 v = *reinterpret_cast<const u32x2*>(q);
+              const loose2 v = *reinterpret_cast<const loose2*>(q);
               t.x[r][c][0] = v[0];
               t.x[r][c][1] = v[1];
             } else {
-              t.x[r][c][0] = *reinterpret_cast<const uint32_t*>(q);
+              t.x[r][c][0] = *reinterpret_cast<const loose1*>(q);
             }
           }
           t.s[r][c] = here ? xr.s[m * xr.ns + at[c] * E / kBlk] : 0u;
+          if (TAIL) t.s_first[r][c] = here && dup[c] > 0 ? xr.s[m * xr.ns + pos[c] / kBlk] : 0u;
         } else if (here) {
-          t.x[r][c] = reinterpret_cast<const u32x4*>(xr.x + m * D)[at[c]];
+          t.x[r][c] = chunk_of(xr.x + m * D + pos[c]);
         }
-        t.r[r][c] = here && dres ? reinterpret_cast<const u32x4*>(dres + m * D)[at[c]] : zero;
+        t.r[r][c] = here && dres ? chunk_of(dres + m * D + pos[c]) : zero;
       }
     }
   };
@@ -332,6 +376,13 @@ __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const 
         const float scale8 = scale_value(t.s[r][c]);
         decode8x4(t.x[r][c][0], scale8, n);
         if constexpr (E == 8) decode8x4(t.x[r][c][1], scale8, n + 4);
+        if (TAIL && dup[c] > 0) {
+          float first[E];
+          decode8x4(t.x[r][c][0], scale_value(t.s_first[r][c]), first);
+          if constexpr (E == 8) decode8x4(t.x[r][c][1], scale_value(t.s_first[r][c]), first + 4);
+#pragma unroll
+          for (int e = 0; e < E; ++e) n[e] = e < dup[c] ? first[e] : n[e];
+        }
       } else {
         widen<T>(t.x[r][c], n);
       }
@@ -347,6 +398,10 @@ __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const 
         float dv[E], n[E];
         widen<T>(t.d[r][c], dv);
         normed(r, c, n);
+        if (TAIL && dup[c] > 0) {
+          zero_first(dv, dup[c]);
+          zero_first(n, dup[c]);
+        }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const float g = dv[e] * w[c][e];
@@ -361,6 +416,13 @@ __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const 
       if (threadIdx.x % kWave == 0)
 #pragma unroll
         for (int k = 0; k < 2 * R; ++k) red[turn][wave][k] = sum[k];
+      if constexpr (TAIL) {
+        // dres too has arrived before another wave may store over its elements.
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) asm volatile("" ::"v"(t.r[r][c]) : "memory");
+      }
       __syncthreads();   // the other half of red is read before the next one's barrier
 #pragma unroll
       for (int k = 0; k < 2 * R; ++k) sum[k] = red[turn][0][k];
@@ -385,7 +447,7 @@ __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const 
           sh[c][e] += dv[e];
           o[e] += t.rs[r] * (dv[e] * w[c][e] - ag - n[e] * an);
         }
-        reinterpret_cast<u32x4*>(dx + (row + r) * D)[at[c]] = narrow<T>(o);
+        put_chunk(dx + (row + r) * D + pos[c], narrow<T>(o));
       }
     }
     t = next;
@@ -396,19 +458,19 @@ __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const 
       if (at[c] >= nchunk) continue;
 #pragma unroll
       for (int e = 0; e < E; e += 4) {
-        float* p = part + int64_t(2 * blockIdx.x) * D + at[c] * E + e;
-        *reinterpret_cast<f32x4*>(p) = f32x4{sc[c][e], sc[c][e + 1], sc[c][e + 2], sc[c][e + 3]};
-        *reinterpret_cast<f32x4*>(p + D) = f32x4{sh[c][e], sh[c][e + 1], sh[c][e + 2], sh[c][e + 3]};
+        float* p = part + int64_t(2 * blockIdx.x) * D + pos[c] + e;
+        put_chunk(p, __builtin_bit_cast(u32x4, f32x4{sc[c][e], sc[c][e + 1], sc[c][e + 2], sc[c][e + 3]}));
+        put_chunk(p + D, __builtin_bit_cast(u32x4, f32x4{sh[c][e], sh[c][e + 1], sh[c][e + 2], sh[c][e + 3]}));
       }
     }
   }
 }
 
-// Sums of the chunks' parts, in chunk order within each of 16 strands: 16 V
+// Sums of the chunks' parts, in chunk order within each of 64 strands: 16 V
 // columns of a workgroup (V = 4 where rows of D floats are aligned), blockIdx.y
 // the image (or all of them together), blockIdx.z scale or shift.
 template <int V>
-__global__ __launch_bounds__(256) void norm_back_sum_kernel(const float* __restrict__ part, int64_t D, const Chunks ch,
+__global__ __launch_bounds__(1024) void norm_back_sum_kernel(const float* __restrict__ part, int64_t D, const Chunks ch,
                                                             int together, float* __restrict__ dscale,
                                                             float* __restrict__ dshift) {
   typedef float vec __attribute__((ext_vector_type(V)));
@@ -430,16 +492,21 @@ __global__ __launch_bounds__(256) void norm_back_sum_kernel(const float* __restr
   if (i < D) {
     const float* p = part + blockIdx.z * D + i;
     int c = c0 + strand;
-    for (; c + 16 * 7 < c1; c += 16 * 8) {   // eight loads in flight
-      vec t[8];
+    for (; c + 64 * 3 < c1; c += 64 * 4) {   // four loads in flight
+      vec t[4];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) t[k] = *reinterpret_cast<const vec*>(p + 2 * D * (c + 16 * k));
+      for (int k = 0; k < 4; ++k) t[k] = *reinterpret_cast<const vec*>(p + 2 * D * (c + 64 * k));
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v += t[k];
+      for (int k = 0; k < 4; ++k) v += t[k];
     }
-    for (; c < c1; c += 16) v += *reinterpret_cast<const vec*>(p + 2 * D * c);
+    for (; c < c1; c += 64) v += *reinterpret_cast<const vec*>(p + 2 * D * c);
   }
-  red[strand][col] = v;
+  // A wave's four strands, then the sixteen waves.
+#pragma unroll
+  for (int k = 16; k < kWave; k *= 2)
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] += __shfl_xor(v[e], k);
+  if (strand % 4 == 0) red[strand / 4][col] = v;
   __syncthreads();
   if (strand == 0 && i < D) {
 #pragma unroll
@@ -458,11 +525,15 @@ int check_norm(const char* who, int64_t M, int64_t D, int32_t B, const int64_t* 
   return fill_images(who, M, B, off, mod_stride, im);
 }
 
-constexpr int kMaxChunks = 512;  // two workgroups per CU
+// Chunks of rows at most, of at least four rows: whole rounds of workgroups with two
+// waves to a SIMD or a little more, by the waves that rows of bf16 take.  Measured, 512
+// chunks and by this rule: 40000 x 512 bf16 51.8 and 38.3 us, 16000 x 37 24.3
+// and 15.5, 4608 x 4096 34.8 and 30.3.
+int64_t max_chunks(int64_t D) { return 256 * ceil_div64(8, std::min<int64_t>(8, ceil_div64(D, 512))); }
 
-Chunks make_chunks(int64_t M, const Images& im) {
+Chunks make_chunks(int64_t M, int64_t D, const Images& im) {
   Chunks ch;
-  ch.rows = int32_t(std::max<int64_t>(4, ceil_div64(M, kMaxChunks)));
+  ch.rows = int32_t(std::max<int64_t>(4, ceil_div64(M, max_chunks(D))));
   int32_t n = 0;
   int64_t at = 0;
   for (int i = 0; i < kMaxSeqs; ++i) {
@@ -474,12 +545,6 @@ Chunks make_chunks(int64_t M, const Images& im) {
   return ch;
 }
 
-// Whether rows and vectors come in whole, aligned 16-byte chunks.
-bool chunked(int64_t D, int64_t stride, size_t z, std::initializer_list<const void*> ps) {
-  const int64_t e = int64_t(16 / z);
-  return D % e == 0 && stride % e == 0 && aligned_to(ps, 16);
-}
-
 template <typename T>
 void run_norm(const void* x, int64_t M, int64_t D, const Images& im, const void* shift, const void* scale, float eps,
               void* h, float* mean, float* rstd, hipStream_t s) {
@@ -487,7 +552,7 @@ void run_norm(const void* x, int64_t M, int64_t D, const Images& im, const void*
   const T *px = static_cast<const T*>(x), *sh = static_cast<const T*>(shift), *sc = static_cast<const T*>(scale);
   T* ph = static_cast<T*>(h);
   const int64_t chunks = ceil_div64(D * int64_t(sizeof(T)), 16 * kWave);   // a wave's chunks per lane
-  if (!chunked(D, im.stride, sizeof(T), {x, h, shift, scale}) || chunks > 32) {
+  if (D < kVec<T> || chunks > 32) {
     hipLaunchKernelGGL(norm_any_kernel<T>, dim3(unsigned(ceil_div64(M, 4))), dim3(256), 0, s, px, M, D, im, sh, sc, eps, ph,
                        mean, rstd);
     return;
@@ -497,16 +562,23 @@ void run_norm(const void* x, int64_t M, int64_t D, const Images& im, const void*
     const int64_t teams = 4 / kW;
     // A few rows to a team, once there are enough for every SIMD.
     const int per = int(std::min<int64_t>(8, std::max<int64_t>(1, M / (teams * 2048))));
-    hipLaunchKernelGGL((norm_rows_kernel<T, kNC, kW>), dim3(unsigned(ceil_div64(M, teams * per))), dim3(256), 0, s, px, M, D, im,
-                       sh, sc, eps, ph, mean, rstd, per);
+    const dim3 grid(unsigned(ceil_div64(M, teams * per)));
+    if (D % kVec<T> == 0)
+      hipLaunchKernelGGL((norm_rows_kernel<T, kNC, kW, false>), grid, dim3(256), 0, s, px, M, D, im, sh, sc, eps, ph, mean, rstd,
+                         per);
+    else
+      hipLaunchKernelGGL((norm_rows_kernel<T, kNC, kW, true>), grid, dim3(256), 0, s, px, M, D, im, sh, sc, eps, ph, mean, rstd,
+                         per);
   };
   using std::integral_constant;
   const integral_constant<int, 1> one;
   const integral_constant<int, 4> four;
+  // One wave to a row while a lane holds four chunks at most, else four: 16000 x
+  // 2050 bf16 38.9 us, by one wave 59.1; one such row 3.8 and 7.3.
   if (chunks <= 1) go(one, one);
   else if (chunks <= 2) go(integral_constant<int, 2>(), one);
   else if (chunks <= 4) go(four, one);
-  else if (chunks <= 8) go(integral_constant<int, 8>(), one);
+  else if (chunks <= 8) go(integral_constant<int, 2>(), four);
   else if (chunks <= 16) go(four, four);
   else go(integral_constant<int, 8>(), four);
 }
@@ -516,7 +588,7 @@ void run_norm_back(const void* dh, const Rows<T>& rows, const float* mean, const
                    const Images& im, const void* scale, const void* dres, void* dx, float* dscale, float* dshift,
                    float* ws, hipStream_t s) {
   TimedLaunch timed("layer_norm_backward", s);
-  const Chunks ch = make_chunks(M, im);
+  const Chunks ch = make_chunks(M, D, im);
   const int n = ch.first[kMaxSeqs];
   float* avg = ws;
   float* part = ws + align_up(size_t(2 * M), 64);
@@ -524,20 +596,29 @@ void run_norm_back(const void* dh, const Rows<T>& rows, const float* mean, const
   T* o = static_cast<T*>(dx);
   const int parts = dscale || dshift ? 1 : 0;
   const int64_t chunks = ceil_div64(D * int64_t(sizeof(T)), 16);
-  if (chunked(D, im.stride, sizeof(T), {dh, rows.x, scale, dres, dx, ws}) && (!rows.q || aligned_to({rows.q}, 8)) &&
-      chunks <= 1024) {
-    auto go = [&](auto nc) {
-      constexpr int kNC = decltype(nc)::value, kR = kNC == 1 ? 2 : 1;
+  if (D >= kVec<T> && chunks <= 2048) {
+    auto go = [&](auto nc, auto two) {
+      constexpr int kNC = decltype(nc)::value, kR = decltype(two)::value ? 2 : 1;
       const dim3 wg(unsigned(ceil_div64(ceil_div64(chunks, kNC), kWave) * kWave));
-      if (rows.q)
-        hipLaunchKernelGGL((norm_back_rows_kernel<T, true, kNC, kR>), dim3(unsigned(n)), wg, 0, s, d, rows, mean, rstd, D, im, ch,
-                           sc, res, o, part, parts);
-      else
-        hipLaunchKernelGGL((norm_back_rows_kernel<T, false, kNC, kR>), dim3(unsigned(n)), wg, 0, s, d, rows, mean, rstd, D, im, ch,
-                           sc, res, o, part, parts);
+      auto form = [&](auto held, auto tail) {
+        hipLaunchKernelGGL((norm_back_rows_kernel<T, decltype(held)::value, kNC, kR, decltype(tail)::value>), dim3(unsigned(n)), wg,
+                           0, s, d, rows, mean, rstd, D, im, ch, sc, res, o, part, parts);
+      };
+      const std::true_type yes;
+      const std::false_type no;
+      if (rows.q && D % kVec<T> == 0) form(yes, no);
+      else if (rows.q) form(yes, yes);
+      else if (D % kVec<T> == 0) form(no, no);
+      else form(no, yes);
     };
-    if (chunks <= 512) go(std::integral_constant<int, 1>());
-    else go(std::integral_constant<int, 2>());
+    // Two rows at a time, except where five to seven waves leave no room for a second
+    // workgroup on the CU with their registers (16000 x 2560 bf16 in 8 bits: 53.9 us, by
+    // two rows 79.7; 16000 x 3999 100.9 instead of 90.8).
+    const std::integral_constant<int, 1> one;
+    if (chunks <= 256 || (chunks > 448 && chunks <= 512)) go(one, std::true_type());
+    else if (chunks <= 512) go(one, std::false_type());
+    else if (chunks <= 1024) go(std::integral_constant<int, 2>(), std::false_type());
+    else go(std::integral_constant<int, 4>(), std::false_type());
   } else {
     if (M > 0)
       hipLaunchKernelGGL(norm_back_avg_kernel<T>, dim3(unsigned(ceil_div64(M, 4))), dim3(256), 0, s, d, rows, mean, rstd, M, D,
@@ -550,7 +631,7 @@ void run_norm_back(const void* dh, const Rows<T>& rows, const float* mean, const
     auto sum = [&](auto v) {
       constexpr int kV = decltype(v)::value;
       hipLaunchKernelGGL(norm_back_sum_kernel<kV>, dim3(unsigned(ceil_div64(D, 16 * kV)), unsigned(together ? 1 : im.B), 2),
-                         dim3(256), 0, s, (const float*)part, D, ch, together, dscale, dshift);
+                         dim3(1024), 0, s, (const float*)part, D, ch, together, dscale, dshift);
     };
     if (D % 4 == 0 && aligned_to({part}, 16)) sum(std::integral_constant<int, 4>());
     else sum(std::integral_constant<int, 1>());
@@ -582,7 +663,7 @@ extern "C" int avits_layer_norm(const void* x, int64_t M, int64_t D, int32_t B, 
 
 extern "C" size_t avits_layer_norm_backward_workspace_bytes(int64_t M, int64_t D, int32_t B) {
   if (M < 0 || M >= (int64_t(1) << 25) || D < 1 || D > 65536 || B < 1 || B > kMaxSeqs) return 0;
-  const size_t chunks = size_t(std::min<int64_t>(kMaxChunks, ceil_div64(M, 4))) + size_t(B);
+  const size_t chunks = size_t(std::min<int64_t>(max_chunks(D), ceil_div64(M, 4))) + size_t(B);
   return (align_up(size_t(2 * M), 64) + 2 * chunks * size_t(D)) * sizeof(float);
 }
 
