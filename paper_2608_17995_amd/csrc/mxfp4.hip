@@ -230,8 +230,10 @@ __device__ __forceinline__ void turn_chunks(u32x4 (&c)[V], int l) {
 // (l, g) has rows mb + 8 l + i and, of each, the columns nb + 16 g .. + 15.
 // Whole 16-byte chunks of a row are turned over between neighbouring lanes, so
 // that a store instruction covers whole rows of the block (16-byte pieces
-// of 64 bytes each took four times as long), by buffer accesses that drop what lies
-// outside; where rows (or the bias) do not start on 16 bytes the columns go one by one.
+// of 64 bytes each took four times as long): by buffer accesses that drop what lies
+// outside, or (VEC false: rows or the bias do not start on 16 bytes) by plain ones,
+// which may lie at any element, and a row's last, partial chunk one by one
+// (4608 x 8195 x 2048 57.7 us, 8192 columns 55.4; column by column it took 164).
 template <typename T, bool GATED, bool VEC>
 struct BlockEnd {
   static constexpr int Z = sizeof(T), E = 16 / Z, V = 16 / E;   // elements of a chunk, chunks of a lane's columns
@@ -264,11 +266,18 @@ struct BlockEnd {
     const int chunk = V * g + (l & (V - 1)), row = 8 * ((l & ~(V - 1)) + q) + i;
     return E * chunk < cols ? uint32_t(row) * uint32_t(N * Z) + 16 * chunk : kNowhere;
   }
+  // The same without alignment: where the chunk starts (elements of the output), and
+  // how many of its elements there are (0: none).
+  __device__ __forceinline__ int64_t loose_at(int i, int q, int& n) const {
+    const int chunk = V * g + (l & (V - 1)), row = 8 * ((l & ~(V - 1)) + q) + i;
+    n = row < rows ? std::max(0, std::min(E, cols - E * chunk)) : 0;
+    return (mb + row) * N + nb + E * chunk;
+  }
   __device__ __forceinline__ void row(int i, float (&v)[16]) {
 #pragma unroll
     for (int c = 0; c < 16; ++c) v[c] += bias.at(c);
-    const int r = 8 * l + i;
     if constexpr (GATED) {
+      const int r = 8 * l + i;
       if (!one) {
         int64_t skip = 0;
         const int64_t stride = a->im.stride, at_row = mb + std::min(r, rows - 1);
@@ -289,29 +298,56 @@ struct BlockEnd {
 #pragma unroll
         for (int q = 0; q < V; ++q)
           res.w[q] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, int(at(i, q)), 0, 0));
-        turn_chunks<V>(res.w, l);
       } else {
-        res.load(static_cast<const T*>(a->resid) + mb * N, int64_t(rows) * N, int64_t(std::min(r, rows - 1)) * N + nb + 16 * g);
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+          int n;
+          const T* p = static_cast<const T*>(a->resid) + loose_at(i, q, n);
+          res.w[q] = u32x4{0u, 0u, 0u, 0u};
+          if (n == E) {
+            const loose4 w = *reinterpret_cast<const loose4*>(p);
+            res.w[q] = u32x4{w[0], w[1], w[2], w[3]};
+          } else if (n > 0) {
+#pragma unroll
+            for (int e = 0; e < E - 1; ++e)
+              if (e < n) res.w[q][e * Z / 4] |= element(p + e) << (Z == 2 && e % 2 ? 16 : 0);
+          }
+        }
       }
+      turn_chunks<V>(res.w, l);
 #pragma unroll
       for (int c = 0; c < 16; ++c) v[c] = res.at(c) + gate.at(c) * v[c];
     }
-    if constexpr (VEC) {
-      u32x4 w[V];
+    u32x4 w[V];
 #pragma unroll
-      for (int q = 0; q < V; ++q)
+    for (int q = 0; q < V; ++q)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          w[q][e] = Z == 4 ? __float_as_uint(v[4 * q % 16 + e]) : pack_bf2(v[(8 * q + 2 * e) % 16], v[(8 * q + 2 * e + 1) % 16]);
-      turn_chunks<V>(w, l);
+      for (int e = 0; e < 4; ++e)
+        w[q][e] = Z == 4 ? __float_as_uint(v[4 * q % 16 + e]) : pack_bf2(v[(8 * q + 2 * e) % 16], v[(8 * q + 2 * e + 1) % 16]);
+    turn_chunks<V>(w, l);
 #pragma unroll
-      for (int q = 0; q < V; ++q) __builtin_amdgcn_raw_buffer_store_b128(w[q], ro, int(at(i, q)), 0, 0);
-    } else if (r < rows) {
-      T* p = static_cast<T*>(a->out) + (mb + r) * N + nb;
+    for (int q = 0; q < V; ++q) {
+      if constexpr (VEC) {
+        __builtin_amdgcn_raw_buffer_store_b128(w[q], ro, int(at(i, q)), 0, 0);
+      } else {
+        int n;
+        T* p = static_cast<T*>(a->out) + loose_at(i, q, n);
+        if (n == E) {
+          *reinterpret_cast<loose4*>(p) = loose4{w[q][0], w[q][1], w[q][2], w[q][3]};
+        } else if (n > 0) {
 #pragma unroll
-      for (int c = 0; c < 16; ++c)
-        if (16 * g + c < cols) st(p, 16 * g + c, v[c]);
+          for (int e = 0; e < E - 1; ++e)
+            if (e < n) {
+              if constexpr (Z == 4) p[e] = __uint_as_float(w[q][e]);
+              else p[e] = bf16_t(w[q][e / 2] >> (e % 2 ? 16 : 0));
+            }
+        }
+      }
     }
+  }
+  static __device__ __forceinline__ uint32_t element(const T* p) {
+    if constexpr (Z == 4) return __float_as_uint(*p);
+    else return uint32_t(*p);
   }
 };
 
@@ -632,8 +668,10 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(const Mx4Args args, const
 // two) and has, for each t, the operand of one bf16 instruction: 8 n of column k.
 // So the result's lane holds 8 consecutive columns of rows 4 g + r.
 // Bound by the conversions (about 220 vector instructions for 8 TM matrix ones).
+// ODD: N is no multiple of 8; dy's rows lie at any element, and of the last group of
+// eight n what is not there counts as 0.
 // blockIdx.y: part of the contraction, summed into its own [M, K] where there are several.
-template <int TM, int NW, typename OUT>
+template <int TM, int NW, bool ODD, typename OUT>
 __global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const bf16_t* __restrict__ dy, int64_t M, int64_t N,
                                                                 const uint8_t* __restrict__ wq, const uint8_t* __restrict__ ws,
                                                                 int64_t K, OUT* __restrict__ dx) {
@@ -654,7 +692,7 @@ __global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const bf16_t* __
   };
   // (Past the last step everything is out of range: zeros, no memory.)
   auto load = [&](int t, Step& v) {
-    const int64_t n = int64_t(t) * 32 + 8 * g;   // N is a multiple of 8: the lane's eight rows are there or not
+    const int64_t n = int64_t(t) * 32 + 8 * g;
     const __amdgpu_buffer_rsrc_t rw = range_of(wq + int64_t(t) * 32 * rowb, (N - int64_t(t) * 32) * rowb);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
@@ -663,9 +701,28 @@ __global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const bf16_t* __
     v.sc = __builtin_bit_cast(
         u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, int(k < K && n < N ? uint32_t((k / 64 * Np + n) * 2) : kNowhere), 0, 0));
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
-      v.y[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                             ry, int(n < N ? uint32_t(((16 * i + l) * N + n) * 2) : kNowhere), 0, 0));
+    for (int i = 0; i < TM; ++i) {
+      if constexpr (!ODD) {
+        v.y[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                               ry, int(n < N ? uint32_t(((16 * i + l) * N + n) * 2) : kNowhere), 0, 0));
+      } else {   // (rows past M repeat the last one, unused)
+        const bf16_t* p = dy + std::min<int64_t>(m0 + 16 * i + l, M - 1) * N + n;
+        v.y[i] = u32x4{0u, 0u, 0u, 0u};
+        if (n + 8 <= N) {
+          const loose4 w = *reinterpret_cast<const loose4*>(p);
+          v.y[i] = u32x4{w[0], w[1], w[2], w[3]};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 7; ++e)
+            if (n + e < N) v.y[i][e / 2] |= uint32_t(p[e]) << (e % 2 ? 16 : 0);
+        }
+      }
+    }
+    if (ODD && n < N && n + 8 > N) {   // (the codes past N read as 0; their scales may be anything)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (n + e >= N) v.sc[e / 2] &= e % 2 ? 0xffffu : 0xffff0000u;
+    }
   };
   const int stride = NW * int(gridDim.y);
   int t = int(blockIdx.y) * NW + wave;
@@ -756,13 +813,30 @@ __global__ __launch_bounds__(256) void transpose4_kernel(const uint8_t* __restri
   }
 }
 
-// Rows of N elements to rows of ld, zeros behind (any alignment).
+// Rows of N elements to rows of ld (a multiple of 64), zeros behind: 16 bytes a lane,
+// read at any element.
 template <typename T>
 __global__ __launch_bounds__(256) void widen_kernel(const T* __restrict__ x, int64_t M, int64_t N, T* __restrict__ y,
                                                     int64_t ld) {
-  const int64_t n = int64_t(blockIdx.y) * 256 + threadIdx.x;
+  constexpr int E = 16 / int(sizeof(T));
+  const int64_t n = (int64_t(blockIdx.y) * 64 + threadIdx.x % 64) * E;
   if (n >= ld) return;
-  for (int64_t m = blockIdx.x; m < M; m += gridDim.x) y[m * ld + n] = n < N ? x[m * N + n] : T(0);
+  for (int64_t m = int64_t(blockIdx.x) * 4 + threadIdx.x / 64; m < M; m += int64_t(gridDim.x) * 4) {
+    const T* p = x + m * N + n;
+    u32x4 w = {0u, 0u, 0u, 0u};
+    if (n + E <= N) {
+      const loose4 v = *reinterpret_cast<const loose4*>(p);
+      w = u32x4{v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+      for (int e = 0; e < E - 1; ++e)
+        if (n + e < N) {
+          if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(p[e]);
+          else w[e / 2] |= uint32_t(p[e]) << (e % 2 ? 16 : 0);
+        }
+    }
+    *reinterpret_cast<u32x4*>(y + m * ld + n) = w;
+  }
 }
 
 int check_product(const char* who, int64_t M, int64_t N, int64_t K, int dtype) {
@@ -779,8 +853,9 @@ int check_product(const char* who, int64_t M, int64_t N, int64_t K, int dtype) {
 // How a product runs: 256 x 256 tiles, each in `splits` parts of the contraction,
 // or (splits == 0) form `rows` of the kernel for few rows.  The least predicted
 // time (us), from what was measured:
-//  - few rows: the larger of the operands' bytes, which each workgroup reads for
-//    itself, at the rate its form reaches, and its chain of steps over its waves;
+//  - few rows: the largest of the operands' bytes, which each workgroup reads for
+//    itself, at the rate its form reaches, its chain of steps over its waves, and the
+//    outputs, stored one by one (16000 x 8192 x 96: 539 us; by tiles 60);
 //  - tiles, in equal rounds of at most one unit per CU: 1.2 (few CUs busy) to 1.5 a
 //    step and 6.5 a unit; parts are written and read at 7 TB/s by a second launch.
 // Measured (bf16 out; forms 1 x 1, 2 x 2, 4 x 2, 4 x 4 strips of 16, tiles whole, in 4 parts):
@@ -807,7 +882,7 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t K) {
     const auto& form = kForms[f];
     const double wgs = double(ceil_div64(M, 16 * form.tm)) * double(ceil_div64(N, 16 * form.tn));
     const double bytes = wgs * 16.0 * (form.tm + form.tn) * double(K) * 0.53e-6;
-    const double us = form.fixed + std::max(bytes / form.rate, std::ceil(steps / form.waves) * form.step);
+    const double us = form.fixed + std::max({bytes / form.rate, std::ceil(steps / form.waves) * form.step, double(M) * double(N) * 3.8e-6});
     if (us >= best) continue;
     best = us;
     p.form = f;
@@ -881,10 +956,9 @@ struct BackPlan {
   size_t wt, dy, part;
   int rows = 0, parts = 1;   // rows > 0: the kernel for few rows with 16 `rows` rows to a workgroup
 };
-// Few rows (bf16, rows of dy whole 16-byte chunks) go straight from the held
-// weight, 16 of them to a workgroup of eight waves (two of which fit a CU) or 64 to
-// one of four, the contraction whole or in parts; the other way is to turn the
-// weight round and run the bf16 product.  The least predicted time (us).  A chain
+// Few rows (bf16) go straight from the held weight, 16 of them to a workgroup of eight
+// waves (two of which fit a CU) or 64 to one of four, the contraction whole or in
+// parts; the other way is to turn the weight round and run the bf16 product.  The least predicted time (us).  A chain
 // step takes 1.0 us (1.7 with two workgroups on a CU; 1.2 with 64 rows), parts a
 // launch and their bytes.  Measured (16 rows whole, in 4; 64 rows in 4; turned round):
 //   16 x 8192 x 2048   33.3  13.6  24.4  45.9     512 x 8192 x 2048  56.6  59.6  48.0  46.9
@@ -897,7 +971,7 @@ BackPlan plan_back(int64_t M, int64_t N, int64_t K, int dtype) {
   p.wt = align_up(size_t(K) * size_t(p.ld) * z, 256);
   p.dy = p.ld != N ? align_up(size_t(M) * size_t(p.ld) * z, 256) : 0;
   p.part = dtype == AVITS_BF16 ? std::min<size_t>(gemm_partial_reserve(M, K), size_t(64) << 20) : 0;
-  if (dtype == AVITS_BF16 && N % 8 == 0) {
+  if (dtype == AVITS_BF16) {
     const double weights = double(N) * double(K) * 1e-6;
     double best = 16.0 + weights * 4.5 / 4.0 + 2.0 * double(M) * weights / 1.1e6;
     for (int rows : {1, 4})
@@ -928,8 +1002,11 @@ int run_back(const void* dy, int64_t M, int64_t N, const uint8_t* wq, const uint
       auto go = [&](auto tm, auto nw, auto* out) {
         constexpr int kTM = decltype(tm)::value, kNW = decltype(nw)::value;
         const dim3 grid(unsigned(ceil_div64(M, 16 * kTM) * ceil_div64(K, 128)), unsigned(p.parts));
-        hipLaunchKernelGGL((mx4_back_rows_kernel<kTM, kNW, std::remove_pointer_t<decltype(out)>>), grid, dim3(64 * kNW), 0, s, y, M,
-                           N, wq, ws, K, out);
+        using Out = std::remove_pointer_t<decltype(out)>;
+        if (N % 8 == 0)
+          hipLaunchKernelGGL((mx4_back_rows_kernel<kTM, kNW, false, Out>), grid, dim3(64 * kNW), 0, s, y, M, N, wq, ws, K, out);
+        else
+          hipLaunchKernelGGL((mx4_back_rows_kernel<kTM, kNW, true, Out>), grid, dim3(64 * kNW), 0, s, y, M, N, wq, ws, K, out);
       };
       using std::integral_constant;
       auto by_rows = [&](auto* out) {
@@ -953,8 +1030,8 @@ int run_back(const void* dy, int64_t M, int64_t N, const uint8_t* wq, const uint
                        K, wt, p.ld);
     if (p.dy) {
       T* wide = reinterpret_cast<T*>(scratch + p.wt);
-      hipLaunchKernelGGL(widen_kernel<T>, dim3(unsigned(std::min<int64_t>(M, 4096)), unsigned(ceil_div64(p.ld, 256))), dim3(256),
-                         0, s, static_cast<const T*>(dy), M, N, wide, p.ld);
+      hipLaunchKernelGGL(widen_kernel<T>, dim3(unsigned(std::min<int64_t>(ceil_div64(M, 4), 4096)), unsigned(ceil_div64(p.ld, 1024 / sizeof(T)))),
+                         dim3(256), 0, s, static_cast<const T*>(dy), M, N, wide, p.ld);
       dy = wide;
     }
   }
