@@ -670,9 +670,34 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(const Mx4Args args, const
 // Bound by the conversions (about 220 vector instructions for 8 TM matrix ones).
 // ODD: N is no multiple of 8; dy's rows lie at any element, and of the last group of
 // eight n what is not there counts as 0.
+// An fp32 dy goes as three bf16 values whose sum it is exactly (8 bits of its 24 each), so
+// their products with the weight's values are exact too and the sums are fp32's.
 // blockIdx.y: part of the contraction, summed into its own [M, K] where there are several.
-template <int TM, int NW, bool ODD, typename OUT>
-__global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const bf16_t* __restrict__ dy, int64_t M, int64_t N,
+struct Thirds {
+  u32x4 v[3];
+};
+__device__ __forceinline__ Thirds thirds_of(const u32x4& lo, const u32x4& hi) {
+  Thirds t;
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    uint32_t bits[3][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float x = __uint_as_float((e < 4 ? lo : hi)[e % 4 + h]);
+      bits[0][h] = __float_as_uint(x) & 0xffff0000u;
+      float r = x - __uint_as_float(bits[0][h]);
+      r = __builtin_isinf(x) ? 0.f : r;   // (of NaN: NaN)
+      bits[1][h] = __float_as_uint(r) & 0xffff0000u;
+      bits[2][h] = __float_as_uint(r - __uint_as_float(bits[1][h]));
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) t.v[k][e / 2] = __builtin_amdgcn_perm(bits[k][1], bits[k][0], 0x07060302u);
+  }
+  return t;
+}
+
+template <int TM, int NW, bool ODD, typename IN, typename OUT>
+__global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const IN* __restrict__ dy, int64_t M, int64_t N,
                                                                 const uint8_t* __restrict__ wq, const uint8_t* __restrict__ ws,
                                                                 int64_t K, OUT* __restrict__ dx) {
   __shared__ float red[NW][TM * 32][kWave];
@@ -682,13 +707,14 @@ __global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const bf16_t* __
   const int64_t k0 = int64_t(blockIdx.x) % tk * 128, m0 = int64_t(blockIdx.x) / tk * (16 * TM);
   const int64_t Np = scale_rows(N), rowb = K / 2, k = k0 + 8 * l;
   const __amdgpu_buffer_rsrc_t rs = range_of(ws, scale_groups(K) * Np * 2);
-  const __amdgpu_buffer_rsrc_t ry = range_of(dy + m0 * N, (M - m0) * N * 2);
+  constexpr int Z = sizeof(IN), V = Z / 2;   // 16-byte words of eight elements
+  const __amdgpu_buffer_rsrc_t ry = range_of(dy + m0 * N, (M - m0) * N * Z);
   const int shift = 8 * int(k / 32 % 2);
   const int steps = int((N + 31) / 32);
   f32x4 acc[TM][8] = {};
   struct Step {
     uint32_t w[8];
-    u32x4 sc, y[TM];
+    u32x4 sc, y[TM][V];
   };
   // (Past the last step everything is out of range: zeros, no memory.)
   auto load = [&](int t, Step& v) {
@@ -703,18 +729,28 @@ __global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const bf16_t* __
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       if constexpr (!ODD) {
-        v.y[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                               ry, int(n < N ? uint32_t(((16 * i + l) * N + n) * 2) : kNowhere), 0, 0));
+#pragma unroll
+        for (int q = 0; q < V; ++q)
+          v.y[i][q] = __builtin_bit_cast(
+              u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                         ry, int(n < N ? uint32_t(((16 * i + l) * N + n) * Z + 16 * q) : kNowhere), 0, 0));
       } else {   // (rows past M repeat the last one, unused)
-        const bf16_t* p = dy + std::min<int64_t>(m0 + 16 * i + l, M - 1) * N + n;
-        v.y[i] = u32x4{0u, 0u, 0u, 0u};
-        if (n + 8 <= N) {
-          const loose4 w = *reinterpret_cast<const loose4*>(p);
-          v.y[i] = u32x4{w[0], w[1], w[2], w[3]};
-        } else {
+        const IN* p = dy + std::min<int64_t>(m0 + 16 * i + l, M - 1) * N + n;
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+          v.y[i][q] = u32x4{0u, 0u, 0u, 0u};
+          if (n + 8 <= N) {
+            const loose4 w = *reinterpret_cast<const loose4*>(p + 16 / Z * q);
+            v.y[i][q] = u32x4{w[0], w[1], w[2], w[3]};
+          }
+        }
+        if (n < N && n + 8 > N) {
 #pragma unroll
           for (int e = 0; e < 7; ++e)
-            if (n + e < N) v.y[i][e / 2] |= uint32_t(p[e]) << (e % 2 ? 16 : 0);
+            if (n + e < N) {
+              if constexpr (Z == 4) v.y[i][e / 4][e % 4] = __float_as_uint(p[e]);
+              else v.y[i][0][e / 2] |= uint32_t(p[e]) << (e % 2 ? 16 : 0);
+            }
         }
       }
     }
@@ -741,9 +777,18 @@ __global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const bf16_t* __
       for (int c = 0; c < 8; ++c) f[c][e / 2] = pack_bf2(a[c], b[c]);
     }
 #pragma unroll
-    for (int c = 0; c < 8; ++c)
+    for (int i = 0; i < TM; ++i) {
+      if constexpr (Z == 2) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i) acc[i][c] = mfma16x16x32(as_bf16x8(cur.y[i]), as_bf16x8(f[c]), acc[i][c]);
+        for (int c = 0; c < 8; ++c) acc[i][c] = mfma16x16x32(as_bf16x8(cur.y[i][0]), as_bf16x8(f[c]), acc[i][c]);
+      } else {
+        const Thirds y = thirds_of(cur.y[i][0], cur.y[i][1]);
+#pragma unroll
+        for (int k = 2; k >= 0; --k)
+#pragma unroll
+          for (int c = 0; c < 8; ++c) acc[i][c] = mfma16x16x32(as_bf16x8(y.v[k]), as_bf16x8(f[c]), acc[i][c]);
+      }
+    }
     cur = next;
   }
 #pragma unroll
@@ -768,9 +813,10 @@ __global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const bf16_t* __
   }
 }
 
-// Sums of `parts` [n] arrays, in their order, as bf16 (n a multiple of 8).
+// Sums of `parts` [n] arrays, in their order, in dx's type (n a multiple of 8).
+template <typename T>
 __global__ __launch_bounds__(256) void mx4_back_join_kernel(const float* __restrict__ part, int64_t n, int parts,
-                                                            bf16_t* __restrict__ dx) {
+                                                            T* __restrict__ dx) {
   const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 8;
   if (i >= n) return;
   float v[8], t[8];
@@ -783,12 +829,11 @@ __global__ __launch_bounds__(256) void mx4_back_join_kernel(const float* __restr
   store8(dx + i, v);
 }
 
-// The weight as T values, transposed: wt [K, ld] with zeros in columns N .. ld.
+// The weight as bf16 values, transposed: wt [K, ld] with zeros in columns N .. ld.
 // A workgroup turns 64 rows x 64 columns round in LDS.
-template <typename T>
 __global__ __launch_bounds__(256) void transpose4_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ s,
-                                                         int64_t N, int64_t K, T* __restrict__ wt, int64_t ld) {
-  __shared__ T tile[64][64 + 16 / sizeof(T)];
+                                                         int64_t N, int64_t K, bf16_t* __restrict__ wt, int64_t ld) {
+  __shared__ bf16_t tile[64][64 + 8];
   const int64_t n0 = int64_t(blockIdx.x) * 64, k0 = int64_t(blockIdx.y) * 64;
   const int64_t Np = scale_rows(N);
 #pragma unroll
@@ -801,10 +846,10 @@ __global__ __launch_bounds__(256) void transpose4_kernel(const uint8_t* __restri
       decode4x8(*reinterpret_cast<const uint32_t*>(q + (n * K + k) / 2), scale_value(c), v);
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) st(&tile[0][0], (8 * ch + e) * int64_t(64 + 16 / sizeof(T)) + row, v[e]);
+    for (int e = 0; e < 8; ++e) st(&tile[0][0], (8 * ch + e) * int64_t(64 + 8) + row, v[e]);
   }
   __syncthreads();
-  constexpr int E = 16 / sizeof(T), kLanes = 64 / E;  // 16 bytes per lane
+  constexpr int E = 8, kLanes = 64 / E;  // 16 bytes per lane
 #pragma unroll
   for (int r = threadIdx.x / kLanes; r < 64; r += 256 / kLanes) {
     const int ch = threadIdx.x % kLanes;
@@ -815,14 +860,13 @@ __global__ __launch_bounds__(256) void transpose4_kernel(const uint8_t* __restri
 
 // Rows of N elements to rows of ld (a multiple of 64), zeros behind: 16 bytes a lane,
 // read at any element.
-template <typename T>
-__global__ __launch_bounds__(256) void widen_kernel(const T* __restrict__ x, int64_t M, int64_t N, T* __restrict__ y,
-                                                    int64_t ld) {
-  constexpr int E = 16 / int(sizeof(T));
+__global__ __launch_bounds__(256) void widen_kernel(const bf16_t* __restrict__ x, int64_t M, int64_t N,
+                                                    bf16_t* __restrict__ y, int64_t ld) {
+  constexpr int E = 8;
   const int64_t n = (int64_t(blockIdx.y) * 64 + threadIdx.x % 64) * E;
   if (n >= ld) return;
   for (int64_t m = int64_t(blockIdx.x) * 4 + threadIdx.x / 64; m < M; m += int64_t(gridDim.x) * 4) {
-    const T* p = x + m * N + n;
+    const bf16_t* p = x + m * N + n;
     u32x4 w = {0u, 0u, 0u, 0u};
     if (n + E <= N) {
       const loose4 v = *reinterpret_cast<const loose4*>(p);
@@ -830,10 +874,7 @@ __global__ __launch_bounds__(256) void widen_kernel(const T* __restrict__ x, int
     } else {
 #pragma unroll
       for (int e = 0; e < E - 1; ++e)
-        if (n + e < N) {
-          if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(p[e]);
-          else w[e / 2] |= uint32_t(p[e]) << (e % 2 ? 16 : 0);
-        }
+        if (n + e < N) w[e / 2] |= uint32_t(p[e]) << (e % 2 ? 16 : 0);
     }
     *reinterpret_cast<u32x4*>(y + m * ld + n) = w;
   }
@@ -949,89 +990,91 @@ void run_product(const Mx4Args& a, const ProductPlan& p, float* part, hipStream_
   });
 }
 
-// Scratch of the input gradient: the weight transposed in dtype, dy widened where
-// its rows are not whole contraction tiles, and split sums of the product.
+// Scratch of the input gradient (bf16): the weight transposed, dy widened where its
+// rows are not whole contraction tiles, and split sums of the product; or parts.
 struct BackPlan {
   int64_t ld;
-  size_t wt, dy, part;
+  size_t wt = 0, dy = 0, part = 0;
   int rows = 0, parts = 1;   // rows > 0: the kernel for few rows with 16 `rows` rows to a workgroup
 };
 // Few rows (bf16) go straight from the held weight, 16 of them to a workgroup of eight
 // waves (two of which fit a CU) or 64 to one of four, the contraction whole or in
 // parts; the other way is to turn the weight round and run the bf16 product.  The least predicted time (us).  A chain
 // step takes 1.0 us (1.7 with two workgroups on a CU; 1.2 with 64 rows), parts a
-// launch and their bytes.  Measured (16 rows whole, in 4; 64 rows in 4; turned round):
+// launch and their bytes.  fp32 always goes from the held weight, by the same
+// figures (within 5 % of its best form from 1 x 1024 x 1024, 6.6 us, to 1741 x 6400 x 2048,
+// 187; the fp32 product with the weight turned round took 13.1 and 723).  Measured (16 rows whole, in 4; 64 rows in 4; turned round):
 //   16 x 8192 x 2048   33.3  13.6  24.4  45.9     512 x 8192 x 2048  56.6  59.6  48.0  46.9
 //   128 x 8192 x 2048  33.0  21.0  25.6  44.1     67 x 1024 x 256     6.6   6.5   9.1  13.4
 //   256 x 8192 x 2048  33.6  34.3  26.8  44.3     64 x 2048 x 8192   10.7  17.9  16.0  32.3
 BackPlan plan_back(int64_t M, int64_t N, int64_t K, int dtype) {
-  const size_t z = dtype == AVITS_BF16 ? 2 : 4;
+  const bool half = dtype == AVITS_BF16;
   BackPlan p;
   p.ld = ceil_div64(N, 64) * 64;
-  p.wt = align_up(size_t(K) * size_t(p.ld) * z, 256);
-  p.dy = p.ld != N ? align_up(size_t(M) * size_t(p.ld) * z, 256) : 0;
-  p.part = dtype == AVITS_BF16 ? std::min<size_t>(gemm_partial_reserve(M, K), size_t(64) << 20) : 0;
-  if (dtype == AVITS_BF16) {
-    const double weights = double(N) * double(K) * 1e-6;
-    double best = 16.0 + weights * 4.5 / 4.0 + 2.0 * double(M) * weights / 1.1e6;
-    for (int rows : {1, 4})
-      for (int parts = 1; parts <= 8; parts *= 2) {
-        const int waves = rows == 1 ? 8 : 4;
-        const int64_t steps = ceil_div64(N, 32), wgs = ceil_div64(M, 16 * rows) * ceil_div64(K, 128) * parts;
-        if (parts > 1 && (steps < parts * waves || size_t(parts) * size_t(M) * size_t(K) * sizeof(float) > kMaxPartBytes)) break;
-        const double step = rows == 4 ? 1.2 : wgs <= kCUs ? 1.0 : 1.7;
-        const double us = 2.5 + double(ceil_div64(steps, waves * parts)) * step * double(ceil_div64(wgs, rows == 4 ? kCUs : 2 * kCUs)) +
-                          (parts > 1 ? 2.5 + double(parts) * double(M) * double(K) * 8e-6 / 4.0 : 0.0);
-        if (us >= best) continue;
-        best = us;
-        p.rows = rows;
-        p.parts = parts;
-      }
+  if (half) {
+    p.wt = align_up(size_t(K) * size_t(p.ld) * 2, 256);
+    p.dy = p.ld != N ? align_up(size_t(M) * size_t(p.ld) * 2, 256) : 0;
+    p.part = std::min<size_t>(gemm_partial_reserve(M, K), size_t(64) << 20);
   }
+  const double weights = double(N) * double(K) * 1e-6;
+  double best = half ? 16.0 + weights * 4.5 / 4.0 + 2.0 * double(M) * weights / 1.1e6 : 1e30;
+  for (int rows : {1, 4})
+    for (int parts = 1; parts <= 8; parts *= 2) {
+      const int waves = rows == 1 ? 8 : 4;
+      const int64_t steps = ceil_div64(N, 32), wgs = ceil_div64(M, 16 * rows) * ceil_div64(K, 128) * parts;
+      if (parts > 1 && (steps < parts * waves || size_t(parts) * size_t(M) * size_t(K) * sizeof(float) > kMaxPartBytes)) break;
+      const double step = rows == 4 ? 1.2 : wgs <= kCUs ? 1.0 : 1.7;
+      const double us = 2.5 + double(ceil_div64(steps, waves * parts)) * step * double(ceil_div64(wgs, rows == 4 ? kCUs : 2 * kCUs)) +
+                        (parts > 1 ? 2.5 + double(parts) * double(M) * double(K) * 8e-6 / 4.0 : 0.0);
+      if (us >= best) continue;
+      best = us;
+      p.rows = rows;
+      p.parts = parts;
+    }
   return p;
 }
 
+// dx by mx4_back_rows_kernel, as the plan says.
 template <typename T>
-int run_back(const void* dy, int64_t M, int64_t N, const uint8_t* wq, const uint8_t* ws, int64_t K, int dtype, void* dx,
-             char* scratch, hipStream_t s) {
-  const BackPlan p = plan_back(M, N, K, dtype);
-  if constexpr (sizeof(T) == 2) {
-    if (p.rows) {
-      TimedLaunch timed("mxfp4_backward", s);
-      const bf16_t* y = static_cast<const bf16_t*>(dy);
-      auto go = [&](auto tm, auto nw, auto* out) {
-        constexpr int kTM = decltype(tm)::value, kNW = decltype(nw)::value;
-        const dim3 grid(unsigned(ceil_div64(M, 16 * kTM) * ceil_div64(K, 128)), unsigned(p.parts));
-        using Out = std::remove_pointer_t<decltype(out)>;
-        if (N % 8 == 0)
-          hipLaunchKernelGGL((mx4_back_rows_kernel<kTM, kNW, false, Out>), grid, dim3(64 * kNW), 0, s, y, M, N, wq, ws, K, out);
-        else
-          hipLaunchKernelGGL((mx4_back_rows_kernel<kTM, kNW, true, Out>), grid, dim3(64 * kNW), 0, s, y, M, N, wq, ws, K, out);
-      };
-      using std::integral_constant;
-      auto by_rows = [&](auto* out) {
-        if (p.rows == 1) go(integral_constant<int, 1>(), integral_constant<int, 8>(), out);
-        else go(integral_constant<int, 4>(), integral_constant<int, 4>(), out);
-      };
-      if (p.parts == 1) {
-        by_rows(static_cast<bf16_t*>(dx));
-        return launch_status("mxfp4_linear_backward");
-      }
-      by_rows(reinterpret_cast<float*>(scratch));
-      hipLaunchKernelGGL(mx4_back_join_kernel, dim3(unsigned(ceil_div64(M * K / 8, 256))), dim3(256), 0, s,
-                         reinterpret_cast<const float*>(scratch), M * K, p.parts, static_cast<bf16_t*>(dx));
-      return launch_status("mxfp4_linear_backward");
-    }
+int run_back_rows(const BackPlan& p, const T* dy, int64_t M, int64_t N, const uint8_t* wq, const uint8_t* ws, int64_t K, T* dx,
+                  float* part, hipStream_t s) {
+  TimedLaunch timed("mxfp4_backward", s);
+  auto go = [&](auto tm, auto nw, auto* out) {
+    constexpr int kTM = decltype(tm)::value, kNW = decltype(nw)::value;
+    using Out = std::remove_pointer_t<decltype(out)>;
+    const dim3 grid(unsigned(ceil_div64(M, 16 * kTM) * ceil_div64(K, 128)), unsigned(p.parts));
+    if (N % 8 == 0)
+      hipLaunchKernelGGL((mx4_back_rows_kernel<kTM, kNW, false, T, Out>), grid, dim3(64 * kNW), 0, s, dy, M, N, wq, ws, K, out);
+    else
+      hipLaunchKernelGGL((mx4_back_rows_kernel<kTM, kNW, true, T, Out>), grid, dim3(64 * kNW), 0, s, dy, M, N, wq, ws, K, out);
+  };
+  using std::integral_constant;
+  auto by_rows = [&](auto* out) {
+    if (p.rows == 1) go(integral_constant<int, 1>(), integral_constant<int, 8>(), out);
+    else go(integral_constant<int, 4>(), integral_constant<int, 4>(), out);
+  };
+  if (p.parts == 1) {
+    by_rows(dx);
+  } else {
+    by_rows(part);
+    hipLaunchKernelGGL(mx4_back_join_kernel<T>, dim3(unsigned(ceil_div64(M * K / 8, 256))), dim3(256), 0, s, (const float*)part,
+                       M * K, p.parts, dx);
   }
-  T* wt = reinterpret_cast<T*>(scratch);
+  return launch_status("mxfp4_linear_backward");
+}
+
+// dx by the bf16 product with the weight turned round.
+int run_back_tiles(const BackPlan& p, const bf16_t* dy, int64_t M, int64_t N, const uint8_t* wq, const uint8_t* ws, int64_t K,
+                   bf16_t* dx, char* scratch, hipStream_t s) {
+  bf16_t* wt = reinterpret_cast<bf16_t*>(scratch);
   {
     TimedLaunch timed("mxfp4_transpose", s);
-    hipLaunchKernelGGL(transpose4_kernel<T>, dim3(unsigned(p.ld / 64), unsigned(ceil_div64(K, 64))), dim3(256), 0, s, wq, ws, N,
-                       K, wt, p.ld);
+    hipLaunchKernelGGL(transpose4_kernel, dim3(unsigned(p.ld / 64), unsigned(ceil_div64(K, 64))), dim3(256), 0, s, wq, ws, N, K,
+                       wt, p.ld);
     if (p.dy) {
-      T* wide = reinterpret_cast<T*>(scratch + p.wt);
-      hipLaunchKernelGGL(widen_kernel<T>, dim3(unsigned(std::min<int64_t>(ceil_div64(M, 4), 4096)), unsigned(ceil_div64(p.ld, 1024 / sizeof(T)))),
-                         dim3(256), 0, s, static_cast<const T*>(dy), M, N, wide, p.ld);
+      bf16_t* wide = reinterpret_cast<bf16_t*>(scratch + p.wt);
+      hipLaunchKernelGGL(widen_kernel, dim3(unsigned(std::min<int64_t>(ceil_div64(M, 4), 4096)), unsigned(ceil_div64(p.ld, 512))),
+                         dim3(256), 0, s, dy, M, N, wide, p.ld);
       dy = wide;
     }
   }
@@ -1044,7 +1087,8 @@ int run_back(const void* dy, int64_t M, int64_t N, const uint8_t* wq, const uint
   GemmProblem& q = g.p[0];
   q.A = dy; q.lda = p.ld; q.W = wt; q.M = M;
   q.out0 = dx; q.ld0 = K;
-  return launch_gemm(g, dtype, s, "mxfp4_backward", p.part ? reinterpret_cast<float*>(scratch + p.wt + p.dy) : nullptr, p.part);
+  return launch_gemm(g, AVITS_BF16, s, "mxfp4_backward", p.part ? reinterpret_cast<float*>(scratch + p.wt + p.dy) : nullptr,
+                     p.part);
 }
 
 }  // namespace
@@ -1105,7 +1149,12 @@ extern "C" int avits_mxfp4_linear_backward(const void* dy, int64_t M, int64_t N,
   AVITS_REQUIRE(aligned_to({workspace}, 16), "mxfp4_linear_backward: workspace must be 16-byte aligned");
   hipStream_t s = static_cast<hipStream_t>(stream);
   char* scratch = static_cast<char*>(workspace);
-  rc = dtype == AVITS_BF16 ? run_back<bf16_t>(dy, M, N, wq, ws, K, dtype, dx, scratch, s)
-                           : run_back<float>(dy, M, N, wq, ws, K, dtype, dx, scratch, s);
+  const BackPlan p = plan_back(M, N, K, dtype);
+  float* part = static_cast<float*>(workspace);
+  if (dtype == AVITS_F32)
+    return run_back_rows(p, static_cast<const float*>(dy), M, N, wq, ws, K, static_cast<float*>(dx), part, s);
+  const bf16_t* y = static_cast<const bf16_t*>(dy);
+  bf16_t* x = static_cast<bf16_t*>(dx);
+  rc = p.rows ? run_back_rows(p, y, M, N, wq, ws, K, x, part, s) : run_back_tiles(p, y, M, N, wq, ws, K, x, scratch, s);
   return rc != AVITS_OK ? rc : launch_status("mxfp4_linear_backward");
 }

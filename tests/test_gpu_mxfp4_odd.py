@@ -70,3 +70,37 @@ def test_backward(gpu, M, N, K):
     ref, err = d @ w, 2.0 ** -23 * (N / 32 + 8) * (np.abs(d) @ np.abs(w))
     assert_within(_np(dx[:M])[good], ref, err + HALF["bf16"] * (np.abs(ref) + err))
     assert torch.isnan(dx[:M][torch.from_numpy(~good).cuda()]).all() and (dx[M] == 7.0).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 1, 32), (3, 9, 160), (70, 33, 96), (65, 1027, 1056), (600, 260, 2048), (1300, 513, 544)])
+def test_backward_in_fp32(gpu, M, N, K):
+    """Values over many powers of two, so that all 24 bits of each count, and a row of NaN."""
+    import torch
+    rng = np.random.default_rng(N * M)
+    wq, ws, w = _held(rng, N, K)
+    dy = torch.from_numpy((rng.standard_normal((M, N)) * np.exp2(rng.integers(-40, 40, (M, N)))).astype(np.float32))
+    if M > 1:
+        dy[M // 2, :] = float("nan")
+    dx = torch.full((M + 1, K), 7.0, device="cuda")
+    gpu.avits_mxfp4_linear_backward(dy.cuda(), wq, ws, dx[:M])
+    good = np.arange(M) != (M // 2 if M > 1 else -1)
+    d = _np(dy)[good]
+    # Exact products of the three parts of a value, 3 N / 32 instructions and a few joins.
+    ref, err = d @ w, 2.0 ** -23 * (3 * N / 32 + 8) * (np.abs(d) @ np.abs(w))
+    assert_within(_np(dx[:M])[good], ref, err + HALF["f32"] * np.abs(ref))
+    assert torch.isnan(dx[:M][torch.from_numpy(~good).cuda()]).all() and (dx[M] == 7.0).all()
+
+
+def test_backward_of_infinities(gpu):
+    """An infinite gradient stays one: its other parts are 0, not NaN."""
+    import torch
+    K, N = 64, 8
+    w = np.ones((N, K))
+    codes, e = oracle.hold(w, 4)
+    wq, ws = (torch.from_numpy(a).cuda() for a in oracle.mx_pack(codes, e))
+    for dt in (torch.float32, torch.bfloat16):
+        dy = torch.zeros(3, N, dtype=dt)
+        dy[0, 3], dy[1, 5], dy[2, 0], dy[2, 1] = float("inf"), -float("inf"), 1.0, 3.0e38
+        dx = torch.empty(3, K, dtype=dt, device="cuda")
+        gpu.avits_mxfp4_linear_backward(dy.cuda(), wq, ws, dx)
+        assert (dx[0] == float("inf")).all() and (dx[1] == -float("inf")).all() and torch.equal(dx[2].cpu(), dy[2, 1].expand(K))
