@@ -94,7 +94,8 @@ __device__ __forceinline__ void finish(const Mx4Args& a, int64_t m, int64_t n, f
 
 // Few rows: a workgroup of NW waves owns 16 TM x 16 TN outputs, the waves take
 // every NW-th step of the contraction straight from memory into registers (the next
-// one while one is multiplied), and their sums meet in LDS.
+// one while one is multiplied), and their sums meet in LDS.  Bound by the latency of a
+// few loads in a row and the launch: 1 x 12288 x 2048 5.9 us for a weight of 13.4 MB.
 template <int TM, int TN, int NW, typename T>
 __global__ __launch_bounds__(64 * NW) void mx4_rows_kernel(const Mx4Args a) {
   __shared__ float red[NW][TM * TN * 4][kWave];
@@ -369,10 +370,17 @@ struct BlockEnd {
 // LDS row 16 i + l of a strip holds its row T l + i, block 2 g + k of a row lies
 // in chunk (4 k + g) ^ (row / 2 mod 8): the 16 lanes that a read serves at once,
 // of two lane groups, then meet every bank once (with the blocks in their own order
-// half of them collided: 8192 x 8192 x 8192 294 us instead of 271).
+// half of them collided: 8192 x 8192 x 8192 took a twelfth longer).
 // The contraction is short (8 steps for K = 2048), so a tile's head and tail
 // are hidden too: a workgroup keeps taking tiles, the next tile's first loads go out before
 // the stores of the last, and the waits for them leave those stores in flight.
+// What bounds it: a phase takes about 1500 cycles instead of its 1024 of matrix
+// instructions, since the fragments' reads and the loads' writes keep LDS busy for 1063
+// of them, and a tile's end stores at HBM's rate.  8192 x 8192 x 8192 241 us (4.56
+// PFLOP/s; matrix instructions alone reach 6.7), 16896 x 8192 x 2048 167 (3.39; its
+// output alone 54 at a copy's rate), 4608 x 8192 x 2048 53, 1741 x 8192 x 2048 22.7.
+// Four waves of 128 x 128 outputs, which read a third less from LDS, were slower (275 us
+// and 208): with one wave per SIMD nothing runs beside its reads.
 // PARTS: a tile is `splits` units, each a part of the contraction, and a unit's sums go
 // to out as the registers lie: 16 bytes of every lane side by side, 256 KB a unit.
 template <typename T, bool GATED, bool VEC, bool PARTS>
@@ -830,32 +838,37 @@ __global__ __launch_bounds__(256) void mx4_back_join_kernel(const float* __restr
 }
 
 // The weight as bf16 values, transposed: wt [K, ld] with zeros in columns N .. ld.
-// A workgroup turns 64 rows x 64 columns round in LDS.
+// A lane takes 8 rows n x 8 columns k (a dword each, as in the kernel above) and has,
+// for each k, 16 bytes of a row of wt; a wave covers 64 n x 64 k, a workgroup 64 x
+// 256, so that both sides move 128 bytes of a row.  8192 x 2048: 10.1 us for 42
+// MB (through LDS 14.1), beside 138 of the product of 4608 rows.
 __global__ __launch_bounds__(256) void transpose4_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ s,
                                                          int64_t N, int64_t K, bf16_t* __restrict__ wt, int64_t ld) {
-  __shared__ bf16_t tile[64][64 + 8];
-  const int64_t n0 = int64_t(blockIdx.x) * 64, k0 = int64_t(blockIdx.y) * 64;
-  const int64_t Np = scale_rows(N);
+  const int lane = threadIdx.x % kWave;
+  const int64_t n = int64_t(blockIdx.x) * 64 + 8 * (lane % 8);
+  const int64_t k = int64_t(blockIdx.y) * 256 + 64 * (threadIdx.x / kWave) + 8 * (lane / 8);
+  if (k >= K) return;
+  uint32_t w[8] = {};
+  u32x4 sc = {0u, 0u, 0u, 0u};
+  if (n < N) {
+    sc = *reinterpret_cast<const u32x4*>(s + (k / 64 * scale_rows(N) + n) * 2);
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int row = threadIdx.x / 8 + 32 * h, ch = threadIdx.x % 8;
-    const int64_t n = n0 + row, k = k0 + 8 * ch;
-    float v[8] = {};
-    if (n < N && k < K) {
-      const uint8_t c = s[((k / 64) * Np + n) * 2 + (k / 32) % 2];
-      decode4x8(*reinterpret_cast<const uint32_t*>(q + (n * K + k) / 2), scale_value(c), v);
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) st(&tile[0][0], (8 * ch + e) * int64_t(64 + 8) + row, v[e]);
+    for (int e = 0; e < 8; ++e)
+      if (n + e < N) w[e] = *reinterpret_cast<const uint32_t*>(q + ((n + e) * K + k) / 2);
   }
-  __syncthreads();
-  constexpr int E = 8, kLanes = 64 / E;  // 16 bytes per lane
+  const int shift = 8 * int(k / 32 % 2);
+  u32x4 f[8];
 #pragma unroll
-  for (int r = threadIdx.x / kLanes; r < 64; r += 256 / kLanes) {
-    const int ch = threadIdx.x % kLanes;
-    const int64_t k = k0 + r, n = n0 + E * ch;
-    if (k < K && n < ld) *reinterpret_cast<u32x4*>(wt + k * ld + n) = *reinterpret_cast<const u32x4*>(&tile[r][E * ch]);
+  for (int e = 0; e < 8; e += 2) {
+    float a[8], b[8];
+    const uint32_t pair = sc[e / 2] >> shift;   // (rows past N may have any scale)
+    decode4x8(w[e], n + e < N ? scale_value(pair & 255u) : 0.f, a);
+    decode4x8(w[e + 1], n + e + 1 < N ? scale_value(pair >> 16 & 255u) : 0.f, b);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) f[c][e / 2] = pack_bf2(a[c], b[c]);
   }
+#pragma unroll
+  for (int c = 0; c < 8; ++c) *reinterpret_cast<u32x4*>(wt + (k + c) * ld + n) = f[c];
 }
 
 // Rows of N elements to rows of ld (a multiple of 64), zeros behind: 16 bytes a lane,
@@ -999,14 +1012,17 @@ struct BackPlan {
 };
 // Few rows (bf16) go straight from the held weight, 16 of them to a workgroup of eight
 // waves (two of which fit a CU) or 64 to one of four, the contraction whole or in
-// parts; the other way is to turn the weight round and run the bf16 product.  The least predicted time (us).  A chain
-// step takes 1.0 us (1.7 with two workgroups on a CU; 1.2 with 64 rows), parts a
-// launch and their bytes.  fp32 always goes from the held weight, by the same
-// figures (within 5 % of its best form from 1 x 1024 x 1024, 6.6 us, to 1741 x 6400 x 2048,
-// 187; the fp32 product with the weight turned round took 13.1 and 723).  Measured (16 rows whole, in 4; 64 rows in 4; turned round):
-//   16 x 8192 x 2048   33.3  13.6  24.4  45.9     512 x 8192 x 2048  56.6  59.6  48.0  46.9
-//   128 x 8192 x 2048  33.0  21.0  25.6  44.1     67 x 1024 x 256     6.6   6.5   9.1  13.4
-//   256 x 8192 x 2048  33.6  34.3  26.8  44.3     64 x 2048 x 8192   10.7  17.9  16.0  32.3
+// parts; the other way is to turn the weight round and run the bf16 product.  The
+// least predicted time (us).  A chain step takes 1.0 us (1.7 with two workgroups on a
+// CU; 1.2 with 64 rows), parts a launch and their bytes; the other way its launches,
+// the weight's bytes and the product at 1.1 PFLOP/s.  fp32 always goes from the held
+// weight, by the same figures (within 5 % of its best form from 1 x 1024 x 1024, 6.6 us,
+// to 1741 x 6400 x 2048, 187; the fp32 product with the weight turned round took 13.1
+// and 723).  Measured (16 rows whole, in 4; 64 rows in 4; turned round):
+//   16 x 8192 x 2048   33.3  13.7  25.7  43.1     512 x 8192 x 2048  56.6  61.1  53.1  43.5
+//   128 x 8192 x 2048  33.4  21.8  28.1  40.5     67 x 1024 x 256     6.5   6.4   9.1  13.5
+//   256 x 8192 x 2048  34.0  34.3  29.5  40.4     64 x 2048 x 8192   11.0  18.0  16.8  29.9
+//   300 x 2051 x 2048  19.2  22.6  26.0  31.9     1741 x 1024 x 512  10.6  20.8  21.5  24.1
 BackPlan plan_back(int64_t M, int64_t N, int64_t K, int dtype) {
   const bool half = dtype == AVITS_BF16;
   BackPlan p;
@@ -1017,7 +1033,7 @@ BackPlan plan_back(int64_t M, int64_t N, int64_t K, int dtype) {
     p.part = std::min<size_t>(gemm_partial_reserve(M, K), size_t(64) << 20);
   }
   const double weights = double(N) * double(K) * 1e-6;
-  double best = half ? 16.0 + weights * 4.5 / 4.0 + 2.0 * double(M) * weights / 1.1e6 : 1e30;
+  double best = half ? (p.dy ? 22.0 : 16.0) + weights * 4.5 / 5.0 + 2.0 * double(M) * weights / 1.1e3 : 1e30;
   for (int rows : {1, 4})
     for (int parts = 1; parts <= 8; parts *= 2) {
       const int waves = rows == 1 ? 8 : 4;
@@ -1069,7 +1085,7 @@ int run_back_tiles(const BackPlan& p, const bf16_t* dy, int64_t M, int64_t N, co
   bf16_t* wt = reinterpret_cast<bf16_t*>(scratch);
   {
     TimedLaunch timed("mxfp4_transpose", s);
-    hipLaunchKernelGGL(transpose4_kernel, dim3(unsigned(p.ld / 64), unsigned(ceil_div64(K, 64))), dim3(256), 0, s, wq, ws, N, K,
+    hipLaunchKernelGGL(transpose4_kernel, dim3(unsigned(p.ld / 64), unsigned(ceil_div64(K, 256))), dim3(256), 0, s, wq, ws, N, K,
                        wt, p.ld);
     if (p.dy) {
       bf16_t* wide = reinterpret_cast<bf16_t*>(scratch + p.wt);
