@@ -528,12 +528,16 @@ int check_norm(const char* who, int64_t M, int64_t D, int32_t B, const int64_t* 
 // Chunks of rows at most, of at least four rows: whole rounds of workgroups with two
 // waves to a SIMD or a little more, by the waves that rows of bf16 take.  Measured, 512
 // chunks and by this rule: 40000 x 512 bf16 51.8 and 38.3 us, 16000 x 37 24.3
-// and 15.5, 4608 x 4096 34.8 and 30.3.
-int64_t max_chunks(int64_t D) { return 256 * ceil_div64(8, std::min<int64_t>(8, ceil_div64(D, 512))); }
+// and 15.5, 4608 x 4096 34.8 and 30.3.  Rows held in 8 bits that take eight waves run in
+// twice as many, one row at a time, so that two workgroups fit a CU: 16000 x 4096 76.4
+// us instead of 89.3 (rows as they were: 89.1 instead of 86.2).
+int64_t max_chunks(int64_t D, bool held) {
+  return 256 * ceil_div64(8, std::min<int64_t>(held && D <= 4096 ? 7 : 8, ceil_div64(D, 512)));
+}
 
-Chunks make_chunks(int64_t M, int64_t D, const Images& im) {
+Chunks make_chunks(int64_t M, int64_t D, bool held, const Images& im) {
   Chunks ch;
-  ch.rows = int32_t(std::max<int64_t>(4, ceil_div64(M, max_chunks(D))));
+  ch.rows = int32_t(std::max<int64_t>(4, ceil_div64(M, max_chunks(D, held))));
   int32_t n = 0;
   int64_t at = 0;
   for (int i = 0; i < kMaxSeqs; ++i) {
@@ -588,7 +592,7 @@ void run_norm_back(const void* dh, const Rows<T>& rows, const float* mean, const
                    const Images& im, const void* scale, const void* dres, void* dx, float* dscale, float* dshift,
                    float* ws, hipStream_t s) {
   TimedLaunch timed("layer_norm_backward", s);
-  const Chunks ch = make_chunks(M, D, im);
+  const Chunks ch = make_chunks(M, D, rows.q != nullptr, im);
   const int n = ch.first[kMaxSeqs];
   float* avg = ws;
   float* part = ws + align_up(size_t(2 * M), 64);
@@ -611,11 +615,12 @@ void run_norm_back(const void* dh, const Rows<T>& rows, const float* mean, const
       else if (D % kVec<T> == 0) form(no, no);
       else form(no, yes);
     };
-    // Two rows at a time, except where five to seven waves leave no room for a second
-    // workgroup on the CU with their registers (16000 x 2560 bf16 in 8 bits: 53.9 us, by
-    // two rows 79.7; 16000 x 3999 100.9 instead of 90.8).
+    // Two rows at a time; one where a second workgroup would not fit the CU with two
+    // rows' registers: five to seven waves (16000 x 2560 bf16 in 8 bits 53.9 us instead
+    // of 79.7), and eight where there are two of them (see max_chunks; with one, 16000 x
+    // 3999 rows as they were take 100.9 one at a time, 90.8 by twos).
     const std::integral_constant<int, 1> one;
-    if (chunks <= 256 || (chunks > 448 && chunks <= 512)) go(one, std::true_type());
+    if (chunks <= 256 || (chunks > 448 && chunks <= 512 && !rows.q)) go(one, std::true_type());
     else if (chunks <= 512) go(one, std::false_type());
     else if (chunks <= 1024) go(std::integral_constant<int, 2>(), std::false_type());
     else go(std::integral_constant<int, 4>(), std::false_type());
@@ -663,7 +668,7 @@ extern "C" int avits_layer_norm(const void* x, int64_t M, int64_t D, int32_t B, 
 
 extern "C" size_t avits_layer_norm_backward_workspace_bytes(int64_t M, int64_t D, int32_t B) {
   if (M < 0 || M >= (int64_t(1) << 25) || D < 1 || D > 65536 || B < 1 || B > kMaxSeqs) return 0;
-  const size_t chunks = size_t(std::min<int64_t>(max_chunks(D), ceil_div64(M, 4))) + size_t(B);
+  const size_t chunks = size_t(std::min<int64_t>(max_chunks(D, true), ceil_div64(M, 4))) + size_t(B);
   return (align_up(size_t(2 * M), 64) + 2 * chunks * size_t(D)) * sizeof(float);
 }
 
