@@ -104,3 +104,26 @@ def test_backward_of_infinities(gpu):
         dx = torch.empty(3, K, dtype=dt, device="cuda")
         gpu.avits_mxfp4_linear_backward(dy.cuda(), wq, ws, dx)
         assert (dx[0] == float("inf")).all() and (dx[1] == -float("inf")).all() and torch.equal(dx[2].cpu(), dy[2, 1].expand(K))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M", [1, 40, 5000])
+def test_smallest_and_largest_weights_count(gpu, M, dtype):
+    """Scales at both ends: held values below the smallest normal number (0.5 x 2^-127) and near the
+    largest, against gradients that bring them back into range."""
+    import torch
+    N, K = 64, 2048
+    rng = np.random.default_rng(5)
+    codes = rng.integers(0, 256, (N, K // 2)).astype(np.uint8)
+    wq = torch.from_numpy(codes).cuda()
+    for code, big in ((0, 2.0 ** 110), (1, 2.0 ** 110), (252, 2.0 ** -110)):
+        shape = gpu.avits_mxfp4_scale_shape(N, K)
+        s = np.full(shape, code, np.uint8)
+        c, e = oracle.mx_unpack(codes, s)
+        w = oracle.held_values(c, e, 4)
+        dy = torch.from_numpy((rng.standard_normal((M, N)) * big).astype(np.float32)).to(TORCH_DT[dtype])
+        dx = torch.empty(M, K, dtype=dy.dtype, device="cuda")
+        gpu.avits_mxfp4_linear_backward(dy.cuda(), wq, torch.from_numpy(s).cuda(), dx)
+        d = _np(dy)
+        ref, err = d @ w, 2.0 ** -23 * (3 * N / 32 + 8) * (np.abs(d) @ np.abs(w))
+        assert_within(_np(dx), ref, err + HALF[dtype] * (np.abs(ref) + err), code)
