@@ -1014,11 +1014,11 @@ struct BackPlan {
 // waves (two of which fit a CU) or 64 to one of four, the contraction whole or in
 // parts; the other way is to turn the weight round and run the bf16 product.  The
 // least predicted time (us).  A chain step takes 1.0 us (1.7 with two workgroups on a
-// CU; 1.2 with 64 rows), parts a launch and their bytes; the other way its launches,
-// the weight's bytes and the product at 1.1 PFLOP/s.  fp32 always goes from the held
-// weight, by the same figures (within 5 % of its best form from 1 x 1024 x 1024, 6.6 us,
-// to 1741 x 6400 x 2048, 187; the fp32 product with the weight turned round took 13.1
-// and 723).  Measured (16 rows whole, in 4; 64 rows in 4; turned round):
+// CU; 1.2 with 64 rows), parts their bytes and a launch, which the host pays too; the
+// other way its launches, the weight's bytes and the product at 1.1 PFLOP/s.  fp32
+// always goes from the held weight, by the same figures (within 5 % of its best form
+// from 1 x 1024 x 1024, 6.6 us, to 1741 x 6400 x 2048, 187; the fp32 product with the
+// weight turned round took 13.1 and 723).  Measured (16 rows whole, in 4; 64 rows in 4; turned round):
 //   16 x 8192 x 2048   33.3  13.7  25.7  43.1     512 x 8192 x 2048  56.6  61.1  53.1  43.5
 //   128 x 8192 x 2048  33.4  21.8  28.1  40.5     67 x 1024 x 256     6.5   6.4   9.1  13.5
 //   256 x 8192 x 2048  34.0  34.3  29.5  40.4     64 x 2048 x 8192   11.0  18.0  16.8  29.9
@@ -1041,7 +1041,7 @@ BackPlan plan_back(int64_t M, int64_t N, int64_t K, int dtype) {
       if (parts > 1 && (steps < parts * waves || size_t(parts) * size_t(M) * size_t(K) * sizeof(float) > kMaxPartBytes)) break;
       const double step = rows == 4 ? 1.2 : wgs <= kCUs ? 1.0 : 1.7;
       const double us = 2.5 + double(ceil_div64(steps, waves * parts)) * step * double(ceil_div64(wgs, rows == 4 ? kCUs : 2 * kCUs)) +
-                        (parts > 1 ? 2.5 + double(parts) * double(M) * double(K) * 8e-6 / 4.0 : 0.0);
+                        (parts > 1 ? 3.5 + double(parts) * double(M) * double(K) * 8e-6 / 4.0 : 0.0);
       if (us >= best) continue;
       best = us;
       p.rows = rows;

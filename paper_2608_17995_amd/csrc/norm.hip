@@ -212,6 +212,13 @@ __device__ __forceinline__ float row_value(const Rows<T>& r, int64_t row, int64_
   return decode8(r.q[row * D + i], scale_value(r.s[row * r.ns + i / kBlk]));
 }
 
+// Where the column sums of the chunks go: chunk c's at scale + c stride, shift + c
+// stride (each may be null).
+struct SumsOut {
+  float *scale, *shift;
+  int64_t stride;
+};
+
 // Row chunks: chunk c covers rows [lo, hi) of one image; every image has at
 // least one, so that an image without rows gets zero sums.
 struct Chunks {
@@ -266,8 +273,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void norm_back_any_kernel(const T* dh, const Rows<T> xr, const float* __restrict__ mean,
                                                             const float* __restrict__ rstd, int64_t D, const Images im,
                                                             const Chunks ch, const T* __restrict__ scale, const T* dres,
-                                                            const float* __restrict__ avg, T* dx, float* __restrict__ part,
-                                                            int parts) {
+                                                            const float* __restrict__ avg, T* dx, const SumsOut sums) {
   const int c = blockIdx.x;
   const int64_t i = int64_t(blockIdx.y) * 256 + threadIdx.x;
   if (i >= D) return;
@@ -284,10 +290,8 @@ __global__ __launch_bounds__(256) void norm_back_any_kernel(const T* dh, const R
     sc = fmaf(d, n, sc);
     sh += d;
   }
-  if (parts) {
-    part[int64_t(2 * c) * D + i] = sc;
-    part[int64_t(2 * c + 1) * D + i] = sh;
-  }
+  if (sums.scale) sums.scale[c * sums.stride + i] = sc;
+  if (sums.shift) sums.shift[c * sums.stride + i] = sh;
 }
 
 // Backward: a workgroup takes a chunk of rows, R at a time; a thread owns NC
@@ -301,7 +305,7 @@ template <typename T, bool HELD, int NC, int R, bool TAIL>
 __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const Rows<T> xr, const float* __restrict__ mean,
                                                              const float* __restrict__ rstd, int64_t D, const Images im,
                                                              const Chunks ch, const T* __restrict__ scale, const T* dres,
-                                                             T* dx, float* __restrict__ part, int parts) {
+                                                             T* dx, const SumsOut sums) {
   constexpr int E = kVec<T>;
   __shared__ float red[2][8][2 * R];
   const int waves = blockDim.x / kWave, wave = threadIdx.x / kWave;
@@ -452,16 +456,16 @@ __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const 
     }
     t = next;
   }
-  if (parts) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      if (at[c] >= nchunk) continue;
+  for (int c = 0; c < NC; ++c) {
+    if (at[c] >= nchunk) continue;
+    const int64_t o = blockIdx.x * sums.stride + pos[c];
 #pragma unroll
-      for (int e = 0; e < E; e += 4) {
-        float* p = part + int64_t(2 * blockIdx.x) * D + pos[c] + e;
-        put_chunk(p, __builtin_bit_cast(u32x4, f32x4{sc[c][e], sc[c][e + 1], sc[c][e + 2], sc[c][e + 3]}));
-        put_chunk(p + D, __builtin_bit_cast(u32x4, f32x4{sh[c][e], sh[c][e + 1], sh[c][e + 2], sh[c][e + 3]}));
-      }
+    for (int e = 0; e < E; e += 4) {
+      if (sums.scale)
+        put_chunk(sums.scale + o + e, __builtin_bit_cast(u32x4, f32x4{sc[c][e], sc[c][e + 1], sc[c][e + 2], sc[c][e + 3]}));
+      if (sums.shift)
+        put_chunk(sums.shift + o + e, __builtin_bit_cast(u32x4, f32x4{sh[c][e], sh[c][e + 1], sh[c][e + 2], sh[c][e + 3]}));
     }
   }
 }
@@ -538,6 +542,11 @@ int64_t max_chunks(int64_t D, bool held) {
 Chunks make_chunks(int64_t M, int64_t D, bool held, const Images& im) {
   Chunks ch;
   ch.rows = int32_t(std::max<int64_t>(4, ceil_div64(M, max_chunks(D, held))));
+  int64_t longest = 0;
+  for (int i = 0; i < im.B; ++i) longest = std::max(longest, im.end[i] - (i ? im.end[i - 1] : 0));
+  // Few rows go as one chunk, whose sums need no second launch: a call with 8 x 2048 bf16
+  // 8.4 us instead of 11.5 (with 16 rows 11.5 either way, with 32 20.9 instead of 11.7).
+  if (longest <= 8) ch.rows = 8;
   int32_t n = 0;
   int64_t at = 0;
   for (int i = 0; i < kMaxSeqs; ++i) {
@@ -598,7 +607,9 @@ void run_norm_back(const void* dh, const Rows<T>& rows, const float* mean, const
   float* part = ws + align_up(size_t(2 * M), 64);
   const T *d = static_cast<const T*>(dh), *sc = static_cast<const T*>(scale), *res = static_cast<const T*>(dres);
   T* o = static_cast<T*>(dx);
-  const int parts = dscale || dshift ? 1 : 0;
+  // One chunk for each gradient's vector: its sums are the gradient.
+  const bool direct = n == (im.stride == 0 ? 1 : im.B), wanted = dscale || dshift;
+  const SumsOut sums = direct || !wanted ? SumsOut{dscale, dshift, D} : SumsOut{part, part + D, 2 * D};
   const int64_t chunks = ceil_div64(D * int64_t(sizeof(T)), 16);
   if (D >= kVec<T> && chunks <= 2048) {
     auto go = [&](auto nc, auto two) {
@@ -606,7 +617,7 @@ void run_norm_back(const void* dh, const Rows<T>& rows, const float* mean, const
       const dim3 wg(unsigned(ceil_div64(ceil_div64(chunks, kNC), kWave) * kWave));
       auto form = [&](auto held, auto tail) {
         hipLaunchKernelGGL((norm_back_rows_kernel<T, decltype(held)::value, kNC, kR, decltype(tail)::value>), dim3(unsigned(n)), wg,
-                           0, s, d, rows, mean, rstd, D, im, ch, sc, res, o, part, parts);
+                           0, s, d, rows, mean, rstd, D, im, ch, sc, res, o, sums);
       };
       const std::true_type yes;
       const std::false_type no;
@@ -629,9 +640,9 @@ void run_norm_back(const void* dh, const Rows<T>& rows, const float* mean, const
       hipLaunchKernelGGL(norm_back_avg_kernel<T>, dim3(unsigned(ceil_div64(M, 4))), dim3(256), 0, s, d, rows, mean, rstd, M, D,
                          im, sc, avg);
     hipLaunchKernelGGL(norm_back_any_kernel<T>, dim3(unsigned(n), unsigned(ceil_div64(D, 256))), dim3(256), 0, s, d, rows,
-                       mean, rstd, D, im, ch, sc, res, (const float*)avg, o, part, parts);
+                       mean, rstd, D, im, ch, sc, res, (const float*)avg, o, sums);
   }
-  if (parts) {
+  if (wanted && !direct) {
     const int together = im.stride == 0 ? 1 : 0;
     auto sum = [&](auto v) {
       constexpr int kV = decltype(v)::value;

@@ -144,3 +144,30 @@ def test_many_rows(gpu, D, dtype):
     ref = rstd.double()[:, None] * (g - g.mean(1, True) - n * (g * n).mean(1, True))
     err = (dx.double() - ref).abs().max() / ref.abs().max()
     assert err < HALF[dtype] + 1e-5
+
+
+@pytest.mark.parametrize("D", [5, 64, 1003])
+@pytest.mark.parametrize("M,B", [(1, 1), (8, 1), (9, 1), (20, 3), (24, 3), (300, 3)])
+def test_one_of_the_sums(gpu, M, B, D):
+    """dscale or dshift alone, with few rows (whose sums are written at once) and with more: the bits of both."""
+    import torch
+    gen = torch.Generator("cuda").manual_seed(M + D)
+    dh, x = (torch.randn(M, D, device="cuda", generator=gen) for _ in range(2))
+    mean, rstd = torch.randn(M, device="cuda", generator=gen), torch.rand(M, device="cuda", generator=gen) + 0.5
+    off = [M * i // B for i in range(B + 1)]
+    for sc, shape in ((torch.randn(B, D, device="cuda", generator=gen), (B + 1, D)), (torch.randn(D, device="cuda", generator=gen), (2, D))):
+        both = [torch.full(shape, 7.0, device="cuda") for _ in range(2)]
+        view = lambda t: t[:-1] if sc.dim() == 2 else t[0]  # noqa: E731
+        dx = [torch.empty_like(x) for _ in range(4)]
+        gpu.avits_layer_norm_backward(dh, mean, rstd, sc, dx[0], view(both[0]), view(both[1]), x=x, off=off)
+        one = [torch.full(shape, 7.0, device="cuda") for _ in range(2)]
+        gpu.avits_layer_norm_backward(dh, mean, rstd, sc, dx[1], view(one[0]), None, x=x, off=off)
+        gpu.avits_layer_norm_backward(dh, mean, rstd, sc, dx[2], None, view(one[1]), x=x, off=off)
+        gpu.avits_layer_norm_backward(dh, mean, rstd, sc, dx[3], None, None, x=x, off=off)
+        assert torch.equal(both[0], one[0]) and torch.equal(both[1], one[1]) and all(torch.equal(dx[0], d) for d in dx[1:])
+        assert (both[0][-1] == 7.0).all() and (both[1][-1] == 7.0).all()
+        n = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+        for got, t in ((both[0], dh.double() * n), (both[1], dh.double())):
+            for i in range(B if sc.dim() == 2 else 1):
+                r = slice(off[i], off[i + 1]) if sc.dim() == 2 else slice(0, M)
+                assert_within(_np(got[i]), _np(t[r].sum(0)), U * 132 * _np(t[r].abs().sum(0)) + 1e-30)
