@@ -235,29 +235,30 @@ __device__ __forceinline__ void turn_chunks(u32x4 (&c)[V], int l) {
 // outside, or (VEC false: rows or the bias do not start on 16 bytes) by plain ones,
 // which may lie at any element, and a row's last, partial chunk one by one
 // (4608 x 8195 x 2048 57.7 us, 8192 columns 55.4; column by column it took 164).
-template <typename T, bool GATED, bool VEC>
+// A row's residual and gate are fetched before the row before it is stored: loads
+// and stores complete in their order, so a wait for loads behind stores is one for the
+// stores too (fp32 16896 x 2048 x 8192 504 us instead of 188, without a gate 150).
+// BIAS_LDS: the block's biases lie in LDS.
+template <typename T, bool GATED, bool VEC, bool BIAS_LDS>
 struct BlockEnd {
   static constexpr int Z = sizeof(T), E = 16 / Z, V = 16 / E;   // elements of a chunk, chunks of a lane's columns
   Mx4ArgsPtr a;
   int64_t mb, nb, N;
   int l, g, rows, cols;
   bool one;
-  Sixteen<T> gate, bias;
+  const T* bias_lds;
+  Sixteen<T> bias;
   __amdgpu_buffer_rsrc_t ro, rr;
+  struct Fetched {
+    Sixteen<T> resid, gate;
+  };
 
-  // bias_lds: the block's biases (VEC), or null to read them from memory.
-  __device__ __forceinline__ BlockEnd(Mx4ArgsPtr args, int64_t mb_, int64_t nb_, int lane, const T* bias_lds)
+  __device__ __forceinline__ BlockEnd(Mx4ArgsPtr args, int64_t mb_, int64_t nb_, int lane, const T* biases)
       : a(args), mb(mb_), nb(nb_), N(args->N), l(lane % 16), g(lane / 16),
         rows(int(std::min<int64_t>(128, args->M - mb_))), cols(int(std::min<int64_t>(64, args->N - nb_))),
-        one(args->im.B == 1 || args->im.stride == 0) {
-    if (VEC && bias_lds) {
-#pragma unroll
-      for (int q = 0; q < V; ++q)
-        bias.w[q] = a->bias ? *reinterpret_cast<const u32x4*>(bias_lds + 16 * g + E * q) : u32x4{0u, 0u, 0u, 0u};
-    } else {
-      bias.load(a->bias, N, nb + 16 * g);
-    }
-    if (GATED && one) gate.load(a->gate, N, nb + 16 * g);
+        one(args->im.B == 1 || args->im.stride == 0), bias_lds(biases) {
+    if (!BIAS_LDS) bias.load(a->bias, N, nb + 16 * g);
+    else if (!GATED) bias_from_lds(bias);
     const int64_t span = ((rows - 1) * N + cols) * Z;
     ro = range_of(static_cast<T*>(a->out) + mb * N + nb, span);
     if (GATED) rr = range_of(static_cast<const T*>(a->resid) + mb * N + nb, span);
@@ -274,50 +275,55 @@ struct BlockEnd {
     n = row < rows ? std::max(0, std::min(E, cols - E * chunk)) : 0;
     return (mb + row) * N + nb + E * chunk;
   }
-  __device__ __forceinline__ void row(int i, float (&v)[16]) {
+  __device__ __forceinline__ void bias_from_lds(Sixteen<T>& b) const {
 #pragma unroll
-    for (int c = 0; c < 16; ++c) v[c] += bias.at(c);
+    for (int q = 0; q < V; ++q)
+      b.w[q] = a->bias ? *reinterpret_cast<const u32x4*>(bias_lds + 16 * g + E * q) : u32x4{0u, 0u, 0u, 0u};
+  }
+  // `n` elements of a chunk, zeros behind.
+  static __device__ __forceinline__ u32x4 some(const T* p, int n) {
+    u32x4 w = {0u, 0u, 0u, 0u};
+    if (n >= E) {
+      const loose4 c = *reinterpret_cast<const loose4*>(p);
+      w = u32x4{c[0], c[1], c[2], c[3]};
+    } else if (n > 0) {
+#pragma unroll
+      for (int e = 0; e < E - 1; ++e)
+        if (e < n) w[e * Z / 4] |= element(p + e) << (Z == 2 && e % 2 ? 16 : 0);
+    }
+    return w;
+  }
+  __device__ __forceinline__ void fetch(int i, Fetched& f) const {
     if constexpr (GATED) {
-      const int r = 8 * l + i;
+      int64_t skip = 0;
       if (!one) {
-        int64_t skip = 0;
-        const int64_t stride = a->im.stride, at_row = mb + std::min(r, rows - 1);
+        const int64_t stride = a->im.stride, at_row = mb + std::min(8 * l + i, rows - 1);
 #pragma unroll 1
         for (int b = 0; b < a->im.B - 1; ++b) skip += at_row >= a->im.end[b] ? stride : 0;  // scalars are short: rolled
-        // (No uniform base: element loads; columns past N repeat the last one, unused.)
-        const T* p = static_cast<const T*>(a->gate) + skip + nb;
-#pragma unroll
-        for (int c = 0; c < 16; ++c) {
-          const int at_c = std::min(16 * g + c, cols - 1);
-          if constexpr (Z == 4) gate.w[c / 4][c % 4] = __float_as_uint(p[at_c]);
-          else if (c % 2 == 0) gate.w[c / 8][c / 2 % 4] = p[at_c];
-          else gate.w[c / 8][c / 2 % 4] |= uint32_t(p[at_c]) << 16;
-        }
       }
-      Sixteen<T> res;
-      if constexpr (VEC) {
+      const T* gate = static_cast<const T*>(a->gate) + skip + nb + 16 * g;
 #pragma unroll
-        for (int q = 0; q < V; ++q)
-          res.w[q] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, int(at(i, q)), 0, 0));
-      } else {
-#pragma unroll
-        for (int q = 0; q < V; ++q) {
+      for (int q = 0; q < V; ++q) {
+        f.gate.w[q] = some(gate + E * q, cols - 16 * g - E * q);
+        if constexpr (VEC) {
+          f.resid.w[q] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rr, int(at(i, q)), 0, 0));
+        } else {
           int n;
           const T* p = static_cast<const T*>(a->resid) + loose_at(i, q, n);
-          res.w[q] = u32x4{0u, 0u, 0u, 0u};
-          if (n == E) {
-            const loose4 w = *reinterpret_cast<const loose4*>(p);
-            res.w[q] = u32x4{w[0], w[1], w[2], w[3]};
-          } else if (n > 0) {
-#pragma unroll
-            for (int e = 0; e < E - 1; ++e)
-              if (e < n) res.w[q][e * Z / 4] |= element(p + e) << (Z == 2 && e % 2 ? 16 : 0);
-          }
+          f.resid.w[q] = some(p, n);
         }
       }
-      turn_chunks<V>(res.w, l);
+    }
+  }
+  __device__ __forceinline__ void row(int i, float (&v)[16], Fetched& f) const {
+    Sixteen<T> b = bias;
+    if (BIAS_LDS && GATED) bias_from_lds(b);   // (registers are short)
 #pragma unroll
-      for (int c = 0; c < 16; ++c) v[c] = res.at(c) + gate.at(c) * v[c];
+    for (int c = 0; c < 16; ++c) v[c] += b.at(c);
+    if constexpr (GATED) {
+      turn_chunks<V>(f.resid.w, l);
+#pragma unroll
+      for (int c = 0; c < 16; ++c) v[c] = f.resid.at(c) + f.gate.at(c) * v[c];
     }
     u32x4 w[V];
 #pragma unroll
@@ -571,13 +577,18 @@ __global__ __launch_bounds__(512) void mx4_tile_kernel(const Mx4Args args, uint3
 #pragma unroll
           for (int j = 0; j < TN; ++j) p[(i * TN + j) * kWave] = acc[i][j];
       } else {
-        BlockEnd<T, GATED, VEC> end(a, mb, nb, lane_id(), reinterpret_cast<const T*>(lds + kB + 1024 * (par ^ 1)) + 64 * sub);
+        using End = BlockEnd<T, GATED, VEC, VEC>;
+        const End end(a, mb, nb, lane_id(), reinterpret_cast<const T*>(lds + kB + 1024 * (par ^ 1)) + 64 * sub);
+        typename End::Fetched cur, nxt;
+        end.fetch(0, cur);
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
+          if (i + 1 < TM) end.fetch(i + 1, nxt);
           float v[16];
 #pragma unroll
           for (int c = 0; c < 16; ++c) v[c] = acc[i][c % 4][c / 4];
-          end.row(i, v);
+          end.row(i, v, cur);
+          cur = nxt;
         }
       }
     }
@@ -650,10 +661,13 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(const Mx4Args args, const
   pp_place(tile, uint32_t((a->N + 255) / 256), uint32_t((a->M + 255) / 256), 0, prob, tm, tn);
   const int64_t mb = int64_t(tm) * 256 + 128 * (block / 4), nb = int64_t(tn) * 256 + 64 * (block % 4);
   if (mb >= a->M || nb >= a->N) return;
-  BlockEnd<T, GATED, VEC> end(a, mb, nb, lane, nullptr);
+  using End = BlockEnd<T, GATED, VEC, false>;
+  const End end(a, mb, nb, lane, nullptr);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int i = 2 * wave + h;
+    typename End::Fetched f;
+    end.fetch(i, f);
     f32x4 sum[4] = {};
     for (uint32_t k = 0; k < splits; ++k) {
       const f32x4* p = reinterpret_cast<const f32x4*>(parts) + ((int64_t(tile) * splits + k) * 8 + block) * (32 * kWave) +
@@ -664,7 +678,7 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(const Mx4Args args, const
     float v[16];
 #pragma unroll
     for (int c = 0; c < 16; ++c) v[c] = sum[c % 4][c / 4];
-    end.row(i, v);
+    end.row(i, v, f);
   }
 }
 
