@@ -950,7 +950,8 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t K) {
     const auto& form = kForms[f];
     const double wgs = double(ceil_div64(M, 16 * form.tm)) * double(ceil_div64(N, 16 * form.tn));
     const double bytes = wgs * 16.0 * (form.tm + form.tn) * double(K) * 0.53e-6;
-    const double us = form.fixed + std::max({bytes / form.rate, std::ceil(steps / form.waves) * form.step, double(M) * double(N) * 3.8e-6});
+    const double us = form.fixed + std::max({bytes / form.rate, std::ceil(steps / form.waves) * form.step,
+                                             double(M) * double(N) * 3.8e-6});
     if (us >= best) continue;
     best = us;
     p.form = f;

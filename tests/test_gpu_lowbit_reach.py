@@ -61,7 +61,8 @@ def test_codes_past_two_to_the_31_bytes(gpu):
     import torch
     K, M, N = 2048, (1 << 21) + 21, 8
     x = _randn(M, K)
-    q, s = torch.empty(M, K // 2, dtype=torch.uint8, device="cuda"), torch.empty(*gpu.avits_mxfp4_scale_shape(M, K), dtype=torch.uint8, device="cuda")
+    q = torch.empty(M, K // 2, dtype=torch.uint8, device="cuda")
+    s = torch.empty(*gpu.avits_mxfp4_scale_shape(M, K), dtype=torch.uint8, device="cuda")
     gpu.avits_mxfp4_quantize(x, q, s)
     codes, e = oracle.hold(_np(x[-21:]), 4)
     qo, so = oracle.mx_pack(codes, e)
@@ -82,7 +83,8 @@ def test_outputs_past_two_to_the_31_elements(gpu):
     rng = np.random.default_rng(1)
     wq, ws, w = _held(rng, N, K)
     x = _randn(M, K)
-    q, s = torch.empty(M, K // 2, dtype=torch.uint8, device="cuda"), torch.empty(*gpu.avits_mxfp4_scale_shape(M, K), dtype=torch.uint8, device="cuda")
+    q = torch.empty(M, K // 2, dtype=torch.uint8, device="cuda")
+    s = torch.empty(*gpu.avits_mxfp4_scale_shape(M, K), dtype=torch.uint8, device="cuda")
     gpu.avits_mxfp4_quantize(x, q, s)
     res, gate = _randn(M, N), _randn(2, N)
     off = [0, M - 9, M]
