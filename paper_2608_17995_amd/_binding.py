@@ -549,6 +549,8 @@ def _mod_rows(name, t, dtype, dev, D, n_images):
     if t is None:
         return None, None
     shape = t.shape
+    if shape == (D,) and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr(), 0
     if len(shape) == 1:
         return _arg(t, name, dtype, dev, D), 0
     if shape != (n_images, D):
@@ -612,9 +614,9 @@ def _scratch(ws, need, dev, stream):
                 stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
             with torch.cuda.stream(stream):
                 ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-    elif ws.get_device() != dev:
-        raise AvitsError(-1, f"workspace must be on the current GPU, got {ws.device}")
-    return ws, _dev(ws, "workspace"), ws.numel() * ws.element_size()
+    elif ws.get_device() != dev or not ws.is_contiguous():
+        raise AvitsError(-1, f"workspace must be contiguous and on the current GPU, got {ws.device}")
+    return ws, ws.data_ptr(), ws.nbytes
 
 
 def avits_layer_norm(x, shift, scale, h, mean=None, rstd=None, off=None, eps=1e-6, stream=None):
@@ -623,7 +625,7 @@ def avits_layer_norm(x, shift, scale, h, mean=None, rstd=None, off=None, eps=1e-
     shift and scale are [B, D] or one shared [D] (each may be None)."""
     M, D = x.shape
     (code, dev), dt, f32 = _code(x), x.dtype, _TYPES["f32"]
-    n, offs = _offsets(off, M, "avits_layer_norm")
+    n, offs = (1, None) if off is None else _offsets(off, M, "avits_layer_norm")
     sh, step = _mod_rows("shift", shift, dt, dev, D, n)
     sc, step2 = _mod_rows("scale", scale, dt, dev, D, n)
     if step is not None and step2 is not None and step != step2:
@@ -650,7 +652,7 @@ def avits_layer_norm_backward(dh, mean, rstd, scale, dx, dscale=None, dshift=Non
     M, D = dh.shape
     (code, dev), dt = _code(dh), dh.dtype
     f32, u8 = _TYPES["f32"], _TYPES["u8"]
-    n, offs = _offsets(off, M, "avits_layer_norm_backward")
+    n, offs = (1, None) if off is None else _offsets(off, M, "avits_layer_norm_backward")
     sc, step = _mod_rows("scale", scale, dt, dev, D, n)
     if step is None:
         grad = dscale if dscale is not None else dshift
@@ -660,8 +662,9 @@ def avits_layer_norm_backward(dh, mean, rstd, scale, dx, dscale=None, dshift=Non
     rc = (_LIB or load()).avits_layer_norm_backward(
         _arg(dh, "dh", dt, dev, M, D), _arg(x, "x", dt, dev, M, D), _arg(x_q8, "x_q8", u8, dev, M, D),
         _arg(x_s8, "x_s8", u8, dev, M, (D + 31) // 32), _arg(mean, "mean", f32, dev, M), _arg(rstd, "rstd", f32, dev, M),
-        M, D, n, offs, sc, step, _arg(dres, "dres", dt, dev, M, D), code, _arg(dx, "dx", dt, dev, M, D), _arg(dscale, "dscale", f32, dev, *shape),
-        _arg(dshift, "dshift", f32, dev, *shape), wsp, wsb, _device_stream(dev) if stream is None else _stream(stream))
+        M, D, n, offs, sc, step, _arg(dres, "dres", dt, dev, M, D), code, _arg(dx, "dx", dt, dev, M, D),
+        _arg(dscale, "dscale", f32, dev, *shape), _arg(dshift, "dshift", f32, dev, *shape), wsp, wsb,
+        _device_stream(dev) if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return dx, dscale, dshift
@@ -715,6 +718,9 @@ def _mx(q, s, name, dev, M, K):
     if K % 2:
         raise ValueError(f"{name}: {K} columns cannot be held in 4 bits")
     u8 = (_TYPES or _types())["u8"]
+    if (q.dtype is u8 and s.dtype is u8 and q.shape == (M, K // 2) and s.shape == ((K + 63) // 64, (M + 7) // 8 * 8, 2) and
+            q.get_device() == s.get_device() == dev and q.is_contiguous() and s.is_contiguous()):
+        return q.data_ptr(), s.data_ptr()
     return _arg(q, name, u8, dev, M, K // 2), _arg(s, f"{name} scales", u8, dev, (K + 63) // 64, (M + 7) // 8 * 8, 2)
 
 
@@ -756,7 +762,7 @@ def avits_mxfp4_linear(xq, xs, wq, ws, b, out, gate=None, resid=None, off=None, 
     (code, dev), dt = _code(out), out.dtype
     xqp, xsp = _mx(xq, xs, "x", dev, M, K)
     wqp, wsp = _mx(wq, ws, "w", dev, N, K)
-    n, offs = _offsets(off, M, "avits_mxfp4_linear")
+    n, offs = (1, None) if off is None else _offsets(off, M, "avits_mxfp4_linear")
     gp, step = _mod_rows("gate", gate, dt, dev, N, n)
     buf, bp, nb = _scratch(workspace, lambda: avits_mxfp4_linear_workspace_bytes(M, N, K), dev, stream)
     rc = (_LIB or load()).avits_mxfp4_linear(xqp, xsp, M, K, wqp, wsp, _arg(b, "b", dt, dev, N), N, n, offs, gp, step or 0,
@@ -779,7 +785,8 @@ def avits_mxfp4_linear_backward(dy, wq, ws, dx, workspace=None, stream=None):
     wqp, wsp = _mx(wq, ws, "w", dev, N, K)
     buf, bp, nb = _scratch(workspace, lambda: avits_mxfp4_linear_backward_workspace_bytes(M, N, K, code), dev, stream)
     rc = (_LIB or load()).avits_mxfp4_linear_backward(_arg(dy, "dy", dt, dev, M, N), M, N, wqp, wsp, K, code,
-                                            _arg(dx, "dx", dt, dev, M, K), bp, nb, _device_stream(dev) if stream is None else _stream(stream))
+                                            _arg(dx, "dx", dt, dev, M, K), bp, nb,
+                                            _device_stream(dev) if stream is None else _stream(stream))
     if rc:
         _check(rc)
     return dx
