@@ -693,13 +693,19 @@ __global__ __launch_bounds__(256) void mx4_join_kernel(const Mx4Args args, const
 // ODD: N is no multiple of 8; dy's rows lie at any element, and of the last group of
 // eight n what is not there counts as 0.
 // An fp32 dy goes as three bf16 values whose sum it is exactly (8 bits of its 24 each), so
-// their products with the weight's values are exact too and the sums are fp32's.
+// their products with the weight's values are exact too and the sums are fp32's.  Only
+// below 2^-110 can bits be left that lie under bf16's smallest, 2^-133: a wave that met
+// some goes over its steps again and adds them as two more values, times 2^16, with the
+// weight times 2^-16.  That is exact where it counts: a weight that 2^-16 takes below
+// 2^-133 is at most 6 x 2^-117, and its product with such a rest is 0 in fp32.
 // blockIdx.y: part of the contraction, summed into its own [M, K] where there are several.
 struct Thirds {
   u32x4 v[3];
+  uint32_t rest;   // its low half is not 0 where the three are less than the values
 };
 __device__ __forceinline__ Thirds thirds_of(const u32x4& lo, const u32x4& hi) {
   Thirds t;
+  t.rest = 0;
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
     uint32_t bits[3][2];
@@ -712,16 +718,37 @@ __device__ __forceinline__ Thirds thirds_of(const u32x4& lo, const u32x4& hi) {
       bits[1][h] = __float_as_uint(r) & 0xffff0000u;
       bits[2][h] = __float_as_uint(r - __uint_as_float(bits[1][h]));
     }
+    t.rest |= bits[2][0] | bits[2][1];
 #pragma unroll
     for (int k = 0; k < 3; ++k) t.v[k][e / 2] = __builtin_amdgcn_perm(bits[k][1], bits[k][0], 0x07060302u);
   }
   return t;
 }
+// What the thirds leave, times 2^16: at most 16 bits from 2^-133 up, as two bf16 values.
+__device__ __forceinline__ void rest_of(const u32x4& lo, const u32x4& hi, u32x4 (&v)[2]) {
+  auto upper = [](float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); };
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    uint32_t bits[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float r = __uint_as_float((e < 4 ? lo : hi)[e % 4 + h]);
+      r = fabsf(r) < 0x1p-110f ? r : 0.f;
+#pragma unroll
+      for (int k = 0; k < 3; ++k) r -= upper(r);
+      r *= 0x1p16f;
+      bits[0][h] = __float_as_uint(upper(r));
+      bits[1][h] = __float_as_uint(r - upper(r));
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) v[k][e / 2] = __builtin_amdgcn_perm(bits[k][1], bits[k][0], 0x07060302u);
+  }
+}
 
 template <int TM, int NW, bool ODD, typename IN, typename OUT>
-__global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const IN* __restrict__ dy, int64_t M, int64_t N,
-                                                                const uint8_t* __restrict__ wq, const uint8_t* __restrict__ ws,
-                                                                int64_t K, OUT* __restrict__ dx) {
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void mx4_back_rows_kernel(
+    const IN* __restrict__ dy, int64_t M, int64_t N, const uint8_t* __restrict__ wq, const uint8_t* __restrict__ ws, int64_t K,
+    OUT* __restrict__ dx) {
   __shared__ float red[NW][TM * 32][kWave];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int l = lane % 16, g = lane / 16;
@@ -739,15 +766,25 @@ __global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const IN* __rest
     u32x4 sc, y[TM][V];
   };
   // (Past the last step everything is out of range: zeros, no memory.)
-  auto load = [&](int t, Step& v) {
-    const int64_t n = int64_t(t) * 32 + 8 * g;
+  // Byte offsets of the lane in the weight's 32 rows, its scales' and dy's rows (all below 2^31).
+  struct At {
+    uint32_t w, s, y;
+  };
+  const uint32_t row_bytes = uint32_t(rowb), n_all = uint32_t(N);
+  auto place = [&](int l, int g) {
+    const int64_t k = k0 + 8 * l;
+    return At{k < K ? uint32_t(8 * g) * row_bytes + uint32_t(k / 2) : kNowhere, k < K ? uint32_t(k / 64 * Np * 2) : kNowhere,
+              uint32_t(l) * n_all * Z};
+  };
+  auto load = [&](int t, Step& v, const At& p, int l, int g) {
+    const uint32_t n = uint32_t(t) * 32 + 8 * g;
     const __amdgpu_buffer_rsrc_t rw = range_of(wq + int64_t(t) * 32 * rowb, (N - int64_t(t) * 32) * rowb);
+    uint32_t at = p.w;
+    asm volatile("" : "+v"(at));   // (eight offsets kept for the loop would spill)
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      v.w[e] = uint32_t(__builtin_amdgcn_raw_buffer_load_b32(
-          rw, int(k < K ? uint32_t((8 * g + e) * rowb + k / 2) : kNowhere), 0, 0));
-    v.sc = __builtin_bit_cast(
-        u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, int(k < K && n < N ? uint32_t((k / 64 * Np + n) * 2) : kNowhere), 0, 0));
+      v.w[e] = uint32_t(__builtin_amdgcn_raw_buffer_load_b32(rw, int(at + e * row_bytes), 0, 0));
+    v.sc = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, int(n < n_all ? p.s + 2 * n : kNowhere), 0, 0));
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       if constexpr (!ODD) {
@@ -755,14 +792,14 @@ __global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const IN* __rest
         for (int q = 0; q < V; ++q)
           v.y[i][q] = __builtin_bit_cast(
               u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                         ry, int(n < N ? uint32_t(((16 * i + l) * N + n) * Z + 16 * q) : kNowhere), 0, 0));
+                         ry, int(n < n_all ? p.y + 16 * i * n_all * Z + n * Z + 16 * q : kNowhere), 0, 0));
       } else {   // (rows past M repeat the last one, unused)
-        const IN* p = dy + std::min<int64_t>(m0 + 16 * i + l, M - 1) * N + n;
+        const IN* d = dy + std::min<int64_t>(m0 + 16 * i + l, M - 1) * N + n;
 #pragma unroll
         for (int q = 0; q < V; ++q) {
           v.y[i][q] = u32x4{0u, 0u, 0u, 0u};
           if (n + 8 <= N) {
-            const loose4 w = *reinterpret_cast<const loose4*>(p + 16 / Z * q);
+            const loose4 w = *reinterpret_cast<const loose4*>(d + 16 / Z * q);
             v.y[i][q] = u32x4{w[0], w[1], w[2], w[3]};
           }
         }
@@ -770,8 +807,8 @@ __global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const IN* __rest
 #pragma unroll
           for (int e = 0; e < 7; ++e)
             if (n + e < N) {
-              if constexpr (Z == 4) v.y[i][e / 4][e % 4] = __float_as_uint(p[e]);
-              else v.y[i][0][e / 2] |= uint32_t(p[e]) << (e % 2 ? 16 : 0);
+              if constexpr (Z == 4) v.y[i][e / 4][e % 4] = __float_as_uint(d[e]);
+              else v.y[i][0][e / 2] |= uint32_t(d[e]) << (e % 2 ? 16 : 0);
             }
         }
       }
@@ -783,21 +820,28 @@ __global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const IN* __rest
     }
   };
   const int stride = NW * int(gridDim.y);
-  int t = int(blockIdx.y) * NW + wave;
-  Step cur, next;
-  load(t, cur);
-  for (; t < steps; t += stride) {
-    load(t + stride, next);
-    u32x4 f[8];
+  // The weight's columns of a step, times a power of two.
+  auto decode = [&](const Step& v, float times, u32x4 (&f)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
       float a[8], b[8];
-      const uint32_t pair = cur.sc[e / 2] >> shift;
-      decode4x8(cur.w[e], scale_value(pair & 255u), a);
-      decode4x8(cur.w[e + 1], scale_value(pair >> 16 & 255u), b);
+      const uint32_t pair = v.sc[e / 2] >> shift;
+      decode4x8(v.w[e], scale_value(pair & 255u) * times, a);
+      decode4x8(v.w[e + 1], scale_value(pair >> 16 & 255u) * times, b);
 #pragma unroll
       for (int c = 0; c < 8; ++c) f[c][e / 2] = pack_bf2(a[c], b[c]);
     }
+  };
+  const int first = int(blockIdx.y) * NW + wave;
+  uint64_t rest = 0;   // (of the wave: scalar)
+  Step cur, next;
+  const At here = place(l, g);
+  load(first, cur, here, l, g);
+  for (int t = first; t < steps; t += stride) {
+    load(t + stride, next, here, l, g);
+    u32x4 f[8];
+    decode(cur, 1.f, f);
+    if (Z == 4 && NW == 8) __builtin_amdgcn_sched_barrier(0);   // (128 registers hold no more at once)
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       if constexpr (Z == 2) {
@@ -805,6 +849,7 @@ __global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const IN* __rest
         for (int c = 0; c < 8; ++c) acc[i][c] = mfma16x16x32(as_bf16x8(cur.y[i][0]), as_bf16x8(f[c]), acc[i][c]);
       } else {
         const Thirds y = thirds_of(cur.y[i][0], cur.y[i][1]);
+        rest |= __ballot((y.rest & 0xffffu) != 0u);
 #pragma unroll
         for (int k = 2; k >= 0; --k)
 #pragma unroll
@@ -813,12 +858,45 @@ __global__ __launch_bounds__(64 * NW) void mx4_back_rows_kernel(const IN* __rest
     }
     cur = next;
   }
+  auto put = [&](bool more) {
 #pragma unroll
-  for (int i = 0; i < TM; ++i)
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int c = 0; c < 8; ++c)
+      for (int c = 0; c < 8; ++c)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) red[wave][(i * 4 + r) * 8 + c][lane] = acc[i][c][r];
+        for (int r = 0; r < 4; ++r) {
+          float& at = red[wave][(i * 4 + r) * 8 + c][lane];
+          at = more ? at + acc[i][c][r] : acc[i][c][r];
+        }
+  };
+  put(false);
+  if constexpr (Z == 4) {
+    if (rest) {   // its steps again, for the rests
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc[i][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+      int l2 = l, g2 = g;
+      asm volatile("" : "+v"(l2), "+v"(g2));   // (no registers for this loop's addresses in the one above)
+      const At again = place(l2, g2);
+#pragma unroll 1
+      for (int t = first; t < steps; t += stride) {
+        load(t, cur, again, l2, g2);
+        u32x4 f[8];
+        decode(cur, 0x1p-16f, f);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          u32x4 y[2];
+          rest_of(cur.y[i][0], cur.y[i][1], y);
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) acc[i][c] = mfma16x16x32(as_bf16x8(y[k]), as_bf16x8(f[c]), acc[i][c]);
+        }
+      }
+      put(true);
+    }
+  }
   __syncthreads();
   dx += int64_t(blockIdx.y) * M * K;
   // The 4 TM groups of eight columns of a lane, dealt over the waves.
@@ -1032,7 +1110,7 @@ struct BackPlan {
 // CU; 1.2 with 64 rows), parts their bytes and a launch, which the host pays too; the
 // other way its launches, the weight's bytes and the product at 1.1 PFLOP/s.  fp32
 // always goes from the held weight, by the same figures (within 5 % of its best form
-// from 1 x 1024 x 1024, 6.6 us, to 1741 x 6400 x 2048, 187; the fp32 product with the
+// from 1 x 1024 x 1024, 7.8 us in a graph, to 1741 x 6400 x 2048, 176; the fp32 product with the
 // weight turned round took 13.1 and 723).  Measured (16 rows whole, in 4; 64 rows in 4; turned round):
 //   16 x 8192 x 2048   33.3  13.7  25.7  43.1     512 x 8192 x 2048  56.6  61.1  53.1  43.5
 //   128 x 8192 x 2048  33.4  21.8  28.1  40.5     67 x 1024 x 256     6.5   6.4   9.1  13.5
