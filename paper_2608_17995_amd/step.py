@@ -703,8 +703,12 @@ class Mxfp4Mlp:
     w1 [F, D], w2 [D, F] (D, F multiples of 32), b1, b2: bf16 or fp32, that
     type is the type of every activation; they are quantised here and not kept.
     All buffers for up to `rows` rows are allocated here (the ones of the backward pass
-    with tune=True); the calls only enqueue.  One object's calls belong on one stream
-    at a time, and backward() belongs to the forward() before it.
+    with tune=True); the calls only enqueue.  The held weights are there, and the buffers
+    free of earlier work, when the constructor returns: it waits for the current stream, so
+    that the calls may use any (in a capture it does not wait: there the calls belong on the
+    capturing stream).  One object's calls belong on one stream
+    at a time, and backward() belongs to the forward() before it; the object has to live
+    until its work on a stream other than the constructor's is done.
     """
 
     def __init__(self, w1, b1, w2, b2, rows: int, tune=False, eps=1e-6):
@@ -739,6 +743,8 @@ class Mxfp4Mlp:
                        B.avits_layer_norm_backward_workspace_bytes(rows, D, 16)]
         self._ws = new(max(nbytes + [16]), dtype=u8)
         self._n = None
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().synchronize()
 
     def _scales(self, buf, M, K):
         return buf[:B.avits_mxfp4_scale_bytes(M, K)].view(B.avits_mxfp4_scale_shape(M, K))
