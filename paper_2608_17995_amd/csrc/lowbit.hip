@@ -375,7 +375,8 @@ extern "C" int avits_gelu_backward(const void* da, const void* m, const uint8_t*
 
 extern "C" size_t avits_mxfp4_scale_bytes(int64_t M, int64_t K) {
   if (M < 0 || M >= (int64_t(1) << 27) || K < kBlk || K >= (int64_t(1) << 24) || K % kBlk != 0) return 0;
-  return size_t(scale_groups(K)) * size_t(scale_rows(M)) * 2;
+  const int64_t bytes = scale_groups(K) * scale_rows(M) * 2;
+  return bytes < (int64_t(1) << 31) ? size_t(bytes) : 0;
 }
 
 extern "C" int avits_mxfp4_quantize(const void* x, int64_t M, int64_t K, int act, int dtype, uint8_t* q, uint8_t* s,
