@@ -48,10 +48,14 @@ def _run(cmd):
 # Kernels that must compile without scratch: the GEMM's loads are
 # asynchronous inline assembly (a spilled destination would be saved before
 # the data lands); a spill in the attention or scoring tile loops costs more
-# than half their speed; the selections keep their keys in registers.
+# than half their speed; the selections and the norms keep their keys and rows in
+# registers.  Of the 4-bit tile kernel's forms the gated ones, and the bf16 one whose rows
+# do not start on 16 bytes, spill one to seven values that live as long as a tile (its
+# loads go to LDS, none into a register): its step loops are free of scratch.
 NO_SCRATCH = {"gemm.hip": ("gemm_bf16",), "attention.hip": ("attn_bf16_kernel",),
-              "score.hip": ("spatial_temporal_bf16", "finalize_select"), "select.hip": ("radix_select",), 
-              "mxfp4.hip": ("mx4_tile_kernelItLb0ELb1", "mx4_tile_kernelIfLb0ELb1")}
+              "score.hip": ("spatial_temporal_bf16", "finalize_select"), "select.hip": ("radix_select",),
+              "norm.hip": ("norm_rows_kernel", "norm_back_rows_kernel"),
+              "mxfp4.hip": ("mx4_rows_kernel", "mx4_join_kernel", "mx4_tile_kernelItLb0ELb1", "mx4_tile_kernelIfLb0ELb1")}
 _USAGE = ["-Rpass-analysis=kernel-resource-usage"]
 
 

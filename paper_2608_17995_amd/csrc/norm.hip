@@ -301,12 +301,18 @@ __global__ __launch_bounds__(256) void norm_back_any_kernel(const T* dh, const R
 // loaded whole before the barrier, so also where two lanes store the same elements.)
 // Measured with the sums of the chunks: 16000 x 2048 bf16 48.0 us (38.6 at a copy's
 // rate), from 8 bits 46.5 (32.1), x 3999 90.7 (75.3), x 8192 fp32 311 (308).
+// Four vectors of bf16 columns to a thread (8193 to 16384 columns) leave no registers for
+// the next rows nor for widened weights: there a row is loaded when its turn comes and
+// what can be made again is.  8000 x 8200 117 us, from 8 bits 121, x 12001 194 and 192, x
+// 16384 177 and 165 (with 40 to 174 registers in memory, as the form of fewer columns has it
+// there: 285 and 230, 733 and 948, 408 and 354).
 template <typename T, bool HELD, int NC, int R, bool TAIL>
 __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const Rows<T> xr, const float* __restrict__ mean,
                                                              const float* __restrict__ rstd, int64_t D, const Images im,
                                                              const Chunks ch, const T* __restrict__ scale, const T* dres,
                                                              T* dx, const SumsOut sums) {
   constexpr int E = kVec<T>;
+  constexpr bool kLean = NC == 4 && E == 8;
   __shared__ float red[2][8][2 * R];
   const int waves = blockDim.x / kWave, wave = threadIdx.x / kWave;
   const int width = int(D), nchunk = (width + E - 1) / E;
@@ -315,7 +321,8 @@ __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const 
   int64_t lo, hi;
   chunk_rows(im, ch, blockIdx.x, b, lo, hi);
   int at[NC], pos[NC], dup[NC];
-  float w[NC][E], sc[NC][E], sh[NC][E];
+  float w[kLean ? 1 : NC][E], sc[NC][E], sh[NC][E];
+  u32x4 w_held[kLean ? NC : 1];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     at[c] = threadIdx.x + blockDim.x * c;
@@ -324,13 +331,25 @@ __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const 
     dup[c] = here.dup;
     u32x4 g = {0u, 0u, 0u, 0u};
     if (scale && at[c] < nchunk) g = chunk_of(scale + b * im.stride + pos[c]);
-    widen<T>(g, w[c]);
+    if constexpr (kLean) w_held[c] = g;
+    else widen<T>(g, w[c]);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      w[c][e] = at[c] < nchunk ? 1.f + w[c][e] : 0.f;
+      if constexpr (!kLean) w[c][e] = at[c] < nchunk ? 1.f + w[c][e] : 0.f;
       sc[c][e] = sh[c][e] = 0.f;
     }
   }
+  auto weight = [&](int c, float (&v)[E]) {   // (past D dh is 0)
+    if constexpr (kLean) {
+      asm volatile("" : "+v"(w_held[c]));   // (opaque, here and below: what is widened is not kept)
+      widen<T>(w_held[c], v);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if constexpr (kLean) v[e] += 1.f;
+      else v[e] = w[c][e];
+    }
+  };
   // The rows' data as loaded; rows past the chunk and columns past D as zeros.
   struct Batch {
     u32x4 d[R][NC], x[R][NC], r[R][NC];
@@ -348,6 +367,7 @@ __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const 
       for (int c = 0; c < NC; ++c) {
         const u32x4 zero = {0u, 0u, 0u, 0u};
         const bool here = in && at[c] < nchunk;
+        if (kLean) asm volatile("" : "+v"(pos[c]));   // (nor are addresses)
         t.d[r][c] = here ? chunk_of(dh + m * D + pos[c]) : zero;
         t.x[r][c] = zero;
         if constexpr (HELD) {
@@ -371,10 +391,11 @@ __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const 
     }
   };
   Batch t, next;
-  if (lo < hi) load(lo, t);
+  if (!kLean && lo < hi) load(lo, t);
   int turn = 0;
   for (int64_t row = lo; row < hi; row += R, turn ^= 1) {
-    if (row + R < hi) load(row + R, next);
+    if (kLean) load(row, t);
+    else if (row + R < hi) load(row + R, next);
     auto normed = [&](int r, int c, float (&n)[E]) {
       if constexpr (HELD) {
         const float scale8 = scale_value(t.s[r][c]);
@@ -399,16 +420,17 @@ __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const 
       sum[2 * r] = sum[2 * r + 1] = 0.f;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        float dv[E], n[E];
+        float dv[E], n[E], wv[E];
         widen<T>(t.d[r][c], dv);
         normed(r, c, n);
+        weight(c, wv);
         if (TAIL && dup[c] > 0) {
           zero_first(dv, dup[c]);
           zero_first(n, dup[c]);
         }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const float g = dv[e] * w[c][e];
+          const float g = dv[e] * wv[e];
           sum[2 * r] += g;
           sum[2 * r + 1] = fmaf(g, n[e], sum[2 * r + 1]);
         }
@@ -438,23 +460,28 @@ __global__ __launch_bounds__(512) void norm_back_rows_kernel(const T* dh, const 
     for (int r = 0; r < R; ++r) {
       if (row + r >= hi) continue;
       const float ag = sum[2 * r] * inv, an = sum[2 * r + 1] * inv;
+      if constexpr (kLean) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(t.d[r][c]), "+v"(t.x[r][c]));
+      }
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         if (at[c] >= nchunk) continue;
-        float dv[E], n[E], o[E];
+        float dv[E], n[E], o[E], wv[E];
         widen<T>(t.d[r][c], dv);
         normed(r, c, n);
+        weight(c, wv);
         widen<T>(t.r[r][c], o);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           sc[c][e] = fmaf(dv[e], n[e], sc[c][e]);
           sh[c][e] += dv[e];
-          o[e] += t.rs[r] * (dv[e] * w[c][e] - ag - n[e] * an);
+          o[e] += t.rs[r] * (dv[e] * wv[e] - ag - n[e] * an);
         }
         put_chunk(dx + (row + r) * D + pos[c], narrow<T>(o));
       }
     }
-    t = next;
+    if (!kLean) t = next;
   }
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
