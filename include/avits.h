@@ -752,9 +752,10 @@ int avits_gelu_backward(const void* da, const void* m, const uint8_t* m_q8, cons
  * avits_mxfp4_linear_backward — the gradient of its input: dx [M, K] = dy W,
  * dy [M, N] and dx of dtype, W as above.
  * Either's workspace query suffices for any number of rows up to its M.
- * Requires 0 <= M < 2^27, 1 <= N < 2^21, K a multiple of 32 in [32, 2^21), and
+ * Requires 0 <= M < 2^27, 1 <= N < 2^21, K a multiple of 32 in [32, 2^21), fewer
+ * than 2^31 scale bytes for M and for N rows of K, and
  * 16-byte aligned q, s, dy, dx, resid, out and workspace (>= the matching
- * query).  M == 0 enqueues nothing.
+ * query; the gradient's is asked for whatever its form uses).  M == 0 enqueues nothing.
  * Errors: AVITS_ERR_INVALID_ARG, AVITS_ERR_UNSUPPORTED (dtype),
  * AVITS_ERR_WORKSPACE.
  * ---------------------------------------------------------------------- */
@@ -789,7 +790,9 @@ int avits_mxfp4_linear_backward(const void* dy, int64_t M, int64_t N, const uint
  * "mxfp4_quantize", "mxfp4_dequantize", "mxfp4_linear" (with the join of
  * split sums), and of
  * avits_mxfp4_linear_backward "mxfp4_transpose" (the weight turned round) and
- * "mxfp4_backward" (its product); "gemm" returns the sum of the six GEMM families (the GEMM kernels alone: the split-K
+ * "mxfp4_backward" (its product; the reduction of a split one is
+ * "splitk_reduce"); "gemm" returns the sum of the six GEMM families (the GEMM
+ * kernels alone: the split-K
  * reduction that follows a split launch is "splitk_reduce").  Unknown
  * family -> AVITS_ERR_INVALID_ARG.
  * avits_timing_reset() waits for pending events and zeroes every total.

@@ -95,7 +95,7 @@ __device__ __forceinline__ void finish(const Mx4Args& a, int64_t m, int64_t n, f
 // Few rows: a workgroup of NW waves owns 16 TM x 16 TN outputs, the waves take
 // every NW-th step of the contraction straight from memory into registers (the next
 // one while one is multiplied), and their sums meet in LDS.  Bound by the latency of a
-// few loads in a row and the launch: 1 x 12288 x 2048 5.9 us for a weight of 13.4 MB.
+// few loads in a row and the launch: 1 x 12288 x 2048 5.6 us in a graph for a weight of 13.4 MB.
 template <int TM, int TN, int NW, typename T>
 __global__ __launch_bounds__(64 * NW) void mx4_rows_kernel(const Mx4Args a) {
   __shared__ float red[NW][TM * TN * 4][kWave];
