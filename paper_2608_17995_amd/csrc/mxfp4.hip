@@ -1109,13 +1109,14 @@ struct BackPlan {
 // least predicted time (us).  A chain step takes 1.0 us (1.7 with two workgroups on a
 // CU; 1.2 with 64 rows), parts their bytes and a launch, which the host pays too; the
 // other way its launches, the weight's bytes and the product at 1.1 PFLOP/s.  fp32
-// always goes from the held weight, by the same figures (within 5 % of its best form
-// from 1 x 1024 x 1024, 7.8 us in a graph, to 1741 x 6400 x 2048, 176; the fp32 product with the
+// always goes from the held weight, by the same figures (within 8 % of its best form from
+// 300 x 2051 x 2048, 24.9 us in a graph, to 1741 x 6400 x 2048, 176-182; 1 x 1024 x 1024 8.2 and in 4
+// parts 6.8, whose second launch the host would pay; the fp32 product with the
 // weight turned round took 13.1 and 723).  Measured (16 rows whole, in 4; 64 rows in 4; turned round):
-//   16 x 8192 x 2048   33.3  13.7  25.7  43.1     512 x 8192 x 2048  56.6  61.1  53.1  43.5
-//   128 x 8192 x 2048  33.4  21.8  28.1  40.5     67 x 1024 x 256     6.5   6.4   9.1  13.5
-//   256 x 8192 x 2048  34.0  34.3  29.5  40.4     64 x 2048 x 8192   11.0  18.0  16.8  29.9
-//   300 x 2051 x 2048  19.2  22.6  26.0  31.9     1741 x 1024 x 512  10.6  20.8  21.5  24.1
+//   16 x 8192 x 2048   30.3  12.7  21.6  44.8     512 x 8192 x 2048  58.6  60.0  53.6  44.0
+//   128 x 8192 x 2048  31.4  21.2  28.5  41.5     67 x 1024 x 256     6.7   6.8   9.7  14.2
+//   256 x 8192 x 2048  33.8  34.7  30.4  41.2     64 x 2048 x 8192   11.2  18.0  15.9  31.0
+//   300 x 2051 x 2048  19.3  22.2  26.2  32.7     1741 x 1024 x 512  10.3  19.9  21.0  24.2
 BackPlan plan_back(int64_t M, int64_t N, int64_t K, int dtype) {
   const bool half = dtype == AVITS_BF16;
   BackPlan p;
