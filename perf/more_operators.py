@@ -175,7 +175,7 @@ def prepare(case, seed):
     words = (max(nk) + 63) // 64
     if kind == "select":
         return dict(s, q_means=empty(sum(nq), H, d, dtype=torch.float64), k_means=empty(sum(nk), Hk, d, dtype=torch.float64),
-                    mask=empty(H, sum(nq), words, dtype=torch.int64), ws=empty(256 << 20, dtype=torch.uint8))
+                    mask=empty(H, sum(nq), words, dtype=torch.int64))
     s["mask"] = _choose(s)
     s["ws"] = empty(1 << 30, dtype=torch.uint8)
     if kind == "attend":
@@ -338,8 +338,7 @@ def _own(s):
         q_lead, k_lead = _lead(c)
         avits.avits_block_means(s["q"], QB, s["q_means"], off=s["q_off"])
         avits.avits_block_means(s["k"], KB, s["k_means"], off=s["k_off"])
-        avits.avits_block_select(s["q_means"], s["k_means"], c["keep"], s["mask"], q_lead=q_lead, k_lead=k_lead,
-                                 workspace=s["ws"], **off)
+        avits.avits_block_select(s["q_means"], s["k_means"], c["keep"], s["mask"], q_lead=q_lead, k_lead=k_lead, **off)
         return s["mask"]
     if kind == "attend":
         avits.avits_sparse_attention(s["q"], s["k"], s["v"], s["o"], mask=s["mask"], lse=s["lse"], workspace=s["ws"], **off)
