@@ -8,7 +8,7 @@ A case is a dict of plain values; its "kind" names the operator:
               of the two gains (avits_qk_norm_rope_backward)
   select      which key blocks each query block attends to: the blocks' means,
               their products, the best of them (avits_block_means for queries and
-              keys, avits_block_select)
+              keys, avits_block_select); the means come back too
   attend      attention over the chosen blocks with its log-sum-exps
               (avits_sparse_attention)
   attend_bwd  its backward: the gradients of queries, keys and values
@@ -176,7 +176,7 @@ def prepare(case, seed):
     if kind == "select":
         return dict(s, q_means=empty(sum(nq), H, d, dtype=torch.float64), k_means=empty(sum(nk), Hk, d, dtype=torch.float64),
                     mask=empty(H, sum(nq), words, dtype=torch.int64))
-    s["mask"] = _choose(s)
+    s["mask"] = _select(s)[2]
     s["ws"] = empty(1 << 30, dtype=torch.uint8)
     if kind == "attend":
         return dict(s, o=empty(M, H, d), lse=empty(H, M, dtype=torch.float32))
@@ -215,15 +215,19 @@ def _means(x, off, size):
     return torch.stack([x[i:min(i + size, b)].mean(0) for a, b in zip(off, off[1:]) for i in range(a, b, size)])
 
 
-def _choose(s):
+def _select(s):
+    qm, km = _means(s["q"], s["q_off"], QB), _means(s["k"], s["k_off"], KB)
+    return qm, km, _choose(s, qm, km)
+
+
+def _choose(s, qm, km):
     """The mask words from the blocks' means."""
     c = s["case"]
     g = c["H"] // c["Hk"]
     q_off, k_off = s["q_off"], s["k_off"]
     (q0, nq), (k0, nk) = _blocks(q_off, QB), _blocks(k_off, KB)
     words = (max(nk) + 63) // 64
-    qm = _means(s["q"], q_off, QB).transpose(0, 1)
-    km = _means(s["k"], k_off, KB).transpose(0, 1).repeat_interleave(g, 0)
+    qm, km = qm.transpose(0, 1), km.transpose(0, 1).repeat_interleave(g, 0)
     q_lead, k_lead = _lead(c)
     out = torch.zeros(c["H"], sum(nq), words, dtype=torch.int64, device="cuda")
     for b in range(c["B"]):
@@ -296,7 +300,7 @@ def _attend_bwd(s):
 def _plain(s):
     c, kind = s["case"], s["case"]["kind"]
     if kind == "select":
-        return _choose(s)
+        return _select(s)
     if kind == "attend":
         return _attend(s)
     if kind == "attend_bwd":
@@ -339,7 +343,7 @@ def _own(s):
         avits.avits_block_means(s["q"], QB, s["q_means"], off=s["q_off"])
         avits.avits_block_means(s["k"], KB, s["k_means"], off=s["k_off"])
         avits.avits_block_select(s["q_means"], s["k_means"], c["keep"], s["mask"], q_lead=q_lead, k_lead=k_lead, **off)
-        return s["mask"]
+        return s["q_means"], s["k_means"], s["mask"]
     if kind == "attend":
         avits.avits_sparse_attention(s["q"], s["k"], s["v"], s["o"], mask=s["mask"], lse=s["lse"], workspace=s["ws"], **off)
         return s["o"], s["lse"]
@@ -374,7 +378,8 @@ def work(case):
         scores += (m + QB - 1) // QB * nk
         choice += (m + QB - 1) // QB * ((nk + 63) // 64)
     if kind == "select":
-        return {"bytes": (M * H + N * Hk) * d * z + 8 * H * choice, "flops": (M * H + N * Hk) * d + 2 * H * scores * d}
+        blocks = [sum(_blocks(off, size)[1]) for off, size in ((q_off, QB), (k_off, KB))]
+        return {"bytes": (M * H + N * Hk) * d * z + 8 * (blocks[0] * H + blocks[1] * Hk) * d + 8 * H * choice, "flops": (M * H + N * Hk) * d + 2 * H * scores * d}
     if kind == "attend":
         return {"bytes": (2 * M * H + 2 * kept * Hk) * d * z + 4 * H * M + 8 * H * choice, "flops": 4 * H * pairs * d}
     return {"bytes": (4 * M * H + 2 * kept * Hk + 2 * N * Hk) * d * z + 4 * H * M + 8 * H * choice, "flops": 10 * H * pairs * d}
@@ -428,6 +433,8 @@ def _exact_select(s):
     q_lead, k_lead = _lead(c)
     words = (max(nk) + 63) // 64
     out = torch.zeros(c["H"], sum(nq), words, dtype=torch.int64)
+    q_means = torch.zeros(sum(nq), c["H"], c["d"], dtype=torch.float64, device="cuda")
+    k_means = torch.zeros(sum(nk), c["Hk"], c["d"], dtype=torch.float64, device="cuda")
     for b, h, hk, qr, kr in _parts(s):
         def mean(x, size):
             n = x.shape[0]
@@ -439,14 +446,16 @@ def _exact_select(s):
             return full.view(blocks, size, -1).sum(1) / count
         if kr.stop == kr.start:
             continue
-        score = (mean(s["q"][qr, h], QB) @ mean(s["k"][kr, hk], KB).t()).cpu()
+        q_means[q0[b]:q0[b] + nq[b], h] = mean(s["q"][qr, h], QB)
+        k_means[k0[b]:k0[b] + nk[b], hk] = mean(s["k"][kr, hk], KB)
+        score = (q_means[q0[b]:q0[b] + nq[b], h] @ k_means[k0[b]:k0[b] + nk[b], hk].t()).cpu()
         first = min(nk[b], -(-k_lead // KB))
         for i in range(nq[b]):
             rest = sorted(range(first, nk[b]), key=lambda j: (-score[i, j].item(), j))[:c["keep"]] if i * QB >= q_lead else range(first, nk[b])
             for w in range(words):
                 bits = sum(1 << (j - 64 * w) for j in (*range(first), *rest) if j // 64 == w)
                 out[h, q0[b] + i, w] = bits - (1 << 64) if bits >> 63 else bits
-    return out.cuda()
+    return q_means, k_means, out.cuda()
 
 
 def _exact_attend(s):
