@@ -775,6 +775,135 @@ int avits_mxfp4_linear_backward(const void* dy, int64_t M, int64_t N, const uint
                                 void* stream);
 
 /* ------------------------------------------------------------------------
+ * The attention half of a block by its parts: norm and rotation of queries and
+ * keys, a choice of key blocks by a cheap score, attention over the chosen
+ * blocks, and the backward passes.  With the block's own formulas (the block
+ * of avits_block_forward) these are its attention where every key block is kept.
+ *
+ * Rows hold heads side by side: element e of head h of row r lies at
+ * p + r * ld + h * d + e, so that queries, keys and values may be columns of
+ * one projection's rows, and their gradients columns of its gradient.  d in {64, 128}.
+ * H query heads share Hk key heads (H a multiple of Hk, at most 1024): query
+ * head h reads key head h / (H / Hk), whose gradients are the sums over its
+ * query heads.  dtype as everywhere; sums and statistics are fp32 (64 bits where it
+ * says so), in an order that depends on the sizes only.
+ *
+ * avits_qk_norm_rope — for each head x of q [M, H, d] and k [M, Hk, d]:
+ *   y = x / sqrt(avg(x^2) + eps) * g        (g_q or g_k [d], NULL: 1)
+ * then each pair (a, b) of y's first `rot` elements, turned by its angle t:
+ *   (a cos t - b sin t, a sin t + b cos t), t = pos[row][axis] pos_scale freq[pair].
+ * eps == 0 leaves the norm out (no gains then), rope == NULL or no rotated
+ * elements the rotation.  Pair m of rot / 2 is elements (2 m, 2 m + 1)
+ * (AVITS_ROPE_PAIRS) or (m, m + rot / 2) (AVITS_ROPE_HALVES); the first dims[0] / 2
+ * pairs turn with axis 0, the next dims[1] / 2 with axis 1, ...; rot = sum of dims <=
+ * d.  Angles are taken in 64 bits.  Either of q and k may be absent (0 heads).
+ * avits_qk_norm_rope_backward — from the gradients of the turned rows, the
+ * gradients dq, dk of q and k as they went in (which it reads; not without a norm), and dg_q, dg_k
+ * [d] fp32 (each may be NULL: not made), the sums over rows and heads.  The workspace is
+ * needed for dg_q or dg_k only.  M == 0 zeroes these.
+ * Outputs may be the inputs of the same rows (q_out = q; dq = dq_out or q) with the same stride;
+ * no other overlap.  Pointers aligned to their element (rows on 16 bytes, and rot a
+ * multiple of 8 in halves, are faster).  0 <= M < 2^31, row strides at least heads * d, below 2^31.
+ * avits_rope_frequencies — fills a HOST array: for each axis theta^(-2 m / dims[axis]),
+ * m < dims[axis] / 2, for longer contexts divided by `factor`; with trained > 0 only the
+ * pairs that turn fewer than `low` times over `trained` positions are divided, those that turn
+ * more than `high` times stay, the ones between are mixed linearly in their turns.
+ * ---------------------------------------------------------------------- */
+enum { AVITS_ROPE_PAIRS = 0, AVITS_ROPE_HALVES = 1 };
+
+typedef struct avits_rope {
+  const int32_t* pos;  /* [M, axes] device */
+  const double* freq;  /* [rot / 2] device: radians to a position */
+  double pos_scale;
+  int32_t layout;      /* AVITS_ROPE_PAIRS or AVITS_ROPE_HALVES */
+  int32_t axes;        /* 1 to 4 */
+  int32_t dims[4];     /* rotated elements of each axis, even */
+} avits_rope;
+
+int avits_rope_frequencies(int32_t axes, const int32_t* dims, double theta, double factor, int64_t trained,
+                           double low, double high, double* freq);
+int avits_qk_norm_rope(const void* q, int64_t q_ld, const void* k, int64_t k_ld, int64_t M, int32_t H,
+                       int32_t Hk, int32_t d, const void* g_q, const void* g_k, float eps,
+                       const avits_rope* rope, int dtype, void* q_out, int64_t qo_ld, void* k_out,
+                       int64_t ko_ld, void* stream);
+size_t avits_qk_norm_rope_backward_workspace_bytes(int64_t M, int32_t H, int32_t Hk, int32_t d);
+int avits_qk_norm_rope_backward(const void* dq_out, int64_t dqo_ld, const void* dk_out, int64_t dko_ld,
+                                const void* q, int64_t q_ld, const void* k, int64_t k_ld, int64_t M,
+                                int32_t H, int32_t Hk, int32_t d, const void* g_q, const void* g_k, float eps,
+                                const avits_rope* rope, int dtype, void* dq, int64_t dq_ld, void* dk,
+                                int64_t dk_ld, float* dg_q, float* dg_k, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Sequences and blocks.  B sequences (1 <= B <= 16) lie one after another:
+ * sequence b's queries are rows [q_off[b], q_off[b+1]), its keys and values
+ * rows [k_off[b], k_off[b+1]); host arrays of B + 1 entries that rise from 0 to at
+ * most M (N) (a sequence may have no rows), or NULL with B == 1 for all rows.  Rows
+ * behind the last sequence are neither read nor written.  Each sequence is cut, from
+ * its own first row, into query blocks of AVITS_Q_BLOCK rows and key blocks of
+ * AVITS_K_BLOCK, the last of each shorter where its rows end; blocks are counted through
+ * all sequences.
+ * A mask says which key blocks of its sequence each query block attends to: bit j % 64 of
+ * word mask[h][i][j / 64] (uint64, [H, query blocks, words]) for key block j of
+ * query block i's sequence; bits past its last key block are not looked at.  A mask may
+ * come from avits_block_select or anywhere else.
+ *
+ * avits_block_means — means [blocks, H, d] in 64 bits of the rows of x [M, H, d],
+ * block = AVITS_Q_BLOCK or AVITS_K_BLOCK rows to a block.
+ * avits_block_select — the mask from the means of queries and keys (Section 3.3's selection, at
+ * the grain of blocks): a query block keeps every key block that holds one of its sequence's
+ * first k_lead rows (the text), and the `keep` others (all if fewer) with the largest
+ * q_means . k_means; a query block that holds one of its sequence's first q_lead rows keeps all.
+ * Scores are in 64 bits; among equal ones the lowest block wins; NaN ranks below every
+ * number.  Bits past a sequence's last key block are 0.  At most 16384 key blocks to a sequence.
+ * ---------------------------------------------------------------------- */
+#define AVITS_Q_BLOCK 128
+#define AVITS_K_BLOCK 64
+
+int avits_block_means(const void* x, int64_t ld, int64_t M, int32_t H, int32_t d, int32_t block, int32_t B,
+                      const int64_t* off, int dtype, double* means, void* stream);
+int avits_block_select(const double* q_means, const double* k_means, int64_t M, int64_t N, int32_t B,
+                       const int64_t* q_off, const int64_t* k_off, int32_t H, int32_t Hk, int32_t d,
+                       int64_t q_lead, int64_t k_lead, int64_t keep, uint64_t* mask, int64_t words,
+                       void* stream);
+
+/* ------------------------------------------------------------------------
+ * avits_sparse_attention — for each query row i of head h, over the keys j of the blocks
+ * that its block keeps (mask NULL: all of its sequence's):
+ *   s_ij = scale q_i . k_j,  lse[h, i] = log sum_j exp s_ij,
+ *   o_i = sum_j exp(s_ij - lse[h, i]) v_j
+ * A row without keys gets o = 0 and lse = -inf.  lse [H, M] fp32 or NULL.
+ * avits_sparse_attention_backward — from dout, the forward's inputs, o and lse:
+ *   p_ij = exp(s_ij - lse_i),  ds_ij = p_ij (dout_i . v_j - dout_i . o_i)
+ *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i
+ * (zeros where nothing is kept).  bf16: probabilities, and ds, are rounded to
+ * bf16 before they are multiplied by v, k, q or dout; a masked block is never read.
+ * Rows on 16 bytes with strides of whole 16 bytes, from heads * d to 2^24 elements; outputs
+ * overlap nothing.  0 <= M, N < 2^31 - 4096.  scale > 0 and finite.
+ * Errors: AVITS_ERR_INVALID_ARG, AVITS_ERR_UNSUPPORTED (dtype, d, key blocks),
+ * AVITS_ERR_WORKSPACE.
+ * ---------------------------------------------------------------------- */
+typedef struct avits_rows {
+  void* p;     /* device */
+  int64_t ld;  /* elements from a row to the next */
+} avits_rows;
+
+size_t avits_sparse_attention_workspace_bytes(int64_t M, int64_t N, int32_t B, int32_t H, int32_t d, int dtype);
+int avits_sparse_attention(const avits_rows* q, const avits_rows* k, const avits_rows* v, int64_t M, int64_t N,
+                           int32_t B, const int64_t* q_off, const int64_t* k_off, int32_t H, int32_t Hk,
+                           int32_t d, const uint64_t* mask, int64_t words, float scale, int dtype,
+                           const avits_rows* o, float* lse, void* workspace, size_t workspace_bytes,
+                           void* stream);
+size_t avits_sparse_attention_backward_workspace_bytes(int64_t M, int64_t N, int32_t B, int32_t H, int32_t Hk,
+                                                       int32_t d, int dtype);
+int avits_sparse_attention_backward(const avits_rows* dout, const avits_rows* q, const avits_rows* k,
+                                    const avits_rows* v, const avits_rows* o, const float* lse, int64_t M,
+                                    int64_t N, int32_t B, const int64_t* q_off, const int64_t* k_off, int32_t H,
+                                    int32_t Hk, int32_t d, const uint64_t* mask, int64_t words, float scale,
+                                    int dtype, const avits_rows* dq, const avits_rows* dk, const avits_rows* dv,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Launch timing (instrumentation for benchmarks; not part of the method).
  * While enabled, every kernel the library enqueues is bracketed by a pair of
  * HIP events on the caller's stream.  avits_timing_read() waits for the
@@ -791,7 +920,9 @@ int avits_mxfp4_linear_backward(const void* dy, int64_t M, int64_t N, const uint
  * split sums), and of
  * avits_mxfp4_linear_backward "mxfp4_transpose" (the weight turned round) and
  * "mxfp4_backward" (its product; the reduction of a split one is
- * "splitk_reduce"); "gemm" returns the sum of the six GEMM families (the GEMM
+ * "splitk_reduce"), "qk_norm_rope", "qk_norm_rope_backward" (its sums too), "block_means",
+ * "block_select", "sparse_attention" (with the join of split rows) and
+ * "sparse_attention_backward" (all its launches); "gemm" returns the sum of the six GEMM families (the GEMM
  * kernels alone: the split-K
  * reduction that follows a split launch is "splitk_reduce").  Unknown
  * family -> AVITS_ERR_INVALID_ARG.

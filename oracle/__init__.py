@@ -30,6 +30,10 @@ from .lowbit import (  # noqa: F401
     E2M1, E4M3, nearest_code, block_exponents, hold, held_values, mx_pack, mx_unpack, ckpt_scales,
     norm_forward, norm_backward, gelu_slope,
 )
+from .attend import (  # noqa: F401
+    rope_turns, pair_index, turn, norm_turn, norm_turn_backward, cut, block_means, block_select, words, allowed,
+    sparse_attention, sparse_attention_backward,
+)
 from .sampler import linear, final_layer, euler_update, euler_integrate  # noqa: F401
 from .noise import (  # noqa: F401
     philox4x32_10, box_muller, pixel_noise_bits, pixel_noise, block_noise, halfunit_noise, reinject,

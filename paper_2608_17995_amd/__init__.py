@@ -30,5 +30,10 @@ from ._binding import (  # noqa: F401
     avits_mxfp4_scale_bytes, avits_mxfp4_scale_shape, avits_mxfp4_quantize, avits_mxfp4_dequantize,
     avits_mxfp4_linear_workspace_bytes, avits_mxfp4_linear, avits_mxfp4_linear_backward_workspace_bytes,
     avits_mxfp4_linear_backward,
+    ROPE_PAIRS, ROPE_HALVES, Q_BLOCK, K_BLOCK, avits_rope_frequencies,
+    avits_qk_norm_rope, avits_qk_norm_rope_backward_workspace_bytes, avits_qk_norm_rope_backward,
+    avits_block_means, avits_block_select,
+    avits_sparse_attention_workspace_bytes, avits_sparse_attention,
+    avits_sparse_attention_backward_workspace_bytes, avits_sparse_attention_backward,
     avits_timing_enable, avits_timing_reset, avits_timing_read,
 )

@@ -11,6 +11,8 @@ F32, BF16 = 0, 1
 UP_NEAREST, UP_BILINEAR = 0, 1
 BLOCK_DOUBLE, BLOCK_SINGLE = 0, 1
 ACT_NONE, ACT_GELU = 0, 1
+ROPE_PAIRS, ROPE_HALVES = 0, 1
+Q_BLOCK, K_BLOCK = 128, 64
 
 _c_void_p, _i64, _i32, _f32, _size = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
 
@@ -40,6 +42,15 @@ class _BlockOutputs(ctypes.Structure):
 class _BlockWeights(ctypes.Structure):
     _fields_ = [("kind", _i32), ("mlp_hidden", _i32), ("txt", _DoubleStream), ("img", _DoubleStream),
                 ("single", _Single)]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("pos", _c_void_p), ("freq", _c_void_p), ("pos_scale", ctypes.c_double), ("layout", _i32), ("axes", _i32),
+                ("dims", _i32 * 4)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("p", _c_void_p), ("ld", _i64)]
 
 
 _SIGS = {
@@ -138,6 +149,28 @@ _SIGS = {
     "avits_mxfp4_linear_backward_workspace_bytes": (_size, [_i64, _i64, _i64, ctypes.c_int]),
     "avits_mxfp4_linear_backward": (ctypes.c_int, [_c_void_p, _i64, _i64, _c_void_p, _c_void_p, _i64, ctypes.c_int,
                                                    _c_void_p, _c_void_p, _size, _c_void_p]),
+    "avits_rope_frequencies": (ctypes.c_int, [_i32, _c_void_p, ctypes.c_double, ctypes.c_double, _i64, ctypes.c_double,
+                                              ctypes.c_double, _c_void_p]),
+    "avits_qk_norm_rope": (ctypes.c_int, [_c_void_p, _i64, _c_void_p, _i64, _i64, _i32, _i32, _i32, _c_void_p, _c_void_p,
+                                          _f32, _c_void_p, ctypes.c_int, _c_void_p, _i64, _c_void_p, _i64, _c_void_p]),
+    "avits_qk_norm_rope_backward_workspace_bytes": (_size, [_i64, _i32, _i32, _i32]),
+    "avits_qk_norm_rope_backward": (ctypes.c_int, [_c_void_p, _i64, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _i64,
+                                                   _i64, _i32, _i32, _i32, _c_void_p, _c_void_p, _f32, _c_void_p,
+                                                   ctypes.c_int, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _c_void_p,
+                                                   _c_void_p, _size, _c_void_p]),
+    "avits_block_means": (ctypes.c_int, [_c_void_p, _i64, _i64, _i32, _i32, _i32, _i32, _c_void_p, ctypes.c_int,
+                                         _c_void_p, _c_void_p]),
+    "avits_block_select": (ctypes.c_int, [_c_void_p, _c_void_p, _i64, _i64, _i32, _c_void_p, _c_void_p, _i32, _i32, _i32,
+                                          _i64, _i64, _i64, _c_void_p, _i64, _c_void_p]),
+    "avits_sparse_attention_workspace_bytes": (_size, [_i64, _i64, _i32, _i32, _i32, ctypes.c_int]),
+    "avits_sparse_attention": (ctypes.c_int, [_c_void_p, _c_void_p, _c_void_p, _i64, _i64, _i32, _c_void_p, _c_void_p,
+                                              _i32, _i32, _i32, _c_void_p, _i64, _f32, ctypes.c_int, _c_void_p, _c_void_p,
+                                              _c_void_p, _size, _c_void_p]),
+    "avits_sparse_attention_backward_workspace_bytes": (_size, [_i64, _i64, _i32, _i32, _i32, _i32, ctypes.c_int]),
+    "avits_sparse_attention_backward": (ctypes.c_int, [_c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p,
+                                                       _i64, _i64, _i32, _c_void_p, _c_void_p, _i32, _i32, _i32, _c_void_p,
+                                                       _i64, _f32, ctypes.c_int, _c_void_p, _c_void_p, _c_void_p, _c_void_p,
+                                                       _size, _c_void_p]),
     "avits_timing_enable": (ctypes.c_int, [ctypes.c_int]),
     "avits_timing_reset": (None, []),
     "avits_timing_read": (ctypes.c_int, [ctypes.c_char_p, ctypes.POINTER(ctypes.c_double),
@@ -790,6 +823,236 @@ def avits_mxfp4_linear_backward(dy, wq, ws, dx, workspace=None, stream=None):
     if rc:
         _check(rc)
     return dx
+
+
+# ---------------------------------------------------------------------------
+# The attention half of a block by its parts.
+
+def _heads(t, name, dtype, dev, rows=None, heads=None, d=None):
+    """Pointer and row stride of heads [rows, heads, d] that lie side by side in
+    rows any number of elements apart (columns of a projection's rows, say)."""
+    shape = t.shape
+    if len(shape) != 3 or (rows is not None and shape != (rows, heads, d)):
+        raise ValueError(f"{name}: expected {'[rows, heads, d]' if rows is None else (rows, heads, d)}, got {tuple(shape)}")
+    ld, step, unit = t.stride()
+    n, m = shape[1], shape[2]
+    if (t.dtype is not dtype or t.get_device() != dev or (unit != 1 and m > 1) or (step != m and n > 1) or
+            (ld < n * m and shape[0] > 1)):
+        raise AvitsError(-1, f"{name} must be a {dtype} tensor on the current GPU with its heads side by side, got {t.dtype} "
+                             f"on {t.device}, strides {t.stride()}")
+    return t.data_ptr(), (ld if shape[0] > 1 else n * m)
+
+
+def avits_rope_frequencies(dims, theta=10000.0, factor=1.0, trained=0, low=1.0, high=32.0):
+    """The turns' frequencies, a float64 tensor [sum(dims) / 2] on the host: for each axis
+    theta^(-2 m / dims[axis]); positions interpolated by `factor`, with trained > 0
+    only those of the pairs that turn fewer than `high` times over `trained` positions (fewer than
+    `low`: wholly)."""
+    import torch
+    out = torch.empty(sum(dims) // 2, dtype=torch.float64)
+    _check(load().avits_rope_frequencies(len(dims), (_i32 * len(dims))(*dims), theta, factor, trained, low, high,
+                                         out.data_ptr() if out.numel() else ctypes.addressof(ctypes.c_double())))
+    return out
+
+
+def _rope(what, pos, freq, dims, pos_scale, layout, M, dev):
+    """The rotation's struct (None: none), and what has to outlive the call."""
+    if pos is None and freq is None and dims is None:
+        return None
+    if pos is None or freq is None:
+        raise ValueError(f"{what}: a rotation needs both pos and freq")
+    import torch
+    if pos.dim() == 1:
+        pos = pos[:, None]
+    axes = pos.shape[1]
+    if dims is None:
+        dims = (2 * freq.numel(),)
+    if len(dims) != axes or not 1 <= axes <= 4 or sum(dims) != 2 * freq.numel():
+        raise ValueError(f"{what}: pos [M, {axes}] and {freq.numel()} frequencies need dims of {axes} axes (1 to 4) that sum to "
+                         f"{2 * freq.numel()}, got {tuple(dims)}")
+    return _Rope(_arg(pos, "pos", torch.int32, dev, M, axes), _arg(freq, "freq", torch.float64, dev, freq.numel()), pos_scale,
+                 layout, axes, (_i32 * 4)(*dims))
+
+
+def _qk(what, q, k):
+    """Rows, heads of each and head dim of the queries and keys (either may be None)."""
+    if q is None and k is None:
+        raise ValueError(f"{what}: neither q nor k")
+    one = q if q is not None else k
+    if one.dim() != 3:
+        raise ValueError(f"{what}: rows must be [M, heads, d], got {tuple(one.shape)}")
+    M, _, d = one.shape
+    return M, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], d
+
+
+def avits_qk_norm_rope(q, k, q_out, k_out, g_q=None, g_k=None, eps=1e-6, pos=None, freq=None, dims=None, pos_scale=1.0,
+                       layout=ROPE_PAIRS, stream=None):
+    """RMS norm (eps 0: none) with the gains g_q, g_k [d] and rotation of q [M, H, d]
+    and k [M, Hk, d] to q_out, k_out (which may be q and k; k and k_out, or q and q_out, may be None).
+    pos [M, axes] int32 and freq [rot / 2] float64 (avits_rope_frequencies) on the GPU;
+    dims: the rotated elements of each axis."""
+    M, H, Hk, d = _qk("avits_qk_norm_rope", q, k)
+    one = q if q is not None else k
+    (code, dev), dt = _code(one), one.dtype
+    rope = _rope("avits_qk_norm_rope", pos, freq, dims, pos_scale, layout, M, dev)
+    qp, kp, qo, ko = ((None, 0) if n == 0 else _heads(t, name, dt, dev, M, n, d) for t, name, n in
+                      ((q, "q", H), (k, "k", Hk), (q_out, "q_out", H), (k_out, "k_out", Hk)))
+    rc = (_LIB or load()).avits_qk_norm_rope(*qp, *kp, M, H, Hk, d, _arg(g_q, "g_q", dt, dev, d), _arg(g_k, "g_k", dt, dev, d), eps,
+                                             None if rope is None else ctypes.addressof(rope), code, *qo, *ko,
+                                             _device_stream(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return q_out, k_out
+
+
+def avits_qk_norm_rope_backward_workspace_bytes(M: int, H: int, Hk: int, d: int) -> int:
+    return load().avits_qk_norm_rope_backward_workspace_bytes(M, H, Hk, d)
+
+
+def avits_qk_norm_rope_backward(dq_out, dk_out, q, k, dq, dk, dg_q=None, dg_k=None, g_q=None, g_k=None, eps=1e-6, pos=None,
+                                freq=None, dims=None, pos_scale=1.0, layout=ROPE_PAIRS, workspace=None, stream=None):
+    """dq, dk (and dg_q, dg_k [d] fp32 where asked for) of avits_qk_norm_rope from
+    dq_out, dk_out and the q and k that went in (not looked at with eps 0)."""
+    what = "avits_qk_norm_rope_backward"
+    M, H, Hk, d = _qk(what, dq_out, dk_out)
+    one = dq_out if dq_out is not None else dk_out
+    (code, dev), dt, f32 = _code(one), one.dtype, _TYPES["f32"]
+    rope = _rope(what, pos, freq, dims, pos_scale, layout, M, dev)
+    norm = eps > 0
+    gq, gk, qp, kp, dqp, dkp = ((None, 0) if n == 0 else _heads(t, name, dt, dev, M, n, d) for t, name, n in
+                                ((dq_out, "dq_out", H), (dk_out, "dk_out", Hk), (q, "q", H if norm else 0),
+                                 (k, "k", Hk if norm else 0), (dq, "dq", H), (dk, "dk", Hk)))
+    wsp, wsb = None, 0
+    if dg_q is not None or dg_k is not None:
+        ws, wsp, wsb = _scratch(workspace, lambda: avits_qk_norm_rope_backward_workspace_bytes(M, H, Hk, d), dev, stream)
+    rc = (_LIB or load()).avits_qk_norm_rope_backward(
+        *gq, *gk, *qp, *kp, M, H, Hk, d, _arg(g_q, "g_q", dt, dev, d), _arg(g_k, "g_k", dt, dev, d), eps,
+        None if rope is None else ctypes.addressof(rope), code, *dqp, *dkp, _arg(dg_q, "dg_q", f32, dev, d),
+        _arg(dg_k, "dg_k", f32, dev, d), wsp, wsb, _device_stream(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return dq, dk, dg_q, dg_k
+
+
+def _sequences(off, rows, what):
+    """Number of sequences, the host array of their offsets (None: one of all rows) and the offsets."""
+    if off is None:
+        return 1, None, (0, rows)
+    n = len(off) - 1
+    if n < 1:
+        raise ValueError(f"{what}: offsets need at least two entries")
+    return n, (_i64 * (n + 1))(*off), off
+
+
+def _block_count(off, block):
+    return sum((b - a + block - 1) // block for a, b in zip(off, off[1:]))
+
+
+def avits_block_means(x, block, means, off=None, stream=None):
+    """means [blocks, H, d] float64: the mean row of every block (Q_BLOCK or K_BLOCK
+    rows) of x [M, H, d], whose sequences start at the host offsets off."""
+    import torch
+    M, H, d = x.shape
+    code, dev = _code(x)
+    n, offs, host = _sequences(off, M, "avits_block_means")
+    rc = (_LIB or load()).avits_block_means(*_heads(x, "x", x.dtype, dev), M, H, d, block, n, offs, code,
+                                            _arg(means, "means", torch.float64, dev, _block_count(host, max(block, 1)), H, d),
+                                            _device_stream(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return means
+
+
+def avits_block_select(q_means, k_means, keep, mask, q_lead=0, k_lead=0, q_off=None, k_off=None, stream=None):
+    """mask [H, query blocks, words] int64: which key blocks each query block attends to,
+    bit j % 64 of word j / 64 for its sequence's key block j: those that hold one of the
+    first k_lead rows and the `keep` others of the largest q_means . k_means; all
+    for the query blocks that hold one of the first q_lead rows."""
+    import torch
+    f64 = torch.float64
+    nq, H, d = q_means.shape
+    nk, Hk, _ = k_means.shape
+    dev = _current_device()
+    # Without offsets, one sequence of whole blocks.
+    B, qo, hq = _sequences(q_off, nq * Q_BLOCK, "avits_block_select")
+    Bk, ko, hk = _sequences(k_off, nk * K_BLOCK, "avits_block_select")
+    if B != Bk or _block_count(hq, Q_BLOCK) != nq or _block_count(hk, K_BLOCK) != nk:
+        raise ValueError(f"avits_block_select: {nq} and {nk} means do not match the offsets {hq} and {hk}")
+    words = mask.shape[-1]
+    rc = (_LIB or load()).avits_block_select(_arg(q_means, "q_means", f64, dev, nq, H, d), _arg(k_means, "k_means", f64, dev, nk, Hk, d),
+                                             hq[-1], hk[-1], B, qo, ko, H, Hk, d, q_lead, k_lead, keep,
+                                             _arg(mask, "mask", torch.int64, dev, H, nq, words), words,
+                                             _device_stream(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return mask
+
+
+def _rows(t, name, dtype, dev, rows, heads, d):
+    return _Rows(*_heads(t, name, dtype, dev, rows, heads, d))
+
+
+def _sparse(what, q, k, v, mask, q_off, k_off, scale, dt, dev):
+    """Sizes, sequences and the mask's pointer, as the calls take them."""
+    import torch
+    M, H, d = q.shape
+    N, Hk, _ = k.shape
+    B, qo, hq = _sequences(q_off, M, what)
+    if k_off is None and q_off is not None and M == N:
+        k_off = q_off
+    Bk, ko, hk = _sequences(k_off, N, what)
+    if B != Bk:
+        raise ValueError(f"{what}: {B} sequences of queries, {Bk} of keys")
+    words = 0 if mask is None else mask.shape[-1]
+    if mask is not None and any(64 * words * K_BLOCK < b - a for a, b in zip(hk, hk[1:])):
+        raise ValueError(f"{what}: {words} words a row do not reach the keys of every sequence")
+    mp = None if mask is None else _arg(mask, "mask", torch.int64, dev, H, _block_count(hq, Q_BLOCK), words)
+    return (M, N, B, H, Hk, d), (qo, ko), (mp, words, d ** -0.5 if scale is None else scale)
+
+
+def avits_sparse_attention_workspace_bytes(M: int, N: int, B: int, H: int, d: int, dtype: int) -> int:
+    return load().avits_sparse_attention_workspace_bytes(M, N, B, H, d, dtype)
+
+
+def avits_sparse_attention(q, k, v, o, mask=None, lse=None, q_off=None, k_off=None, scale=None, workspace=None, stream=None):
+    """o [M, H, d], and lse [H, M] fp32 where asked for: attention of q [M, H, d] over the
+    keys k, v [N, Hk, d] of the blocks in mask (None: all), scale d^-1/2 unless given.  q_off, k_off:
+    host offsets of packed sequences (k_off: q_off where M == N)."""
+    (code, dev), dt = _code(q), q.dtype
+    (M, N, B, H, Hk, d), (qo, ko), (mp, words, scale) = _sparse("avits_sparse_attention", q, k, v, mask, q_off, k_off, scale, dt, dev)
+    ref = ctypes.byref
+    qr, kr, vr = _rows(q, "q", dt, dev, M, H, d), _rows(k, "k", dt, dev, N, Hk, d), _rows(v, "v", dt, dev, N, Hk, d)
+    out = _rows(o, "o", dt, dev, M, H, d)
+    ws, wsp, wsb = _scratch(workspace, lambda: avits_sparse_attention_workspace_bytes(M, N, B, H, d, code), dev, stream)
+    rc = (_LIB or load()).avits_sparse_attention(ref(qr), ref(kr), ref(vr), M, N, B, qo, ko, H, Hk, d, mp, words, scale, code,
+                                                 ref(out), _arg(lse, "lse", _TYPES["f32"], dev, H, M), wsp, wsb,
+                                                 _device_stream(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return o
+
+
+def avits_sparse_attention_backward_workspace_bytes(M: int, N: int, B: int, H: int, Hk: int, d: int, dtype: int) -> int:
+    return load().avits_sparse_attention_backward_workspace_bytes(M, N, B, H, Hk, d, dtype)
+
+
+def avits_sparse_attention_backward(dout, q, k, v, o, lse, dq, dk, dv, mask=None, q_off=None, k_off=None, scale=None,
+                                    workspace=None, stream=None):
+    """dq [M, H, d], dk and dv [N, Hk, d] of avits_sparse_attention from dout, its inputs, o and lse."""
+    (code, dev), dt = _code(q), q.dtype
+    (M, N, B, H, Hk, d), (qo, ko), (mp, words, scale) = _sparse("avits_sparse_attention_backward", q, k, v, mask, q_off, k_off, scale,
+                                                                dt, dev)
+    ref = ctypes.byref
+    wide = [_rows(t, n, dt, dev, M, H, d) for t, n in ((dout, "dout"), (q, "q"), (o, "o"), (dq, "dq"))]
+    narrow = [_rows(t, n, dt, dev, N, Hk, d) for t, n in ((k, "k"), (v, "v"), (dk, "dk"), (dv, "dv"))]
+    ws, wsp, wsb = _scratch(workspace, lambda: avits_sparse_attention_backward_workspace_bytes(M, N, B, H, Hk, d, code), dev, stream)
+    rc = (_LIB or load()).avits_sparse_attention_backward(
+        ref(wide[0]), ref(wide[1]), ref(narrow[0]), ref(narrow[1]), ref(wide[2]), _arg(lse, "lse", _TYPES["f32"], dev, H, M), M, N, B,
+        qo, ko, H, Hk, d, mp, words, scale, code, ref(wide[3]), ref(narrow[2]), ref(narrow[3]), wsp, wsb,
+        _device_stream(dev) if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+    return dq, dk, dv
 
 
 def avits_timing_enable(on: bool = True):

@@ -20,7 +20,7 @@ LIB = os.path.join(PKG, "libavits.so")
 ARCH = "gfx950"
 
 SOURCES = ("abi.hip", "score.hip", "select.hip", "relayout.hip", "gemm.hip", "attention.hip", "block.hip",
-           "noise.hip", "norm.hip", "lowbit.hip", "mxfp4.hip")
+           "noise.hip", "norm.hip", "lowbit.hip", "mxfp4.hip", "rope.hip", "blocks.hip", "sparse.hip")
 
 CXXFLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",

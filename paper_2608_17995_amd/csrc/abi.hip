@@ -36,7 +36,9 @@ static const char* const kFamilies[] = {"score_spatial", "score_combine", "score
                                         "splitk_reduce", "qk_rope", "attention", "joint_lse",
                                         "gather_mixed", "scatter_mixed", "linear", "final_linear", "euler", "noise",
                                         "layer_norm", "layer_norm_backward", "ckpt8", "gelu_backward", "mxfp4_quantize",
-                                        "mxfp4_dequantize", "mxfp4_linear", "mxfp4_transpose", "mxfp4_backward"};
+                                        "mxfp4_dequantize", "mxfp4_linear", "mxfp4_transpose", "mxfp4_backward",
+                                        "qk_norm_rope", "qk_norm_rope_backward", "block_means", "block_select",
+                                        "sparse_attention", "sparse_attention_backward"};
 constexpr int kNumFamilies = sizeof(kFamilies) / sizeof(kFamilies[0]);
 
 struct Pending {

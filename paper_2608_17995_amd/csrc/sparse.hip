@@ -1,0 +1,435 @@
+// Attention over chosen key blocks and its backward pass: fp32, and the plans,
+// checks and entry points of both types.
+//
+// For a query row i of head h and the keys j of the blocks that its query block keeps:
+//   s_ij = scale q_i . k_j,  lse_i = log sum_j exp s_ij,  o_i = sum_j exp(s_ij - lse_i) v_j
+// and from do, with delta_i = do_i . o_i and p_ij = exp(s_ij - lse_i),
+//   ds_ij = p_ij (do_i . v_j - delta_i),  dq_i = scale sum_j ds_ij k_j,
+//   dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i.
+// A row whose block keeps nothing has o = 0 and lse = -inf.
+//
+// No sum crosses workgroups in a varying order: dq is made by the owners of the
+// query rows, dk and dv by the owners of the key blocks (which walk the mask's
+// columns), at the price of making the probabilities twice.
+#include "sparse_attn.h"
+
+namespace avits {
+namespace {
+
+// ---------------------------------------------------------------------------
+// On v_mfma_f32_16x16x4_f32, whatever the rows' type.  A workgroup owns 64 query rows (half a query
+// block), 16 to a wave; key tiles of 64 rows pass through LDS.  Products are
+// transposed (S^T = K Q^T, O^T = V^T P^T): lane l holds query row l % 16, register r
+// key 4 (l / 16) + r, so the probabilities are the second product's operand as they stand.
+constexpr int kFT = 64;  // rows to a tile
+
+template <typename T>
+__device__ __forceinline__ f32x4 load4(const T* p) {
+  if constexpr (sizeof(T) == 4) {
+    return *reinterpret_cast<const f32x4*>(p);
+  } else {
+    const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+    return f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u), __uint_as_float(w[1] << 16),
+                 __uint_as_float(w[1] & 0xffff0000u)};
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* p, const f32x4& v) {
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(p) = v;
+  else *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3])};
+}
+
+// A tile of rows [row, row + 64) of a head, rows from `end` on as zeros, to LDS.
+template <typename T, int DH>
+__device__ __forceinline__ void load_tile(float* dst, const T* src, int64_t ld, int row, int end) {
+  constexpr int kQ = DH / 4, kP = DH + 4;
+#pragma unroll
+  for (int i = 0; i < kFT * kQ / 256; ++i) {
+    const int e = threadIdx.x + 256 * i, r = e / kQ, c = e % kQ;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (row + r < end) v = load4(src + int64_t(row + r) * ld + 4 * c);
+    *reinterpret_cast<f32x4*>(dst + r * kP + 4 * c) = v;
+  }
+}
+
+// 16 rows' fragments in registers: lane l has row l % 16, elements 16 j + 4 (l / 16) + e.
+template <typename T, int DH>
+__device__ __forceinline__ void load_rows(f32x4* f, const T* src, int64_t ld, int row, int end) {
+  const int lane = threadIdx.x % kWave, r = row + lane % 16;
+#pragma unroll
+  for (int j = 0; j < DH / 16; ++j)
+    f[j] = r < end ? load4(src + int64_t(r) * ld + 16 * j + 4 * (lane / 16)) : f32x4{0.f, 0.f, 0.f, 0.f};
+}
+
+// sum over d of tile[row0 + lane % 16][d] f[d]: 16 rows of an LDS tile against 16 register rows.
+template <int DH>
+__device__ __forceinline__ f32x4 rows_product(const float* tile, int row0, const f32x4* f) {
+  constexpr int kP = DH + 4;
+  const int lane = threadIdx.x % kWave;
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < DH / 16; ++j) {
+    const f32x4 t = *reinterpret_cast<const f32x4*>(tile + (row0 + lane % 16) * kP + 16 * j + 4 * (lane / 16));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s = mfma16x16x4(t[e], f[j][e], s);
+  }
+  return s;
+}
+
+// acc[dt] += tile^T p over the 16 tile rows from row0: p's register r is tile row row0 + 4 (lane / 16) + r.
+template <int DH>
+__device__ __forceinline__ void columns_product(const float* tile, int row0, const f32x4& p, f32x4* acc) {
+  constexpr int kP = DH + 4;
+  const int lane = threadIdx.x % kWave;
+  const float* src = tile + (row0 + 4 * (lane / 16)) * kP + lane % 16;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int dt = 0; dt < DH / 16; ++dt) acc[dt] = mfma16x16x4(src[r * kP + 16 * dt], p[r], acc[dt]);
+}
+
+__device__ __forceinline__ float quad_max(float v) { return max_xor32(fmaxf(v, __shfl_xor(v, 16))); }
+__device__ __forceinline__ float quad_sum(float v) { return sum_xor32(v + __shfl_xor(v, 16)); }
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void sparse_simple_kernel(const SparseArgs a) {
+  constexpr int kP = DH + 4, kD = DH / 16;
+  __shared__ __attribute__((aligned(16))) float kt[kFT * kP], vt[kFT * kP];
+  const int blk = blockIdx.x / 2, h = blockIdx.y, lane = threadIdx.x % kWave;
+  const Seq s = seq_of<false>(a.seq, blk);
+  const int wave = threadIdx.x / kWave, first = s.q_lo + (blk - s.qb) * kQB + 64 * (blockIdx.x % 2);
+  if (first >= s.q_hi) return;
+  const T* K = static_cast<const T*>(a.k) + int64_t(h / a.group) * DH;
+  const T* V = static_cast<const T*>(a.v) + int64_t(h / a.group) * DH;
+  f32x4 q[kD], o[kD];
+  load_rows<T, DH>(q, static_cast<const T*>(a.q) + int64_t(h) * DH, a.q_ld, first + 16 * wave, s.q_hi);
+#pragma unroll
+  for (int j = 0; j < kD; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  BlockWalk walk(a, h, blk, s.nk);
+  for (int j = walk.next(); j >= 0; j = walk.next()) {
+    const int row = s.k_lo + j * kKB;
+    __syncthreads();
+    load_tile<T, DH>(kt, K, a.k_ld, row, s.k_hi);
+    load_tile<T, DH>(vt, V, a.v_ld, row, s.k_hi);
+    __syncthreads();
+    const int n = s.k_hi - row;
+    f32x4 x[4];
+    float mx = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      x[t] = rows_product<DH>(kt, 16 * t, q);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[t][r] = 16 * t + 4 * (lane / 16) + r < n ? x[t][r] * a.scale : -INFINITY;
+        mx = fmaxf(mx, x[t][r]);
+      }
+    }
+    mx = fmaxf(m, quad_max(mx));
+    const float ref = mx == -INFINITY ? 0.f : mx, corr = expf(m - ref);
+    m = mx;
+    l *= corr;
+#pragma unroll
+    for (int d = 0; d < kD; ++d) o[d] *= corr;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[t][r] = expf(x[t][r] - ref);
+        l += x[t][r];
+      }
+      columns_product<DH>(vt, 16 * t, x[t], o);
+    }
+  }
+  l = quad_sum(l);
+  const int row = first + 16 * wave + lane % 16;
+  if (row >= s.q_hi) return;
+  const bool none = walk.total == 0;
+  if (a.lse && lane < 16) a.lse[int64_t(h) * a.M + row] = none ? -INFINITY : m + logf(l);
+  T* dst = static_cast<T*>(a.o) + int64_t(row) * a.o_ld + int64_t(h) * DH + 4 * (lane / 16);
+#pragma unroll
+  for (int d = 0; d < kD; ++d) store4(dst + 16 * d, none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[d] / l);
+}
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void sparse_dq_simple_kernel(const SparseArgs a) {
+  constexpr int kP = DH + 4, kD = DH / 16;
+  __shared__ __attribute__((aligned(16))) float kt[kFT * kP], vt[kFT * kP];
+  const int blk = blockIdx.x / 2, h = blockIdx.y, lane = threadIdx.x % kWave;
+  const Seq s = seq_of<false>(a.seq, blk);
+  const int wave = threadIdx.x / kWave, first = s.q_lo + (blk - s.qb) * kQB + 64 * (blockIdx.x % 2);
+  if (first >= s.q_hi) return;
+  const T* K = static_cast<const T*>(a.k) + int64_t(h / a.group) * DH;
+  const T* V = static_cast<const T*>(a.v) + int64_t(h / a.group) * DH;
+  f32x4 q[kD], g[kD], dq[kD];
+  load_rows<T, DH>(q, static_cast<const T*>(a.q) + int64_t(h) * DH, a.q_ld, first + 16 * wave, s.q_hi);
+  load_rows<T, DH>(g, static_cast<const T*>(a.dout) + int64_t(h) * DH, a.do_ld, first + 16 * wave, s.q_hi);
+#pragma unroll
+  for (int j = 0; j < kD; ++j) dq[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int row = first + 16 * wave + lane % 16;
+  const float lse = row < s.q_hi ? a.lse[int64_t(h) * a.M + row] : INFINITY;
+  const float delta = row < s.q_hi ? a.delta[int64_t(h) * a.M + row] : 0.f;
+  BlockWalk walk(a, h, blk, s.nk);
+  for (int j = walk.next(); j >= 0; j = walk.next()) {
+    const int key = s.k_lo + j * kKB;
+    __syncthreads();
+    load_tile<T, DH>(kt, K, a.k_ld, key, s.k_hi);
+    load_tile<T, DH>(vt, V, a.v_ld, key, s.k_hi);
+    __syncthreads();
+    const int n = s.k_hi - key;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const f32x4 x = rows_product<DH>(kt, 16 * t, q), dp = rows_product<DH>(vt, 16 * t, g);
+      f32x4 ds;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        ds[r] = 16 * t + 4 * (lane / 16) + r < n ? expf(x[r] * a.scale - lse) * (dp[r] - delta) : 0.f;
+      columns_product<DH>(kt, 16 * t, ds, dq);
+    }
+  }
+  if (row >= s.q_hi) return;
+  T* dst = static_cast<T*>(a.dq) + int64_t(row) * a.dq_ld + int64_t(h) * DH + 4 * (lane / 16);
+#pragma unroll
+  for (int d = 0; d < kD; ++d) store4(dst + 16 * d, dq[d] * a.scale);
+}
+
+// dk and dv of a key block: 16 keys to a wave, the query rows that keep the block
+// pass through LDS, 64 at a time.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void sparse_dkv_simple_kernel(const SparseArgs a) {
+  constexpr int kP = DH + 4, kD = DH / 16;
+  __shared__ __attribute__((aligned(16))) float qt[kFT * kP], gt[kFT * kP];
+  __shared__ float ls[kFT], dl[kFT];
+  const int blk = blockIdx.x, hk = blockIdx.y, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const Seq s = seq_of<true>(a.seq, blk);
+  const int first = s.k_lo + (blk - s.kb) * kKB + 16 * wave;
+  f32x4 k[kD], v[kD], dk[kD], dv[kD];
+  load_rows<T, DH>(k, static_cast<const T*>(a.k) + int64_t(hk) * DH, a.k_ld, first, s.k_hi);
+  load_rows<T, DH>(v, static_cast<const T*>(a.v) + int64_t(hk) * DH, a.v_ld, first, s.k_hi);
+#pragma unroll
+  for (int j = 0; j < kD; ++j) dk[j] = dv[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int nq = (s.q_hi - s.q_lo + kQB - 1) / kQB;
+  for (int h = hk * a.group; h < (hk + 1) * a.group; ++h) {
+    const T* Q = static_cast<const T*>(a.q) + int64_t(h) * DH;
+    const T* G = static_cast<const T*>(a.dout) + int64_t(h) * DH;
+    for (int i = 0; i < nq; ++i) {
+      if (!kept(a, h, s.qb + i, blk - s.kb)) continue;
+      for (int row = s.q_lo + i * kQB; row < std::min(s.q_hi, s.q_lo + (i + 1) * kQB); row += kFT) {
+        __syncthreads();
+        load_tile<T, DH>(qt, Q, a.q_ld, row, s.q_hi);
+        load_tile<T, DH>(gt, G, a.do_ld, row, s.q_hi);
+        if (threadIdx.x < kFT) {
+          const int r = row + threadIdx.x;
+          ls[threadIdx.x] = r < s.q_hi ? a.lse[int64_t(h) * a.M + r] : INFINITY;  // rows past the end: no probability
+          dl[threadIdx.x] = r < s.q_hi ? a.delta[int64_t(h) * a.M + r] : 0.f;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const f32x4 x = rows_product<DH>(qt, 16 * t, k), dp = rows_product<DH>(gt, 16 * t, v);
+          f32x4 p, ds;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int e = 16 * t + 4 * (lane / 16) + r;
+            p[r] = expf(x[r] * a.scale - ls[e]);
+            ds[r] = p[r] * (dp[r] - dl[e]);
+          }
+          columns_product<DH>(gt, 16 * t, p, dv);
+          columns_product<DH>(qt, 16 * t, ds, dk);
+        }
+      }
+    }
+  }
+  const int row = first + lane % 16;
+  if (row >= s.k_hi) return;
+  T* pk = static_cast<T*>(a.dk) + int64_t(row) * a.dk_ld + int64_t(hk) * DH + 4 * (lane / 16);
+  T* pv = static_cast<T*>(a.dv) + int64_t(row) * a.dv_ld + int64_t(hk) * DH + 4 * (lane / 16);
+#pragma unroll
+  for (int d = 0; d < kD; ++d) {
+    store4(pk + 16 * d, dk[d] * a.scale);
+    store4(pv + 16 * d, dv[d]);
+  }
+}
+
+// delta = do . o of every row and head: DH / 8 lanes to a head.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void sparse_delta_kernel(const SparseArgs a) {
+  constexpr int kL = DH / 8;
+  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) / kL;
+  const int c = threadIdx.x % kL * 8;
+  const int64_t row = i / a.H, h = i % a.H;
+  if (row >= a.seq.q_row[kMaxSeqs]) return;  // whole groups of lanes leave together
+  const T* g = static_cast<const T*>(a.dout) + row * a.do_ld + h * DH + c;
+  const T* o = static_cast<const T*>(a.o) + row * a.o_ld + h * DH + c;
+  float sum = 0.f;
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int e = 0; e < 8; e += 4) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(g + e), y = *reinterpret_cast<const f32x4*>(o + e);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum += x[r] * y[r];
+    }
+  } else {
+    const u32x4 x = *reinterpret_cast<const u32x4*>(g), y = *reinterpret_cast<const u32x4*>(o);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      sum += __uint_as_float(x[r] << 16) * __uint_as_float(y[r] << 16);
+      sum += __uint_as_float(x[r] & 0xffff0000u) * __uint_as_float(y[r] & 0xffff0000u);
+    }
+  }
+  sum = group_sum(sum, kL);
+  if (c == 0) a.delta[h * a.M + row] = sum;
+}
+
+template <typename T, int DH>
+void forward_simple(const SparseArgs& a, hipStream_t s) {
+  const dim3 grid(2 * unsigned(a.seq.q_blk[a.seq.B]), unsigned(a.H));
+  hipLaunchKernelGGL((sparse_simple_kernel<T, DH>), grid, dim3(256), 0, s, a);
+}
+
+template <typename T, int DH>
+void backward_simple(const SparseArgs& a, hipStream_t s) {
+  const int nq = a.seq.q_blk[a.seq.B], nk = a.seq.k_blk[a.seq.B];
+  if (nq > 0) hipLaunchKernelGGL((sparse_dq_simple_kernel<T, DH>), dim3(2 * unsigned(nq), unsigned(a.H)), dim3(256), 0, s, a);
+  if (nk > 0) hipLaunchKernelGGL((sparse_dkv_simple_kernel<T, DH>), dim3(unsigned(nk), unsigned(a.H / a.group)), dim3(256), 0, s, a);
+}
+
+int fill(SparseArgs& a, const char* what, const avits_rows* q, const avits_rows* k, const avits_rows* v, int64_t M, int64_t N,
+         int32_t B, const int64_t* q_off, const int64_t* k_off, int32_t H, int32_t Hk, int32_t d, const uint64_t* mask, int64_t words,
+         float scale, int dtype) {
+  a = SparseArgs{};
+  const int rc = seq_blocks(a.seq, what, B, q_off, M, k_off, N);
+  if (rc != AVITS_OK) return rc;
+  AVITS_REQUIRE(Hk >= 1 && H >= Hk && H % Hk == 0 && H <= 1024, "%s: H=%d must be a multiple of Hk=%d, at most 1024", what, H, Hk);
+  if (d != 64 && d != 128) return set_error(AVITS_ERR_UNSUPPORTED, "%s: head dim %d (need 64 or 128)", what, d);
+  if (dtype != AVITS_F32 && dtype != AVITS_BF16) return set_error(AVITS_ERR_UNSUPPORTED, "%s: dtype %d unsupported", what, dtype);
+  AVITS_REQUIRE(scale > 0.f && scale < INFINITY, "%s: scale must be positive and finite", what);
+  int nk = 0;
+  for (int b = 0; b < B; ++b) nk = std::max(nk, a.seq.k_blk[b + 1] - a.seq.k_blk[b]);
+  AVITS_REQUIRE(!mask || (words >= (nk + 63) / 64 && words < (int64_t(1) << 20)), "%s: %lld words a row for %d key blocks", what,
+                (long long)words, nk);
+  AVITS_REQUIRE(reinterpret_cast<uintptr_t>(mask) % 8 == 0, "%s: the mask is not aligned to its words", what);
+  AVITS_REQUIRE(q && k && v, "%s: null rows", what);
+  a.q = q->p, a.k = k->p, a.v = v->p;
+  a.q_ld = q->ld, a.k_ld = k->ld, a.v_ld = v->ld;
+  a.mask = mask;
+  a.words = words;
+  a.M = M;
+  a.H = H;
+  a.group = H / Hk;
+  a.d = d;
+  a.scale = scale;
+  a.seq.q_row[kMaxSeqs] = a.seq.q_row[B];
+  a.seq.q_blk[kMaxSeqs] = a.seq.q_blk[B];
+  return AVITS_OK;
+}
+
+// Rows of `heads` heads: there (unless there are none), on 16 bytes and apart.
+int check_rows(const char* what, const char* name, const avits_rows* r, int64_t rows, int64_t heads, int d, int dtype) {
+  if (rows == 0) return AVITS_OK;
+  AVITS_REQUIRE(r && r->p, "%s: null %s", what, name);
+  const int64_t elem = dtype == AVITS_BF16 ? 2 : 4;
+  AVITS_REQUIRE(reinterpret_cast<uintptr_t>(r->p) % 16 == 0 && (rows == 1 || r->ld * elem % 16 == 0),
+                "%s: the rows of %s must lie on 16 bytes (row stride %lld)", what, name, (long long)r->ld);
+  AVITS_REQUIRE(rows == 1 || (r->ld >= heads * d && r->ld < (int64_t(1) << 24)), "%s: row stride %lld of %s (heads * d to 2^24)", what,
+                (long long)r->ld, name);
+  return AVITS_OK;
+}
+
+#define AVITS_ROWS(name, rows, heads)                                                   \
+  do {                                                                                  \
+    const int rc_ = check_rows(what, #name, name, rows, heads, d, dtype);               \
+    if (rc_ != AVITS_OK) return rc_;                                                    \
+  } while (0)
+
+size_t delta_bytes(int64_t M, int32_t H) { return align_up(size_t(M) * size_t(H) * sizeof(float), 256); }
+
+}  // namespace
+}  // namespace avits
+
+using namespace avits;
+
+extern "C" size_t avits_sparse_attention_workspace_bytes(int64_t M, int64_t N, int32_t B, int32_t H, int32_t d, int dtype) {
+  return 0;
+}
+
+extern "C" int avits_sparse_attention(const avits_rows* q, const avits_rows* k, const avits_rows* v, int64_t M, int64_t N, int32_t B,
+                                      const int64_t* q_off, const int64_t* k_off, int32_t H, int32_t Hk, int32_t d,
+                                      const uint64_t* mask, int64_t words, float scale, int dtype, const avits_rows* o, float* lse,
+                                      void* workspace, size_t workspace_bytes, void* stream) {
+  const char* what = "sparse_attention";
+  SparseArgs a;
+  const int rc = fill(a, what, q, k, v, M, N, B, q_off, k_off, H, Hk, d, mask, words, scale, dtype);
+  if (rc != AVITS_OK) return rc;
+  const int64_t m = a.seq.q_row[B], n = a.seq.k_row[B];
+  AVITS_ROWS(q, m, H);
+  AVITS_ROWS(k, n, Hk);
+  AVITS_ROWS(v, n, Hk);
+  AVITS_ROWS(o, m, H);
+  if (m == 0) return AVITS_OK;
+  a.o = o->p;
+  a.o_ld = o->ld;
+  a.lse = lse;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  TimedLaunch timed(what, s);
+  if (dtype == AVITS_F32) d == 128 ? forward_simple<float, 128>(a, s) : forward_simple<float, 64>(a, s);
+  else d == 128 ? forward_simple<bf16_t, 128>(a, s) : forward_simple<bf16_t, 64>(a, s);
+  return launch_status(what);
+}
+
+extern "C" size_t avits_sparse_attention_backward_workspace_bytes(int64_t M, int64_t N, int32_t B, int32_t H, int32_t Hk, int32_t d, int dtype) {
+  if (M < 0 || N < 0 || M >= (int64_t(1) << 31) - 4096 || N >= (int64_t(1) << 31) - 4096 || H < 1 || H > 1024) return 0;
+  return delta_bytes(M, H);
+}
+
+extern "C" int avits_sparse_attention_backward(const avits_rows* dout, const avits_rows* q, const avits_rows* k, const avits_rows* v,
+                                               const avits_rows* o, const float* lse, int64_t M, int64_t N, int32_t B,
+                                               const int64_t* q_off, const int64_t* k_off, int32_t H, int32_t Hk, int32_t d,
+                                               const uint64_t* mask, int64_t words, float scale, int dtype, const avits_rows* dq,
+                                               const avits_rows* dk, const avits_rows* dv, void* workspace, size_t workspace_bytes,
+                                               void* stream) {
+  const char* what = "sparse_attention_backward";
+  SparseArgs a;
+  const int rc = fill(a, what, q, k, v, M, N, B, q_off, k_off, H, Hk, d, mask, words, scale, dtype);
+  if (rc != AVITS_OK) return rc;
+  const int64_t m = a.seq.q_row[B], n = a.seq.k_row[B];
+  AVITS_ROWS(q, m, H);
+  AVITS_ROWS(k, n, Hk);
+  AVITS_ROWS(v, n, Hk);
+  AVITS_ROWS(o, m, H);
+  AVITS_ROWS(dout, m, H);
+  AVITS_ROWS(dq, m, H);
+  AVITS_ROWS(dk, n, Hk);
+  AVITS_ROWS(dv, n, Hk);
+  if (m == 0 && n == 0) return AVITS_OK;
+  AVITS_REQUIRE(lse || m == 0, "%s: null lse", what);
+  const size_t need = avits_sparse_attention_backward_workspace_bytes(M, N, B, H, Hk, d, dtype);
+  if (need > 0 && (!workspace || workspace_bytes < need))
+    return set_error(AVITS_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", what, workspace ? workspace_bytes : size_t(0), need);
+  AVITS_REQUIRE(reinterpret_cast<uintptr_t>(workspace) % 16 == 0, "%s: the workspace is not 16-byte aligned", what);
+  if (m > 0) {
+    a.dout = dout->p, a.o = o->p, a.dq = dq->p;
+    a.do_ld = dout->ld, a.o_ld = o->ld, a.dq_ld = dq->ld;
+  }
+  if (n > 0) {
+    a.dk = dk->p, a.dv = dv->p;
+    a.dk_ld = dk->ld, a.dv_ld = dv->ld;
+  }
+  a.lse = const_cast<float*>(lse);
+  a.delta = static_cast<float*>(workspace);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  TimedLaunch timed(what, s);
+  if (m > 0) {
+    const dim3 grid(unsigned(ceil_div64(m * H, 256 / (d / 8))));
+    if (dtype == AVITS_BF16) {
+      if (d == 128) hipLaunchKernelGGL((sparse_delta_kernel<bf16_t, 128>), grid, dim3(256), 0, s, a);
+      else hipLaunchKernelGGL((sparse_delta_kernel<bf16_t, 64>), grid, dim3(256), 0, s, a);
+    } else {
+      if (d == 128) hipLaunchKernelGGL((sparse_delta_kernel<float, 128>), grid, dim3(256), 0, s, a);
+      else hipLaunchKernelGGL((sparse_delta_kernel<float, 64>), grid, dim3(256), 0, s, a);
+    }
+  }
+  if (dtype == AVITS_F32) d == 128 ? backward_simple<float, 128>(a, s) : backward_simple<float, 64>(a, s);
+  else d == 128 ? backward_simple<bf16_t, 128>(a, s) : backward_simple<bf16_t, 64>(a, s);
+  return launch_status(what);
+}
