@@ -20,7 +20,7 @@ LIB = os.path.join(PKG, "libavits.so")
 ARCH = "gfx950"
 
 SOURCES = ("abi.hip", "score.hip", "select.hip", "relayout.hip", "gemm.hip", "attention.hip", "block.hip",
-           "noise.hip", "norm.hip", "lowbit.hip", "mxfp4.hip", "rope.hip", "blocks.hip", "sparse.hip")
+           "noise.hip", "norm.hip", "lowbit.hip", "mxfp4.hip", "rope.hip", "blocks.hip", "sparse.hip", "sparse_bf16.hip")
 
 CXXFLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
@@ -55,6 +55,7 @@ def _run(cmd):
 NO_SCRATCH = {"gemm.hip": ("gemm_bf16",), "attention.hip": ("attn_bf16_kernel",),
               "score.hip": ("spatial_temporal_bf16", "finalize_select"), "select.hip": ("radix_select",),
               "norm.hip": ("norm_rows_kernel", "norm_back_rows_kernel"),
+              "sparse_bf16.hip": ("sparse_bf16_kernel",),
               "mxfp4.hip": ("mx4_rows_kernel", "mx4_join_kernel", "mx4_tile_kernelItLb0ELb1", "mx4_tile_kernelIfLb0ELb1")}
 _USAGE = ["-Rpass-analysis=kernel-resource-usage"]
 

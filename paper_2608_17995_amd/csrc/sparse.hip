@@ -342,6 +342,19 @@ int check_rows(const char* what, const char* name, const avits_rows* r, int64_t 
     if (rc_ != AVITS_OK) return rc_;                                                    \
   } while (0)
 
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - 4096;
+
+// Bytes of one number of blocks' pieces, and of the most that up to M rows of B sequences need.
+size_t piece_bytes(int64_t blocks, int64_t pieces, int32_t H, int32_t d) {
+  return pieces > 1 ? size_t(pieces) * size_t(blocks) * size_t(H) * kQB * size_t(d + 2) * sizeof(float) : 0;
+}
+size_t most_piece_bytes(int64_t M, int64_t N, int32_t B, int32_t H, int32_t d) {
+  size_t most = 0;
+  for (int64_t blocks = 1; blocks <= ceil_div64(M, kQB) + B && blocks * H < 512; ++blocks)
+    most = std::max(most, piece_bytes(blocks, sparse_pieces(blocks * H, ceil_div64(N, kKB)), H, d));
+  return most;
+}
+
 size_t delta_bytes(int64_t M, int32_t H) { return align_up(size_t(M) * size_t(H) * sizeof(float), 256); }
 
 }  // namespace
@@ -350,7 +363,8 @@ size_t delta_bytes(int64_t M, int32_t H) { return align_up(size_t(M) * size_t(H)
 using namespace avits;
 
 extern "C" size_t avits_sparse_attention_workspace_bytes(int64_t M, int64_t N, int32_t B, int32_t H, int32_t d, int dtype) {
-  return 0;
+  if (M < 0 || N < 0 || M >= kMaxRows || N >= kMaxRows || B < 1 || B > kMaxSeqs || H < 1 || H > 1024 || (d != 64 && d != 128)) return 0;
+  return dtype == AVITS_BF16 ? most_piece_bytes(M, N, B, H, d) : 0;
 }
 
 extern "C" int avits_sparse_attention(const avits_rows* q, const avits_rows* k, const avits_rows* v, int64_t M, int64_t N, int32_t B,
@@ -370,10 +384,24 @@ extern "C" int avits_sparse_attention(const avits_rows* q, const avits_rows* k, 
   a.o = o->p;
   a.o_ld = o->ld;
   a.lse = lse;
+  a.pieces = 1;
+  if (dtype == AVITS_BF16) {
+    int most = 0;
+    for (int b = 0; b < B; ++b) most = std::max(most, a.seq.k_blk[b + 1] - a.seq.k_blk[b]);
+    a.pieces = sparse_pieces(int64_t(a.seq.q_blk[B]) * H, most);
+    if (a.pieces > 1) {
+      const size_t need = piece_bytes(a.seq.q_blk[B], a.pieces, H, d);
+      if (!workspace || workspace_bytes < need)
+        return set_error(AVITS_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", what, workspace ? workspace_bytes : size_t(0), need);
+      AVITS_REQUIRE(reinterpret_cast<uintptr_t>(workspace) % 16 == 0, "%s: the workspace is not 16-byte aligned", what);
+      a.part = static_cast<float*>(workspace);
+      a.part_ml = a.part + need / sizeof(float) / (d + 2) * d;
+    }
+  }
   const hipStream_t s = static_cast<hipStream_t>(stream);
   TimedLaunch timed(what, s);
   if (dtype == AVITS_F32) d == 128 ? forward_simple<float, 128>(a, s) : forward_simple<float, 64>(a, s);
-  else d == 128 ? forward_simple<bf16_t, 128>(a, s) : forward_simple<bf16_t, 64>(a, s);
+  else launch_sparse_bf16(a, s);
   return launch_status(what);
 }
 

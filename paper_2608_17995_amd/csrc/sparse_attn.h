@@ -16,6 +16,9 @@ struct SparseArgs {
   int64_t M;
   int H, group, d;       // query heads, query heads to a key head
   float scale;
+  int pieces;            // of each query block's list, joined afterwards (1: none)
+  float* part;           // [pieces][query blocks][H][128][d] unnormalised outputs
+  float* part_ml;        // [pieces][query blocks][H][128] (maximum in the log2 domain, sum)
   SeqBlocks seq;         // q_row, q_blk: the totals also in their last entry
 };
 
@@ -47,7 +50,29 @@ struct BlockWalk {
     cur &= cur - 1;
     return j;
   }
+  __device__ __forceinline__ void skip(int n) {
+    if (n == 0) return;
+    while (n >= int(__popcll(cur))) {
+      n -= __popcll(cur);
+      cur = 0;
+      ++w;
+      if (64 * w >= nk) return;
+      cur = word(w);
+    }
+    for (; n > 0; --n) cur &= cur - 1;
+  }
 };
+
+constexpr int kMaxPieces = 64;
+int sparse_pieces(int64_t units, int64_t most_tiles);
+void launch_sparse_bf16(const SparseArgs& a, hipStream_t s);
+
+// Transposing read: of 16 lanes, lane i gives the address of four 16-bit elements of row i / 4,
+// columns 4 (i % 4) .., and receives column i of the four rows.
+__device__ __forceinline__ u32x2 lds_read_tr(const char* p) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p)));
+}
 
 // Whether query block blk of head h keeps its sequence's key block j.
 __device__ __forceinline__ bool kept(const SparseArgs& a, int h, int blk, int j) {
