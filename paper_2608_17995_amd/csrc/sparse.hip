@@ -458,6 +458,6 @@ extern "C" int avits_sparse_attention_backward(const avits_rows* dout, const avi
     }
   }
   if (dtype == AVITS_F32) d == 128 ? backward_simple<float, 128>(a, s) : backward_simple<float, 64>(a, s);
-  else d == 128 ? backward_simple<bf16_t, 128>(a, s) : backward_simple<bf16_t, 64>(a, s);
+  else launch_sparse_back_bf16(a, s);
   return launch_status(what);
 }

@@ -66,6 +66,7 @@ struct BlockWalk {
 constexpr int kMaxPieces = 64;
 int sparse_pieces(int64_t units, int64_t most_tiles);
 void launch_sparse_bf16(const SparseArgs& a, hipStream_t s);
+void launch_sparse_back_bf16(const SparseArgs& a, hipStream_t s);
 
 // Transposing read: of 16 lanes, lane i gives the address of four 16-bit elements of row i / 4,
 // columns 4 (i % 4) .., and receives column i of the four rows.
