@@ -59,9 +59,6 @@ NO_SCRATCH = {"gemm.hip": ("gemm_bf16",), "attention.hip": ("attn_bf16_kernel",)
               "sparse_bf16.hip": ("sparse_bf16_kernel",),
               "sparse_bf16_back.hip": ("sparse_dq_bf16", "sparse_dkv_bf16"),
               "mxfp4.hip": ("mx4_rows_kernel", "mx4_join_kernel", "mx4_tile_kernelItLb0ELb1", "mx4_tile_kernelIfLb0ELb1")}
-# The backward pass's sums fill the accumulation registers: its other products go to ordinary
-# ones, which the compiler's own rule (all products in accumulation registers) leaves no room for.
-EXTRA_FLAGS = {"sparse_bf16_back.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 _USAGE = ["-Rpass-analysis=kernel-resource-usage"]
 
 
@@ -88,7 +85,7 @@ def build(verbose: bool = False, jobs: int | None = None) -> str:
     for src in SOURCES:
         obj = os.path.join(BUILD, src.replace(".hip", ".o"))
         objs.append(obj)
-        extra = EXTRA_FLAGS.get(src, []) + (_USAGE if src in NO_SCRATCH else [])
+        extra = _USAGE if src in NO_SCRATCH else []
         cmds.append([cc, *CXXFLAGS, *extra, f"-I{INCLUDE}", f"-I{CSRC}", "-c", os.path.join(CSRC, src), "-o", obj])
     jobs = jobs or min(len(cmds), os.cpu_count() or 4, 8)
     with cf.ThreadPoolExecutor(jobs) as ex:

@@ -88,8 +88,10 @@ __global__ __launch_bounds__(256) void block_means_kernel(const MeanArgs a) {
 // ---------------------------------------------------------------------------
 // Scores and choice.  A workgroup takes up to 16 query blocks of a head of one
 // sequence: their scores against all key blocks by 16x16x4 products in 64 bits into
-// LDS, then a wave for each row finds the n-th largest by its bits, from the highest.
-constexpr int kSelWaves = 8;
+// LDS, then a wave for each row finds the n-th largest by its bits, from the highest, with the keys in registers
+// where a row has at most 64 kHeld of them (read from LDS for each bit they took 41 us at 264 key blocks, 132
+// query blocks and 16 heads).
+constexpr int kSelWaves = 16;
 constexpr int kMaxKeyBlocks = 16384;  // 128 KiB of scores for one row
 
 struct SelectArgs {
@@ -109,6 +111,54 @@ __device__ __forceinline__ uint64_t order_key(double v) {
   if (v != v) return 0;
   const uint64_t u = uint64_t(__double_as_longlong(v + 0.0));
   return u >> 63 ? ~u : u | (uint64_t(1) << 63);
+}
+
+constexpr int kHeld = 8;
+
+// The choice of one row by a wave: key(t) is the ordered score of key block 64 t + lane (0 past the last).
+template <bool HELD, class Key>
+__device__ __forceinline__ void choose(const Key& key, int tiles, int nk, int lead, int n, bool all, int words, uint64_t* out) {
+  const int lane = threadIdx.x % kWave;
+  // Which of a tile's blocks compete: those past the leading ones.
+  auto rest = [&](int t) {
+    const int lo = std::min(64, std::max(0, lead - 64 * t)), up = std::min(64, std::max(0, nk - 64 * t));
+    const uint64_t below = up == 64 ? ~uint64_t(0) : (uint64_t(1) << up) - 1;
+    return lo == 64 ? 0 : below & (~uint64_t(0) << lo);
+  };
+  // The largest threshold that n keys reach, bit by bit; `exact`: just n do.
+  uint64_t top = 0;
+  bool exact = all || n == 0 || n == nk - lead;
+  for (int bit = 63; bit >= 0 && !exact; --bit) {
+    const uint64_t cand = top | (uint64_t(1) << bit);
+    int count = 0;
+    _Pragma("unroll(HELD ? kHeld : 1)") for (int t = 0; t < (HELD ? kHeld : tiles); ++t)
+      if (t < tiles) count += __popcll(__ballot(key(t) >= cand) & rest(t));
+    if (count >= n) top = cand;
+    exact = count == n;
+  }
+  int spare = 0;  // how many of the keys equal to the threshold count
+  if (!exact) {
+    int above = 0;
+    _Pragma("unroll(HELD ? kHeld : 1)") for (int t = 0; t < (HELD ? kHeld : tiles); ++t)
+      if (t < tiles) above += __popcll(__ballot(key(t) > top) & rest(t));
+    spare = n - above;
+  }
+  _Pragma("unroll(HELD ? kHeld : 1)") for (int t = 0; t < (HELD ? kHeld : tiles); ++t) {
+    if (t >= tiles) continue;
+    const uint64_t in = rest(t), k = key(t);
+    const uint64_t past = nk - 64 * t >= 64 ? ~uint64_t(0) : (uint64_t(1) << (nk - 64 * t)) - 1;
+    uint64_t on = past & ~in;  // the leading ones
+    if (all) on = past;
+    else if (n > 0) on |= __ballot(exact ? k >= top : k > top) & in;
+    if (!exact) {
+      const uint64_t tie = __ballot(k == top) & in;
+      const int before = __popcll(tie & ((uint64_t(1) << lane) - 1));
+      on |= __ballot((tie >> lane & 1) && before < spare);
+      spare -= std::min(spare, int(__popcll(tie)));
+    }
+    if (lane == 0) out[t] = on;
+  }
+  for (int w = tiles + lane; w < words; w += kWave) out[w] = 0;
 }
 
 __global__ __launch_bounds__(64 * kSelWaves) void block_select_kernel(const SelectArgs a) {
@@ -141,40 +191,19 @@ __global__ __launch_bounds__(64 * kSelWaves) void block_select_kernel(const Sele
     }
   }
   __syncthreads();
+  const int tiles = (nk + 63) / 64, n = std::min(a.keep, nk - lead);
   for (int r = wave; r < n_rows; r += kSelWaves) {
     const int i = i0 + r;
     const bool all = int64_t(i) * kQB < a.q_lead;
     const uint64_t* row = keys + int64_t(r) * nk;
-    const int n = std::min(a.keep, nk - lead);
-    // The largest threshold that n keys reach, bit by bit; `exact`: just n do.
-    uint64_t top = 0;
-    bool exact = all || n == 0 || n == nk - lead;
-    for (int bit = 63; bit >= 0 && !exact; --bit) {
-      const uint64_t cand = top | (uint64_t(1) << bit);
-      int count = 0;
-      for (int j = lead + lane; j - lane < nk; j += kWave) count += __popcll(__ballot(j < nk && row[j] >= cand));
-      if (count >= n) top = cand;
-      exact = count == n;
-    }
-    int spare = 0;  // how many of the keys equal to the threshold count
-    if (!exact) {
-      int above = 0;
-      for (int j = lead + lane; j - lane < nk; j += kWave) above += __popcll(__ballot(j < nk && row[j] > top));
-      spare = n - above;
-    }
     uint64_t* out = a.mask + (int64_t(h) * a.seq.q_blk[kMaxSeqs] + q_blk + i) * a.words;
-    for (int w = 0; w < a.words; ++w) {
-      const int j = kWave * w + lane;
-      const uint64_t key = j < nk ? row[j] : 0;
-      const uint64_t rest = __ballot(j >= lead && j < nk);
-      uint64_t on = __ballot(j < nk && (j < lead || all || (n > 0 && (exact ? key >= top : key > top))));
-      if (!exact) {
-        const uint64_t tie = __ballot(key == top) & rest;
-        const int before = __popcll(tie & ((uint64_t(1) << lane) - 1));
-        on |= __ballot((tie >> lane & 1) && before < spare);
-        spare -= std::min(spare, int(__popcll(tie)));
-      }
-      if (lane == 0) out[w] = on;
+    if (tiles <= kHeld) {
+      uint64_t held[kHeld];
+#pragma unroll
+      for (int t = 0; t < kHeld; ++t) held[t] = 64 * t + lane < nk ? row[64 * t + lane] : 0;
+      choose<true>([&](int t) { return held[t]; }, tiles, nk, lead, n, all, int(a.words), out);
+    } else {
+      choose<false>([&](int t) { return 64 * t + lane < nk ? row[64 * t + lane] : 0; }, tiles, nk, lead, n, all, int(a.words), out);
     }
   }
 }

@@ -11,7 +11,7 @@
 // No sum crosses workgroups in a varying order: dq is made by the owners of the
 // query rows, dk and dv by the owners of the key blocks (which walk the mask's
 // columns), at the price of making the probabilities twice.
-#include "sparse_attn.h"
+#include "sparse_plan.h"
 
 namespace avits {
 namespace {
@@ -167,8 +167,8 @@ __global__ __launch_bounds__(256) void sparse_dq_simple_kernel(const SparseArgs 
 #pragma unroll
   for (int j = 0; j < kD; ++j) dq[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int row = first + 16 * wave + lane % 16;
-  const float lse = row < s.q_hi ? a.lse[int64_t(h) * a.M + row] : INFINITY;
-  const float delta = row < s.q_hi ? a.delta[int64_t(h) * a.M + row] : 0.f;
+  const float2 st = row < s.q_hi ? a.stats[int64_t(h) * a.M + row] : make_float2(INFINITY, 0.f);
+  const float lse = st.x, delta = st.y;
   BlockWalk walk(a, h, blk, s.nk);
   for (int j = walk.next(); j >= 0; j = walk.next()) {
     const int key = s.k_lo + j * kKB;
@@ -220,8 +220,9 @@ __global__ __launch_bounds__(256) void sparse_dkv_simple_kernel(const SparseArgs
         load_tile<T, DH>(gt, G, a.do_ld, row, s.q_hi);
         if (threadIdx.x < kFT) {
           const int r = row + threadIdx.x;
-          ls[threadIdx.x] = r < s.q_hi ? a.lse[int64_t(h) * a.M + r] : INFINITY;  // rows past the end: no probability
-          dl[threadIdx.x] = r < s.q_hi ? a.delta[int64_t(h) * a.M + r] : 0.f;
+          const float2 st = r < s.q_hi ? a.stats[int64_t(h) * a.M + r] : make_float2(INFINITY, 0.f);  // past the end: no probability
+          ls[threadIdx.x] = st.x;
+          dl[threadIdx.x] = st.y;
         }
         __syncthreads();
 #pragma unroll
@@ -251,34 +252,42 @@ __global__ __launch_bounds__(256) void sparse_dkv_simple_kernel(const SparseArgs
   }
 }
 
-// delta = do . o of every row and head: DH / 8 lanes to a head.
+// delta = do . o of every row and head, beside lse: DH / 8 lanes to a head; a workgroup takes 16 rows of up to
+// 64 heads, whose results pass through LDS so that they are written row after row (straight from the
+// lanes, 8 bytes to a place M apart, 9.5 us at 4608 rows of 16 heads of 128).  The first workgroups make
+// the plans of dq and of dk and dv meanwhile.
+constexpr int kDeltaRows = 16, kDeltaHeads = 64;
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void sparse_delta_kernel(const SparseArgs a) {
-  constexpr int kL = DH / 8;
-  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) / kL;
-  const int c = threadIdx.x % kL * 8;
-  const int64_t row = i / a.H, h = i % a.H;
-  if (row >= a.seq.q_row[kMaxSeqs]) return;  // whole groups of lanes leave together
-  const T* g = static_cast<const T*>(a.dout) + row * a.do_ld + h * DH + c;
-  const T* o = static_cast<const T*>(a.o) + row * a.o_ld + h * DH + c;
-  float sum = 0.f;
-  if constexpr (sizeof(T) == 4) {
+__global__ __launch_bounds__(1024) void sparse_delta_kernel(const SparseArgs a, SparsePlan* plan_q, SparsePlan* plan_k) {
+  constexpr int kL = DH / 8, kStep = 1024 / kL / kDeltaRows;  // lanes to a head, heads at once
+  __shared__ int counts[kMaxUnits];
+  __shared__ uint64_t sums[1024];
+  __shared__ float out[kDeltaHeads][kDeltaRows + 1];
+  int64_t wg = blockIdx.x;
+  if (plan_q && wg-- == 0) return sparse_plan<false, 1024>(a, plan_q, counts, sums);
+  if (plan_k && wg-- == 0) return sparse_plan<true, 1024>(a, plan_k, counts, sums);
+  const int chunks = (a.H + kDeltaHeads - 1) / kDeltaHeads, h0 = int(wg % chunks) * kDeltaHeads, nh = std::min(kDeltaHeads, a.H - h0);
+  const int64_t row0 = wg / chunks * kDeltaRows;
+  const int g = threadIdx.x / kL, c = threadIdx.x % kL * 8, r = g / kStep;
+  const int64_t row = row0 + r;
+  for (int hh = g % kStep; hh < nh && row < a.seq.q_row[kMaxSeqs]; hh += kStep) {  // groups of lanes leave together
+    const T* x = static_cast<const T*>(a.dout) + row * a.do_ld + int64_t(h0 + hh) * DH + c;
+    const T* y = static_cast<const T*>(a.o) + row * a.o_ld + int64_t(h0 + hh) * DH + c;
+    float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; e += 4) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(g + e), y = *reinterpret_cast<const f32x4*>(o + e);
+      const f32x4 u = load4(x + e), v = load4(y + e);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sum += x[r] * y[r];
+      for (int k = 0; k < 4; ++k) sum += u[k] * v[k];
     }
-  } else {
-    const u32x4 x = *reinterpret_cast<const u32x4*>(g), y = *reinterpret_cast<const u32x4*>(o);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      sum += __uint_as_float(x[r] << 16) * __uint_as_float(y[r] << 16);
-      sum += __uint_as_float(x[r] & 0xffff0000u) * __uint_as_float(y[r] & 0xffff0000u);
-    }
+    sum = group_sum(sum, kL);
+    if (c == 0) out[hh][r] = sum;
   }
-  sum = group_sum(sum, kL);
-  if (c == 0) a.delta[h * a.M + row] = sum;
+  __syncthreads();
+  for (int i = threadIdx.x; i < nh * kDeltaRows; i += 1024) {
+    const int64_t to = row0 + i % kDeltaRows, at = (h0 + i / kDeltaRows) * a.M + to;
+    if (to < a.seq.q_row[kMaxSeqs]) a.stats[at] = make_float2(a.lse[at], out[i / kDeltaRows][i % kDeltaRows]);
+  }
 }
 
 template <typename T, int DH>
@@ -321,6 +330,7 @@ int fill(SparseArgs& a, const char* what, const avits_rows* q, const avits_rows*
   a.scale = scale;
   a.seq.q_row[kMaxSeqs] = a.seq.q_row[B];
   a.seq.q_blk[kMaxSeqs] = a.seq.q_blk[B];
+  a.seq.k_blk[kMaxSeqs] = a.seq.k_blk[B];
   return AVITS_OK;
 }
 
@@ -344,18 +354,29 @@ int check_rows(const char* what, const char* name, const avits_rows* r, int64_t 
 
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 4096;
 
-// Bytes of one number of blocks' pieces, and of the most that up to M rows of B sequences need.
-size_t piece_bytes(int64_t blocks, int64_t pieces, int32_t H, int32_t d) {
-  return pieces > 1 ? size_t(pieces) * size_t(blocks) * size_t(H) * kQB * size_t(d + 2) * sizeof(float) : 0;
-}
-size_t most_piece_bytes(int64_t M, int64_t N, int32_t B, int32_t H, int32_t d) {
-  size_t most = 0;
-  for (int64_t blocks = 1; blocks <= ceil_div64(M, kQB) + B && blocks * H < 512; ++blocks)
-    most = std::max(most, piece_bytes(blocks, sparse_pieces(blocks * H, ceil_div64(N, kKB)), H, d));
-  return most;
+// Bytes of a slot of a query block's (max, sum) and outputs.
+size_t slot_bytes(int32_t d) { return size_t(kQB) * size_t(d + 2) * sizeof(float); }
+size_t plan_bytes() { return align_up(sizeof(SparsePlan), 256); }
+
+// Whether the lists of so many units are cut by a plan: more than a few (which are all cut alike), and not so many that
+// they even out.
+bool planned(int64_t units, bool mask) { return mask && units > kFewUnits && units <= kMaxUnits; }
+// A forward pass: up to 2048 units make fewer than four rounds of the chip's 512 workgroups.
+bool planned_forward(int64_t units, bool mask) { return planned(units, mask) && units <= 2048; }
+
+// What the forward pass of `units` units with lists of at most `most` blocks needs.
+size_t forward_bytes(int64_t units, int64_t most, int32_t d, bool mask) {
+  if (planned_forward(units, mask)) return plan_bytes() + size_t(sparse_slots(units, most)) * slot_bytes(d);
+  const int p = sparse_pieces(units, most);
+  return p > 1 ? size_t(p) * size_t(units) * slot_bytes(d) : 0;
 }
 
-size_t delta_bytes(int64_t M, int32_t H) { return align_up(size_t(M) * size_t(H) * sizeof(float), 256); }
+// One side of a backward pass, for up to so many units.
+size_t side_bytes(int64_t units, int64_t most, int32_t d) {
+  return plan_bytes() + size_t(sparse_slots(std::min<int64_t>(units, kMaxUnits), most)) * kQB * d * sizeof(float);
+}
+
+size_t stats_bytes(int64_t M, int32_t H) { return align_up(size_t(M) * size_t(H) * sizeof(float2), 256); }
 
 }  // namespace
 }  // namespace avits
@@ -364,7 +385,11 @@ using namespace avits;
 
 extern "C" size_t avits_sparse_attention_workspace_bytes(int64_t M, int64_t N, int32_t B, int32_t H, int32_t d, int dtype) {
   if (M < 0 || N < 0 || M >= kMaxRows || N >= kMaxRows || B < 1 || B > kMaxSeqs || H < 1 || H > 1024 || (d != 64 && d != 128)) return 0;
-  return dtype == AVITS_BF16 ? most_piece_bytes(M, N, B, H, d) : 0;
+  if (dtype != AVITS_BF16) return 0;
+  size_t most = 0;  // fewer rows, or fewer sequences, may need more
+  for (int64_t blocks = 1; blocks <= ceil_div64(M, kQB) + B && blocks * H <= 2048; ++blocks)
+    for (bool mask : {false, true}) most = std::max(most, forward_bytes(blocks * H, ceil_div64(N, kKB), d, mask));
+  return most;
 }
 
 extern "C" int avits_sparse_attention(const avits_rows* q, const avits_rows* k, const avits_rows* v, int64_t M, int64_t N, int32_t B,
@@ -388,15 +413,24 @@ extern "C" int avits_sparse_attention(const avits_rows* q, const avits_rows* k, 
   if (dtype == AVITS_BF16) {
     int most = 0;
     for (int b = 0; b < B; ++b) most = std::max(most, a.seq.k_blk[b + 1] - a.seq.k_blk[b]);
-    a.pieces = sparse_pieces(int64_t(a.seq.q_blk[B]) * H, most);
-    if (a.pieces > 1) {
-      const size_t need = piece_bytes(a.seq.q_blk[B], a.pieces, H, d);
+    const int64_t units = int64_t(a.seq.q_blk[B]) * H;
+    const size_t need = forward_bytes(units, most, d, mask != nullptr);
+    if (need > 0) {
       if (!workspace || workspace_bytes < need)
         return set_error(AVITS_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", what, workspace ? workspace_bytes : size_t(0), need);
       AVITS_REQUIRE(reinterpret_cast<uintptr_t>(workspace) % 16 == 0, "%s: the workspace is not 16-byte aligned", what);
-      a.part = static_cast<float*>(workspace);
-      a.part_ml = a.part + need / sizeof(float) / (d + 2) * d;
     }
+    char* at = static_cast<char*>(workspace);
+    if (planned_forward(units, mask != nullptr)) {
+      a.slots = sparse_slots(units, most);
+      a.plan = reinterpret_cast<const SparsePlan*>(at);
+      at += plan_bytes();
+    } else {
+      a.pieces = sparse_pieces(units, most);
+      a.slots = a.pieces > 1 ? units * a.pieces : 0;
+    }
+    a.part = reinterpret_cast<float*>(at);
+    a.part_ml = a.part + a.slots * kQB * d;
   }
   const hipStream_t s = static_cast<hipStream_t>(stream);
   TimedLaunch timed(what, s);
@@ -406,8 +440,11 @@ extern "C" int avits_sparse_attention(const avits_rows* q, const avits_rows* k, 
 }
 
 extern "C" size_t avits_sparse_attention_backward_workspace_bytes(int64_t M, int64_t N, int32_t B, int32_t H, int32_t Hk, int32_t d, int dtype) {
-  if (M < 0 || N < 0 || M >= (int64_t(1) << 31) - 4096 || N >= (int64_t(1) << 31) - 4096 || H < 1 || H > 1024) return 0;
-  return delta_bytes(M, H);
+  if (M < 0 || N < 0 || M >= kMaxRows || N >= kMaxRows || B < 1 || B > kMaxSeqs || H < 1 || H > 1024 || Hk < 1 || H % Hk != 0 || (d != 64 && d != 128)) return 0;
+  size_t most = stats_bytes(M, H);
+  if (dtype != AVITS_BF16) return most;
+  const int64_t nq = ceil_div64(M, kQB) + B, nk = ceil_div64(N, kKB) + B;  // blocks, at most
+  return most + side_bytes(nq * H, nk, d) + side_bytes(nk * Hk, nq * (H / Hk), d);
 }
 
 extern "C" int avits_sparse_attention_backward(const avits_rows* dout, const avits_rows* q, const avits_rows* k, const avits_rows* v,
@@ -444,20 +481,44 @@ extern "C" int avits_sparse_attention_backward(const avits_rows* dout, const avi
     a.dk_ld = dk->ld, a.dv_ld = dv->ld;
   }
   a.lse = const_cast<float*>(lse);
-  a.delta = static_cast<float*>(workspace);
+  a.stats = static_cast<float2*>(workspace);
+  a.pieces = 1;
+  // The plans of dq and of dk and dv, and their slots.
+  SparseArgs ak = a;
+  SparsePlan *plan_q = nullptr, *plan_k = nullptr;
+  if (dtype == AVITS_BF16 && m > 0 && n > 0) {
+    int most_q = 0, most_k = 0;
+    for (int b = 0; b < B; ++b) {
+      most_q = std::max(most_q, a.seq.k_blk[b + 1] - a.seq.k_blk[b]);
+      most_k = std::max(most_k, (a.seq.q_blk[b + 1] - a.seq.q_blk[b]) * a.group);
+    }
+    char* at = static_cast<char*>(workspace) + stats_bytes(M, H);
+    const int64_t uq = int64_t(a.seq.q_blk[B]) * H, uk = int64_t(a.seq.k_blk[B]) * Hk;
+    if (planned(uq, mask != nullptr)) {
+      a.plan = plan_q = reinterpret_cast<SparsePlan*>(at);
+      a.slots = sparse_slots(uq, most_q);
+      a.part = reinterpret_cast<float*>(at + plan_bytes());
+      at += plan_bytes() + size_t(a.slots) * kQB * d * sizeof(float);
+    }
+    if (planned(uk, mask != nullptr) && most_k <= 4096) {  // a cut list is walked at once
+      ak.plan = plan_k = reinterpret_cast<SparsePlan*>(at);
+      ak.slots = sparse_slots(uk, most_k);
+      ak.part = reinterpret_cast<float*>(at + plan_bytes());
+    }
+  }
   const hipStream_t s = static_cast<hipStream_t>(stream);
   TimedLaunch timed(what, s);
   if (m > 0) {
-    const dim3 grid(unsigned(ceil_div64(m * H, 256 / (d / 8))));
+    const dim3 grid(unsigned(ceil_div64(m, kDeltaRows) * ceil_div64(H, kDeltaHeads) + (plan_q != nullptr) + (plan_k != nullptr)));
     if (dtype == AVITS_BF16) {
-      if (d == 128) hipLaunchKernelGGL((sparse_delta_kernel<bf16_t, 128>), grid, dim3(256), 0, s, a);
-      else hipLaunchKernelGGL((sparse_delta_kernel<bf16_t, 64>), grid, dim3(256), 0, s, a);
+      if (d == 128) hipLaunchKernelGGL((sparse_delta_kernel<bf16_t, 128>), grid, dim3(1024), 0, s, a, plan_q, plan_k);
+      else hipLaunchKernelGGL((sparse_delta_kernel<bf16_t, 64>), grid, dim3(1024), 0, s, a, plan_q, plan_k);
     } else {
-      if (d == 128) hipLaunchKernelGGL((sparse_delta_kernel<float, 128>), grid, dim3(256), 0, s, a);
-      else hipLaunchKernelGGL((sparse_delta_kernel<float, 64>), grid, dim3(256), 0, s, a);
+      if (d == 128) hipLaunchKernelGGL((sparse_delta_kernel<float, 128>), grid, dim3(1024), 0, s, a, plan_q, plan_k);
+      else hipLaunchKernelGGL((sparse_delta_kernel<float, 64>), grid, dim3(1024), 0, s, a, plan_q, plan_k);
     }
   }
   if (dtype == AVITS_F32) d == 128 ? backward_simple<float, 128>(a, s) : backward_simple<float, 64>(a, s);
-  else launch_sparse_back_bf16(a, s);
+  else launch_sparse_back_bf16(a, ak, s);
   return launch_status(what);
 }

@@ -12,14 +12,16 @@ struct SparseArgs {
   const uint64_t* mask;  // [H][query blocks][words], or null: every block
   int64_t words;
   float* lse;            // [H][M]
-  float* delta;          // [H][M]: do . o
+  float2* stats;         // [H][M]: lse and do . o, for the backward pass
   int64_t M;
   int H, group, d;       // query heads, query heads to a key head
   float scale;
-  int pieces;            // of each query block's list, joined afterwards (1: none)
-  float* part;           // [pieces][query blocks][H][128][d] unnormalised outputs
-  float* part_ml;        // [pieces][query blocks][H][128] (maximum in the log2 domain, sum)
-  SeqBlocks seq;         // q_row, q_blk: the totals also in their last entry
+  const struct SparsePlan* plan;  // which lists are cut, by the mask; or null:
+  int64_t slots;         // with a plan: its slots
+  int pieces;            // of each unit's list, joined afterwards (1: none)
+  float* part;           // slots of unfinished sums: [128][d] of outputs or dq, or [2][64][d] of dk and dv
+  float* part_ml;        // slots of [128] (maximum in the log2 domain, sum)
+  SeqBlocks seq;         // q_row, q_blk, k_blk: the totals also in their last entry
 };
 
 // The key blocks that query block blk of head h keeps, in order (wave-uniform).
@@ -63,10 +65,14 @@ struct BlockWalk {
   }
 };
 
-constexpr int kMaxPieces = 64;
-int sparse_pieces(int64_t units, int64_t most_tiles);
+// Pieces of every list where there are few units: two workgroups to each of 256 CUs, each with two blocks at least.
+constexpr int kMaxPieces = 64, kFewUnits = 64;
+inline int sparse_pieces(int64_t units, int64_t most_list) {
+  if (units > kFewUnits || units == 0) return 1;
+  return int(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / units, most_list / 2), kMaxPieces)));
+}
 void launch_sparse_bf16(const SparseArgs& a, hipStream_t s);
-void launch_sparse_back_bf16(const SparseArgs& a, hipStream_t s);
+void launch_sparse_back_bf16(const SparseArgs& q, const SparseArgs& k, hipStream_t s);  // one plan for each
 
 // Transposing read: of 16 lanes, lane i gives the address of four 16-bit elements of row i / 4,
 // columns 4 (i % 4) .., and receives column i of the four rows.

@@ -15,11 +15,11 @@
 // Probabilities are rounded to bf16 for the product with V, which the matrix
 // instruction takes; maxima, sums and outputs are fp32.
 //
-// Few query blocks: the list of each is cut into pieces, whose unnormalised outputs and (max,
-// sum) a second kernel joins in key order.
+// Long lists are cut into pieces (by a plan, or all alike where there are few units), whose
+// unnormalised outputs and (max, sum) a second kernel joins in key order.
 #include <type_traits>
 
-#include "sparse_attn.h"
+#include "sparse_plan.h"
 
 namespace avits {
 namespace {
@@ -46,8 +46,10 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
   // reads (16 rows of one chunk; four rows of four chunks) touch every bank once.
   __shared__ __attribute__((aligned(16))) char smem[4 * kTB];
 
-  const int H = a.H, h = blockIdx.x % H, unit = blockIdx.x / H;
-  const int piece = unit % a.pieces, blk = unit / a.pieces;
+  const int H = a.H, units = a.seq.q_blk[kMaxSeqs] * H;
+  const int4 item = sparse_item(a, units, blockIdx.x);
+  if (item.x < 0) return;
+  const int h = item.x % H, blk = item.x / H, piece = item.y, pieces = item.z;
   const Seq s = seq_of<false>(a.seq, blk);
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -56,7 +58,7 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
   const int row = q_first + wave * 32 + l32;
 
   BlockWalk walk(a, h, blk, s.nk);
-  const int t_lo = int(int64_t(walk.total) * piece / a.pieces), t_hi = int(int64_t(walk.total) * (piece + 1) / a.pieces);
+  const int t_lo = int(int64_t(walk.total) * piece / pieces), t_hi = int(int64_t(walk.total) * (piece + 1) / pieces);
   const int n_tiles = t_hi - t_lo;
   walk.skip(t_lo);
 
@@ -292,8 +294,8 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
 
   const float l = sum_xor32(lrow);
   if (row >= q_end) return;
-  if (a.pieces > 1) {
-    const int64_t at = ((int64_t(piece) * a.seq.q_blk[kMaxSeqs] + blk) * H + h) * kQB + (row - q_first);
+  if (pieces > 1) {
+    const int64_t at = sparse_slot(a, units, item.w, piece) * kQB + (row - q_first);
     float* po = a.part + at * DH + 4 * hi;
 #pragma unroll
     for (int dt = 0; dt < kDT; ++dt)
@@ -320,33 +322,52 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
 }
 
 // The pieces of each row joined in key order: with a piece's running maximum m_p, sum l_p and
-// unnormalised output O_p, o = sum 2^(m_p - m) O_p / sum 2^(m_p - m) l_p, m the largest.
+// unnormalised output O_p, o = sum 2^(m_p - m) O_p / sum 2^(m_p - m) l_p, m the largest.  Eight pieces' loads
+// are under way together.
 template <int DH>
 __global__ __launch_bounds__(256) void sparse_join_kernel(const SparseArgs a) {
-  constexpr int kL = DH / 8;  // lanes to a row
-  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) / kL, unit = i / kQB;  // (block, head) and its row
-  const int c = threadIdx.x % kL * 8, blk = int(unit / a.H), h = int(unit % a.H);
+  constexpr int kL = DH / 8, kR = 256 / kL, kPer = kQB / kR;  // lanes to a row, rows to a workgroup, workgroups to a unit
+  const int units = a.seq.q_blk[kMaxSeqs] * a.H;
+  const int4 cut = sparse_cut(a, blockIdx.x / kPer);
+  if (cut.x < 0) return;
+  const int blk = cut.x / a.H, h = cut.x % a.H, pieces = cut.y, r = blockIdx.x % kPer * kR + threadIdx.x / kL, c = threadIdx.x % kL * 8;
   const Seq s = seq_of<false>(a.seq, blk);
-  const int row = s.q_lo + (blk - s.qb) * kQB + int(i % kQB);
+  const int row = s.q_lo + (blk - s.qb) * kQB + r;
   if (row >= s.q_hi) return;
-  const int64_t step = int64_t(a.seq.q_blk[kMaxSeqs]) * a.H * kQB, at = i;
+  const int64_t step = sparse_slot(a, units, cut.z, 1) - cut.z, at = cut.z * int64_t(kQB) + r;
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + at;
   const float* po = a.part + at * DH + c;
-  float m = kNone;
-  for (int p = 0; p < a.pieces; ++p) m = fmaxf(m, ml[p * step].x);
-  float den = 0.f, acc[8];
+  float m = kNone, den = 0.f, acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-#pragma unroll 4
-  for (int p = 0; p < a.pieces; ++p) {
-    const float2 v = ml[p * step];
-    const float w = __builtin_amdgcn_exp2f(v.x - m);
-    den = fmaf(w, v.y, den);
-    const f32x4 x = *reinterpret_cast<const f32x4*>(po + p * step * DH), y = *reinterpret_cast<const f32x4*>(po + p * step * DH + 4);
+  for (int p0 = 0; p0 < pieces; p0 += 8) {
+    float2 v[8];
+    f32x4 x[8], y[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      acc[e] = fmaf(w, x[e], acc[e]);
-      acc[4 + e] = fmaf(w, y[e], acc[4 + e]);
+    for (int u = 0; u < 8; ++u) {
+      const int64_t p = std::min(p0 + u, pieces - 1) * step * kQB;
+      v[u] = ml[p];
+      x[u] = *reinterpret_cast<const f32x4*>(po + p * DH);
+      y[u] = *reinterpret_cast<const f32x4*>(po + p * DH + 4);
+    }
+    float top = m;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) top = fmaxf(top, v[u].x);
+    const float old = __builtin_amdgcn_exp2f(m - top);
+    m = top;
+    den *= old;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] *= old;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float w = p0 + u < pieces ? __builtin_amdgcn_exp2f(v[u].x - top) : 0.f;
+      if (p0 + u >= pieces) continue;
+      den = fmaf(w, v[u].y, den);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc[e] = fmaf(w, x[u][e], acc[e]);
+        acc[4 + e] = fmaf(w, y[u][e], acc[4 + e]);
+      }
     }
   }
   const bool none = m == kNone && den == 0.f;  // no piece had a key
@@ -357,21 +378,23 @@ __global__ __launch_bounds__(256) void sparse_join_kernel(const SparseArgs a) {
             pack_bf2(acc[6] * inv, acc[7] * inv)};
 }
 
-}  // namespace
-
-int sparse_pieces(int64_t units, int64_t most_tiles) {
-  // Two workgroups to each of 256 CUs, each with two tiles at least.
-  if (units >= 512 || units == 0) return 1;
-  return int(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / units, most_tiles / 2), kMaxPieces)));
+// The plan of a forward pass alone.
+__global__ __launch_bounds__(1024) void sparse_plan_kernel(const SparseArgs a, SparsePlan* plan) {
+  __shared__ int counts[kMaxUnits];
+  __shared__ uint64_t sums[1024];
+  sparse_plan<false, 1024>(a, plan, counts, sums);
 }
+
+}  // namespace
 
 template <int DH>
 static void launch_forward(const SparseArgs& a, hipStream_t s) {
-  const unsigned n = unsigned(a.seq.q_blk[kMaxSeqs]) * unsigned(a.H) * unsigned(a.pieces);
-  hipLaunchKernelGGL((sparse_bf16_kernel<DH>), dim3(n), dim3(256), 0, s, a);
-  if (a.pieces > 1)
-    hipLaunchKernelGGL((sparse_join_kernel<DH>), dim3(unsigned(a.seq.q_blk[kMaxSeqs]) * unsigned(a.H) * (kQB * (DH / 8) / 256)),
-                       dim3(256), 0, s, a);
+  const int64_t units = int64_t(a.seq.q_blk[kMaxSeqs]) * a.H;
+  if (a.plan) hipLaunchKernelGGL(sparse_plan_kernel, dim3(1), dim3(1024), 0, s, a, const_cast<SparsePlan*>(a.plan));
+  const int64_t n = a.plan ? units + a.slots : units * a.pieces, cuts = a.plan ? std::min<int64_t>(kShares, a.slots) : a.pieces > 1 ? units : 0;
+  hipLaunchKernelGGL((sparse_bf16_kernel<DH>), dim3(unsigned(n)), dim3(256), 0, s, a);
+  if (cuts > 0)
+    hipLaunchKernelGGL((sparse_join_kernel<DH>), dim3(unsigned(cuts * (kQB * DH / 8 / 256))), dim3(256), 0, s, a);
 }
 
 void launch_sparse_bf16(const SparseArgs& a, hipStream_t s) {

@@ -5,16 +5,26 @@
 // heads that keep it.  Both make the logits and probabilities again from lse, so seven
 // products run where five would do, and no sum crosses workgroups.
 //
-// What bounds such kernels is the LDS: a 32x32x16 product takes 32 cycles of a SIMD and its LDS operand
-// 8 cycles of the CU's LDS, all of it with four SIMDs.  So each wave covers 64 x 32 rows and keys: one
-// fragment feeds two products, at one wave to a SIMD with all its registers (the other operands
-// and the sums stay in them).
 // Probabilities and ds are rounded to bf16 for the second products, which the matrix instruction
 // takes; everything else is fp32.
-#include "sparse_attn.h"
+#include <utility>
+
+#include "sparse_plan.h"
 
 namespace avits {
 namespace {
+
+// f(0), f(1), ... f(N - 1) with compile-time arguments.
+template <int... I, class F>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F&& f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void each(F&& f) {
+  each_of(std::make_integer_sequence<int, N>{}, f);
+}
+template <int N> using Int = std::integral_constant<int, N>;
+#define AVITS_INLINE __attribute__((always_inline))
 
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -59,461 +69,434 @@ __device__ __forceinline__ void put(bf16x8& chunk, int r, float lo, float up) {
   chunk = as_bf16x8(v);
 }
 
-// Byte offsets of one load instruction's lanes: rows of DH elements, 1 KB to an instruction.
-template <int DH>
-__device__ __forceinline__ uint32_t load_off(int i, int64_t ld) {
-  constexpr int kCH = DH / 8, kR = kWave / kCH;
-  const int lane = threadIdx.x % kWave, r = kR * i + lane / kCH;
-  return uint32_t(r) * uint32_t(ld * 2) + uint32_t(((lane % kCH) ^ swz<DH>(r)) * 16);
-}
-
-// Buffer over rows [first, end) of a head: what lies behind reads as zeros.
-__device__ __forceinline__ u32x4 rows_rsrc(const bf16_t* base, int64_t ld, int first, int end, int width) {
-  const int64_t bytes = end > first ? (int64_t(end - first - 1) * ld + width) * 2 : 0;
-  u32x4 r = buffer_rsrc(base + int64_t(first) * ld, range32(bytes));
+// A wave's share of a tile of ROWS rows that four (64 rows) or eight waves load: instructions of 1 KB, whose
+// lanes fill LDS in order, so the swizzle is in where each lane reads.  The instruction's own offset moves
+// both the source and the LDS address: the sources are given less it.
+template <int DH, int ROWS, int NW = ROWS == 128 ? 8 : 4>
+struct TileLoad {
+  static constexpr int kCH = DH / 8, kR = kWave / kCH, kN = ROWS * DH * 2 / 1024 / NW;
+  uint32_t row, chunk;  // the first instruction's row and swizzled chunk, in bytes
+  int64_t ld2;          // bytes to a row
+  __device__ __forceinline__ TileLoad(int64_t ld, int wave) : ld2(ld * 2) {
+    const int lane = threadIdx.x % kWave, r = kR * kN * wave + lane / kCH;
+    row = uint32_t(r) * uint32_t(ld * 2);
+    chunk = uint32_t(((lane % kCH) ^ swz<DH>(r)) * 16);
+  }
+  // Instruction i is kR i rows on, where the swizzle differs in bits of i (rows kR kN wave are even enough).
+  __device__ __forceinline__ uint32_t off(int i) const {
+    return row + (chunk ^ uint32_t((DH == 128 ? 16 : 32) * i)) + i * (kR * uint32_t(ld2) - 1024);
+  }
+  __device__ __forceinline__ void fresh() { asm volatile("" : "+v"(row), "+v"(chunk)); }
+  // Rows first .. of a head to LDS byte dst, those from `end` on as zeros.
+  __device__ __forceinline__ void go(const bf16_t* base, int first, int end, uint32_t dst) const {
+    const int64_t bytes = end > first ? (end - first - 1) * ld2 + DH * 2 : 0;
+    u32x4 r = buffer_rsrc(reinterpret_cast<const char*>(base) + first * ld2, range32(bytes));
 #pragma unroll
-  for (int e = 0; e < 4; ++e) r[e] = __builtin_amdgcn_readfirstlane(r[e]);
-  return r;
-}
+    for (int e = 0; e < 4; ++e) r[e] = __builtin_amdgcn_readfirstlane(r[e]);
+    static_assert(kN == 1 || kN == 2 || kN == 4, "the offset has twelve bits");
+    if constexpr (kN == 4)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
+                   "buffer_load_dwordx4 %2, %5, 0 offen offset:1024 lds\n\tbuffer_load_dwordx4 %3, %5, 0 offen offset:2048 lds\n\t"
+                   "buffer_load_dwordx4 %4, %5, 0 offen offset:3072 lds" ::"s"(dst), "v"(off(0)), "v"(off(1)), "v"(off(2)), "v"(off(3)), "s"(r)
+                   : "memory", "m0");
+    else if constexpr (kN == 1)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(off(0)), "s"(r) : "memory", "m0");
+    else
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %3, 0 offen lds\n\t"
+                   "buffer_load_dwordx4 %2, %3, 0 offen offset:1024 lds" ::"s"(dst), "v"(off(0)), "v"(off(1)), "s"(r)
+                   : "memory", "m0");
+  }
+};
 
 __device__ __forceinline__ uint32_t lds_offset(const char* p) {
   return __builtin_amdgcn_readfirstlane(uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)(p))));
 }
 
-// 16 bytes' worth of fp32 sums to bf16.
-__device__ __forceinline__ u32x4 pack_sums(const f32x4& x, const f32x4& y, float f) {
-  return u32x4{pack_bf2(x[0] * f, x[1] * f), pack_bf2(x[2] * f, x[3] * f), pack_bf2(y[0] * f, y[1] * f), pack_bf2(y[2] * f, y[3] * f)};
+// The lane's sums of one row (register r of tile dt: column 32 dt + 8 (r / 4) + 4 (l / 32) + r % 4), times f.
+template <int DH>
+__device__ __forceinline__ void store_sums(bf16_t* dst, const f32x16* o, float f) {
+#pragma unroll
+  for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<u32x2*>(dst + 32 * dt + 8 * q) =
+          u32x2{pack_bf2(o[dt][4 * q] * f, o[dt][4 * q + 1] * f), pack_bf2(o[dt][4 * q + 2] * f, o[dt][4 * q + 3] * f)};
 }
 
 // ---------------------------------------------------------------------------
-// dq.  Wave (q, k) = (w % 2, w / 2) takes rows 64 q .. of the block and keys 32 k .. of each 64-key tile;
-// the two waves of a row half meet in LDS at the end.
-// A step interleaves, in a fixed order, the products dP(t) = V dO^T with the exponentials of S(t), then S(t + 1) =
-// K Q^T with ds(t), then dQ^T += K^T dS^T(t): the matrix pipe does not wait for the vector units.
+// dq: 32 rows to a wave.  A step takes a 64-key tile in two halves of 32 keys; the exponentials of one run
+// under the products of the other, and under the other wave's of the SIMD.
 template <int DH>
-__global__ __launch_bounds__(256, 1) void sparse_dq_bf16_kernel(const SparseArgs a) {
-  constexpr int kC = DH / 16, kDT = DH / 32, kTB = kKB * DH * 2, kL = kTB / 4096, kBuf = 4;
-  constexpr int kP = DH + 4;  // floats to a row of the sums
-  constexpr int kBytes = std::max(2 * kBuf * kTB, 2 * 64 * kP * 4);
-  __shared__ __attribute__((aligned(16))) char smem[kBytes];
-  const int H = a.H, h = blockIdx.x % H, blk = blockIdx.x / H;
+__global__ __launch_bounds__(256, 2) void sparse_dq_bf16_kernel(const SparseArgs a) {
+  constexpr int kC = DH / 16, kDT = DH / 32, kTB = kKB * DH * 2, kL = kTB / 4096;
+  __shared__ __attribute__((aligned(16))) char smem[4 * kTB];
+  const int H = a.H, units = a.seq.q_blk[kMaxSeqs] * H;
+  const int4 item = sparse_item(a, units, blockIdx.x);
+  if (item.x < 0) return;
+  const int h = item.x % H, blk = item.x / H;
   const Seq s = seq_of<false>(a.seq, blk);
   const int lane = threadIdx.x % kWave, l32 = lane % 32, hi = lane / 32;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wq = wave % 2, wk = wave / 2;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int q_first = s.q_lo + (blk - s.qb) * kQB, q_end = std::min(s.q_hi, q_first + kQB);
   const bf16_t* K = static_cast<const bf16_t*>(a.k) + int64_t(h / a.group) * DH;
   const bf16_t* V = static_cast<const bf16_t*>(a.v) + int64_t(h / a.group) * DH;
   BlockWalk walk(a, h, blk, s.nk);
-  const int n_tiles = walk.total;
+  const int t_lo = int(int64_t(walk.total) * item.y / item.z), n_tiles = int(int64_t(walk.total) * (item.y + 1) / item.z) - t_lo;
+  const int row = q_first + 32 * wave + l32;
+  walk.skip(t_lo);
 
-  bf16x8 qf[2][kC], gf[2][kC];
-  float lse2[2], delta[2];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int row = std::min(q_first + 64 * wq + 32 * t + l32, q_end - 1);
-    const bf16_t* q = static_cast<const bf16_t*>(a.q) + int64_t(row) * a.q_ld + h * DH + 8 * hi;
-    const bf16_t* g = static_cast<const bf16_t*>(a.dout) + int64_t(row) * a.do_ld + h * DH + 8 * hi;
+  bf16x8 qf[kC], gf[kC];
+  f32x16 acc[kDT];
+  const int from = std::min(row, q_end - 1);
+  {
+    const bf16_t* q = static_cast<const bf16_t*>(a.q) + int64_t(from) * a.q_ld + h * DH + 8 * hi;
+    const bf16_t* g = static_cast<const bf16_t*>(a.dout) + int64_t(from) * a.do_ld + h * DH + 8 * hi;
 #pragma unroll
     for (int c = 0; c < kC; ++c) {
-      qf[t][c] = as_bf16x8(*reinterpret_cast<const u32x4*>(q + 16 * c));
-      gf[t][c] = as_bf16x8(*reinterpret_cast<const u32x4*>(g + 16 * c));
+      qf[c] = as_bf16x8(*reinterpret_cast<const u32x4*>(q + 16 * c));
+      gf[c] = as_bf16x8(*reinterpret_cast<const u32x4*>(g + 16 * c));
     }
-    lse2[t] = a.lse[int64_t(h) * a.M + row] * kLog2e;
-    delta[t] = a.delta[int64_t(h) * a.M + row];
-  }
-  f32x16 acc[2][kDT];
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[t][dt][r] = 0.f;
-  const float scale2 = kLog2e * a.scale;
-  const Frag<DH> frag;
-  uint32_t k_off[kL], v_off[kL];
-#pragma unroll
-  for (int i = 0; i < kL; ++i) {
-    k_off[i] = load_off<DH>(wave + 4 * i, a.k_ld);
-    v_off[i] = load_off<DH>(wave + 4 * i, a.v_ld);
+      for (int r = 0; r < 16; ++r) acc[dt][r] = 0.f;
   }
-  const uint32_t lds_w = lds_offset(smem) + wave * 1024;
+  const float2 st = a.stats[int64_t(h) * a.M + from];
+  const float lse2 = st.x * kLog2e, delta = st.y;
+  const float scale2 = kLog2e * a.scale;
+  Frag<DH> frag;
+  TileLoad<DH, kKB> lk(a.k_ld, wave), lv(a.v_ld, wave);
+  const uint32_t lds_w = lds_offset(smem) + wave * (kL * 1024);
   auto load = [&](int buf, int j) {
-    const int first = s.k_lo + j * kKB;
-    const u32x4 rk = rows_rsrc(K, a.k_ld, first, s.k_hi, DH), rv = rows_rsrc(V, a.v_ld, first, s.k_hi, DH);
-#pragma unroll
-    for (int i = 0; i < kL; ++i) lds_load16(lds_w + 2 * buf * kTB, k_off[i], rk, 0, 4096 * i);
-#pragma unroll
-    for (int i = 0; i < kL; ++i) lds_load16(lds_w + (2 * buf + 1) * kTB, v_off[i], rv, 0, 4096 * i);
+    lk.go(K, s.k_lo + j * kKB, s.k_hi, lds_w + 2 * buf * kTB);
+    lv.go(V, s.k_lo + j * kKB, s.k_hi, lds_w + (2 * buf + 1) * kTB);
   };
-  // Waits until at most `n` later tiles' loads are in flight.
-  auto landed = [](int n) {
-    if (n >= 2) vm_wait<4 * kL>();
-    else if (n == 1) vm_wait<2 * kL>();
-    else vm_wait<0>();
-  };
-  typedef f32x16 Pair[2];
-  // Slots of a step: kC of dP, kC of S, 2 kDT of dQ, each a fragment and its two products.
-  constexpr int kRd = 4, kSlots = 2 * kC + 2 * kDT;
-  const char* half = smem + 32 * wk * (DH * 2);
-  auto fragment = [&](int i, int buf, int nbuf) {
-    if (i < kC) return frag.rows(half + (2 * buf + 1) * kTB, i);
-    if (i < 2 * kC) return frag.rows(half + 2 * nbuf * kTB, i - kC);
-    return frag.columns(half + 2 * buf * kTB, (i - 2 * kC) / kDT, (i - 2 * kC) % kDT);
-  };
-  // Keys past the last: no probability.
-  auto mask = [&](int j, Pair& x) {
-    const int up = s.k_hi - s.k_lo - j * kKB - 32 * wk;
-    if (up >= 32) return;
-    asm volatile("" ::: "memory");
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-      if (8 * (r / 4) + r % 4 + 4 * hi >= up) x[0][r] = x[1][r] = -INFINITY;
-  };
-  // x: S(t), becoming probabilities; xn: S(t + 1).
+  // Slots of a step, each a fragment and its product: S and dP of half 0, of half 1, dQ of half 0, of half 1.
+  constexpr int kRd = 4, kG = 2 * kC, kQ = 2 * kDT, kSlots = 2 * kG + 2 * kQ;
+  f32x16 x[2], dp[2];
   bf16x8 ds[2][2];
-  auto step = [&](Pair& x, Pair& xn, int buf, int nbuf, auto before_s) {
-    Pair dp = {};
-    bf16x8 f[kRd];
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < kRd; ++i) f[i] = fragment(i, buf, nbuf);
-#pragma unroll
-    for (int i = 0; i < kSlots; ++i) {
-      __builtin_amdgcn_sched_barrier(0);
-      // The next tile's fragments may be read from here on.
-      if (i + kRd == kC) before_s();
-      const bf16x8 w = f[i % kRd];
-      if (i < kC) {
-        dp[0] = mfma32(w, gf[0][i], dp[0]);
-        dp[1] = mfma32(w, gf[1][i], dp[1]);
-      } else if (i < 2 * kC) {
-        const int c = i - kC;
-        xn[0] = mfma32(w, qf[0][c], c == 0 ? f32x16{} : xn[0]);
-        xn[1] = mfma32(w, qf[1][c], c == 0 ? f32x16{} : xn[1]);
-      } else {
-        const int c = (i - 2 * kC) / kDT, dt = (i - 2 * kC) % kDT;
-        acc[0][dt] = mfma32(w, ds[0][c], acc[0][dt]);
-        acc[1][dt] = mfma32(w, ds[1][c], acc[1][dt]);
-      }
-      if (i + kRd < kSlots) f[i % kRd] = fragment(i + kRd, buf, nbuf);
-      if (i < kC) {  // exponentials of 16 / kC registers of both
-#pragma unroll
-        for (int r = 16 * i / kC; r < 16 * (i + 1) / kC; ++r)
-#pragma unroll
-          for (int t = 0; t < 2; ++t) x[t][r] = __builtin_amdgcn_exp2f(fmaf(x[t][r], scale2, -lse2[t]));
-      } else if (i < 2 * kC) {  // ds, packed in pairs
-#pragma unroll
-        for (int r = 16 * (i - kC) / kC; r < 16 * (i - kC + 1) / kC; ++r)
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            x[t][r] *= dp[t][r] - delta[t];
-            if (r % 2 == 1) put(ds[t][r / 8], r, x[t][r - 1], x[t][r]);
-          }
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);
+  // Of half t: probabilities and ds, element n of 16.
+  auto grad = [&](auto tt, auto nn) AVITS_INLINE {
+    constexpr int t = decltype(tt)::value, n = decltype(nn)::value;
+    x[t][n] = __builtin_amdgcn_exp2f(fmaf(x[t][n], scale2, -lse2)) * (dp[t][n] - delta);
+    if constexpr (n % 2 == 1) put(ds[t][n / 8], n, x[t][n - 1], x[t][n]);
   };
   if (n_tiles > 0) {
-    // Key blocks of tiles t and t + 1; loads run up to three tiles ahead.
-    int j0 = walk.next(), j1 = -1, j2 = -1;
+    int j0 = walk.next(), buf = 0;
     load(0, j0);
-    if (n_tiles > 1) load(1, j1 = walk.next());
-    if (n_tiles > 2) load(2, j2 = walk.next());
-    landed(n_tiles - 1);
-    lds_barrier();
-    Pair xa = {}, xb = {};
+    for (int t = 0; t < n_tiles; ++t) {
+      // This tile has landed for every wave, and every wave is done with the last, whose place the next takes.
+      vm_wait<0>();
+      lds_barrier();
+      const int j = j0;
+      if (t + 1 < n_tiles) load(buf ^ 1, j0 = walk.next());
+      const char* kt = smem + 2 * buf * kTB;
+      const char* vt = kt + kTB;
+      const int up = s.k_hi - s.k_lo - j * kKB - 4 * hi;
+      frag.fresh();
+      auto fragment = [&](auto ii) AVITS_INLINE {
+        constexpr int i = decltype(ii)::value;
+        if constexpr (i < 2 * kG) {
+          constexpr int half = i / kG, c = i % kG;
+          return frag.rows((c < kC ? kt : vt) + 32 * half * (DH * 2), c % kC);
+        } else {
+          constexpr int k = i - 2 * kG;
+          return frag.columns(kt, k / kDT, k % kDT);
+        }
+      };
+      bf16x8 f[kRd];
+      __builtin_amdgcn_sched_barrier(0);
+      each<kRd>([&](auto i) AVITS_INLINE { f[decltype(i)::value] = fragment(i); });
+      each<kSlots>([&](auto slot) AVITS_INLINE {
+        constexpr int i = decltype(slot)::value;
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (i == kG || i == 2 * kG) {
+          // Keys past the last: no probability.
+          constexpr int half = i / kG - 1;
+          if (up - 32 * half < 32 - 4 * hi) {
+            asm volatile("" ::: "memory");
 #pragma unroll
-    for (int c = 0; c < kC; ++c) {
-      const bf16x8 f = frag.rows(half, c);
-      xa[0] = mfma32(f, qf[0][c], xa[0]);
-      xa[1] = mfma32(f, qf[1][c], xa[1]);
-    }
-    auto one = [&](int t, Pair& x, Pair& xn) {
-      mask(j0, x);
-      step(x, xn, t & 3, (t + 1) & 3, [&]() {
-        // Tile t + 1 has landed for every wave, and every wave is done with tile t - 1, whose place tile t + 3 takes.
-        // (On the last tile what lies in the next place is read, and its products are not used.)
-        if (t + 1 >= n_tiles) return;
-        landed(std::min(1, n_tiles - t - 2));  // tile t + 2 may be on its way
-        lds_barrier();
-        j0 = j1;
-        j1 = j2;
-        if (t + 3 < n_tiles) load((t + 3) & 3, j2 = walk.next());
+            for (int r = 0; r < 16; ++r)
+              if (32 * half + 8 * (r / 4) + r % 4 >= up) x[half][r] = -INFINITY;
+          }
+        }
+        if constexpr (i < 2 * kG) {
+          constexpr int half = i / kG, c = i % kG;
+          if constexpr (c < kC) x[half] = mfma32(f[i % kRd], qf[c], c == 0 ? f32x16{} : x[half]);
+          else dp[half] = mfma32(f[i % kRd], gf[c - kC], c == kC ? f32x16{} : dp[half]);
+        } else {
+          constexpr int k = i - 2 * kG, c = k / kDT;
+          acc[k % kDT] = mfma32(f[i % kRd], ds[c / 2][c % 2], acc[k % kDT]);
+        }
+        if constexpr (i + kRd < kSlots) f[i % kRd] = fragment(Int<i + kRd>{});
+        if constexpr (i >= kG && i < 2 * kG) {
+          constexpr int n = i - kG;
+          each<16 * (n + 1) / kG - 16 * n / kG>([&](auto e) AVITS_INLINE { grad(Int<0>{}, Int<16 * n / kG + decltype(e)::value>{}); });
+        } else if constexpr (i >= 2 * kG && i < 2 * kG + kQ) {
+          constexpr int n = i - 2 * kG;
+          each<16 * (n + 1) / kQ - 16 * n / kQ>([&](auto e) AVITS_INLINE { grad(Int<1>{}, Int<16 * n / kQ + decltype(e)::value>{}); });
+        }
       });
-    };
-    int t = 0;
-    for (; t + 1 < n_tiles; t += 2) {
-      one(t, xa, xb);
-      one(t + 1, xb, xa);
+      __builtin_amdgcn_sched_barrier(0);
+      buf ^= 1;
     }
-    if (t < n_tiles) one(t, xa, xb);
   }
-  // The two key halves: each wave leaves one 32-row half of its sums and adds the other's.
-  lds_barrier();
-  float* sums = reinterpret_cast<float*>(smem) + wq * 64 * kP;
-  {
-    const int give = 1 - wk;
+  if (row >= q_end) return;
+  if (item.z > 1) {  // a piece: its sums to its slot
+    float* to = a.part + (sparse_slot(a, units, item.w, item.y) * kQB + (row - q_first)) * DH + 4 * hi;
 #pragma unroll
     for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f32x16& o = give ? acc[1][dt] : acc[0][dt];
-        *reinterpret_cast<f32x4*>(sums + (32 * give + l32) * kP + 32 * dt + 8 * q + 4 * hi) =
-            f32x4{o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]};
-      }
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4*>(to + 32 * dt + 8 * q) =
+            f32x4{acc[dt][4 * q], acc[dt][4 * q + 1], acc[dt][4 * q + 2], acc[dt][4 * q + 3]};
+    return;
   }
-  lds_barrier();
-  const int row = q_first + 64 * wq + 32 * wk + l32;
-  if (row >= q_end) return;
   bf16_t* dst = static_cast<bf16_t*>(a.dq) + int64_t(row) * a.dq_ld + h * DH + 4 * hi;
-#pragma unroll
-  for (int dt = 0; dt < kDT; ++dt)
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const f32x16& o = wk ? acc[1][dt] : acc[0][dt];
-      f32x4 v = *reinterpret_cast<const f32x4*>(sums + (32 * wk + l32) * kP + 32 * dt + 8 * q + 4 * hi);
-      // Key half 0 first, whichever wave adds.
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = (o[4 * q + e] + v[e]) * a.scale;
-      *reinterpret_cast<u32x2*>(dst + 32 * dt + 8 * q) = u32x2{pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3])};
-    }
+  store_sums<DH>(dst, acc, a.scale);
 }
 
 // ---------------------------------------------------------------------------
-// dk and dv.  Wave w takes rows 32 w .. of every query block, all 64 keys, from LDS of its own: no
-// barrier until the four waves' sums meet at the end.
+// dk and dv.  Eight waves: wave (k, q) = (w % 2, w / 2) takes keys 32 k .. and rows 32 q .. of each query block; the
+// four waves of a key half meet in LDS at the end.
+// The values' fragments stay in registers, the keys' are read from LDS: with both in registers no more
+// than two fragments could be under way, and every product waited for its own (205 us at 4608
+// rows, 16 heads of 128, where this takes TODO).
 constexpr int kItems = 4096;  // (head, query block) pairs looked at together
 
 template <int DH>
-__global__ __launch_bounds__(256, 1) void sparse_dkv_bf16_kernel(const SparseArgs a) {
-  constexpr int kC = DH / 16, kDT = DH / 32, kTB = 32 * DH * 2, kL = kTB / 1024;
-  constexpr int kP = DH + 4, kWaveBytes = 4 * kTB;  // two of the queries' and two of the gradients' tiles
-  constexpr int kBytes = std::max(4 * kWaveBytes, 4 * 64 * kP * 4);
+__global__ __launch_bounds__(512, 2) void sparse_dkv_bf16_kernel(const SparseArgs a) {
+  constexpr int kC = DH / 16, kDT = DH / 32, kTB = kQB * DH * 2;
+  constexpr int kP = DH + 4;  // floats to a row of the sums
+  constexpr int kBytes = std::max(4 * kTB, 8 * 32 * kP * 4);
   __shared__ __attribute__((aligned(16))) char smem[kBytes];
-  __shared__ __attribute__((aligned(16))) char vt[kKB * DH * 2];  // the key block's values
-  __shared__ __attribute__((aligned(16))) float stats[4][64];
+  __shared__ __attribute__((aligned(16))) char keys[kKB * DH * 2];
+  __shared__ __attribute__((aligned(16))) float stats[8][64];
   __shared__ uint64_t bits[kItems / 64];
-  const int Hk = a.H / a.group, hk = blockIdx.x % Hk, blk = blockIdx.x / Hk;
+  const int Hk = a.H / a.group, units = a.seq.k_blk[kMaxSeqs] * Hk;
+  const int4 item = sparse_item(a, units, blockIdx.x);
+  if (item.x < 0) return;
+  const int hk = item.x % Hk, blk = item.x / Hk;
   const Seq s = seq_of<true>(a.seq, blk);
   const int lane = threadIdx.x % kWave, l32 = lane % 32, hi = lane / 32;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wk = wave % 2, wq = wave / 2;
   const int k_first = s.k_lo + (blk - s.kb) * kKB, nq = (s.q_hi - s.q_lo + kQB - 1) / kQB, items = nq * a.group;
+  const int row = k_first + 32 * wk + l32;
 
-  // The keys stay in registers; for the values there is no room beside the sums (they spilled 89 registers).
-  bf16x8 kf[2][kC];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int row = std::min(k_first + 32 * t + l32, s.k_hi - 1);  // keys past the last: not stored
-    const bf16_t* k = static_cast<const bf16_t*>(a.k) + int64_t(row) * a.k_ld + hk * DH + 8 * hi;
-#pragma unroll
-    for (int c = 0; c < kC; ++c) kf[t][c] = as_bf16x8(*reinterpret_cast<const u32x4*>(k + 16 * c));
-  }
+  bf16x8 vf[kC];
   {
-    const u32x4 rv = rows_rsrc(static_cast<const bf16_t*>(a.v) + int64_t(hk) * DH, a.v_ld, k_first, s.k_hi, DH);
+    const int from = std::min(row, s.k_hi - 1);  // keys past the last: not stored
+    const bf16_t* v = static_cast<const bf16_t*>(a.v) + int64_t(from) * a.v_ld + hk * DH + 8 * hi;
 #pragma unroll
-    for (int i = 0; i < kKB * DH * 2 / 4096; ++i)
-      lds_load16(lds_offset(vt) + wave * 1024, load_off<DH>(wave + 4 * i, a.v_ld), rv, 0, 4096 * i);
-    vm_wait<0>();  // the barriers before the first step make it every wave's
+    for (int c = 0; c < kC; ++c) vf[c] = as_bf16x8(*reinterpret_cast<const u32x4*>(v + 16 * c));
   }
-  f32x16 dk[2][kDT], dv[2][kDT];
+  f32x16 dk[kDT], dv[kDT];
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+  for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
-    for (int dt = 0; dt < kDT; ++dt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) dk[t][dt][r] = dv[t][dt][r] = 0.f;
+    for (int r = 0; r < 16; ++r) dk[dt][r] = dv[dt][r] = 0.f;
   const float scale2 = kLog2e * a.scale, unscale = 1.f / a.scale;
   Frag<DH> frag;
-  // An instruction's rows repeat their swizzle after kOff instructions.
-  constexpr int kR = kWave / (DH / 8), kOff = 16 / kR, kRd = 4, kSlots = 2 * kC + 4 * kDT;
-  static_assert(kSlots % kRd == 0, "the fragments' ring closes over a step");
-  uint32_t q_off[kOff], g_off[kOff];
-#pragma unroll
-  for (int i = 0; i < kOff; ++i) {
-    q_off[i] = load_off<DH>(i, a.q_ld);
-    g_off[i] = load_off<DH>(i, a.do_ld);
-  }
-  char* mine = smem + wave * kWaveBytes;
-  const uint32_t lds_w = lds_offset(mine);
+  TileLoad<DH, kQB> lq(a.q_ld, wave), lg(a.do_ld, wave);
+  constexpr int kShare = kTB / 8;  // bytes of a tile that a wave loads
+  const uint32_t lds_w = lds_offset(smem) + wave * kShare;
+  TileLoad<DH, kKB, 8>(a.k_ld, wave).go(static_cast<const bf16_t*>(a.k) + int64_t(hk) * DH, k_first, s.k_hi,
+                                     lds_offset(keys) + wave * (kKB * DH * 2 / 8));
 
+  int left = 0x7fffffff, skip = 0;  // pairs of this piece still to come, and those before it
   for (int base = 0; base < items; base += kItems) {
     const int n = std::min(kItems, items - base);
     __syncthreads();
-    for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += 256) {
+    for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += 512) {
       const int e = base + i;
       const bool on = i < n && kept(a, hk * a.group + e / nq, s.qb + e % nq, blk - s.kb);
       const uint64_t w = __ballot(on);
       if (lane == 0) bits[i / 64] = w;
     }
     __syncthreads();
+    if (item.z > 1 && base == 0) {  // only lists that fit at once are cut
+      int total = 0;
+      for (int w = 0; 64 * w < n; ++w) total += __popcll(bits[w]);
+      total = __builtin_amdgcn_readfirstlane(total);
+      skip = int(int64_t(total) * item.y / item.z);
+      left = int(int64_t(total) * (item.y + 1) / item.z) - skip;
+    }
     // The kept pairs, one ahead of the products.
     int word = -1;
     uint64_t cur = 0;
     auto next = [&]() {
+      if (left == 0) return -1;
       while (cur == 0) {
         if (64 * ++word >= n) return -1;
         const uint64_t w = bits[word];
         cur = uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(w >> 32)))) << 32 | uint32_t(__builtin_amdgcn_readfirstlane(int(w)));
+        for (; skip > 0 && cur != 0; --skip) cur &= cur - 1;
       }
-      const int i = 64 * word + __builtin_ctzll(cur);
+      --left;
+      const int e = base + 64 * word + __builtin_ctzll(cur);
       cur &= cur - 1;
-      return base + i;
+      return e;
     };
-    float stat = 0.f;  // lanes 0 .. 31: lse of the pair's rows that are on their way, the others: delta
+    float stat = 0.f;  // lanes 0 .. 31: lse of the wave's rows of the tile on its way, the others: delta
     auto load = [&](int buf, int e) {
-      const int h = hk * a.group + e / nq, first = s.q_lo + (e % nq) * kQB + 32 * wave;
-      const u32x4 rq = rows_rsrc(static_cast<const bf16_t*>(a.q) + int64_t(h) * DH, a.q_ld, first, s.q_hi, DH);
-      const u32x4 rg = rows_rsrc(static_cast<const bf16_t*>(a.dout) + int64_t(h) * DH, a.do_ld, first, s.q_hi, DH);
-      const uint32_t q_step = uint32_t(a.q_ld) * (2 * kR), g_step = uint32_t(a.do_ld) * (2 * kR);
-#pragma unroll
-      for (int i = 0; i < kL; ++i) lds_load16(lds_w + 2 * buf * kTB, q_off[i % kOff], rq, i / kOff * kOff * q_step, 1024 * i);
-#pragma unroll
-      for (int i = 0; i < kL; ++i) lds_load16(lds_w + (2 * buf + 1) * kTB, g_off[i % kOff], rg, i / kOff * kOff * g_step, 1024 * i);
+      const int h = hk * a.group + e / nq, first = s.q_lo + (e % nq) * kQB;
+      lq.go(static_cast<const bf16_t*>(a.q) + int64_t(h) * DH, first, s.q_hi, lds_w + 2 * buf * kTB);
+      lg.go(static_cast<const bf16_t*>(a.dout) + int64_t(h) * DH, first, s.q_hi, lds_w + (2 * buf + 1) * kTB);
       // Rows past the last: no probability.
-      const float* p = hi ? a.delta : a.lse;
+      const int r = first + 32 * wq + l32;
       stat = hi ? 0.f : INFINITY;
-      if (first + l32 < s.q_hi) stat = p[int64_t(h) * a.M + first + l32];
+      if (r < s.q_hi) stat = reinterpret_cast<const float*>(a.stats + int64_t(h) * a.M)[2 * int64_t(r) + hi];
     };
-    // A step's 32 (DH = 64: 16) slots, each a fragment and its two products, in a fixed order: S, dP with the
-    // exponentials, dV with ds, dK with the start of the next step.
-    f32x16 x[2], dp[2];
-    bf16x8 f[kRd], vv[2][2], pb[2][2], db[2][2];
-    auto fragment = [&](int i, const char* qt) {
-      const char* gt = qt + kTB;
-      if (i < kC) return frag.rows(qt, i);
-      if (i < 2 * kC) return frag.rows(gt, i - kC);
-      if (i < 2 * kC + 2 * kDT) return frag.columns(gt, (i - 2 * kC) / kDT, (i - 2 * kC) % kDT);
-      return frag.columns(qt, (i - 2 * kC - 2 * kDT) / kDT, (i - 2 * kC - 2 * kDT) % kDT);
-    };
-    // The pair that has landed: logits less lse / scale, and dp less delta, start from what is taken away.
-    auto begin = [&]() {
+    // Slots of a step, each a fragment and its product: S (with a fragment of the keys too), dP, dV, dK.
+    constexpr int kRd = 4, kRk = 3, kQ = 2 * kDT, kSlots = 2 * kC + 2 * kQ;
+    int e1 = next(), buf = 0;
+    if (e1 >= 0) load(0, e1);
+    while (e1 >= 0) {
+      // The tile has landed for every wave, and every wave is done with the last, whose place the next takes.
       vm_wait<0>();
       stats[wave][lane] = hi ? -stat : -stat * unscale;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f32x4 m = *reinterpret_cast<const f32x4*>(&stats[wave][8 * q + 4 * hi]);
-        const f32x4 d = *reinterpret_cast<const f32x4*>(&stats[wave][32 + 8 * q + 4 * hi]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          x[0][4 * q + r] = x[1][4 * q + r] = m[r];
-          dp[0][4 * q + r] = dp[1][4 * q + r] = d[r];
-        }
-      }
-    };
-    int e0 = next(), e1 = -1, buf = 0;
-    if (e0 >= 0) {
-      load(0, e0);
-      begin();
-      if ((e1 = next()) >= 0) load(1, e1);
-#pragma unroll
-      for (int i = 0; i < kRd; ++i) f[i] = fragment(i, mine);
-    }
-    while (e0 >= 0) {
-      const char* qt = mine + 2 * buf * kTB;
-      const char* nt = mine + 2 * (buf ^ 1) * kTB;
+      lds_barrier();
+      e1 = next();
+      if (e1 >= 0) load(buf ^ 1, e1);
+      const char* qt = smem + 2 * buf * kTB + 32 * wq * (DH * 2);
+      const char* gt = qt + kTB;
+      const char* kt = keys + 32 * wk * (DH * 2);
+      f32x16 x, dp;
+      bf16x8 f[kRd], fk[kRk], pb[2], db[2];
       frag.fresh();
+      lq.fresh();
+      lg.fresh();
+      auto fragment = [&](auto ii) AVITS_INLINE {
+        constexpr int i = decltype(ii)::value;
+        if constexpr (i < kC) return frag.rows(qt, i);
+        else if constexpr (i < 2 * kC) return frag.rows(gt, i - kC);
+        else if constexpr (i < 2 * kC + kQ) return frag.columns(gt, (i - 2 * kC) / kDT, (i - 2 * kC) % kDT);
+        else return frag.columns(qt, (i - 2 * kC - kQ) / kDT, (i - 2 * kC - kQ) % kDT);
+      };
+      // Logits less lse / scale, and dp less delta, start from what is taken away.
+      auto begin = [&](f32x16& y, int at) AVITS_INLINE {
 #pragma unroll
-      for (int i = 0; i < kSlots; ++i) {
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 m = *reinterpret_cast<const f32x4*>(&stats[wave][at + 8 * q + 4 * hi]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) y[4 * q + r] = m[r];
+        }
+      };
+      begin(x, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      each<kRk>([&](auto i) AVITS_INLINE { fk[decltype(i)::value] = frag.rows(kt, decltype(i)::value); });
+      each<kRd>([&](auto i) AVITS_INLINE { f[decltype(i)::value] = fragment(i); });
+      each<kSlots>([&](auto slot) AVITS_INLINE {
+        constexpr int i = decltype(slot)::value;
         __builtin_amdgcn_sched_barrier(0);
         const bf16x8 w = f[i % kRd];
-        if (i < kC) {
-          x[0] = mfma32(w, kf[0][i], x[0]);
-          x[1] = mfma32(w, kf[1][i], x[1]);
-        } else if (i < 2 * kC) {
-          dp[0] = mfma32(w, vv[i % 2][0], dp[0]);
-          dp[1] = mfma32(w, vv[i % 2][1], dp[1]);
-        } else if (i < 2 * kC + 2 * kDT) {
-          const int c = (i - 2 * kC) / kDT, dt = (i - 2 * kC) % kDT;
-          dv[0][dt] = mfma32(w, pb[0][c], dv[0][dt]);
-          dv[1][dt] = mfma32(w, pb[1][c], dv[1][dt]);
-        } else {
-          const int c = (i - 2 * kC - 2 * kDT) / kDT, dt = (i - 2 * kC - 2 * kDT) % kDT;
-          dk[0][dt] = mfma32(w, db[0][c], dk[0][dt]);
-          dk[1][dt] = mfma32(w, db[1][c], dk[1][dt]);
+        if constexpr (i < kC) x = mfma32(w, fk[i % kRk], x);
+        else if constexpr (i < 2 * kC) dp = mfma32(w, vf[i - kC], dp);
+        else if constexpr (i < 2 * kC + kQ) dv[(i - 2 * kC) % kDT] = mfma32(w, pb[(i - 2 * kC) / kDT], dv[(i - 2 * kC) % kDT]);
+        else dk[(i - 2 * kC - kQ) % kDT] = mfma32(w, db[(i - 2 * kC - kQ) / kDT], dk[(i - 2 * kC - kQ) % kDT]);
+        if constexpr (i + kRk < kC) fk[i % kRk] = frag.rows(kt, i + kRk);
+        if constexpr (i == kC - kRk) begin(dp, 32);
+        if constexpr (i + kRd < kSlots) f[i % kRd] = fragment(Int<i + kRd>{});
+        if constexpr (i >= kC && i < 2 * kC) {  // exponentials under dP
+          constexpr int k = i - kC;
+          each<16 * (k + 1) / kC - 16 * k / kC>([&](auto e) AVITS_INLINE {
+            constexpr int r = 16 * k / kC + decltype(e)::value;
+            x[r] = __builtin_amdgcn_exp2f(x[r] * scale2);
+            if constexpr (r % 2 == 1) put(pb[r / 8], r, x[r - 1], x[r]);
+          });
+        } else if constexpr (i >= 2 * kC && i < 2 * kC + kQ) {  // ds under dV
+          constexpr int k = i - 2 * kC;
+          each<16 * (k + 1) / kQ - 16 * k / kQ>([&](auto e) AVITS_INLINE {
+            constexpr int r = 16 * k / kQ + decltype(e)::value;
+            dp[r] *= x[r];
+            if constexpr (r % 2 == 1) put(db[r / 8], r, dp[r - 1], dp[r]);
+          });
         }
-        if (i == 2 * kC + 2 * kDT && e1 >= 0) begin();
-        if (i + 2 >= kC && i + 2 < 2 * kC) {
-          vv[i % 2][0] = frag.rows(vt, i + 2 - kC);
-          vv[i % 2][1] = frag.rows(vt + 32 * (DH * 2), i + 2 - kC);
-        }
-        // Near the end the next pair's first fragments (stale ones, unused, where there is none).
-        f[i % kRd] = i + kRd < kSlots ? fragment(i + kRd, qt) : fragment(i + kRd - kSlots, nt);
-        if (i >= kC && i < 2 * kC) {
-#pragma unroll
-          for (int r = 16 * (i - kC) / kC; r < 16 * (i - kC + 1) / kC; ++r)
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-              x[t][r] = __builtin_amdgcn_exp2f(x[t][r] * scale2);
-              if (r % 2 == 1) put(pb[t][r / 8], r, x[t][r - 1], x[t][r]);
-            }
-        } else if (i >= 2 * kC && i < 2 * kC + 2 * kDT) {
-          const int n = 2 * kDT, k = i - 2 * kC;
-#pragma unroll
-          for (int r = 16 * k / n; r < 16 * (k + 1) / n; ++r)
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-              dp[t][r] *= x[t][r];
-              if (r % 2 == 1) put(db[t][r / 8], r, dp[t][r - 1], dp[t][r]);
-            }
-        }
-      }
+      });
       __builtin_amdgcn_sched_barrier(0);
-      // This pair's reads are done: its place is the one after the next's.
-      e0 = e1;
-      if (e0 >= 0) {
-        asm volatile("s_waitcnt lgkmcnt(%0)" ::"n"(kRd) : "memory");
-        if ((e1 = next()) >= 0) load(buf, e1);
-      }
       buf ^= 1;
     }
   }
-  // The waves' sums, dk's then dv's.
+  // The four row quarters of a key half, dk's then dv's; each of its waves adds up a quarter of the columns.
   float* sums = reinterpret_cast<float*>(smem);
-#pragma unroll
-  for (int which = 0; which < 2; ++which) {
+  each<2>([&](auto which) AVITS_INLINE {
+    constexpr bool is_dv = decltype(which)::value;
     __syncthreads();
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
-      for (int dt = 0; dt < kDT; ++dt)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x16& o = which ? dv[t][dt] : dk[t][dt];
-          *reinterpret_cast<f32x4*>(sums + (64 * wave + 32 * t + l32) * kP + 32 * dt + 8 * q + 4 * hi) =
-              f32x4{o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]};
-        }
+      for (int q = 0; q < 4; ++q) {
+        const f32x16& o = is_dv ? dv[dt] : dk[dt];
+        *reinterpret_cast<f32x4*>(sums + (64 * wq + 32 * wk + l32) * kP + 32 * dt + 8 * q + 4 * hi) =
+            f32x4{o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]};
+      }
     __syncthreads();
-    bf16_t* out = static_cast<bf16_t*>(which ? a.dv : a.dk);
-    const int64_t ld = which ? a.dv_ld : a.dk_ld;
-    for (int i = threadIdx.x; i < 64 * (DH / 8); i += 256) {
+    bf16_t* out = static_cast<bf16_t*>(is_dv ? a.dv : a.dk);
+    const int64_t ld = is_dv ? a.dv_ld : a.dk_ld;
+    const float f = is_dv ? 1.f : a.scale;
+    float* slot = a.part + (sparse_slot(a, units, item.w, item.y) * 2 + is_dv) * (kKB * DH);
+    for (int i = threadIdx.x; i < kKB * DH / 8; i += 512) {
       const int r = i / (DH / 8), c = i % (DH / 8) * 8;
       if (k_first + r >= s.k_hi) continue;
       f32x4 v[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const float* p = sums + r * kP + c + 4 * u;
         f32x4 w[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const f32x4*>(p + 64 * k * kP);
+        for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const f32x4*>(sums + (64 * k + r) * kP + c + 4 * u);
         v[u] = (w[0] + w[1]) + (w[2] + w[3]);
+        if (item.z > 1) *reinterpret_cast<f32x4*>(slot + r * DH + c + 4 * u) = v[u];
+        v[u] *= f;
       }
-      *reinterpret_cast<u32x4*>(out + int64_t(k_first + r) * ld + int64_t(hk) * DH + c) = pack_sums(v[0], v[1], which ? 1.f : a.scale);
+      if (item.z > 1) continue;
+      *reinterpret_cast<u32x4*>(out + int64_t(k_first + r) * ld + int64_t(hk) * DH + c) =
+          u32x4{pack_bf2(v[0][0], v[0][1]), pack_bf2(v[0][2], v[0][3]), pack_bf2(v[1][0], v[1][1]), pack_bf2(v[1][2], v[1][3])};
     }
+  });
+}
+
+// The pieces of cut lists added up in order: eight columns to a thread.  dq: 128 rows to a unit; dk, dv: 64 of each.
+template <int DH, bool KEYS>
+__global__ __launch_bounds__(256) void sparse_sum_kernel(const SparseArgs a) {
+  constexpr int kL = DH / 8, kR = 256 / kL, kPer = kQB / kR;
+  const int4 cut = sparse_cut(a, blockIdx.x / kPer);
+  if (cut.x < 0) return;
+  const int Hu = KEYS ? a.H / a.group : a.H, units = a.seq.q_blk[kMaxSeqs] * Hu;
+  const int blk = cut.x / Hu, h = cut.x % Hu, r = blockIdx.x % kPer * kR + threadIdx.x / kL, c = threadIdx.x % kL * 8;
+  const Seq s = seq_of<KEYS>(a.seq, blk);
+  const bool is_dv = KEYS && r >= kKB;
+  const int row = KEYS ? s.k_lo + (blk - s.kb) * kKB + r % kKB : s.q_lo + (blk - s.qb) * kQB + r;
+  if (row >= (KEYS ? s.k_hi : s.q_hi)) return;
+  const float* p = a.part + (cut.z * int64_t(kQB) + r) * DH + c;
+  const int64_t step = (sparse_slot(a, units, cut.z, 1) - cut.z) * kQB * DH;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+#pragma unroll 4
+  for (int i = 0; i < cut.y; ++i) {
+    x += *reinterpret_cast<const f32x4*>(p + i * step);
+    y += *reinterpret_cast<const f32x4*>(p + i * step + 4);
   }
+  if (!is_dv) x *= a.scale, y *= a.scale;
+  bf16_t* out = static_cast<bf16_t*>(KEYS ? (is_dv ? a.dv : a.dk) : a.dq);
+  const int64_t ld = KEYS ? (is_dv ? a.dv_ld : a.dk_ld) : a.dq_ld;
+  *reinterpret_cast<u32x4*>(out + int64_t(row) * ld + int64_t(h) * DH + c) =
+      u32x4{pack_bf2(x[0], x[1]), pack_bf2(x[2], x[3]), pack_bf2(y[0], y[1]), pack_bf2(y[2], y[3])};
 }
 
 template <int DH>
-void launch_back(const SparseArgs& a, hipStream_t s) {
-  const unsigned nq = unsigned(a.seq.q_blk[kMaxSeqs]), nk = unsigned(a.seq.k_blk[a.seq.B]);
-  if (nq > 0) hipLaunchKernelGGL((sparse_dq_bf16_kernel<DH>), dim3(nq * unsigned(a.H)), dim3(256), 0, s, a);
-  if (nk > 0) hipLaunchKernelGGL((sparse_dkv_bf16_kernel<DH>), dim3(nk * unsigned(a.H / a.group)), dim3(256), 0, s, a);
+void launch_back(const SparseArgs& q, const SparseArgs& k, hipStream_t s) {
+  constexpr int kPer = kQB * DH / 8 / 256;
+  const int64_t uq = int64_t(q.seq.q_blk[kMaxSeqs]) * q.H, uk = int64_t(q.seq.k_blk[kMaxSeqs]) * (q.H / q.group);
+  if (uq > 0) hipLaunchKernelGGL((sparse_dq_bf16_kernel<DH>), dim3(unsigned(uq + q.slots)), dim3(256), 0, s, q);
+  if (uk > 0) hipLaunchKernelGGL((sparse_dkv_bf16_kernel<DH>), dim3(unsigned(uk + k.slots)), dim3(512), 0, s, k);
+  if (q.plan) hipLaunchKernelGGL((sparse_sum_kernel<DH, false>), dim3(unsigned(std::min<int64_t>(kShares, q.slots) * kPer)), dim3(256), 0, s, q);
+  if (k.plan) hipLaunchKernelGGL((sparse_sum_kernel<DH, true>), dim3(unsigned(std::min<int64_t>(kShares, k.slots) * kPer)), dim3(256), 0, s, k);
 }
 
 }  // namespace
 
-void launch_sparse_back_bf16(const SparseArgs& a, hipStream_t s) {
-  if (a.d == 128) launch_back<128>(a, s);
-  else launch_back<64>(a, s);
+void launch_sparse_back_bf16(const SparseArgs& q, const SparseArgs& k, hipStream_t s) {
+  if (q.d == 128) launch_back<128>(q, k, s);
+  else launch_back<64>(q, k, s);
 }
 
 }  // namespace avits
