@@ -89,9 +89,11 @@ __global__ __launch_bounds__(256) void block_means_kernel(const MeanArgs a) {
 // Scores and choice.  A workgroup takes up to 16 query blocks of a head of one
 // sequence: their scores against all key blocks by 16x16x4 products in 64 bits into
 // LDS, then a wave for each row finds the n-th largest by its bits, from the highest, with the keys in registers
-// where a row has at most 64 kHeld of them (read from LDS for each bit they took 41 us at 264 key blocks, 132
-// query blocks and 16 heads).
-constexpr int kSelWaves = 16;
+// where there are at most 512.
+// Times at 264 key blocks, 132 query blocks and 16 heads of 128: keys read from LDS for each bit 42 us, from registers 30;
+// the products' operands fetched as a lane needs them, 64 bytes of each of 16 rows to an instruction, kept the L1
+// cache busy for 20 us of these: a row's bytes are now fetched together and change lanes in LDS.
+constexpr int kSelWaves = 8;
 constexpr int kMaxKeyBlocks = 16384;  // 128 KiB of scores for one row
 
 struct SelectArgs {
@@ -104,6 +106,7 @@ struct SelectArgs {
   int groups[kMaxSeqs + 1];  // workgroups (of a head) before each sequence
 };
 
+typedef double f64x2 __attribute__((ext_vector_type(2)));
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 
 // Order-preserving: NaN below every number, -0 as +0.
@@ -113,10 +116,9 @@ __device__ __forceinline__ uint64_t order_key(double v) {
   return u >> 63 ? ~u : u | (uint64_t(1) << 63);
 }
 
-constexpr int kHeld = 8;
-
-// The choice of one row by a wave: key(t) is the ordered score of key block 64 t + lane (0 past the last).
-template <bool HELD, class Key>
+// The choice of one row by a wave: key(t) is the ordered score of key block 64 t + lane, 0 for those that do not
+// compete (the leading ones, and past the last).  HELD: the number of tiles, from registers (0: any).
+template <int HELD, class Key>
 __device__ __forceinline__ void choose(const Key& key, int tiles, int nk, int lead, int n, bool all, int words, uint64_t* out) {
   const int lane = threadIdx.x % kWave;
   // Which of a tile's blocks compete: those past the leading ones.
@@ -131,19 +133,17 @@ __device__ __forceinline__ void choose(const Key& key, int tiles, int nk, int le
   for (int bit = 63; bit >= 0 && !exact; --bit) {
     const uint64_t cand = top | (uint64_t(1) << bit);
     int count = 0;
-    _Pragma("unroll(HELD ? kHeld : 1)") for (int t = 0; t < (HELD ? kHeld : tiles); ++t)
-      if (t < tiles) count += __popcll(__ballot(key(t) >= cand) & rest(t));
+    _Pragma("unroll(HELD ? HELD : 1)") for (int t = 0; t < (HELD ? HELD : tiles); ++t) count += __popcll(__ballot(key(t) >= cand));
     if (count >= n) top = cand;
     exact = count == n;
   }
   int spare = 0;  // how many of the keys equal to the threshold count
   if (!exact) {
     int above = 0;
-    _Pragma("unroll(HELD ? kHeld : 1)") for (int t = 0; t < (HELD ? kHeld : tiles); ++t)
-      if (t < tiles) above += __popcll(__ballot(key(t) > top) & rest(t));
+    _Pragma("unroll(HELD ? HELD : 1)") for (int t = 0; t < (HELD ? HELD : tiles); ++t) above += __popcll(__ballot(key(t) > top));
     spare = n - above;
   }
-  _Pragma("unroll(HELD ? kHeld : 1)") for (int t = 0; t < (HELD ? kHeld : tiles); ++t) {
+  _Pragma("unroll(HELD ? HELD : 1)") for (int t = 0; t < (HELD ? HELD : tiles); ++t) {
     if (t >= tiles) continue;
     const uint64_t in = rest(t), k = key(t);
     const uint64_t past = nk - 64 * t >= 64 ? ~uint64_t(0) : (uint64_t(1) << (nk - 64 * t)) - 1;
@@ -161,33 +161,56 @@ __device__ __forceinline__ void choose(const Key& key, int tiles, int nk, int le
   for (int w = tiles + lane; w < words; w += kWave) out[w] = 0;
 }
 
+template <int D>
 __global__ __launch_bounds__(64 * kSelWaves) void block_select_kernel(const SelectArgs a) {
-  extern __shared__ __attribute__((aligned(16))) uint64_t keys[];  // [rows][nk]
-  const int h = blockIdx.y, hk = h / (a.H / a.Hk), lane = threadIdx.x % kWave, l16 = lane % 16, g = lane / 16;
+  extern __shared__ __attribute__((aligned(16))) uint64_t keys[];
+  // Heads vary fastest over the workgroups: a head's stay on one XCD (for multiples of eight), whose L2 then reads its
+  // keys' means once.
+  const int h = blockIdx.x % a.H, group = blockIdx.x / a.H, hk = h / (a.H / a.Hk), lane = threadIdx.x % kWave, l16 = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   int q_blk = a.seq.q_blk[0], q_end = a.seq.q_blk[1], k_blk = a.seq.k_blk[0], nk = a.seq.k_blk[1] - k_blk, g0 = 0;
 #pragma unroll
   for (int b = 1; b < kMaxSeqs; ++b)
-    if (b < a.seq.B && int(blockIdx.x) >= a.groups[b])
+    if (b < a.seq.B && group >= a.groups[b])
       q_blk = a.seq.q_blk[b], q_end = a.seq.q_blk[b + 1], k_blk = a.seq.k_blk[b], nk = a.seq.k_blk[b + 1] - k_blk, g0 = a.groups[b];
-  const int i0 = (int(blockIdx.x) - g0) * a.rows;  // the workgroup's first query block of its sequence
+  const int i0 = (group - g0) * a.rows;  // the workgroup's first query block of its sequence
   const int n_rows = std::min(a.rows, q_end - q_blk - i0);
   const int lead = std::min(nk, (a.k_lead + kKB - 1) / kKB);
-  const double* Q = a.qm + (int64_t(q_blk + i0 + std::min(l16, n_rows - 1)) * a.H + h) * a.d;
+  // 16 rows in product order (lane l: row l % 16, of each eight elements those at 2 (l / 16)), fetched a
+  // quarter (or half) row to 16 lanes, 16-byte chunk c of row r through LDS at c ^ r.
+  char* mine = reinterpret_cast<char*>(keys) + wave * 4096;
+  auto rows16 = [&](const double* base, int64_t ld, int last, f64x2(&f)[D / 8]) __attribute__((always_inline)) {
+    f64x2 raw[D / 8];
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        raw[4 * c + i] = *reinterpret_cast<const f64x2*>(base + std::min(4 * i + g, last) * ld + 32 * c + 2 * l16);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<f64x2*>(mine + (4 * i + g) * 256 + ((l16 ^ (4 * i + g)) * 16)) = raw[4 * c + i];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[4 * c + i] = *reinterpret_cast<const f64x2*>(mine + l16 * 256 + (((4 * i + g) ^ l16) * 16));
+    }
+  };
+  uint64_t* scores = keys + kSelWaves * 512;  // [rows][nk]
+  f64x2 q[D / 8];
+  if (16 * wave < nk) rows16(a.qm + (int64_t(q_blk + i0) * a.H + h) * D, int64_t(a.H) * D, n_rows - 1, q);
   for (int t = wave; 16 * t < nk; t += kSelWaves) {
-    const double* K = a.km + (int64_t(k_blk + std::min(16 * t + l16, nk - 1)) * a.Hk + hk) * a.d;
-    f64x4 acc = {0.0, 0.0, 0.0, 0.0};
-#pragma unroll 8
-    for (int c = 0; c < a.d; c += 8) {
-      const double2 q = *reinterpret_cast<const double2*>(Q + c + 2 * g), k = *reinterpret_cast<const double2*>(K + c + 2 * g);
-      acc = __builtin_amdgcn_mfma_f64_16x16x4f64(q.x, k.x, acc, 0, 0, 0);
-      acc = __builtin_amdgcn_mfma_f64_16x16x4f64(q.y, k.y, acc, 0, 0, 0);
+    f64x2 k[D / 8];
+    rows16(a.km + (int64_t(k_blk + 16 * t) * a.Hk + hk) * D, int64_t(a.Hk) * D, nk - 16 * t - 1, k);
+    f64x4 acc = {0.0, 0.0, 0.0, 0.0}, odd = acc;
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) {
+      acc = __builtin_amdgcn_mfma_f64_16x16x4f64(q[c].x, k[c].x, acc, 0, 0, 0);
+      odd = __builtin_amdgcn_mfma_f64_16x16x4f64(q[c].y, k[c].y, odd, 0, 0, 0);
     }
     // Register r holds row 4 r + lane / 16 of column lane % 16.
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int row = 4 * r + g;
-      if (row < n_rows && 16 * t + l16 < nk) keys[int64_t(row) * nk + 16 * t + l16] = order_key(acc[r]);
+      if (row < n_rows && 16 * t + l16 < nk) scores[int64_t(row) * nk + 16 * t + l16] = order_key(acc[r] + odd[r]);
     }
   }
   __syncthreads();
@@ -195,16 +218,21 @@ __global__ __launch_bounds__(64 * kSelWaves) void block_select_kernel(const Sele
   for (int r = wave; r < n_rows; r += kSelWaves) {
     const int i = i0 + r;
     const bool all = int64_t(i) * kQB < a.q_lead;
-    const uint64_t* row = keys + int64_t(r) * nk;
+    const uint64_t* row = scores + int64_t(r) * nk;
     uint64_t* out = a.mask + (int64_t(h) * a.seq.q_blk[kMaxSeqs] + q_blk + i) * a.words;
-    if (tiles <= kHeld) {
-      uint64_t held[kHeld];
+    auto at = [&](int t) { return 64 * t + lane < nk && 64 * t + lane >= lead ? row[64 * t + lane] : 0; };
+    auto held = [&](auto tag) {
+      constexpr int T = decltype(tag)::value;
+      uint64_t k[T];
 #pragma unroll
-      for (int t = 0; t < kHeld; ++t) held[t] = 64 * t + lane < nk ? row[64 * t + lane] : 0;
-      choose<true>([&](int t) { return held[t]; }, tiles, nk, lead, n, all, int(a.words), out);
-    } else {
-      choose<false>([&](int t) { return 64 * t + lane < nk ? row[64 * t + lane] : 0; }, tiles, nk, lead, n, all, int(a.words), out);
-    }
+      for (int t = 0; t < T; ++t) k[t] = at(t);
+      choose<T>([&](int t) { return k[t]; }, tiles, nk, lead, n, all, int(a.words), out);
+    };
+    if (tiles <= 1) held(std::integral_constant<int, 1>());
+    else if (tiles <= 2) held(std::integral_constant<int, 2>());
+    else if (tiles <= 4) held(std::integral_constant<int, 4>());
+    else if (tiles <= 8) held(std::integral_constant<int, 8>());
+    else choose<0>(at, tiles, nk, lead, n, all, int(a.words), out);
   }
 }
 
@@ -277,12 +305,13 @@ extern "C" int avits_block_select(const double* q_means, const double* k_means, 
   a.rows = std::max(1, std::min(16, kMaxKeyBlocks / std::max(nk, 1)));
   for (int b = 0; b < B; ++b) a.groups[b + 1] = a.groups[b] + (a.seq.q_blk[b + 1] - a.seq.q_blk[b] + a.rows - 1) / a.rows;
   a.seq.q_blk[kMaxSeqs] = nq;
-  const size_t lds = size_t(a.rows) * nk * sizeof(uint64_t);
+  const size_t lds = size_t(a.rows) * nk * sizeof(uint64_t) + kSelWaves * 4096;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(&block_select_kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                             kMaxKeyBlocks * int(sizeof(uint64_t))) != hipSuccess)
+  const auto kernel = d == 128 ? &block_select_kernel<128> : &block_select_kernel<64>;
+  if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                             kMaxKeyBlocks * int(sizeof(uint64_t)) + kSelWaves * 4096) != hipSuccess)
     return set_error(AVITS_ERR_HIP, "block_select: no %zu bytes of LDS", lds);
   TimedLaunch timed("block_select", s);
-  hipLaunchKernelGGL(block_select_kernel, dim3(unsigned(a.groups[B]), unsigned(H)), dim3(64 * kSelWaves), lds, s, a);
+  hipLaunchKernelGGL(kernel, dim3(unsigned(a.groups[B]) * unsigned(H)), dim3(64 * kSelWaves), lds, s, a);
   return launch_status("block_select");
 }
