@@ -57,8 +57,9 @@ __device__ __forceinline__ void turn_of(float f, float& s, float& c) {
 // whole vectors, as neighbours otherwise.
 template <typename T, bool HALVES, bool VEC>
 struct Lane {
-  int a[VEC ? 1 : 4], b[VEC ? 1 : 4];
-  __device__ __forceinline__ Lane(int p0, int rot) {
+  uint32_t a[VEC ? 1 : 4], b[VEC ? 1 : 4];
+  // head: where the lane's head of a step starts.
+  __device__ __forceinline__ Lane(int p0, int rot, int head) {
     if constexpr (VEC) {
       a[0] = 2 * p0;
       b[0] = 2 * p0 + 4;
@@ -66,66 +67,67 @@ struct Lane {
         a[0] = p0;
         b[0] = p0 + rot / 2;
       }
+      a[0] += head;
+      b[0] += head;
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int p = p0 + i;
         const bool split = HALVES && p < rot / 2;
-        a[i] = split ? p : 2 * p;
-        b[i] = split ? p + rot / 2 : 2 * p + 1;
+        a[i] = head + (split ? p : 2 * p);
+        b[i] = head + (split ? p + rot / 2 : 2 * p + 1);
       }
     }
   }
-  __device__ __forceinline__ static void four(const T* p, float* v) {
-    if constexpr (sizeof(T) == 4) {
-      const f32x4 w = *reinterpret_cast<const f32x4*>(p);
+  // Eight elements as they lie in memory.
+  static constexpr int kWords = VEC ? 2 * sizeof(T) : 8;
+  struct Raw {
+    uint32_t w[kWords];
+  };
+  __device__ __forceinline__ Raw fetch(const T* p) const {
+    Raw r;
+    if constexpr (!VEC) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = w[i];
-    } else {
-      const u32x2 w = *reinterpret_cast<const u32x2*>(p);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) r.w[i] = __float_as_uint(p[a[i]]), r.w[4 + i] = __float_as_uint(p[b[i]]);
+        else r.w[i] = uint32_t(p[a[i]]) << 16, r.w[4 + i] = uint32_t(p[b[i]]) << 16;
       }
+    } else if constexpr (sizeof(T) == 4) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(p + a[0]), y = *reinterpret_cast<const u32x4*>(p + b[0]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.w[i] = x[i], r.w[4 + i] = y[i];
+    } else if constexpr (HALVES) {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(p + a[0]), y = *reinterpret_cast<const u32x2*>(p + b[0]);
+      r.w[0] = x[0], r.w[1] = x[1], r.w[2] = y[0], r.w[3] = y[1];
+    } else {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(p + a[0]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.w[i] = x[i];
+    }
+    return r;
+  }
+  // The first and the second elements of the four pairs.
+  __device__ __forceinline__ static void unpack(const Raw& r, float* va, float* vb) {
+    float v[8];
+    if constexpr (kWords == 8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.w[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(r.w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(r.w[i] & 0xffff0000u);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      va[i] = v[HALVES || !VEC ? i : 2 * i];
+      vb[i] = v[HALVES || !VEC ? 4 + i : 2 * i + 1];
     }
   }
   __device__ __forceinline__ static void put4(T* p, const float* v) {
     if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
     else *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3])};
-  }
-  // The first and the second elements of the four pairs.
-  __device__ __forceinline__ void load(const T* p, float* va, float* vb) const {
-    if constexpr (VEC) {
-      if constexpr (HALVES) {
-        four(p + a[0], va);
-        four(p + b[0], vb);
-      } else {
-        float v[8];
-        if constexpr (sizeof(T) == 4) {
-          four(p + a[0], v);
-          four(p + a[0] + 4, v + 4);
-        } else {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(p + a[0]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          va[i] = v[2 * i];
-          vb[i] = v[2 * i + 1];
-        }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        va[i] = ld(p, a[i]);
-        vb[i] = ld(p, b[i]);
-      }
-    }
   }
   __device__ __forceinline__ void store(T* p, const float* va, const float* vb) const {
     if constexpr (VEC) {
@@ -150,200 +152,210 @@ struct Lane {
   }
 };
 
-// The turns of a row's four pairs of this lane (pairs past rot: none).
+// The turns of a row's four pairs of this lane; `on` of them turn, the first ones.
 template <typename T>
 struct Turns {
-  double f[4];
-  int axis[4];
+  double f[4];  // turns to a position
+  int axis[4], on;
   __device__ __forceinline__ Turns(const RopeArgs& a, int p0) {
+    on = std::min(4, std::max(0, a.rot / 2 - p0));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int p = p0 + i;
-      axis[i] = -1;
       f[i] = 0.0;
-      if (2 * p < a.rot) {
-        f[i] = a.freq[p];
-        axis[i] = 0;
+      axis[i] = 0;
+      if (i < on) {
+        f[i] = a.freq[p0 + i] * a.pos_scale * 0.15915494309189533577;
 #pragma unroll
-        for (int x = 0; x < kMaxAxes - 1; ++x) axis[i] += x < a.axes - 1 && p >= a.end[x] ? 1 : 0;
+        for (int x = 0; x < kMaxAxes - 1; ++x) axis[i] += x < a.axes - 1 && p0 + i >= a.end[x] ? 1 : 0;
       }
     }
   }
   __device__ __forceinline__ void at(const RopeArgs& a, int64_t row, float* s, float* c) const {
+    if (on == 0) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      s[i] = 0.f;
-      c[i] = 1.f;
-      if (axis[i] >= 0) {
-        const double turns = double(a.pos[row * a.axes + axis[i]]) * a.pos_scale * f[i] * 0.15915494309189533577;
-        turn_of<T>(float(turns - rint(turns)), s[i], c[i]);
+      const double turns = double(a.pos[row * a.axes + axis[i]]) * f[i];
+      turn_of<T>(float(turns - rint(turns)), s[i], c[i]);
+    }
+  }
+  // (a, b) to (a c - b s, a s + b c).  Elements that do not turn are no pair: what one holds is not the other's.
+  __device__ __forceinline__ void turn(float* va, float* vb, const float* s, const float* c) const {
+    if (on == 0) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = va[i] * c[i] - vb[i] * s[i], y = va[i] * s[i] + vb[i] * c[i];
+      if (on == 4 || i < on) {
+        va[i] = x;
+        vb[i] = y;
       }
     }
   }
 };
 
+// The part of the queries' (or keys') steps, kHPW heads each, that falls to part p of n.
+struct Span {
+  int lo, up;
+  __device__ __forceinline__ Span(int heads, int hpw, int p, int n) {
+    const int steps = (heads + hpw - 1) / hpw;
+    lo = steps * p / n;
+    up = steps * (p + 1) / n;
+  }
+};
+
+template <typename T, int DH, bool HALVES, bool VEC>
+__device__ __forceinline__ void load_gain(const Lane<T, HALVES, VEC>& at, uint32_t head, const void* gain, float* ga, float* gb) {
+  const T* p = static_cast<const T*>(gain);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    ga[i] = gb[i] = 1.f;
+    if (p) {  // the gain itself need not lie on 16 bytes
+      ga[i] = ld(p, (VEC ? (HALVES ? at.a[0] + i : at.a[0] + 2 * i) : at.a[VEC ? 0 : i]) - head);
+      gb[i] = ld(p, (VEC ? (HALVES ? at.b[0] + i : at.a[0] + 2 * i + 1) : at.b[VEC ? 0 : i]) - head);
+    }
+  }
+}
+
+// Bound by HBM: each row is read and written once.  The first kU steps of the queries and of the keys are under
+// way together (16 heads of 128 each: the whole row), as they lie in memory, to hold few registers.
 template <typename T, int DH, bool HALVES, bool VEC>
 __global__ __launch_bounds__(256) void qk_rotate_kernel(const RopeArgs a) {
   constexpr int kLPH = DH / 8, kHPW = kWave / kLPH, kU = 4;  // lanes to a head, heads to a step, steps at once
+  typedef Lane<T, HALVES, VEC> At;
   const int lane = threadIdx.x % kWave, p0 = 4 * (lane % kLPH), sub = lane / kLPH;
-  const int64_t wave = int64_t(blockIdx.x) * 4 + threadIdx.x / kWave;
+  const int64_t wave = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int part = int(wave % a.parts);
   const int64_t first = wave / a.parts * a.per, last = std::min(a.M, first + a.per);
-  const int heads = a.H[0] + a.H[1], steps = (heads + kHPW - 1) / kHPW;
-  const int s_lo = steps * part / a.parts, s_hi = steps * (part + 1) / a.parts;
   if (first >= last) return;
-  const Lane<T, HALVES, VEC> at(p0, a.rot);
+  const At at(p0, a.rot, sub * DH);
   const Turns<T> turns(a, p0);
-  float g[2][8];
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) g[w][i] = 1.f;
-    if (a.g[w]) {
-      const Lane<T, HALVES, false> one(p0, a.rot);
-      const T* gw = static_cast<const T*>(a.g[w]);
-      if constexpr (VEC) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          g[w][i] = ld(gw, HALVES ? at.a[0] + i : 2 * (p0 + i));
-          g[w][4 + i] = ld(gw, HALVES ? at.b[0] + i : 2 * (p0 + i) + 1);
-        }
-      } else {
-        one.load(gw, g[w], g[w] + 4);
-      }
-    }
-  }
+  const Span span[2] = {Span(a.H[0], kHPW, part, a.parts), Span(a.H[1], kHPW, part, a.parts)};
   for (int64_t row = first; row < last; ++row) {
+    typename At::Raw raw[2][kU];
+    auto fetch = [&](int w, int st) {
+      const T* in = static_cast<const T*>(a.x[w]) + row * a.x_ld[w];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int t = (st + u) * kHPW + sub;
+        if (st + u < span[w].up && t < a.H[w]) raw[w][u] = at.fetch(in + (st + u) * (kHPW * DH));
+      }
+    };
+#pragma unroll
+    for (int w = 0; w < 2; ++w) fetch(w, span[w].lo);
     float s[4], c[4];
     turns.at(a, row, s, c);
-    for (int st = s_lo; st < s_hi; st += kU) {
-      float va[kU][4], vb[kU][4];
 #pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        const int t = (st + u) * kHPW + sub;
-        if (st + u < s_hi && t < heads) {
-          const int w = t >= a.H[0];
-          const T* p = static_cast<const T*>(w ? a.x[1] : a.x[0]) + row * (w ? a.x_ld[1] : a.x_ld[0]) +
-                       int64_t(w ? t - a.H[0] : t) * DH;
-          at.load(p, va[u], vb[u]);
+    for (int w = 0; w < 2; ++w) {
+      if (span[w].lo >= span[w].up) continue;
+      float ga[4], gb[4];
+      load_gain<T, DH>(at, sub * DH, a.g[w], ga, gb);
+      T* out = static_cast<T*>(a.out[w]) + row * a.out_ld[w];
+      for (int st = span[w].lo; st < span[w].up; st += kU) {
+        if (st > span[w].lo) fetch(w, st);
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const int t = (st + u) * kHPW + sub;
+          if (st + u >= span[w].up || t >= a.H[w]) continue;
+          float va[4], vb[4];
+          at.unpack(raw[w][u], va, vb);
+          if (a.eps > 0.f) {
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += va[i] * va[i] + vb[i] * vb[i];
+            const float r = rsqrtf(group_sum(sum, kLPH) * (1.f / DH) + a.eps);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              va[i] *= r * ga[i];
+              vb[i] *= r * gb[i];
+            }
+          }
+          turns.turn(va, vb, s, c);
+          at.store(out + (st + u) * (kHPW * DH), va, vb);
         }
-      }
-#pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        const int t = (st + u) * kHPW + sub;
-        if (st + u >= s_hi || t >= heads) continue;
-        const int w = t >= a.H[0];
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum += va[u][i] * va[u][i] + vb[u][i] * vb[u][i];
-        sum = group_sum(sum, kLPH);
-        const float r = a.eps > 0.f ? rsqrtf(sum * (1.f / DH) + a.eps) : 1.f;
-        float oa[4], ob[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float ya = va[u][i] * r * (w ? g[1][i] : g[0][i]), yb = vb[u][i] * r * (w ? g[1][4 + i] : g[0][4 + i]);
-          // Elements that do not turn are no pair: what one holds is not the other's.
-          const bool on = turns.axis[i] >= 0;
-          oa[i] = on ? ya * c[i] - yb * s[i] : ya;
-          ob[i] = on ? ya * s[i] + yb * c[i] : yb;
-        }
-        T* p = static_cast<T*>(w ? a.out[1] : a.out[0]) + row * (w ? a.out_ld[1] : a.out_ld[0]) +
-               int64_t(w ? t - a.H[0] : t) * DH;
-        at.store(p, oa, ob);
       }
     }
   }
 }
 
+constexpr int kBackWaves = 8;  // waves of a workgroup of the backward pass
+
 template <typename T, int DH, bool HALVES, bool VEC>
-__global__ __launch_bounds__(256) void qk_rotate_back_kernel(const RopeArgs a) {
+__global__ __launch_bounds__(64 * kBackWaves, VEC && sizeof(T) == 2 ? 3 : 2) void qk_rotate_back_kernel(const RopeArgs a) {
   constexpr int kLPH = DH / 8, kHPW = kWave / kLPH, kU = 2;
-  __shared__ float red[4][2][DH];
+  __shared__ float red[kBackWaves][2][DH];
   const int lane = threadIdx.x % kWave, p0 = 4 * (lane % kLPH), sub = lane / kLPH;
-  const int64_t wave = int64_t(blockIdx.x) * 4 + threadIdx.x / kWave;
-  const int part = int(wave % a.parts);
-  const int64_t first = wave / a.parts * a.per, last = std::min(a.M, first + a.per);
-  const int heads = a.H[0] + a.H[1], steps = (heads + kHPW - 1) / kHPW;
-  const int s_lo = steps * part / a.parts, s_hi = steps * (part + 1) / a.parts;
-  const Lane<T, HALVES, VEC> at(p0, a.rot);
+  const int64_t wave = int64_t(blockIdx.x) * kBackWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  // (row, part) pairs, a.per of them one after another to a wave.
+  const int64_t first = wave * a.per, last = std::min(a.M * a.parts, first + a.per);
+  typedef Lane<T, HALVES, VEC> At;
+  const At at(p0, a.rot, sub * DH);
   const Turns<T> turns(a, p0);
-  float g[2][8], acc[2][8];
+  float acc[2][8];
 #pragma unroll
-  for (int w = 0; w < 2; ++w) {
+  for (int w = 0; w < 2; ++w)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) g[w][i] = 1.f, acc[w][i] = 0.f;
-    if (a.g[w]) {
-      const T* gw = static_cast<const T*>(a.g[w]);
-      if constexpr (VEC) {
+    for (int i = 0; i < 8; ++i) acc[w][i] = 0.f;
+  for (int64_t unit = first; unit < last; ++unit) {
+    const int64_t row = unit / a.parts;
+    const int part = int(unit % a.parts);
+    const Span span[2] = {Span(a.H[0], kHPW, part, a.parts), Span(a.H[1], kHPW, part, a.parts)};
+    typename At::Raw rx[2][kU], ry[2][kU];
+    auto fetch = [&](int w, int st) {
+      const T* in = static_cast<const T*>(a.x[w]) + row * a.x_ld[w];
+      const T* dy = static_cast<const T*>(a.dy[w]) + row * a.dy_ld[w];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          g[w][i] = ld(gw, HALVES ? at.a[0] + i : 2 * (p0 + i));
-          g[w][4 + i] = ld(gw, HALVES ? at.b[0] + i : 2 * (p0 + i) + 1);
+      for (int u = 0; u < kU; ++u) {
+        const int t = (st + u) * kHPW + sub;
+        if (st + u < span[w].up && t < a.H[w]) {
+          ry[w][u] = at.fetch(dy + (st + u) * (kHPW * DH));
+          rx[w][u] = at.fetch(in + (st + u) * (kHPW * DH));
         }
-      } else {
-        at.load(gw, g[w], g[w] + 4);
       }
-    }
-  }
-  for (int64_t row = first; row < last; ++row) {
+    };
+#pragma unroll
+    for (int w = 0; w < 2; ++w) fetch(w, span[w].lo);
     float s[4], c[4];
     turns.at(a, row, s, c);
-    for (int st = s_lo; st < s_hi; st += kU) {
-      float va[kU][4], vb[kU][4], ea[kU][4], eb[kU][4];
 #pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        const int t = (st + u) * kHPW + sub;
-        if (st + u < s_hi && t < heads) {
-          const int w = t >= a.H[0];
-          const int64_t col = int64_t(w ? t - a.H[0] : t) * DH;
-          at.load(static_cast<const T*>(w ? a.x[1] : a.x[0]) + row * (w ? a.x_ld[1] : a.x_ld[0]) + col, va[u], vb[u]);
-          at.load(static_cast<const T*>(w ? a.dy[1] : a.dy[0]) + row * (w ? a.dy_ld[1] : a.dy_ld[0]) + col, ea[u], eb[u]);
-        }
-      }
+    for (int i = 0; i < 4; ++i) s[i] = -s[i];  // back
 #pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        const int t = (st + u) * kHPW + sub;
-        if (st + u >= s_hi || t >= heads) continue;
-        const int w = t >= a.H[0];
-        // The gradient turned back.
+    for (int w = 0; w < 2; ++w) {
+      if (span[w].lo >= span[w].up) continue;
+      float ga[4], gb[4];
+      load_gain<T, DH>(at, sub * DH, a.g[w], ga, gb);
+      T* out = static_cast<T*>(a.out[w]) + row * a.out_ld[w];
+      for (int st = span[w].lo; st < span[w].up; st += kU) {
+        if (st > span[w].lo) fetch(w, st);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float da = ea[u][i] * c[i] + eb[u][i] * s[i], db = eb[u][i] * c[i] - ea[u][i] * s[i];
-          const bool on = turns.axis[i] >= 0;
-          ea[u][i] = on ? da : ea[u][i];
-          eb[u][i] = on ? db : eb[u][i];
-        }
-        if (a.eps > 0.f) {
-          float sum = 0.f;
+        for (int u = 0; u < kU; ++u) {
+          const int t = (st + u) * kHPW + sub;
+          if (st + u >= span[w].up || t >= a.H[w]) continue;
+          float va[4], vb[4], ea[4], eb[4];
+          at.unpack(ry[w][u], ea, eb);
+          at.unpack(rx[w][u], va, vb);
+          turns.turn(ea, eb, s, c);
+          if (a.eps > 0.f) {
+            float sum = 0.f, dot = 0.f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sum += va[u][i] * va[u][i] + vb[u][i] * vb[u][i];
-          const float r = rsqrtf(group_sum(sum, kLPH) * (1.f / DH) + a.eps);
-          float dot = 0.f;
+            for (int i = 0; i < 4; ++i) sum += va[i] * va[i] + vb[i] * vb[i];
+            const float r = rsqrtf(group_sum(sum, kLPH) * (1.f / DH) + a.eps);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float na = va[u][i] * r, nb = vb[u][i] * r;
-            const float ta = ea[u][i] * na, tb = eb[u][i] * nb;
-            acc[0][i] += w ? 0.f : ta;
-            acc[0][4 + i] += w ? 0.f : tb;
-            acc[1][i] += w ? ta : 0.f;
-            acc[1][4 + i] += w ? tb : 0.f;
-            const float ga = w ? g[1][i] : g[0][i], gb = w ? g[1][4 + i] : g[0][4 + i];
-            ea[u][i] *= ga;
-            eb[u][i] *= gb;
-            dot += ta * ga + tb * gb;
-            va[u][i] = na;
-            vb[u][i] = nb;
+            for (int i = 0; i < 4; ++i) {
+              va[i] *= r;
+              vb[i] *= r;
+              const float ta = ea[i] * va[i], tb = eb[i] * vb[i];
+              acc[w][i] += ta;
+              acc[w][4 + i] += tb;
+              dot += ta * ga[i] + tb * gb[i];
+            }
+            dot = group_sum(dot, kLPH) * (1.f / DH);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              ea[i] = r * (ea[i] * ga[i] - va[i] * dot);
+              eb[i] = r * (eb[i] * gb[i] - vb[i] * dot);
+            }
           }
-          dot = group_sum(dot, kLPH) * (1.f / DH);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            ea[u][i] = r * (ea[u][i] - va[u][i] * dot);
-            eb[u][i] = r * (eb[u][i] - vb[u][i] * dot);
-          }
+          at.store(out + (st + u) * (kHPW * DH), ea, eb);
         }
-        T* p = static_cast<T*>(w ? a.out[1] : a.out[0]) + row * (w ? a.out_ld[1] : a.out_ld[0]) +
-               int64_t(w ? t - a.H[0] : t) * DH;
-        at.store(p, ea[u], eb[u]);
       }
     }
   }
@@ -359,44 +371,63 @@ __global__ __launch_bounds__(256) void qk_rotate_back_kernel(const RopeArgs a) {
       if (sub == 0) {
         int e;
         if constexpr (VEC) e = HALVES ? (i < 4 ? at.a[0] + i : at.b[0] + i - 4) : 2 * (p0 + i % 4) + i / 4;
-        else e = i < 4 ? at.a[i % 4] : at.b[i % 4];
+        else e = i < 4 ? at.a[i % 4] : at.b[i % 4];  // head 0's lanes: no offset
         red[threadIdx.x / kWave][w][e] = v;
       }
     }
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * DH; i += 256) {
-    const float* r = &red[0][0][0] + i;
-    a.part[int64_t(blockIdx.x) * 2 * DH + i] = (r[0] + r[2 * DH]) + (r[4 * DH] + r[6 * DH]);
+  for (int i = threadIdx.x; i < 2 * DH; i += 64 * kBackWaves) {
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < kBackWaves; ++k) v += red[k][i / DH][i % DH];
+    a.part[int64_t(blockIdx.x) * 2 * DH + i] = v;
   }
 }
 
-// The workgroups' sums added up: 32 columns, eight strands of rows to a workgroup.
-__global__ __launch_bounds__(256) void gain_sum_kernel(const float* part, int64_t n, int d, float* dgq, float* dgk) {
-  __shared__ float red[8][32];
-  const int col = blockIdx.x * 32 + threadIdx.x % 32, strand = threadIdx.x / 32;
+// The workgroups' sums added up: 32 columns, 32 strands of rows to a workgroup.
+__global__ __launch_bounds__(1024) void gain_sum_kernel(const float* part, int64_t n, int d, float* dgq, float* dgk) {
+  __shared__ float red[32][33];
+  const int lane = threadIdx.x % 32, col = blockIdx.x * 32 + lane, strand = threadIdx.x / 32;
   float v = 0.f;
-#pragma unroll 8
-  for (int64_t i = strand; i < n; i += 8) v += part[i * 2 * d + col];
-  red[strand][threadIdx.x % 32] = v;
+  for (int64_t i = strand; i < n; i += 32 * 8) {  // eight rows under way together
+    float x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = i + 32 * u < n ? part[(i + 32 * u) * 2 * d + col] : 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v += x[u];
+  }
+  red[strand][lane] = v;
   __syncthreads();
   if (strand != 0) return;
   v = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v += red[i][threadIdx.x];
+  for (int i = 0; i < 32; ++i) v += red[i][lane];
   float* dst = col < d ? dgq : dgk;
   if (dst) dst[col % d] = v;
 }
 
-// Rows of a wave and waves to a row: enough waves for every SIMD of the chip
-// to hold several, then as many heads to a wave as that leaves.
-void plan(RopeArgs& a, int d, int64_t waves) {
-  const int hpw = kWave / (d / 8), steps = (a.H[0] + a.H[1] + hpw - 1) / hpw;
-  a.per = std::max<int64_t>(1, ceil_div64(a.M, waves));
-  a.parts = int(std::min<int64_t>(steps, std::max<int64_t>(1, waves / ceil_div64(a.M, a.per))));
+// Forward: rows of a wave, and waves to a row where rows are few: about kForwardWaves waves (fewer where a wave would
+// have no step of the queries or the keys).
+constexpr int64_t kForwardWaves = 16384;
+int most_parts(const RopeArgs& a, int d) {
+  const int hpw = kWave / (d / 8);
+  return (std::max(a.H[0], a.H[1]) + hpw - 1) / hpw;
 }
-constexpr int64_t kForwardWaves = 16384, kBackwardWaves = 2048;
-
-int64_t workgroups(const RopeArgs& a) { return ceil_div64(ceil_div64(a.M, a.per) * a.parts, 4); }
+void plan_forward(RopeArgs& a, int d) {
+  a.per = std::max<int64_t>(1, a.M / kForwardWaves);
+  const int64_t units = ceil_div64(a.M, a.per);
+  a.parts = int(std::min<int64_t>(most_parts(a, d), std::max<int64_t>(1, (kForwardWaves + units / 2) / units)));
+}
+// Backward: each wave ends with a sum over its lanes and its workgroup's, so there are no more than the chip holds
+// at once, with as many (row, part) pairs each; parts of two steps of the queries and two of the keys, which
+// are under way together.
+constexpr int64_t kBackwardWaves = 3072;
+void plan_backward(RopeArgs& a, int d) {
+  a.parts = std::max(1, most_parts(a, d) / 2);
+  if (a.M * a.parts < kBackwardWaves) a.parts = int(std::min<int64_t>(most_parts(a, d), ceil_div64(kBackwardWaves, a.M)));
+  a.per = ceil_div64(a.M * a.parts, kBackwardWaves);
+}
+int64_t back_workgroups(const RopeArgs& a) { return ceil_div64(ceil_div64(a.M * a.parts, a.per), kBackWaves); }
 
 bool whole(const void* p, int64_t ld, size_t elem) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * int64_t(elem) % 16 == 0;
@@ -404,7 +435,8 @@ bool whole(const void* p, int64_t ld, size_t elem) {
 
 template <typename T, bool BACK, int DH, bool HALVES>
 void launch_layout(const RopeArgs& a, bool vec, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(workgroups(a))), block(256);
+  const dim3 grid(static_cast<unsigned>(BACK ? back_workgroups(a) : ceil_div64(ceil_div64(a.M, a.per) * a.parts, 4)));
+  const dim3 block(BACK ? 64 * kBackWaves : 256);
   if constexpr (BACK) {
     if (vec) hipLaunchKernelGGL((qk_rotate_back_kernel<T, DH, HALVES, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((qk_rotate_back_kernel<T, DH, HALVES, false>), grid, block, 0, s, a);
@@ -481,9 +513,10 @@ int fill(RopeArgs& a, const char* what, const void* q, int64_t q_ld, const void*
 
 // Enough for the plan of any number of rows up to M.
 size_t part_bytes(int64_t M, int32_t H, int32_t Hk, int32_t d) {
-  const int hpw = kWave / (d / 8), steps = (H + Hk + hpw - 1) / hpw;
-  const int64_t wgs = ceil_div64(std::min<int64_t>(kBackwardWaves, std::max<int64_t>(M, 1) * steps), 4);
-  return size_t(wgs) * 2 * d * sizeof(float);
+  RopeArgs a{};
+  a.H[0] = H, a.H[1] = Hk;
+  const int64_t waves = std::min<int64_t>(kBackwardWaves, std::max<int64_t>(M, 1) * most_parts(a, d));
+  return size_t(ceil_div64(waves, kBackWaves)) * 2 * d * sizeof(float);
 }
 
 }  // namespace
@@ -516,7 +549,7 @@ extern "C" int avits_qk_norm_rope(const void* q, int64_t q_ld, const void* k, in
   RopeArgs a;
   const int rc = fill(a, "qk_norm_rope", q, q_ld, k, k_ld, M, H, Hk, d, g_q, g_k, eps, rope, dtype, q_out, qo_ld, k_out, ko_ld);
   if (rc != AVITS_OK || M == 0) return rc;
-  plan(a, d, kForwardWaves);
+  plan_forward(a, d);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const bool halves = rope && rope->layout == AVITS_ROPE_HALVES;
   TimedLaunch timed("qk_norm_rope", s);
@@ -563,15 +596,15 @@ extern "C" int avits_qk_norm_rope_backward(const void* dq_out, int64_t dqo_ld, c
     a.part = static_cast<float*>(workspace);
   }
   if (M == 0 && !sums) return AVITS_OK;
-  if (M > 0) plan(a, d, kBackwardWaves);
+  if (M > 0) plan_backward(a, d);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const bool halves = rope && rope->layout == AVITS_ROPE_HALVES;
   TimedLaunch timed(what, s);
-  const int64_t n = M == 0 ? 0 : workgroups(a);
+  const int64_t n = M == 0 ? 0 : back_workgroups(a);
   if (M > 0) {
     if (dtype == AVITS_BF16) launch_type<bf16_t, true>(a, d, halves, s);
     else launch_type<float, true>(a, d, halves, s);
   }
-  if (sums) hipLaunchKernelGGL(gain_sum_kernel, dim3(2 * d / 32), dim3(256), 0, s, a.part, n, d, dg_q, dg_k);
+  if (sums) hipLaunchKernelGGL(gain_sum_kernel, dim3(2 * d / 32), dim3(1024), 0, s, a.part, n, d, dg_q, dg_k);
   return launch_status(what);
 }
