@@ -500,7 +500,7 @@ extern "C" int avits_sparse_attention_backward(const avits_rows* dout, const avi
       a.part = reinterpret_cast<float*>(at + plan_bytes());
       at += plan_bytes() + size_t(a.slots) * kQB * d * sizeof(float);
     }
-    if (planned(uk, mask != nullptr) && most_k <= 4096) {  // a cut list is walked at once
+    if (planned(uk, mask != nullptr)) {
       ak.plan = plan_k = reinterpret_cast<SparsePlan*>(at);
       ak.slots = sparse_slots(uk, most_k);
       ak.part = reinterpret_cast<float*>(at + plan_bytes());

@@ -49,7 +49,7 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
   const int H = a.H, units = a.seq.q_blk[kMaxSeqs] * H;
   const int4 item = sparse_item(a, units, blockIdx.x);
   if (item.x < 0) return;
-  const int h = item.x % H, blk = item.x / H, piece = item.y, pieces = item.z;
+  const int h = item.x % H, blk = item.x / H, piece = item.y & 0xffff, pieces = item.y >> 16;
   const Seq s = seq_of<false>(a.seq, blk);
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -97,10 +97,13 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
       return r;
     };
     // Rows past the sequence's last come back as zeros.
-    auto load_tile = [&](const bf16_t* base, int64_t ld, const uint32_t* off, int j, uint32_t dst) {
+    auto rows_of = [&](const bf16_t* base, int64_t ld, int j) {
       const int first = s.k_lo + j * kKB;
       const int64_t bytes = (int64_t(s.k_hi - first - 1) * ld + DH) * 2;
-      const u32x4 r = uniform(buffer_rsrc(base + int64_t(first) * ld, range32(bytes)));
+      return uniform(buffer_rsrc(base + int64_t(first) * ld, range32(bytes)));
+    };
+    auto load_tile = [&](const bf16_t* base, int64_t ld, const uint32_t* off, int j, uint32_t dst) {
+      const u32x4 r = rows_of(base, ld, j);
 #pragma unroll
       for (int i = 0; i < kL; ++i) lds_load16(dst, off[i], r, 0, 1024 * NW * i);
     };
@@ -195,7 +198,10 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
     };
     // Slots [lo, up) of a step (the V fragments' products, then the K fragments') with the softmax of
     // (x, p) spread over them, in this order.
-    auto run = [&](auto lo_tag, auto up_tag, auto soft_tag, int kbuf, int vbuf, STile& x, STile& sn, const PTile& pp, PTile& p) {
+    // `loads(k)`, k < 2 kL, are spread over the first slots: issued together they hold up the wave, and the products
+    // behind them, until the CU has taken them (1 KB in 16 cycles).
+    auto run = [&](auto lo_tag, auto up_tag, auto soft_tag, int kbuf, int vbuf, STile& x, STile& sn, const PTile& pp, PTile& p,
+                   auto loads) {
       constexpr int lo = decltype(lo_tag)::value, up = decltype(up_tag)::value;
       constexpr bool soft = decltype(soft_tag)::value;
       constexpr int n = up - lo > 10 ? up - lo : 10;  // slots
@@ -210,6 +216,7 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
           product(i, f[(i - lo) % kRd], sn, pp);
           if (i + kRd < up) f[(i - lo) % kRd] = fragment(i + kRd, kbuf, vbuf);
         }
+        if ((i - lo) % 2 == 0 && (i - lo) / 2 < 2 * kL) loads((i - lo) / 2);
         if (soft) softmax_slice(i - lo, n, x, p);
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -225,6 +232,7 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
       lds_barrier();
       __builtin_amdgcn_sched_barrier(0);
     };
+    auto none_on_its_way = [](int) {};
     STile sa, sb;
     PTile pa, pb;
     load_k(0, j0);
@@ -233,7 +241,7 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
     if (n_tiles > 1) vm_wait<2 * kL>();
     else vm_wait<kL>();
     lds_barrier();
-    run(Pv(), All(), No(), 0, 0, sb, sa, pa, pa);
+    run(Pv(), All(), No(), 0, 0, sb, sa, pa, pa, none_on_its_way);
     auto pin = [&](STile& sn, PTile& p) {  // the step's results are made in it, not sunk to where they are used
 #pragma unroll
       for (int i = 0; i < kKT / 32; ++i) asm volatile("" : "+v"(sn[i]));
@@ -250,11 +258,19 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
     };
     auto middle = [&](int t, int buf, STile& x, STile& sn, PTile& pp, PTile& p) {  // buf = (t - 1) & 1
       step_barrier();
-      advance(t);
-      load_k(t + 2, j2);
-      load_v(t, j0);
-      mask(j0, x);
-      run(Zero(), All(), Yes(), buf, buf, x, sn, pp, p);
+      const bool more = t + 2 < n_tiles;
+      u32x4 rk, rv;
+      const uint32_t k_at = lds_w + (t & 1) * kTB, v_at = lds_w + (2 + (t & 1)) * kTB;
+      mask(j1, x);
+      run(Zero(), All(), Yes(), buf, buf, x, sn, pp, p, [&](int k) {
+        if (k == 0) {
+          advance(t);
+          rv = rows_of(V, a.v_ld, j0);
+          if (more) rk = rows_of(K, a.k_ld, j2);
+        }
+        if (k < kL) lds_load16(v_at, v_off[k], rv, 0, 1024 * NW * k);
+        else if (more) lds_load16(k_at, k_off[k - kL], rk, 0, 1024 * NW * (k - kL));
+      });
       pin(sn, p);
       finish();
     };
@@ -262,8 +278,8 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
     j2 = n_tiles > 2 ? walk.next() : -1;
     load_k(2, j2);
     mask(j0, sa);
-    if (n_tiles > 1) run(Pv(), All(), No(), 1, 0, sb, sb, pa, pa);
-    run(Zero(), Zero(), Yes(), 0, 0, sa, sb, pa, pa);
+    if (n_tiles > 1) run(Pv(), All(), No(), 1, 0, sb, sb, pa, pa, none_on_its_way);
+    run(Zero(), Zero(), Yes(), 0, 0, sa, sb, pa, pa, none_on_its_way);
     finish();
     if (n_tiles > 1) {
       int t = 1;
@@ -283,13 +299,13 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
       advance(t);
       load_v(t, j0);
       mask(j0, sb);
-      run(Zero(), Pv(), Yes(), 0, (t - 1) & 1, sb, sa, pa, pb);
+      run(Zero(), Pv(), Yes(), 0, (t - 1) & 1, sb, sa, pa, pb, none_on_its_way);
       finish();
 #pragma unroll
       for (int i = 0; i < kKT / 16; ++i) pa[i] = pb[i];
     }
     step_barrier();
-    run(Zero(), Pv(), No(), 0, (n_tiles - 1) & 1, sb, sa, pa, pb);
+    run(Zero(), Pv(), No(), 0, (n_tiles - 1) & 1, sb, sa, pa, pb, none_on_its_way);
   }
 
   const float l = sum_xor32(lrow);

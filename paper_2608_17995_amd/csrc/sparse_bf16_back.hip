@@ -70,8 +70,7 @@ __device__ __forceinline__ void put(bf16x8& chunk, int r, float lo, float up) {
 }
 
 // A wave's share of a tile of ROWS rows that four (64 rows) or eight waves load: instructions of 1 KB, whose
-// lanes fill LDS in order, so the swizzle is in where each lane reads.  The instruction's own offset moves
-// both the source and the LDS address: the sources are given less it.
+// lanes fill LDS in order, so the swizzle is in where each lane reads.
 template <int DH, int ROWS, int NW = ROWS == 128 ? 8 : 4>
 struct TileLoad {
   static constexpr int kCH = DH / 8, kR = kWave / kCH, kN = ROWS * DH * 2 / 1024 / NW;
@@ -84,27 +83,26 @@ struct TileLoad {
   }
   // Instruction i is kR i rows on, where the swizzle differs in bits of i (rows kR kN wave are even enough).
   __device__ __forceinline__ uint32_t off(int i) const {
-    return row + (chunk ^ uint32_t((DH == 128 ? 16 : 32) * i)) + i * (kR * uint32_t(ld2) - 1024);
+    return row + (chunk ^ uint32_t((DH == 128 ? 16 : 32) * i)) + i * (kR * uint32_t(ld2));
   }
   __device__ __forceinline__ void fresh() { asm volatile("" : "+v"(row), "+v"(chunk)); }
-  // Rows first .. of a head to LDS byte dst, those from `end` on as zeros.
-  __device__ __forceinline__ void go(const bf16_t* base, int first, int end, uint32_t dst) const {
-    const int64_t bytes = end > first ? (end - first - 1) * ld2 + DH * 2 : 0;
-    u32x4 r = buffer_rsrc(reinterpret_cast<const char*>(base) + first * ld2, range32(bytes));
+  // Rows first .. of a head, those from `end` on as zeros.  (A tile that starts past the last row is not asked for.)
+  __device__ __forceinline__ u32x4 rows(const bf16_t* base, int first, int end) const {
+    return at(reinterpret_cast<const char*>(base) + first * ld2, int64_t(end - first - 1) * ld2 + DH * 2);
+  }
+  __device__ __forceinline__ static u32x4 at(const char* p, int64_t bytes) {
+    u32x4 r = buffer_rsrc(p, bytes >> 32 ? 0xffffffffu : uint32_t(bytes));
 #pragma unroll
     for (int e = 0; e < 4; ++e) r[e] = __builtin_amdgcn_readfirstlane(r[e]);
-    static_assert(kN == 1 || kN == 2 || kN == 4, "the offset has twelve bits");
-    if constexpr (kN == 4)
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
-                   "buffer_load_dwordx4 %2, %5, 0 offen offset:1024 lds\n\tbuffer_load_dwordx4 %3, %5, 0 offen offset:2048 lds\n\t"
-                   "buffer_load_dwordx4 %4, %5, 0 offen offset:3072 lds" ::"s"(dst), "v"(off(0)), "v"(off(1)), "v"(off(2)), "v"(off(3)), "s"(r)
-                   : "memory", "m0");
-    else if constexpr (kN == 1)
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(dst), "v"(off(0)), "s"(r) : "memory", "m0");
-    else
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %3, 0 offen lds\n\t"
-                   "buffer_load_dwordx4 %2, %3, 0 offen offset:1024 lds" ::"s"(dst), "v"(off(0)), "v"(off(1)), "s"(r)
-                   : "memory", "m0");
+    return r;
+  }
+  // Load i of them, to LDS byte dst + 1024 i.
+  __device__ __forceinline__ void one(int i, const u32x4& r, uint32_t dst) const {
+    lds_load16(dst, off(i), r, 0, 1024 * i);
+  }
+  __device__ __forceinline__ void all(const u32x4& r, uint32_t dst) const {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) one(i, r, dst);
   }
 };
 
@@ -133,7 +131,7 @@ __global__ __launch_bounds__(256, 2) void sparse_dq_bf16_kernel(const SparseArgs
   const int H = a.H, units = a.seq.q_blk[kMaxSeqs] * H;
   const int4 item = sparse_item(a, units, blockIdx.x);
   if (item.x < 0) return;
-  const int h = item.x % H, blk = item.x / H;
+  const int h = item.x % H, blk = item.x / H, piece = item.y & 0xffff, pieces = item.y >> 16;
   const Seq s = seq_of<false>(a.seq, blk);
   const int lane = threadIdx.x % kWave, l32 = lane % 32, hi = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -141,7 +139,7 @@ __global__ __launch_bounds__(256, 2) void sparse_dq_bf16_kernel(const SparseArgs
   const bf16_t* K = static_cast<const bf16_t*>(a.k) + int64_t(h / a.group) * DH;
   const bf16_t* V = static_cast<const bf16_t*>(a.v) + int64_t(h / a.group) * DH;
   BlockWalk walk(a, h, blk, s.nk);
-  const int t_lo = int(int64_t(walk.total) * item.y / item.z), n_tiles = int(int64_t(walk.total) * (item.y + 1) / item.z) - t_lo;
+  const int t_lo = int(int64_t(walk.total) * piece / pieces), n_tiles = int(int64_t(walk.total) * (piece + 1) / pieces) - t_lo;
   const int row = q_first + 32 * wave + l32;
   walk.skip(t_lo);
 
@@ -167,9 +165,12 @@ __global__ __launch_bounds__(256, 2) void sparse_dq_bf16_kernel(const SparseArgs
   Frag<DH> frag;
   TileLoad<DH, kKB> lk(a.k_ld, wave), lv(a.v_ld, wave);
   const uint32_t lds_w = lds_offset(smem) + wave * (kL * 1024);
-  auto load = [&](int buf, int j) {
-    lk.go(K, s.k_lo + j * kKB, s.k_hi, lds_w + 2 * buf * kTB);
-    lv.go(V, s.k_lo + j * kKB, s.k_hi, lds_w + (2 * buf + 1) * kTB);
+  // The next tile's buffers; its loads are spread over a step's first products: issued together they hold
+  // up the wave, and the products behind them, until the CU has taken them (1 KB in 16 cycles).
+  u32x4 rk, rv;
+  auto next_tile = [&](int j) {
+    rk = lk.rows(K, s.k_lo + j * kKB, s.k_hi);
+    rv = lv.rows(V, s.k_lo + j * kKB, s.k_hi);
   };
   // Slots of a step, each a fragment and its product: S and dP of half 0, of half 1, dQ of half 0, of half 1.
   constexpr int kRd = 4, kG = 2 * kC, kQ = 2 * kDT, kSlots = 2 * kG + 2 * kQ;
@@ -183,13 +184,16 @@ __global__ __launch_bounds__(256, 2) void sparse_dq_bf16_kernel(const SparseArgs
   };
   if (n_tiles > 0) {
     int j0 = walk.next(), buf = 0;
-    load(0, j0);
+    next_tile(j0);
+    lk.all(rk, lds_w);
+    lv.all(rv, lds_w + kTB);
     for (int t = 0; t < n_tiles; ++t) {
       // This tile has landed for every wave, and every wave is done with the last, whose place the next takes.
       vm_wait<0>();
       lds_barrier();
       const int j = j0;
-      if (t + 1 < n_tiles) load(buf ^ 1, j0 = walk.next());
+      const bool more = t + 1 < n_tiles;
+      const uint32_t next_at = lds_w + 2 * (buf ^ 1) * kTB;
       const char* kt = smem + 2 * buf * kTB;
       const char* vt = kt + kTB;
       const int up = s.k_hi - s.k_lo - j * kKB - 4 * hi;
@@ -229,6 +233,12 @@ __global__ __launch_bounds__(256, 2) void sparse_dq_bf16_kernel(const SparseArgs
           acc[k % kDT] = mfma32(f[i % kRd], ds[c / 2][c % 2], acc[k % kDT]);
         }
         if constexpr (i + kRd < kSlots) f[i % kRd] = fragment(Int<i + kRd>{});
+        if constexpr (i == 1)
+          if (more) next_tile(j0 = walk.next());
+        if constexpr (i >= 3 && i % 2 == 1 && i / 2 - 1 < 2 * kL) {
+          constexpr int k = i / 2 - 1;
+          if (more) k < kL ? lk.one(k, rk, next_at) : lv.one(k - kL, rv, next_at + kTB);
+        }
         if constexpr (i >= kG && i < 2 * kG) {
           constexpr int n = i - kG;
           each<16 * (n + 1) / kG - 16 * n / kG>([&](auto e) AVITS_INLINE { grad(Int<0>{}, Int<16 * n / kG + decltype(e)::value>{}); });
@@ -242,8 +252,8 @@ __global__ __launch_bounds__(256, 2) void sparse_dq_bf16_kernel(const SparseArgs
     }
   }
   if (row >= q_end) return;
-  if (item.z > 1) {  // a piece: its sums to its slot
-    float* to = a.part + (sparse_slot(a, units, item.w, item.y) * kQB + (row - q_first)) * DH + 4 * hi;
+  if (pieces > 1) {  // a piece: its sums to its slot
+    float* to = a.part + (sparse_slot(a, units, item.w, piece) * kQB + (row - q_first)) * DH + 4 * hi;
 #pragma unroll
     for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
@@ -262,7 +272,7 @@ __global__ __launch_bounds__(256, 2) void sparse_dq_bf16_kernel(const SparseArgs
 // The values' fragments stay in registers, the keys' are read from LDS: with both in registers no more
 // than two fragments could be under way, and every product waited for its own (205 us at 4608
 // rows, 16 heads of 128, where this takes TODO).
-constexpr int kItems = 4096;  // (head, query block) pairs looked at together
+constexpr int kItems = 1024;  // (head, query block) pairs looked at together
 
 template <int DH>
 __global__ __launch_bounds__(512, 2) void sparse_dkv_bf16_kernel(const SparseArgs a) {
@@ -273,10 +283,11 @@ __global__ __launch_bounds__(512, 2) void sparse_dkv_bf16_kernel(const SparseArg
   __shared__ __attribute__((aligned(16))) char keys[kKB * DH * 2];
   __shared__ __attribute__((aligned(16))) float stats[8][64];
   __shared__ uint64_t bits[kItems / 64];
+  __shared__ __attribute__((aligned(8))) int2 list[kItems];  // kept pairs: first row less the sequence's, head of the group
   const int Hk = a.H / a.group, units = a.seq.k_blk[kMaxSeqs] * Hk;
   const int4 item = sparse_item(a, units, blockIdx.x);
   if (item.x < 0) return;
-  const int hk = item.x % Hk, blk = item.x / Hk;
+  const int hk = item.x % Hk, blk = item.x / Hk, piece = item.y & 0xffff, pieces = item.y >> 16;
   const Seq s = seq_of<true>(a.seq, blk);
   const int lane = threadIdx.x % kWave, l32 = lane % 32, hi = lane / 32;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), wk = wave % 2, wq = wave / 2;
@@ -300,10 +311,17 @@ __global__ __launch_bounds__(512, 2) void sparse_dkv_bf16_kernel(const SparseArg
   TileLoad<DH, kQB> lq(a.q_ld, wave), lg(a.do_ld, wave);
   constexpr int kShare = kTB / 8;  // bytes of a tile that a wave loads
   const uint32_t lds_w = lds_offset(smem) + wave * kShare;
-  TileLoad<DH, kKB, 8>(a.k_ld, wave).go(static_cast<const bf16_t*>(a.k) + int64_t(hk) * DH, k_first, s.k_hi,
-                                     lds_offset(keys) + wave * (kKB * DH * 2 / 8));
+  {
+    const TileLoad<DH, kKB, 8> lk(a.k_ld, wave);
+    lk.all(lk.rows(static_cast<const bf16_t*>(a.k) + int64_t(hk) * DH, k_first, s.k_hi), lds_offset(keys) + wave * (kKB * DH * 2 / 8));
+  }
 
-  int left = 0x7fffffff, skip = 0;  // pairs of this piece still to come, and those before it
+  // Pairs before this piece's, and its own.
+  int skip = int(int64_t(item.z) * piece / pieces), left = pieces > 1 ? int(int64_t(item.z) * (piece + 1) / pieces) - skip : 0x7fffffff;
+  const int64_t q_bytes = int64_t(s.q_hi - s.q_lo - 1) * lq.ld2 + DH * 2, g_bytes = int64_t(s.q_hi - s.q_lo - 1) * lg.ld2 + DH * 2;
+  const char* Q = static_cast<const char*>(a.q) + int64_t(s.q_lo) * lq.ld2 + int64_t(hk) * a.group * (DH * 2);
+  const char* G = static_cast<const char*>(a.dout) + int64_t(s.q_lo) * lg.ld2 + int64_t(hk) * a.group * (DH * 2);
+  const float2* stats_of = a.stats + int64_t(hk) * a.group * a.M + s.q_lo;
   for (int base = 0; base < items; base += kItems) {
     const int n = std::min(kItems, items - base);
     __syncthreads();
@@ -314,50 +332,59 @@ __global__ __launch_bounds__(512, 2) void sparse_dkv_bf16_kernel(const SparseArg
       if (lane == 0) bits[i / 64] = w;
     }
     __syncthreads();
-    if (item.z > 1 && base == 0) {  // only lists that fit at once are cut
-      int total = 0;
-      for (int w = 0; 64 * w < n; ++w) total += __popcll(bits[w]);
-      total = __builtin_amdgcn_readfirstlane(total);
-      skip = int(int64_t(total) * item.y / item.z);
-      left = int(int64_t(total) * (item.y + 1) / item.z) - skip;
+    int found = 0;  // the kept pairs, in order
+    for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += 512) {
+      const int e = base + i;
+      int before = 0;
+      for (int w = 0; w < i / 64; ++w) before += __popcll(bits[w]);
+      const uint64_t w = bits[i / 64];
+      if (w >> lane & 1) list[before + __popcll(w & ((uint64_t(1) << lane) - 1))] = make_int2(e % nq * kQB, e / nq);
     }
-    // The kept pairs, one ahead of the products.
-    int word = -1;
-    uint64_t cur = 0;
-    auto next = [&]() {
-      if (left == 0) return -1;
-      while (cur == 0) {
-        if (64 * ++word >= n) return -1;
-        const uint64_t w = bits[word];
-        cur = uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(w >> 32)))) << 32 | uint32_t(__builtin_amdgcn_readfirstlane(int(w)));
-        for (; skip > 0 && cur != 0; --skip) cur &= cur - 1;
-      }
-      --left;
-      const int e = base + 64 * word + __builtin_ctzll(cur);
-      cur &= cur - 1;
-      return e;
+    for (int w = 0; 64 * w < n; ++w) found += __popcll(bits[w]);
+    found = __builtin_amdgcn_readfirstlane(found);
+    __syncthreads();
+    int at = std::min(skip, found);
+    const int end = int(std::min<int64_t>(found, int64_t(at) + left));
+    skip -= at;
+    left -= end - at;
+    int h1 = 0, row1 = 0;  // the pair whose rows come next
+    auto read = [&](int k) {
+      const int2 e = list[k];
+      row1 = __builtin_amdgcn_readfirstlane(e.x);
+      h1 = __builtin_amdgcn_readfirstlane(e.y);
     };
     float stat = 0.f;  // lanes 0 .. 31: lse of the wave's rows of the tile on its way, the others: delta
-    auto load = [&](int buf, int e) {
-      const int h = hk * a.group + e / nq, first = s.q_lo + (e % nq) * kQB;
-      lq.go(static_cast<const bf16_t*>(a.q) + int64_t(h) * DH, first, s.q_hi, lds_w + 2 * buf * kTB);
-      lg.go(static_cast<const bf16_t*>(a.dout) + int64_t(h) * DH, first, s.q_hi, lds_w + (2 * buf + 1) * kTB);
+    // The next pair's buffers; its loads are spread over a step's first products: issued together they hold
+    // up the wave, and the products behind them, until the CU has taken them (1 KB in 16 cycles).
+    u32x4 rq, rg;
+    constexpr int kN = TileLoad<DH, kQB>::kN;
+    auto next_pair = [&]() AVITS_INLINE {
+      const int64_t qo = row1 * lq.ld2, go = row1 * lg.ld2;
+      rq = lq.at(Q + qo + h1 * (DH * 2), q_bytes - qo);
+      rg = lg.at(G + go + h1 * (DH * 2), g_bytes - go);
       // Rows past the last: no probability.
-      const int r = first + 32 * wq + l32;
+      const int r = row1 + 32 * wq + l32;
       stat = hi ? 0.f : INFINITY;
-      if (r < s.q_hi) stat = reinterpret_cast<const float*>(a.stats + int64_t(h) * a.M)[2 * int64_t(r) + hi];
+      const float* st = reinterpret_cast<const float*>(stats_of + int64_t(h1) * a.M + row1);
+      if (r < s.q_hi - s.q_lo) stat = st[uint32_t(2 * (32 * wq + l32) + hi)];
     };
     // Slots of a step, each a fragment and its product: S (with a fragment of the keys too), dP, dV, dK.
     constexpr int kRd = 4, kRk = 3, kQ = 2 * kDT, kSlots = 2 * kC + 2 * kQ;
-    int e1 = next(), buf = 0;
-    if (e1 >= 0) load(0, e1);
-    while (e1 >= 0) {
+    int buf = 0;
+    if (at < end) {
+      read(at);
+      next_pair();
+      lq.all(rq, lds_w);
+      lg.all(rg, lds_w + kTB);
+    }
+    for (; at < end; ++at) {
       // The tile has landed for every wave, and every wave is done with the last, whose place the next takes.
       vm_wait<0>();
       stats[wave][lane] = hi ? -stat : -stat * unscale;
+      const bool more = at + 1 < end;
+      if (more) read(at + 1);
       lds_barrier();
-      e1 = next();
-      if (e1 >= 0) load(buf ^ 1, e1);
+      const uint32_t next_at = lds_w + 2 * (buf ^ 1) * kTB;
       const char* qt = smem + 2 * buf * kTB + 32 * wq * (DH * 2);
       const char* gt = qt + kTB;
       const char* kt = keys + 32 * wk * (DH * 2);
@@ -397,6 +424,12 @@ __global__ __launch_bounds__(512, 2) void sparse_dkv_bf16_kernel(const SparseArg
         if constexpr (i + kRk < kC) fk[i % kRk] = frag.rows(kt, i + kRk);
         if constexpr (i == kC - kRk) begin(dp, 32);
         if constexpr (i + kRd < kSlots) f[i % kRd] = fragment(Int<i + kRd>{});
+        if constexpr (i == 1)
+          if (more) next_pair();
+        if constexpr (i >= 3 && i % 2 == 1 && i / 2 - 1 < 2 * kN) {
+          constexpr int k = i / 2 - 1;
+          if (more) k < kN ? lq.one(k, rq, next_at) : lg.one(k - kN, rg, next_at + kTB);
+        }
         if constexpr (i >= kC && i < 2 * kC) {  // exponentials under dP
           constexpr int k = i - kC;
           each<16 * (k + 1) / kC - 16 * k / kC>([&](auto e) AVITS_INLINE {
@@ -417,42 +450,54 @@ __global__ __launch_bounds__(512, 2) void sparse_dkv_bf16_kernel(const SparseArg
       buf ^= 1;
     }
   }
-  // The four row quarters of a key half, dk's then dv's; each of its waves adds up a quarter of the columns.
+  // The four row quarters p of a key half, as (p0 + p2) + (p1 + p3): quarters 0 and 1 take dk and give dv, 2 and 3 the
+  // other way round; then quarter 1 gives its dk to 0, and 3 its dv to 2.
   float* sums = reinterpret_cast<float*>(smem);
-  each<2>([&](auto which) AVITS_INLINE {
-    constexpr bool is_dv = decltype(which)::value;
-    __syncthreads();
+  auto give = [&](const f32x16* o) {
+#pragma unroll
+    for (int dt = 0; dt < kDT; ++dt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4*>(sums + (32 * wave + l32) * kP + 32 * dt + 8 * q + 4 * hi) =
+            f32x4{o[dt][4 * q], o[dt][4 * q + 1], o[dt][4 * q + 2], o[dt][4 * q + 3]};
+  };
+  auto take = [&](f32x16* o, int from, bool first) {  // first: the other's sum stands first
 #pragma unroll
     for (int dt = 0; dt < kDT; ++dt)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const f32x16& o = is_dv ? dv[dt] : dk[dt];
-        *reinterpret_cast<f32x4*>(sums + (64 * wq + 32 * wk + l32) * kP + 32 * dt + 8 * q + 4 * hi) =
-            f32x4{o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]};
-      }
-    __syncthreads();
-    bf16_t* out = static_cast<bf16_t*>(is_dv ? a.dv : a.dk);
-    const int64_t ld = is_dv ? a.dv_ld : a.dk_ld;
-    const float f = is_dv ? 1.f : a.scale;
-    float* slot = a.part + (sparse_slot(a, units, item.w, item.y) * 2 + is_dv) * (kKB * DH);
-    for (int i = threadIdx.x; i < kKB * DH / 8; i += 512) {
-      const int r = i / (DH / 8), c = i % (DH / 8) * 8;
-      if (k_first + r >= s.k_hi) continue;
-      f32x4 v[2];
+        const f32x4 v = *reinterpret_cast<const f32x4*>(sums + (32 * from + l32) * kP + 32 * dt + 8 * q + 4 * hi);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        f32x4 w[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const f32x4*>(sums + (64 * k + r) * kP + c + 4 * u);
-        v[u] = (w[0] + w[1]) + (w[2] + w[3]);
-        if (item.z > 1) *reinterpret_cast<f32x4*>(slot + r * DH + c + 4 * u) = v[u];
-        v[u] *= f;
+        for (int r = 0; r < 4; ++r) o[dt][4 * q + r] = first ? v[r] + o[dt][4 * q + r] : o[dt][4 * q + r] + v[r];
       }
-      if (item.z > 1) continue;
-      *reinterpret_cast<u32x4*>(out + int64_t(k_first + r) * ld + int64_t(hk) * DH + c) =
-          u32x4{pack_bf2(v[0][0], v[0][1]), pack_bf2(v[0][2], v[0][3]), pack_bf2(v[1][0], v[1][1]), pack_bf2(v[1][2], v[1][3])};
-    }
-  });
+  };
+  __syncthreads();
+  if (wq < 2) give(dv);
+  else give(dk);
+  __syncthreads();
+  if (wq < 2) take(dk, wave + 4, false);
+  else take(dv, wave - 4, true);
+  __syncthreads();
+  if (wq == 1) give(dk);
+  if (wq == 3) give(dv);
+  __syncthreads();
+  if (wq % 2 == 1) return;
+  if (wq == 0) take(dk, wave + 2, false);
+  else take(dv, wave + 2, false);
+  if (row >= s.k_hi) return;
+  if (pieces > 1) {
+    float* slot = a.part + ((sparse_slot(a, units, item.w, piece) * 2 + (wq == 2)) * kKB + 32 * wk + l32) * DH + 4 * hi;
+#pragma unroll
+    for (int dt = 0; dt < kDT; ++dt)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x16& o = wq == 2 ? dv[dt] : dk[dt];
+        *reinterpret_cast<f32x4*>(slot + 32 * dt + 8 * q) = f32x4{o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]};
+      }
+    return;
+  }
+  if (wq == 2) store_sums<DH>(static_cast<bf16_t*>(a.dv) + int64_t(row) * a.dv_ld + int64_t(hk) * DH + 4 * hi, dv, 1.f);
+  else store_sums<DH>(static_cast<bf16_t*>(a.dk) + int64_t(row) * a.dk_ld + int64_t(hk) * DH + 4 * hi, dk, a.scale);
 }
 
 // The pieces of cut lists added up in order: eight columns to a thread.  dq: 128 rows to a unit; dk, dv: 64 of each.

@@ -14,7 +14,7 @@ namespace avits {
 
 constexpr int kMaxUnits = 4096, kShares = 512, kMaxSlots = 2 * kShares, kMinList = 8;
 
-// One side's plan in memory: n_items, n_cut, then kMaxSlots + units items (unit, piece, pieces, first slot), then
+// One side's plan in memory: n_items, n_cut, then kMaxSlots + units items (unit, piece | pieces << 16, list's length, first slot), then
 // the cut lists (unit, pieces, first slot).
 struct SparsePlan {
   int4 head;
@@ -83,21 +83,21 @@ __device__ void sparse_plan(const SparseArgs& a, SparsePlan* plan, int* counts, 
     const uint64_t w = weigh(counts[u]);
     if (w & 0xffff) {
       const int first = int(at & 0xffff), pieces = int(w & 0xffff);
-      for (int p = 0; p < pieces; ++p) plan->items[first + p] = make_int4(u, p, pieces, first);
+      for (int p = 0; p < pieces; ++p) plan->items[first + p] = make_int4(u, p | pieces << 16, counts[u], first);
       plan->cut[at >> 16 & 0xffff] = make_int4(u, pieces, first, 0);
     } else {
       const int place = w >> 32 & 0xffff ? int(at >> 32 & 0xffff) : long_all + int(at >> 48);
-      plan->items[pieces_all + place] = make_int4(u, 0, 1, 0);
+      plan->items[pieces_all + place] = make_int4(u, 1 << 16, counts[u], 0);
     }
     at += w;
   }
   if (tid == 0) plan->head = make_int4(pieces_all + long_all + int(all >> 48), int(all >> 16 & 0xffff), 0, 0);
 }
 
-// The work of workgroup b: unit, piece, pieces and first slot; unit -1: none.
+// The work of workgroup b: unit, piece | pieces << 16, the list's length (from a plan) and first slot; unit -1: none.
 __device__ __forceinline__ int4 sparse_item(const SparseArgs& a, int units, int b) {
-  if (!a.plan) return make_int4(b % units, b / units, a.pieces, b % units);
-  if (b >= a.plan->head.x) return make_int4(-1, 0, 1, 0);
+  if (!a.plan) return make_int4(b % units, b / units | a.pieces << 16, 0, b % units);
+  if (b >= a.plan->head.x) return make_int4(-1, 1 << 16, 0, 0);
   return a.plan->items[b];
 }
 // The slot of a piece.
