@@ -796,3 +796,124 @@ class Mxfp4Mlp:
         return B.avits_layer_norm_backward(dh, self._mean[:M], self._rstd[:M], scale, dx, dscale, dshift,
                                            x_q8=self._x8[:M], x_s8=self._xs[:M], dres=dres, off=self._off,
                                            workspace=self._ws, stream=stream)
+
+
+class SparseAttention:
+    """The attention half of a block between its q, k, v projection and its output projection, over
+    key blocks that the rows themselves choose (Section 3.3's selection, at the grain of blocks):
+
+        q, k = norm and rotation of the projection's heads      (avits_qk_norm_rope)
+        mask = text blocks, and the `keep` best others of each block of 128 queries
+               (avits_block_means, avits_block_select; text queries keep all)
+        out  = softmax over the kept keys                       (avits_sparse_attention)
+
+    run() is the inference form.  forward() and backward() tune it: backward() gives the gradients of
+    the projection and of the two gains; the choice itself has none.
+
+    qkv [M, H + 2 Hk, d] holds the query heads, the key heads, then the value heads (a projection's
+    output [M, (H + 2 Hk) d] is such a tensor); out is [M, H, d]; both may be columns of wider rows.  pos
+    [M, axes] int32, rotated over dims[axis] elements of each head (dims None: no rotation, pos not looked
+    at).  The rows are one sequence, or up to `batch` packed ones at the host offsets off; the first `lead`
+    rows of each are text.  Rows behind the last sequence are neither read nor written.
+
+    All buffers for up to `rows` rows are allocated here (the ones of the backward pass with tune=True);
+    the calls only enqueue, and may be captured.  The constructor waits for the current stream, so that the
+    calls may use any; it may not be captured.  One object's calls belong on one stream at a time, and
+    backward() belongs to the forward() before it; the object has to live until its work on a stream other
+    than the constructor's is done.
+    """
+
+    def __init__(self, rows: int, H: int, d: int, keep: int, dims=(16, 56, 56), Hk=None, lead=0, g_q=None, g_k=None, theta=10000.0,
+                 layout=B.ROPE_PAIRS, eps=1e-6, batch=1, tune=False, dtype=None, device="cuda"):
+        import torch
+        Hk = H if Hk is None else Hk
+        if rows < 1 or batch < 1 or H < 1 or Hk < 1 or H % Hk != 0 or d not in (64, 128):
+            raise ValueError(f"SparseAttention: rows = {rows}, batch = {batch}, H = {H}, Hk = {Hk}, d = {d}")
+        if torch.cuda.is_current_stream_capturing():
+            raise ValueError("SparseAttention: made in a capture")
+        self.rows, self.H, self.Hk, self.d, self.keep, self.lead, self.batch = rows, H, Hk, d, keep, lead, batch
+        self.eps, self.layout, self.tune, self.dtype = eps, layout, tune, dtype or torch.bfloat16
+        self.g_q, self.g_k, self.dims = g_q, g_k, None if dims is None else tuple(dims)
+        self._freq = None if dims is None else B.avits_rope_frequencies(self.dims, theta).to(device)
+
+        def new(*shape, dtype=None):
+            return torch.empty(*shape, dtype=dtype or self.dtype, device=device)
+
+        # Each sequence ends with a shorter block.
+        nq, nk = -(-rows // B.Q_BLOCK) + batch, -(-rows // B.K_BLOCK) + batch
+        self._q, self._k = new(rows, H, d), new(rows, Hk, d)
+        self._qm, self._km = new(nq, H, d, dtype=torch.float64), new(nk, Hk, d, dtype=torch.float64)
+        self._mask = new(H * nq * -(-nk // 64), dtype=torch.int64)
+        code = B._dtype_code(self._q)
+        nbytes = [16, B.avits_sparse_attention_workspace_bytes(rows, rows, batch, H, d, code)]
+        if tune:
+            self._lse = new(H * rows, dtype=torch.float32)
+            nbytes += [B.avits_sparse_attention_backward_workspace_bytes(rows, rows, batch, H, Hk, d, code),
+                       B.avits_qk_norm_rope_backward_workspace_bytes(rows, H, Hk, d)]
+        self._ws = new(max(nbytes), dtype=torch.uint8)
+        self._n = None
+        torch.cuda.current_stream(self._q.device).synchronize()
+
+    def _heads(self, qkv, name="qkv"):
+        if qkv.dim() == 2 and qkv.shape[1] == (self.H + 2 * self.Hk) * self.d:
+            qkv = qkv.unflatten(1, (-1, self.d))
+        if qkv.dim() != 3 or qkv.shape[0] > self.rows or tuple(qkv.shape[1:]) != (self.H + 2 * self.Hk, self.d):
+            raise ValueError(f"SparseAttention: {name} must be [at most {self.rows}, {self.H + 2 * self.Hk}, {self.d}], "
+                             f"got {tuple(qkv.shape)}")
+        return qkv.split([self.H, self.Hk, self.Hk], 1)
+
+    def _turns(self, pos, pos_scale, m):
+        rope = {} if self.dims is None else dict(pos=pos[:m], freq=self._freq, dims=self.dims, pos_scale=pos_scale)
+        return dict(g_q=self.g_q, g_k=self.g_k, eps=self.eps, layout=self.layout, **rope)
+
+    def _attend(self, qkv, pos, out, off, pos_scale, stream, keep_lse=False):
+        q, k, v = self._heads(qkv)
+        M = q.shape[0]
+        host = [0, M] if off is None else [int(o) for o in off]
+        if not 1 <= len(host) - 1 <= self.batch:
+            raise ValueError(f"SparseAttention: {len(host) - 1} sequences, built for {self.batch}")
+        if host[0] != 0 or host[-1] > M or any(b < a for a, b in zip(host, host[1:])):
+            raise ValueError(f"SparseAttention: offsets {host} for {M} rows")
+        m = host[-1]
+        nq, nk = B._block_count(host, B.Q_BLOCK), B._block_count(host, B.K_BLOCK)
+        words = max(1, max(-(-(b - a) // (64 * B.K_BLOCK)) for a, b in zip(host, host[1:])))
+        qn, kn, qm, km = self._q[:M], self._k[:M], self._qm[:nq], self._km[:nk]
+        mask = self._mask[:self.H * nq * words].view(self.H, nq, words)
+        lse = self._lse[:self.H * M].view(self.H, M) if keep_lse else None
+        B.avits_qk_norm_rope(q[:m], k[:m], qn[:m], kn[:m], stream=stream, **self._turns(pos, pos_scale, m))
+        B.avits_block_means(qn, B.Q_BLOCK, qm, off=host, stream=stream)
+        B.avits_block_means(kn, B.K_BLOCK, km, off=host, stream=stream)
+        B.avits_block_select(qm, km, self.keep, mask, q_lead=self.lead, k_lead=self.lead, q_off=host, k_off=host, stream=stream)
+        B.avits_sparse_attention(qn, kn, v, out, mask, lse, q_off=host, k_off=host, workspace=self._ws, stream=stream)
+        return M, host, mask, lse
+
+    def run(self, qkv, pos, out, off=None, pos_scale=1.0, stream=None):
+        """out [M, H, d] of qkv at positions pos pos_scale."""
+        self._attend(qkv, pos, out, off, pos_scale, stream)
+        return out
+
+    def forward(self, qkv, pos, out, off=None, pos_scale=1.0, stream=None):
+        """run(), with what backward() needs kept."""
+        if not self.tune:
+            raise ValueError("SparseAttention: built without tune=True")
+        self._n = None
+        self._n, self._off, self._kept, self._row_lse = self._attend(qkv, pos, out, off, pos_scale, stream, True)
+        self._pos_scale = pos_scale
+        return out
+
+    def backward(self, dout, qkv, pos, out, dqkv, dg_q=None, dg_k=None, stream=None):
+        """dqkv, shaped as qkv, and dg_q, dg_k [d] fp32 where asked for, of the last
+        forward(), whose qkv, pos and out these are, from dout [M, H, d]."""
+        if self._n is None:
+            raise ValueError("SparseAttention: backward() without a forward()")
+        q, k, v = self._heads(qkv)
+        dq, dk, dv = self._heads(dqkv, "dqkv")
+        M, off = self._n, self._off
+        if q.shape[0] != M or dq.shape[0] != M:
+            raise ValueError(f"SparseAttention: backward() of {q.shape[0]} rows into {dq.shape[0]}, forward() had {M}")
+        m = off[-1]
+        B.avits_sparse_attention_backward(dout, self._q[:M], self._k[:M], v, out, self._row_lse, dq, dk, dv, self._kept, q_off=off,
+                                          k_off=off, workspace=self._ws, stream=stream)
+        B.avits_qk_norm_rope_backward(dq[:m], dk[:m], q[:m], k[:m], dq[:m], dk[:m], dg_q, dg_k, workspace=self._ws, stream=stream,
+                                      **self._turns(pos, self._pos_scale, m))
+        return dqkv
