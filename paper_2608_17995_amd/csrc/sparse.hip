@@ -17,8 +17,8 @@ namespace avits {
 namespace {
 
 // ---------------------------------------------------------------------------
-// On v_mfma_f32_16x16x4_f32, whatever the rows' type.  A workgroup owns 64 query rows (half a query
-// block), 16 to a wave; key tiles of 64 rows pass through LDS.  Products are
+// fp32, on v_mfma_f32_16x16x4_f32.  A workgroup owns 64 query rows (half a query block), 16 to a
+// wave; key tiles of 64 rows pass through LDS.  Products are
 // transposed (S^T = K Q^T, O^T = V^T P^T): lane l holds query row l % 16, register r
 // key 4 (l / 16) + r, so the probabilities are the second product's operand as they stand.
 constexpr int kFT = 64;  // rows to a tile
@@ -33,28 +33,38 @@ __device__ __forceinline__ f32x4 load4(const T* p) {
                  __uint_as_float(w[1] & 0xffff0000u)};
   }
 }
-template <typename T>
-__device__ __forceinline__ void store4(T* p, const f32x4& v) {
-  if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(p) = v;
-  else *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3])};
-}
+__device__ __forceinline__ void store4(float* p, const f32x4& v) { *reinterpret_cast<f32x4*>(p) = v; }
 
-// A tile of rows [row, row + 64) of a head, rows from `end` on as zeros, to LDS.
-template <typename T, int DH>
-__device__ __forceinline__ void load_tile(float* dst, const T* src, int64_t ld, int row, int end) {
-  constexpr int kQ = DH / 4, kP = DH + 4;
+// Tiles of rows [row, row + 64) of a head of two tensors, rows from `end` on as zeros: on their way in
+// registers while the tiles before them are worked on, then in LDS.
+template <int DH>
+struct NextTiles {
+  static constexpr int kQ = DH / 4, kP = DH + 4, kN = kFT * kQ / 256;
+  f32x4 x[kN], y[kN];
+  __device__ __forceinline__ void fetch(const float* a, int64_t a_ld, const float* b, int64_t b_ld, int row, int end) {
 #pragma unroll
-  for (int i = 0; i < kFT * kQ / 256; ++i) {
-    const int e = threadIdx.x + 256 * i, r = e / kQ, c = e % kQ;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (row + r < end) v = load4(src + int64_t(row + r) * ld + 4 * c);
-    *reinterpret_cast<f32x4*>(dst + r * kP + 4 * c) = v;
+    for (int i = 0; i < kN; ++i) {
+      const int e = threadIdx.x + 256 * i, r = row + e / kQ, c = 4 * (e % kQ);
+      x[i] = y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (r < end) {
+        x[i] = load4(a + int64_t(r) * a_ld + c);
+        y[i] = load4(b + int64_t(r) * b_ld + c);
+      }
+    }
   }
-}
+  __device__ __forceinline__ void put(float* a, float* b) const {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const int e = threadIdx.x + 256 * i, at = e / kQ * kP + 4 * (e % kQ);
+      store4(a + at, x[i]);
+      store4(b + at, y[i]);
+    }
+  }
+};
 
 // 16 rows' fragments in registers: lane l has row l % 16, elements 16 j + 4 (l / 16) + e.
-template <typename T, int DH>
-__device__ __forceinline__ void load_rows(f32x4* f, const T* src, int64_t ld, int row, int end) {
+template <int DH>
+__device__ __forceinline__ void load_rows(f32x4* f, const float* src, int64_t ld, int row, int end) {
   const int lane = threadIdx.x % kWave, r = row + lane % 16;
 #pragma unroll
   for (int j = 0; j < DH / 16; ++j)
@@ -91,37 +101,61 @@ __device__ __forceinline__ void columns_product(const float* tile, int row0, con
 __device__ __forceinline__ float quad_max(float v) { return max_xor32(fmaxf(v, __shfl_xor(v, 16))); }
 __device__ __forceinline__ float quad_sum(float v) { return sum_xor32(v + __shfl_xor(v, 16)); }
 
-template <typename T, int DH>
-__global__ __launch_bounds__(256) void sparse_simple_kernel(const SparseArgs a) {
-  constexpr int kP = DH + 4, kD = DH / 16;
-  __shared__ __attribute__((aligned(16))) float kt[kFT * kP], vt[kFT * kP];
-  const int blk = blockIdx.x / 2, h = blockIdx.y, lane = threadIdx.x % kWave;
-  const Seq s = seq_of<false>(a.seq, blk);
-  const int wave = threadIdx.x / kWave, first = s.q_lo + (blk - s.qb) * kQB + 64 * (blockIdx.x % 2);
-  if (first >= s.q_hi) return;
-  const T* K = static_cast<const T*>(a.k) + int64_t(h / a.group) * DH;
-  const T* V = static_cast<const T*>(a.v) + int64_t(h / a.group) * DH;
-  f32x4 q[kD], o[kD];
-  load_rows<T, DH>(q, static_cast<const T*>(a.q) + int64_t(h) * DH, a.q_ld, first + 16 * wave, s.q_hi);
+// The sums of a workgroup's waves over the same 16 rows: each wave's to LDS, then (the caller waits between)
+// elements c .. c + 3 of row i added up in the waves' order.
+template <int DH>
+__device__ __forceinline__ void put_sums(float* to, int wave, const f32x4* acc) {
+  const int lane = threadIdx.x % kWave;
 #pragma unroll
-  for (int j = 0; j < kD; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
+  for (int d = 0; d < DH / 16; ++d) store4(to + (16 * wave + lane % 16) * (DH + 4) + 16 * d + 4 * (lane / 16), acc[d]);
+}
+template <int DH>
+__device__ __forceinline__ f32x4 add_sums(const float* from, int i, int c) {
+  f32x4 v = load4(from + i * (DH + 4) + c);
+#pragma unroll
+  for (int p = 1; p < 4; ++p) v += load4(from + (16 * p + i) * (DH + 4) + c);
+  return v;
+}
+
+// The forward pass.  SPLIT, for few rows: a workgroup owns 16 of them, each of its waves a quarter of every
+// tile's keys, and the waves' maxima and sums meet in LDS at the end.
+template <int DH, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void sparse_f32_kernel(const SparseArgs a) {
+  constexpr int kP = DH + 4, kD = DH / 16, kQ = DH / 4, kT = SPLIT ? 1 : 4, kRows = SPLIT ? 16 : 64;
+  __shared__ __attribute__((aligned(16))) float kt[kFT * kP], vt[kFT * kP];
+  __shared__ float top[4][16], sum[4][16];
+  const int blk = blockIdx.x / (kQB / kRows), h = blockIdx.y, lane = threadIdx.x % kWave;
+  const Seq s = seq_of<false>(a.seq, blk);
+  const int wave = threadIdx.x / kWave, first = s.q_lo + (blk - s.qb) * kQB + kRows * (blockIdx.x % (kQB / kRows));
+  if (first >= s.q_hi) return;
+  const int row = first + (SPLIT ? 0 : 16 * wave) + lane % 16, key0 = SPLIT ? 16 * wave : 0;
+  const float* K = static_cast<const float*>(a.k) + int64_t(h / a.group) * DH;
+  const float* V = static_cast<const float*>(a.v) + int64_t(h / a.group) * DH;
+  f32x4 q[kD], o[kD];
+  NextTiles<DH> ahead;
+  auto fetch = [&](int j) { ahead.fetch(K, a.k_ld, V, a.v_ld, s.k_lo + j * kKB, s.k_hi); };
   BlockWalk walk(a, h, blk, s.nk);
-  for (int j = walk.next(); j >= 0; j = walk.next()) {
-    const int row = s.k_lo + j * kKB;
+  int j = walk.next();
+  if (j >= 0) fetch(j);
+  load_rows<DH>(q, static_cast<const float*>(a.q) + int64_t(h) * DH, a.q_ld, row - lane % 16, s.q_hi);
+#pragma unroll
+  for (int d = 0; d < kD; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  while (j >= 0) {
     __syncthreads();
-    load_tile<T, DH>(kt, K, a.k_ld, row, s.k_hi);
-    load_tile<T, DH>(vt, V, a.v_ld, row, s.k_hi);
+    ahead.put(kt, vt);
+    const int n = s.k_hi - (s.k_lo + j * kKB);
+    j = walk.next();
+    if (j >= 0) fetch(j);
     __syncthreads();
-    const int n = s.k_hi - row;
-    f32x4 x[4];
+    f32x4 x[kT];
     float mx = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      x[t] = rows_product<DH>(kt, 16 * t, q);
+    for (int t = 0; t < kT; ++t) {
+      x[t] = rows_product<DH>(kt, key0 + 16 * t, q);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        x[t][r] = 16 * t + 4 * (lane / 16) + r < n ? x[t][r] * a.scale : -INFINITY;
+        x[t][r] = key0 + 16 * t + 4 * (lane / 16) + r < n ? x[t][r] * a.scale : -INFINITY;
         mx = fmaxf(mx, x[t][r]);
       }
     }
@@ -132,123 +166,191 @@ __global__ __launch_bounds__(256) void sparse_simple_kernel(const SparseArgs a) 
 #pragma unroll
     for (int d = 0; d < kD; ++d) o[d] *= corr;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
+    for (int t = 0; t < kT; ++t) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         x[t][r] = expf(x[t][r] - ref);
         l += x[t][r];
       }
-      columns_product<DH>(vt, 16 * t, x[t], o);
+      columns_product<DH>(vt, key0 + 16 * t, x[t], o);
     }
   }
   l = quad_sum(l);
-  const int row = first + 16 * wave + lane % 16;
-  if (row >= s.q_hi) return;
   const bool none = walk.total == 0;
-  if (a.lse && lane < 16) a.lse[int64_t(h) * a.M + row] = none ? -INFINITY : m + logf(l);
-  T* dst = static_cast<T*>(a.o) + int64_t(row) * a.o_ld + int64_t(h) * DH + 4 * (lane / 16);
+  if constexpr (SPLIT) {
+    const int r = lane % 16;
+    if (lane < 16) top[wave][r] = m;
+    __syncthreads();  // also: the tiles are done with
+    m = fmaxf(fmaxf(top[0][r], top[1][r]), fmaxf(top[2][r], top[3][r]));
+    const float w = expf(top[wave][r] - (m == -INFINITY ? 0.f : m));
+    if (lane < 16) sum[wave][r] = l * w;
 #pragma unroll
-  for (int d = 0; d < kD; ++d) store4(dst + 16 * d, none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[d] / l);
+    for (int d = 0; d < kD; ++d) o[d] *= w;
+    put_sums<DH>(kt, wave, o);
+    __syncthreads();
+    for (int e = threadIdx.x; e < 16 * kQ; e += 256) {
+      const int i = e / kQ, c = 4 * (e % kQ), to = first + i;
+      if (to >= s.q_hi) return;
+      const float den = sum[0][i] + sum[1][i] + sum[2][i] + sum[3][i];
+      if (a.lse && c == 0)
+        a.lse[int64_t(h) * a.M + to] =
+            none ? -INFINITY : fmaxf(fmaxf(top[0][i], top[1][i]), fmaxf(top[2][i], top[3][i])) + logf(den);
+      store4(static_cast<float*>(a.o) + int64_t(to) * a.o_ld + int64_t(h) * DH + c, none ? f32x4{0.f, 0.f, 0.f, 0.f} : add_sums<DH>(kt, i, c) / den);
+    }
+  } else {
+    if (row >= s.q_hi) return;
+    if (a.lse && lane < 16) a.lse[int64_t(h) * a.M + row] = none ? -INFINITY : m + logf(l);
+    float* dst = static_cast<float*>(a.o) + int64_t(row) * a.o_ld + int64_t(h) * DH + 4 * (lane / 16);
+#pragma unroll
+    for (int d = 0; d < kD; ++d) store4(dst + 16 * d, none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[d] / l);
+  }
 }
 
-template <typename T, int DH>
-__global__ __launch_bounds__(256) void sparse_dq_simple_kernel(const SparseArgs a) {
-  constexpr int kP = DH + 4, kD = DH / 16;
+template <int DH, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void sparse_dq_f32_kernel(const SparseArgs a) {
+  constexpr int kP = DH + 4, kD = DH / 16, kQ = DH / 4, kT = SPLIT ? 1 : 4, kRows = SPLIT ? 16 : 64;
   __shared__ __attribute__((aligned(16))) float kt[kFT * kP], vt[kFT * kP];
-  const int blk = blockIdx.x / 2, h = blockIdx.y, lane = threadIdx.x % kWave;
+  const int blk = blockIdx.x / (kQB / kRows), h = blockIdx.y, lane = threadIdx.x % kWave;
   const Seq s = seq_of<false>(a.seq, blk);
-  const int wave = threadIdx.x / kWave, first = s.q_lo + (blk - s.qb) * kQB + 64 * (blockIdx.x % 2);
+  const int wave = threadIdx.x / kWave, first = s.q_lo + (blk - s.qb) * kQB + kRows * (blockIdx.x % (kQB / kRows));
   if (first >= s.q_hi) return;
-  const T* K = static_cast<const T*>(a.k) + int64_t(h / a.group) * DH;
-  const T* V = static_cast<const T*>(a.v) + int64_t(h / a.group) * DH;
+  const int row = first + (SPLIT ? 0 : 16 * wave) + lane % 16, key0 = SPLIT ? 16 * wave : 0;
+  const float* K = static_cast<const float*>(a.k) + int64_t(h / a.group) * DH;
+  const float* V = static_cast<const float*>(a.v) + int64_t(h / a.group) * DH;
   f32x4 q[kD], g[kD], dq[kD];
-  load_rows<T, DH>(q, static_cast<const T*>(a.q) + int64_t(h) * DH, a.q_ld, first + 16 * wave, s.q_hi);
-  load_rows<T, DH>(g, static_cast<const T*>(a.dout) + int64_t(h) * DH, a.do_ld, first + 16 * wave, s.q_hi);
+  NextTiles<DH> ahead;
+  auto fetch = [&](int j) { ahead.fetch(K, a.k_ld, V, a.v_ld, s.k_lo + j * kKB, s.k_hi); };
+  BlockWalk walk(a, h, blk, s.nk);
+  int j = walk.next();
+  if (j >= 0) fetch(j);
+  load_rows<DH>(q, static_cast<const float*>(a.q) + int64_t(h) * DH, a.q_ld, row - lane % 16, s.q_hi);
+  load_rows<DH>(g, static_cast<const float*>(a.dout) + int64_t(h) * DH, a.do_ld, row - lane % 16, s.q_hi);
 #pragma unroll
-  for (int j = 0; j < kD; ++j) dq[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int row = first + 16 * wave + lane % 16;
+  for (int d = 0; d < kD; ++d) dq[d] = f32x4{0.f, 0.f, 0.f, 0.f};
   const float2 st = row < s.q_hi ? a.stats[int64_t(h) * a.M + row] : make_float2(INFINITY, 0.f);
   const float lse = st.x, delta = st.y;
-  BlockWalk walk(a, h, blk, s.nk);
-  for (int j = walk.next(); j >= 0; j = walk.next()) {
-    const int key = s.k_lo + j * kKB;
+  while (j >= 0) {
     __syncthreads();
-    load_tile<T, DH>(kt, K, a.k_ld, key, s.k_hi);
-    load_tile<T, DH>(vt, V, a.v_ld, key, s.k_hi);
+    ahead.put(kt, vt);
+    const int n = s.k_hi - (s.k_lo + j * kKB);
+    j = walk.next();
+    if (j >= 0) fetch(j);
     __syncthreads();
-    const int n = s.k_hi - key;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const f32x4 x = rows_product<DH>(kt, 16 * t, q), dp = rows_product<DH>(vt, 16 * t, g);
+    for (int t = 0; t < kT; ++t) {
+      const f32x4 x = rows_product<DH>(kt, key0 + 16 * t, q), dp = rows_product<DH>(vt, key0 + 16 * t, g);
       f32x4 ds;
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        ds[r] = 16 * t + 4 * (lane / 16) + r < n ? expf(x[r] * a.scale - lse) * (dp[r] - delta) : 0.f;
-      columns_product<DH>(kt, 16 * t, ds, dq);
+        ds[r] = key0 + 16 * t + 4 * (lane / 16) + r < n ? expf(x[r] * a.scale - lse) * (dp[r] - delta) : 0.f;
+      columns_product<DH>(kt, key0 + 16 * t, ds, dq);
     }
   }
-  if (row >= s.q_hi) return;
-  T* dst = static_cast<T*>(a.dq) + int64_t(row) * a.dq_ld + int64_t(h) * DH + 4 * (lane / 16);
+  if constexpr (SPLIT) {
+    __syncthreads();
+    put_sums<DH>(kt, wave, dq);
+    __syncthreads();
+    for (int e = threadIdx.x; e < 16 * kQ; e += 256) {
+      const int i = e / kQ, c = 4 * (e % kQ);
+      if (first + i >= s.q_hi) return;
+      store4(static_cast<float*>(a.dq) + int64_t(first + i) * a.dq_ld + int64_t(h) * DH + c, add_sums<DH>(kt, i, c) * a.scale);
+    }
+  } else {
+    if (row >= s.q_hi) return;
+    float* dst = static_cast<float*>(a.dq) + int64_t(row) * a.dq_ld + int64_t(h) * DH + 4 * (lane / 16);
 #pragma unroll
-  for (int d = 0; d < kD; ++d) store4(dst + 16 * d, dq[d] * a.scale);
+    for (int d = 0; d < kD; ++d) store4(dst + 16 * d, dq[d] * a.scale);
+  }
 }
 
-// dk and dv of a key block: 16 keys to a wave, the query rows that keep the block
-// pass through LDS, 64 at a time.
-template <typename T, int DH>
-__global__ __launch_bounds__(256) void sparse_dkv_simple_kernel(const SparseArgs a) {
-  constexpr int kP = DH + 4, kD = DH / 16;
+// dk and dv of a key block: 16 keys to a wave, the query rows that keep the block pass through LDS, 64 at a time.
+// SPLIT: a quarter of the block to a workgroup, a quarter of every 64 rows to each wave.
+// Two workgroups to a CU, though 256 registers leave 36 bytes of scratch at heads of 128 (4096 rows of
+// 16 heads, 30 % kept: the pass 1620 us, with one workgroup and no scratch 1840).
+template <int DH, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void sparse_dkv_f32_kernel(const SparseArgs a) {
+  constexpr int kP = DH + 4, kD = DH / 16, kQ = DH / 4, kT = SPLIT ? 1 : 4;
   __shared__ __attribute__((aligned(16))) float qt[kFT * kP], gt[kFT * kP];
   __shared__ float ls[kFT], dl[kFT];
-  const int blk = blockIdx.x, hk = blockIdx.y, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int blk = SPLIT ? blockIdx.x / 4 : blockIdx.x, hk = blockIdx.y, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const Seq s = seq_of<true>(a.seq, blk);
-  const int first = s.k_lo + (blk - s.kb) * kKB + 16 * wave;
+  const int first = s.k_lo + (blk - s.kb) * kKB + 16 * (SPLIT ? blockIdx.x % 4 : wave), row0 = SPLIT ? 16 * wave : 0;
+  if (SPLIT && first >= s.k_hi) return;
   f32x4 k[kD], v[kD], dk[kD], dv[kD];
-  load_rows<T, DH>(k, static_cast<const T*>(a.k) + int64_t(hk) * DH, a.k_ld, first, s.k_hi);
-  load_rows<T, DH>(v, static_cast<const T*>(a.v) + int64_t(hk) * DH, a.v_ld, first, s.k_hi);
-#pragma unroll
-  for (int j = 0; j < kD; ++j) dk[j] = dv[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int nq = (s.q_hi - s.q_lo + kQB - 1) / kQB;
-  for (int h = hk * a.group; h < (hk + 1) * a.group; ++h) {
-    const T* Q = static_cast<const T*>(a.q) + int64_t(h) * DH;
-    const T* G = static_cast<const T*>(a.dout) + int64_t(h) * DH;
-    for (int i = 0; i < nq; ++i) {
-      if (!kept(a, h, s.qb + i, blk - s.kb)) continue;
-      for (int row = s.q_lo + i * kQB; row < std::min(s.q_hi, s.q_lo + (i + 1) * kQB); row += kFT) {
-        __syncthreads();
-        load_tile<T, DH>(qt, Q, a.q_ld, row, s.q_hi);
-        load_tile<T, DH>(gt, G, a.do_ld, row, s.q_hi);
-        if (threadIdx.x < kFT) {
-          const int r = row + threadIdx.x;
-          const float2 st = r < s.q_hi ? a.stats[int64_t(h) * a.M + r] : make_float2(INFINITY, 0.f);  // past the end: no probability
-          ls[threadIdx.x] = st.x;
-          dl[threadIdx.x] = st.y;
+  // The next 64 rows of a query block that keeps this key block.
+  int h = hk * a.group, i = -1, row = -1;
+  auto next = [&]() {
+    if (row >= 0 && row + kFT < std::min(s.q_hi, s.q_lo + (i + 1) * kQB)) {
+      row += kFT;
+      return true;
+    }
+    for (; h < (hk + 1) * a.group; ++h, i = -1)
+      while (++i < nq)
+        if (kept(a, h, s.qb + i, blk - s.kb)) {
+          row = s.q_lo + i * kQB;
+          return true;
         }
-        __syncthreads();
+    return false;
+  };
+  NextTiles<DH> ahead;
+  float2 st;
+  auto fetch = [&]() {
+    ahead.fetch(static_cast<const float*>(a.q) + int64_t(h) * DH, a.q_ld, static_cast<const float*>(a.dout) + int64_t(h) * DH, a.do_ld, row, s.q_hi);
+    const int r = row + threadIdx.x % kFT;
+    st = r < s.q_hi ? a.stats[int64_t(h) * a.M + r] : make_float2(INFINITY, 0.f);  // past the end: no probability
+  };
+  bool more = next();
+  if (more) fetch();
+  load_rows<DH>(k, static_cast<const float*>(a.k) + int64_t(hk) * DH, a.k_ld, first, s.k_hi);
+  load_rows<DH>(v, static_cast<const float*>(a.v) + int64_t(hk) * DH, a.v_ld, first, s.k_hi);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const f32x4 x = rows_product<DH>(qt, 16 * t, k), dp = rows_product<DH>(gt, 16 * t, v);
-          f32x4 p, ds;
+  for (int d = 0; d < kD; ++d) dk[d] = dv[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  while (more) {
+    __syncthreads();
+    ahead.put(qt, gt);
+    if (threadIdx.x < kFT) {
+      ls[threadIdx.x] = st.x;
+      dl[threadIdx.x] = st.y;
+    }
+    more = next();
+    if (more) fetch();
+    __syncthreads();
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int e = 16 * t + 4 * (lane / 16) + r;
-            p[r] = expf(x[r] * a.scale - ls[e]);
-            ds[r] = p[r] * (dp[r] - dl[e]);
-          }
-          columns_product<DH>(gt, 16 * t, p, dv);
-          columns_product<DH>(qt, 16 * t, ds, dk);
-        }
+    for (int t = 0; t < kT; ++t) {
+      const f32x4 x = rows_product<DH>(qt, row0 + 16 * t, k), dp = rows_product<DH>(gt, row0 + 16 * t, v);
+      f32x4 p, ds;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int e = row0 + 16 * t + 4 * (lane / 16) + r;
+        p[r] = expf(x[r] * a.scale - ls[e]);
+        ds[r] = p[r] * (dp[r] - dl[e]);
       }
+      columns_product<DH>(gt, row0 + 16 * t, p, dv);
+      columns_product<DH>(qt, row0 + 16 * t, ds, dk);
     }
   }
-  const int row = first + lane % 16;
-  if (row >= s.k_hi) return;
-  T* pk = static_cast<T*>(a.dk) + int64_t(row) * a.dk_ld + int64_t(hk) * DH + 4 * (lane / 16);
-  T* pv = static_cast<T*>(a.dv) + int64_t(row) * a.dv_ld + int64_t(hk) * DH + 4 * (lane / 16);
+  float* pk = static_cast<float*>(a.dk) + int64_t(hk) * DH;
+  float* pv = static_cast<float*>(a.dv) + int64_t(hk) * DH;
+  if constexpr (SPLIT) {
+    __syncthreads();
+    put_sums<DH>(qt, wave, dk);
+    put_sums<DH>(gt, wave, dv);
+    __syncthreads();
+    for (int e = threadIdx.x; e < 16 * kQ; e += 256) {
+      const int r = e / kQ, c = 4 * (e % kQ);
+      if (first + r >= s.k_hi) return;
+      store4(pk + int64_t(first + r) * a.dk_ld + c, add_sums<DH>(qt, r, c) * a.scale);
+      store4(pv + int64_t(first + r) * a.dv_ld + c, add_sums<DH>(gt, r, c));
+    }
+  } else {
+    const int to = first + lane % 16, c = 4 * (lane / 16);
+    if (to >= s.k_hi) return;
 #pragma unroll
-  for (int d = 0; d < kD; ++d) {
-    store4(pk + 16 * d, dk[d] * a.scale);
-    store4(pv + 16 * d, dv[d]);
+    for (int d = 0; d < kD; ++d) {
+      store4(pk + int64_t(to) * a.dk_ld + c + 16 * d, dk[d] * a.scale);
+      store4(pv + int64_t(to) * a.dv_ld + c + 16 * d, dv[d]);
+    }
   }
 }
 
@@ -290,17 +392,28 @@ __global__ __launch_bounds__(1024) void sparse_delta_kernel(const SparseArgs a, 
   }
 }
 
-template <typename T, int DH>
-void forward_simple(const SparseArgs& a, hipStream_t s) {
-  const dim3 grid(2 * unsigned(a.seq.q_blk[a.seq.B]), unsigned(a.H));
-  hipLaunchKernelGGL((sparse_simple_kernel<T, DH>), grid, dim3(256), 0, s, a);
+// 16 rows (keys) to a workgroup up to 256 workgroups of 64, one to a CU.  1024 rows of 16 heads of 128, half the
+// blocks kept: 82 us, 64 to a workgroup 93; 2048 rows of 16 heads of 64, 131 and 128.
+bool split(int64_t workgroups) { return workgroups <= 256; }
+
+template <int DH>
+void forward_f32(const SparseArgs& a, hipStream_t s) {
+  const unsigned n = 2 * unsigned(a.seq.q_blk[a.seq.B]), heads = unsigned(a.H);
+  if (split(int64_t(n) * heads)) hipLaunchKernelGGL((sparse_f32_kernel<DH, true>), dim3(4 * n, heads), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((sparse_f32_kernel<DH, false>), dim3(n, heads), dim3(256), 0, s, a);
 }
 
-template <typename T, int DH>
-void backward_simple(const SparseArgs& a, hipStream_t s) {
-  const int nq = a.seq.q_blk[a.seq.B], nk = a.seq.k_blk[a.seq.B];
-  if (nq > 0) hipLaunchKernelGGL((sparse_dq_simple_kernel<T, DH>), dim3(2 * unsigned(nq), unsigned(a.H)), dim3(256), 0, s, a);
-  if (nk > 0) hipLaunchKernelGGL((sparse_dkv_simple_kernel<T, DH>), dim3(unsigned(nk), unsigned(a.H / a.group)), dim3(256), 0, s, a);
+template <int DH>
+void backward_f32(const SparseArgs& a, hipStream_t s) {
+  const unsigned nq = 2 * unsigned(a.seq.q_blk[a.seq.B]), nk = unsigned(a.seq.k_blk[a.seq.B]), H = unsigned(a.H), Hk = unsigned(a.H / a.group);
+  if (nq > 0) {
+    if (split(int64_t(nq) * H)) hipLaunchKernelGGL((sparse_dq_f32_kernel<DH, true>), dim3(4 * nq, H), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((sparse_dq_f32_kernel<DH, false>), dim3(nq, H), dim3(256), 0, s, a);
+  }
+  if (nk > 0) {
+    if (split(int64_t(nk) * Hk)) hipLaunchKernelGGL((sparse_dkv_f32_kernel<DH, true>), dim3(4 * nk, Hk), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((sparse_dkv_f32_kernel<DH, false>), dim3(nk, Hk), dim3(256), 0, s, a);
+  }
 }
 
 int fill(SparseArgs& a, const char* what, const avits_rows* q, const avits_rows* k, const avits_rows* v, int64_t M, int64_t N,
@@ -361,6 +474,11 @@ size_t plan_bytes() { return align_up(sizeof(SparsePlan), 256); }
 // Whether the lists of so many units are cut by a plan: more than a few (which are all cut alike), and not so many that
 // they even out.
 bool planned(int64_t units, bool mask) { return mask && units > kFewUnits && units <= kMaxUnits; }
+// A side of a backward pass: with few units also without a mask, and with lists that are worth cutting (4096 rows of one
+// head, all kept: 158 -> 73 us; lists of 9 blocks: 31 us with or without, and two launches more).
+bool planned_backward(int64_t units, int64_t most, bool mask) {
+  return units > kFewUnits ? planned(units, mask) : units > 0 && most > 2 * kMinList;
+}
 // A forward pass: up to 2048 units make fewer than four rounds of the chip's 512 workgroups.
 bool planned_forward(int64_t units, bool mask) { return planned(units, mask) && units <= 2048; }
 
@@ -434,7 +552,7 @@ extern "C" int avits_sparse_attention(const avits_rows* q, const avits_rows* k, 
   }
   const hipStream_t s = static_cast<hipStream_t>(stream);
   TimedLaunch timed(what, s);
-  if (dtype == AVITS_F32) d == 128 ? forward_simple<float, 128>(a, s) : forward_simple<float, 64>(a, s);
+  if (dtype == AVITS_F32) d == 128 ? forward_f32<128>(a, s) : forward_f32<64>(a, s);
   else launch_sparse_bf16(a, s);
   return launch_status(what);
 }
@@ -494,13 +612,13 @@ extern "C" int avits_sparse_attention_backward(const avits_rows* dout, const avi
     }
     char* at = static_cast<char*>(workspace) + stats_bytes(M, H);
     const int64_t uq = int64_t(a.seq.q_blk[B]) * H, uk = int64_t(a.seq.k_blk[B]) * Hk;
-    if (planned(uq, mask != nullptr)) {
+    if (planned_backward(uq, most_q, mask != nullptr)) {
       a.plan = plan_q = reinterpret_cast<SparsePlan*>(at);
       a.slots = sparse_slots(uq, most_q);
       a.part = reinterpret_cast<float*>(at + plan_bytes());
       at += plan_bytes() + size_t(a.slots) * kQB * d * sizeof(float);
     }
-    if (planned(uk, mask != nullptr)) {
+    if (planned_backward(uk, most_k, mask != nullptr)) {
       ak.plan = plan_k = reinterpret_cast<SparsePlan*>(at);
       ak.slots = sparse_slots(uk, most_k);
       ak.part = reinterpret_cast<float*>(at + plan_bytes());
@@ -518,7 +636,7 @@ extern "C" int avits_sparse_attention_backward(const avits_rows* dout, const avi
       else hipLaunchKernelGGL((sparse_delta_kernel<float, 64>), grid, dim3(1024), 0, s, a, plan_q, plan_k);
     }
   }
-  if (dtype == AVITS_F32) d == 128 ? backward_simple<float, 128>(a, s) : backward_simple<float, 64>(a, s);
+  if (dtype == AVITS_F32) d == 128 ? backward_f32<128>(a, s) : backward_f32<64>(a, s);
   else launch_sparse_back_bf16(a, ak, s);
   return launch_status(what);
 }

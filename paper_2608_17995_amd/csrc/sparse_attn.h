@@ -65,7 +65,7 @@ struct BlockWalk {
   }
 };
 
-// Pieces of every list where there are few units: two workgroups to each of 256 CUs, each with two blocks at least.
+// The forward pass's pieces of every list where there are few units: two workgroups to each of 256 CUs, each with two blocks at least.
 constexpr int kMaxPieces = 64, kFewUnits = 64;
 inline int sparse_pieces(int64_t units, int64_t most_list) {
   if (units > kFewUnits || units == 0) return 1;

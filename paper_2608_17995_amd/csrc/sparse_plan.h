@@ -34,10 +34,10 @@ __device__ void sparse_plan(const SparseArgs& a, SparsePlan* plan, int* counts, 
   for (int e = tid; e < nq * a.H; e += NT) {  // a query block of a head: its words
     const int blk = e / a.H, h = e % a.H;
     const Seq s = seq_of<false>(a.seq, blk);
-    const uint64_t* row = a.mask + (int64_t(h) * nq + blk) * a.words;
+    const uint64_t* row = a.mask ? a.mask + (int64_t(h) * nq + blk) * a.words : nullptr;
     int n = 0;
     for (int w = 0; 64 * w < s.nk; ++w) {
-      uint64_t on = row[w];
+      uint64_t on = row ? row[w] : ~uint64_t(0);
       if (s.nk - 64 * w < 64) on &= (uint64_t(1) << (s.nk - 64 * w)) - 1;
       if constexpr (KEYS) {
         for (; on != 0; on &= on - 1) atomicAdd(&counts[(s.kb + 64 * w + __builtin_ctzll(on)) * Hk + h / a.group], 1);
