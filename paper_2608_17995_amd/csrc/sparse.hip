@@ -471,20 +471,19 @@ constexpr int64_t kMaxRows = (int64_t(1) << 31) - 4096;
 size_t slot_bytes(int32_t d) { return size_t(kQB) * size_t(d + 2) * sizeof(float); }
 size_t plan_bytes() { return align_up(sizeof(SparsePlan), 256); }
 
-// Whether the lists of so many units are cut by a plan: more than a few (which are all cut alike), and not so many that
-// they even out.
-bool planned(int64_t units, bool mask) { return mask && units > kFewUnits && units <= kMaxUnits; }
-// A side of a backward pass: with few units also without a mask, and with lists that are worth cutting (4096 rows of one
-// head, all kept: 158 -> 73 us; lists of 9 blocks: 31 us with or without, and two launches more).
-bool planned_backward(int64_t units, int64_t most, bool mask) {
-  return units > kFewUnits ? planned(units, mask) : units > 0 && most > 2 * kMinList;
+// Whether a plan cuts the lists of so many units: not short ones, for which the launches cost more (1000 rows of 16 heads of 64,
+// half kept: 16 us, with a plan 22).
+bool planned(int64_t units, int64_t most, bool mask) {
+  return mask && units > kFewUnits && units <= kMaxUnits && most > 2 * kMinList;
 }
-// A forward pass: up to 2048 units make fewer than four rounds of the chip's 512 workgroups.
-bool planned_forward(int64_t units, bool mask) { return planned(units, mask) && units <= 2048; }
+// A side of a backward pass: with few units also without a mask (4096 rows of one head, all kept: 158 -> 73 us).
+bool planned_backward(int64_t units, int64_t most, bool mask) {
+  return units > kFewUnits ? planned(units, most, mask) : units > 0 && most > 2 * kMinList;
+}
 
 // What the forward pass of `units` units with lists of at most `most` blocks needs.
 size_t forward_bytes(int64_t units, int64_t most, int32_t d, bool mask) {
-  if (planned_forward(units, mask)) return plan_bytes() + size_t(sparse_slots(units, most)) * slot_bytes(d);
+  if (planned(units, most, mask)) return plan_bytes() + size_t(sparse_slots(units, most)) * slot_bytes(d);
   const int p = sparse_pieces(units, most);
   return p > 1 ? size_t(p) * size_t(units) * slot_bytes(d) : 0;
 }
@@ -505,7 +504,7 @@ extern "C" size_t avits_sparse_attention_workspace_bytes(int64_t M, int64_t N, i
   if (M < 0 || N < 0 || M >= kMaxRows || N >= kMaxRows || B < 1 || B > kMaxSeqs || H < 1 || H > 1024 || (d != 64 && d != 128)) return 0;
   if (dtype != AVITS_BF16) return 0;
   size_t most = 0;  // fewer rows, or fewer sequences, may need more
-  for (int64_t blocks = 1; blocks <= ceil_div64(M, kQB) + B && blocks * H <= 2048; ++blocks)
+  for (int64_t blocks = 1; blocks <= ceil_div64(M, kQB) + B && blocks * H <= kMaxUnits; ++blocks)
     for (bool mask : {false, true}) most = std::max(most, forward_bytes(blocks * H, ceil_div64(N, kKB), d, mask));
   return most;
 }
@@ -539,7 +538,7 @@ extern "C" int avits_sparse_attention(const avits_rows* q, const avits_rows* k, 
       AVITS_REQUIRE(reinterpret_cast<uintptr_t>(workspace) % 16 == 0, "%s: the workspace is not 16-byte aligned", what);
     }
     char* at = static_cast<char*>(workspace);
-    if (planned_forward(units, mask != nullptr)) {
+    if (planned(units, most, mask != nullptr)) {
       a.slots = sparse_slots(units, most);
       a.plan = reinterpret_cast<const SparsePlan*>(at);
       at += plan_bytes();

@@ -5,14 +5,17 @@
 // own; their sums go to slots, and a second kernel joins them in order.  There are at most 512 such
 // lists and 1024 pieces.  Pieces run first, then the longer of the uncut lists: a long list (a block
 // of text rows keeps everything) that one workgroup walked would go on when the chip is done with the rest.
-// Units are few enough for their counts to fit LDS (kMaxUnits); more make many rounds, which need no plan.
+// More than kMaxUnits, a round and a half of the 512 workgroups, even out by themselves.  With text of a sixteenth
+// of the blocks and a quarter of the rest kept: 4600 rows of 8 heads of 128 (288 units) 73 us, without a plan 88; 5171 rows
+// of 16 heads of 64 (656 units), forward kernels 50 and 58; 8200 rows of 16 heads of 128 (1040 units) 226 and 206; dk and dv
+// at 1152 units of 128, 10 us of 290 slower with one.
 #pragma once
 
 #include "sparse_attn.h"
 
 namespace avits {
 
-constexpr int kMaxUnits = 4096, kShares = 512, kMaxSlots = 2 * kShares, kMinList = 8;
+constexpr int kMaxUnits = 768, kShares = 512, kMaxSlots = 2 * kShares, kMinList = 8;
 
 // One side's plan in memory: n_items, n_cut, then kMaxSlots + units items (unit, piece | pieces << 16, list's length, first slot), then
 // the cut lists (unit, pieces, first slot).
