@@ -140,6 +140,24 @@ def test_rows_far_apart(gpu, dtype):
         assert torch.equal(*means)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,M,N", [(2, 300, 300), (1, 5, 3000)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_huge_equal_logits(gpu, H, M, N, sign, dtype):
+    """All logits +-2^117 / 8: the mean of the values, whatever their size."""
+    import torch
+    s = make(H, H, 64, (0, M), (0, N), dtype, seed=49, extra=0, packed=False)
+    s["q"].zero_()
+    s["k"].zero_()
+    s["q"][:, :, 0], s["k"][:, :, 0] = 2.0 ** 60, sign * 2.0 ** 57
+    forward(gpu, s, mask=None)
+    v = s["v"].double()
+    # The probabilities are exactly 1: N additions and a division in fp32, then one rounding.
+    tol = (N + 2) * 2.0 ** -24 * v.abs().mean(0) + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * v.mean(0).abs()
+    assert ((s["o"].double() - v.mean(0)).abs() <= 1.01 * tol).all()
+    assert ((s["lse"] / (sign * 2.0 ** 114) - 1).abs() < 2.0 ** -21).all()
+
+
 def test_two_at_once(gpu):
     """Two streams, a workspace each, many times over: the results of one after the other."""
     import torch
