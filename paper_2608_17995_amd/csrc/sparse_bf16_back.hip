@@ -6,7 +6,10 @@
 // products run where five would do, and no sum crosses workgroups.
 //
 // Probabilities and ds are rounded to bf16 for the second products, which the matrix instruction
-// takes; everything else is fp32.
+// takes; everything else is fp32.  For dq what the rounding of ds leaves over goes in as well, as a second operand: a row's
+// ds add up to zero, so dq has nothing of what all keys have in common, but the roundings' errors do (with keys of which a
+// third is shared by their neighbours, 110 rows: dq off by 0.0026 of its size, with the rest by 0.0017, its own rounding's;
+// it costs 25 of 136 us at 4608 rows, 16 heads of 128, 30 % kept).  dk and dv are off by 0.0024.
 #include <utility>
 
 #include "sparse_plan.h"
@@ -62,11 +65,12 @@ struct Frag {
   }
 };
 
-// Registers r - 1 and r (odd) of a product into their chunk of the next product's operand.
-__device__ __forceinline__ void put(bf16x8& chunk, int r, float lo, float up) {
+// Registers r - 1 and r (odd) of a product into their chunk of the next product's operand; the pair as it was rounded.
+__device__ __forceinline__ uint32_t put(bf16x8& chunk, int r, float lo, float up) {
   u32x4 v = __builtin_bit_cast(u32x4, chunk);
   v[(r % 8) / 2] = pack_bf2(lo, up);
   chunk = as_bf16x8(v);
+  return v[(r % 8) / 2];
 }
 
 // A wave's share of a tile of ROWS rows that four (64 rows) or eight waves load: instructions of 1 KB, whose
@@ -175,12 +179,15 @@ __global__ __launch_bounds__(256, 2) void sparse_dq_bf16_kernel(const SparseArgs
   // Slots of a step, each a fragment and its product: S and dP of half 0, of half 1, dQ of half 0, of half 1.
   constexpr int kRd = 4, kG = 2 * kC, kQ = 2 * kDT, kSlots = 2 * kG + 2 * kQ;
   f32x16 x[2], dp[2];
-  bf16x8 ds[2][2];
+  bf16x8 ds[2][2], rest[2][2];
   // Of half t: probabilities and ds, element n of 16.
   auto grad = [&](auto tt, auto nn) AVITS_INLINE {
     constexpr int t = decltype(tt)::value, n = decltype(nn)::value;
     x[t][n] = __builtin_amdgcn_exp2f(fmaf(x[t][n], scale2, -lse2)) * (dp[t][n] - delta);
-    if constexpr (n % 2 == 1) put(ds[t][n / 8], n, x[t][n - 1], x[t][n]);
+    if constexpr (n % 2 == 1) {
+      const uint32_t pair = put(ds[t][n / 8], n, x[t][n - 1], x[t][n]);
+      put(rest[t][n / 8], n, x[t][n - 1] - __uint_as_float(pair << 16), x[t][n] - __uint_as_float(pair & 0xffff0000u));
+    }
   };
   if (n_tiles > 0) {
     int j0 = walk.next(), buf = 0;
@@ -231,6 +238,7 @@ __global__ __launch_bounds__(256, 2) void sparse_dq_bf16_kernel(const SparseArgs
         } else {
           constexpr int k = i - 2 * kG, c = k / kDT;
           acc[k % kDT] = mfma32(f[i % kRd], ds[c / 2][c % 2], acc[k % kDT]);
+          acc[k % kDT] = mfma32(f[i % kRd], rest[c / 2][c % 2], acc[k % kDT]);
         }
         if constexpr (i + kRd < kSlots) f[i % kRd] = fragment(Int<i + kRd>{});
         if constexpr (i == 1)

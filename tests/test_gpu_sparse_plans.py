@@ -158,6 +158,33 @@ def test_huge_equal_logits(gpu, H, M, N, sign, dtype):
     assert ((s["lse"] / (sign * 2.0 ** 114) - 1).abs() < 2.0 ** -21).all()
 
 
+@pytest.mark.parametrize("M", [3, 110, 700])
+def test_keys_alike(gpu, M):
+    """Keys that share more than they differ by: a row's ds add up to zero, and what the keys share does not reach dq."""
+    import torch
+    s = make(4, 2, 64, (0, M), (0, M), "bf16", seed=51, extra=0, packed=False)
+    s["k"] = (s["k"].float() + 8 * torch.randn(1, 2, 64, generator=torch.Generator().manual_seed(52)).cuda()).to(torch.bfloat16)
+    s["q"].mul_(0.25)
+    forward(gpu, s, mask=None)
+    backward(gpu, s, mask=None)
+    check_backward(s, None)
+    q, k, v, do, o, lse = (s[n].double() for n in ("q", "k", "v", "do", "o", "lse"))
+    for h in range(4):
+        j = h // 2
+        x = q[:, h] @ k[:, j].T * s["scale"]
+        p = torch.exp(x - lse[h][:, None])
+        delta = (do[:, h] * o[:, h]).sum(1)[:, None]
+        ds = p * (do[:, h] @ v[:, j].T - delta)
+        want = s["scale"] * ds @ k[:, j]
+        # ds to two parts of 8 bits, 2^-16; logits, dout . v and delta of 64 products in fp32, sums of M.
+        es = 2.0 ** -24 * (66 * (q[:, h].abs() @ k[:, j].T.abs()) * s["scale"] + 4 * x.abs() + 4 * lse[h].abs()[:, None] + 6)
+        eds = ds.abs() * (es + 2.0 ** -16 + (M / 4 + 24) * 2.0 ** -24) + p * 68 * 2.0 ** -24 * (
+            do[:, h].abs() @ v[:, j].T.abs() + (do[:, h] * o[:, h]).abs().sum(1)[:, None])
+        tol = s["scale"] * eds @ k[:, j].abs()
+        err = (s["dq"][:, h].double() - want).abs()
+        assert (err <= tol + 2.0 ** -8 * (want.abs() + tol)).all(), (h, float((err - tol - 2.0 ** -8 * want.abs()).max()))
+
+
 def test_two_at_once(gpu):
     """Two streams, a workspace each, many times over: the results of one after the other."""
     import torch
