@@ -618,6 +618,7 @@ def _types():
     import torch
     _TYPES.update({torch.float32: F32, torch.bfloat16: BF16})
     _TYPES["u8"], _TYPES["f32"] = torch.uint8, torch.float32
+    _TYPES["i32"], _TYPES["i64"], _TYPES["f64"] = torch.int32, torch.int64, torch.float64
     return _TYPES
 
 
@@ -861,17 +862,19 @@ def _rope(what, pos, freq, dims, pos_scale, layout, M, dev):
         return None
     if pos is None or freq is None:
         raise ValueError(f"{what}: a rotation needs both pos and freq")
-    import torch
     if pos.dim() == 1:
         pos = pos[:, None]
-    axes = pos.shape[1]
+    axes, rot = pos.shape[1], 2 * freq.numel()
     if dims is None:
-        dims = (2 * freq.numel(),)
-    if len(dims) != axes or not 1 <= axes <= 4 or sum(dims) != 2 * freq.numel():
-        raise ValueError(f"{what}: pos [M, {axes}] and {freq.numel()} frequencies need dims of {axes} axes (1 to 4) that sum to "
-                         f"{2 * freq.numel()}, got {tuple(dims)}")
-    return _Rope(_arg(pos, "pos", torch.int32, dev, M, axes), _arg(freq, "freq", torch.float64, dev, freq.numel()), pos_scale,
-                 layout, axes, (_i32 * 4)(*dims))
+        dims = (rot,)
+    if len(dims) != axes or not 1 <= axes <= 4 or sum(dims) != rot:
+        raise ValueError(f"{what}: pos [M, {axes}] and {rot // 2} frequencies need dims of {axes} axes (1 to 4) that sum to "
+                         f"{rot}, got {tuple(dims)}")
+    return _Rope(_arg(pos, "pos", _TYPES["i32"], dev, M, axes), _arg(freq, "freq", _TYPES["f64"], dev, rot // 2), pos_scale, layout,
+                 axes, _DIMS(*dims))
+
+
+_DIMS = _i32 * 4
 
 
 def _qk(what, q, k):
@@ -951,12 +954,11 @@ def _block_count(off, block):
 def avits_block_means(x, block, means, off=None, stream=None):
     """means [blocks, H, d] float64: the mean row of every block (Q_BLOCK or K_BLOCK
     rows) of x [M, H, d], whose sequences start at the host offsets off."""
-    import torch
     M, H, d = x.shape
     code, dev = _code(x)
     n, offs, host = _sequences(off, M, "avits_block_means")
     rc = (_LIB or load()).avits_block_means(*_heads(x, "x", x.dtype, dev), M, H, d, block, n, offs, code,
-                                            _arg(means, "means", torch.float64, dev, _block_count(host, max(block, 1)), H, d),
+                                            _arg(means, "means", _TYPES["f64"], dev, _block_count(host, max(block, 1)), H, d),
                                             _device_stream(dev) if stream is None else _stream(stream))
     if rc:
         _check(rc)
@@ -968,8 +970,7 @@ def avits_block_select(q_means, k_means, keep, mask, q_lead=0, k_lead=0, q_off=N
     bit j % 64 of word j / 64 for its sequence's key block j: those that hold one of the
     first k_lead rows and the `keep` others of the largest q_means . k_means; all
     for the query blocks that hold one of the first q_lead rows."""
-    import torch
-    f64 = torch.float64
+    f64 = (_TYPES or _types())["f64"]
     nq, H, d = q_means.shape
     nk, Hk, _ = k_means.shape
     dev = _current_device()
@@ -981,7 +982,7 @@ def avits_block_select(q_means, k_means, keep, mask, q_lead=0, k_lead=0, q_off=N
     words = mask.shape[-1]
     rc = (_LIB or load()).avits_block_select(_arg(q_means, "q_means", f64, dev, nq, H, d), _arg(k_means, "k_means", f64, dev, nk, Hk, d),
                                              hq[-1], hk[-1], B, qo, ko, H, Hk, d, q_lead, k_lead, keep,
-                                             _arg(mask, "mask", torch.int64, dev, H, nq, words), words,
+                                             _arg(mask, "mask", _TYPES["i64"], dev, H, nq, words), words,
                                              _device_stream(dev) if stream is None else _stream(stream))
     if rc:
         _check(rc)
@@ -994,7 +995,6 @@ def _rows(t, name, dtype, dev, rows, heads, d):
 
 def _sparse(what, q, k, v, mask, q_off, k_off, scale, dt, dev):
     """Sizes, sequences and the mask's pointer, as the calls take them."""
-    import torch
     M, H, d = q.shape
     N, Hk, _ = k.shape
     B, qo, hq = _sequences(q_off, M, what)
@@ -1006,7 +1006,7 @@ def _sparse(what, q, k, v, mask, q_off, k_off, scale, dt, dev):
     words = 0 if mask is None else mask.shape[-1]
     if mask is not None and any(64 * words * K_BLOCK < b - a for a, b in zip(hk, hk[1:])):
         raise ValueError(f"{what}: {words} words a row do not reach the keys of every sequence")
-    mp = None if mask is None else _arg(mask, "mask", torch.int64, dev, H, _block_count(hq, Q_BLOCK), words)
+    mp = None if mask is None else _arg(mask, "mask", _TYPES["i64"], dev, H, _block_count(hq, Q_BLOCK), words)
     return (M, N, B, H, Hk, d), (qo, ko), (mp, words, d ** -0.5 if scale is None else scale)
 
 

@@ -460,6 +460,7 @@ __global__ __launch_bounds__(512, 2) void sparse_dkv_bf16_kernel(const SparseArg
   }
   // The four row quarters p of a key half, as (p0 + p2) + (p1 + p3): quarters 0 and 1 take dk and give dv, 2 and 3 the
   // other way round; then quarter 1 gives its dk to 0, and 3 its dv to 2.
+  vm_wait<0>();  // the keys, where no pair was kept
   float* sums = reinterpret_cast<float*>(smem);
   auto give = [&](const f32x16* o) {
 #pragma unroll
