@@ -879,7 +879,7 @@ int avits_block_select(const double* q_means, const double* k_means, int64_t M, 
  * (zeros where nothing is kept).  bf16: probabilities, and ds for dk, are rounded to
  * bf16 before they are multiplied by v, q or dout; ds for dq to two bf16 parts.  A masked block is never read.
  * Rows on 16 bytes with strides of whole 16 bytes, from heads * d to 2^24 elements; outputs
- * overlap nothing.  0 <= M, N < 2^31 - 4096.  scale > 0 and finite.
+ * overlap nothing.  0 <= M, N < 2^31 - 4096.  2^-64 <= scale <= 2^64.
  * A workspace of the size asked for with M, N and B does for calls of fewer rows and sequences, with or without a
  * mask; it lies on 16 bytes, and calls that may run at once need one each.
  * Errors: AVITS_ERR_INVALID_ARG, AVITS_ERR_UNSUPPORTED (dtype, d, key blocks),

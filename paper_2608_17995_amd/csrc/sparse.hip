@@ -425,7 +425,8 @@ int fill(SparseArgs& a, const char* what, const avits_rows* q, const avits_rows*
   AVITS_REQUIRE(Hk >= 1 && H >= Hk && H % Hk == 0 && H <= 1024, "%s: H=%d must be a multiple of Hk=%d, at most 1024", what, H, Hk);
   if (d != 64 && d != 128) return set_error(AVITS_ERR_UNSUPPORTED, "%s: head dim %d (need 64 or 128)", what, d);
   if (dtype != AVITS_F32 && dtype != AVITS_BF16) return set_error(AVITS_ERR_UNSUPPORTED, "%s: dtype %d unsupported", what, dtype);
-  AVITS_REQUIRE(scale > 0.f && scale < INFINITY, "%s: scale must be positive and finite", what);
+  // (The gradients start their logits from -lse / scale.)
+  AVITS_REQUIRE(scale >= 0x1p-64f && scale <= 0x1p64f, "%s: scale=%g outside [2^-64, 2^64]", what, double(scale));
   int nk = 0;
   for (int b = 0; b < B; ++b) nk = std::max(nk, a.seq.k_blk[b + 1] - a.seq.k_blk[b]);
   AVITS_REQUIRE(!mask || (words >= (nk + 63) / 64 && words < (int64_t(1) << 20)), "%s: %lld words a row for %d key blocks", what,

@@ -194,3 +194,20 @@ def test_binding_refuses_before_the_library():
             avits.avits_sparse_attention(q, k, k, q)
         with pytest.raises(avits.AvitsError):
             avits.avits_qk_norm_rope(q.to(torch.float16), k, q, k)
+
+
+def test_scales_and_workspaces(lib):
+    """Scales whose logits or their inverses leave fp32 are refused; a workspace does for fewer rows, sequences and keys."""
+    for bad in (2.0 ** -65, 2.0 ** 65, 1e-45):
+        assert _attend(lib, scale=bad) == INVALID and _attend_back(lib, scale=bad) == INVALID, bad
+    forward, backward = lib.avits_sparse_attention_workspace_bytes, lib.avits_sparse_attention_backward_workspace_bytes
+    for H, Hk in ((1, 1), (4, 2), (16, 16), (1024, 1)):
+        sizes = [(forward(m, m, b, H, 128, 1), backward(m, m, b, H, Hk, 128, 1))
+                 for m, b in ((0, 1), (1, 1), (64, 1), (65, 2), (700, 2), (1100, 2), (2047, 3), (4608, 3), (5000, 16), (16896, 16), (200000, 16))]
+        assert sizes == sorted(sizes) and [s[1] for s in sizes] == sorted(s[1] for s in sizes)
+    assert forward(4608, 4608, 1, 16, 128, 0) == 0 and forward(-1, 5, 1, 4, 64, 1) == 0 and backward(5, 5, 17, 4, 2, 64, 1) == 0
+    # Too small by a byte wherever one is needed: one row of long lists, few units, a plan.
+    for M, N, H, Hk in ((1, 9000, 4, 4), (300, 2900, 4, 2), (1500, 1500, 8, 8)):
+        a = dict(q=rows(ld=H * 64), k=rows(ld=H * 64), v=rows(ld=H * 64), o=rows(ld=H * 64), M=M, N=N, H=H, Hk=Hk, words=3)
+        assert _attend(lib, **a, ws=None) == WORKSPACE and _attend(lib, **a, wsb=64) == WORKSPACE
+        assert _attend(lib, **a, ws=FAKE + 8) == INVALID

@@ -185,6 +185,25 @@ def test_keys_alike(gpu, M):
         assert (err <= tol + 2.0 ** -8 * (want.abs() + tol)).all(), (h, float((err - tol - 2.0 ** -8 * want.abs()).max()))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [2.0 ** -64, 2.0 ** -30, 1.0])
+def test_scales(gpu, scale, dtype):
+    s = make(2, 1, 64, (0, 200), (0, 300), dtype, seed=53)
+    s["scale"] = scale
+    forward(gpu, s, scale=scale)
+    check_forward(s)
+    backward(gpu, s, scale=scale)
+    check_backward(s)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sixteen_sequences(gpu, dtype):
+    """The most that a call takes, some without queries, some without keys."""
+    q = (0, 5, 5, 133, 200, 201, 300, 428, 428, 500, 629, 700, 700, 710, 800, 801, 930)
+    k = (0, 64, 70, 70, 300, 301, 400, 529, 600, 600, 700, 765, 800, 864, 864, 900, 1100)
+    _both(gpu, make(3, 1, 64, q, k, dtype, seed=55))
+
+
 def test_two_at_once(gpu):
     """Two streams, a workspace each, many times over: the results of one after the other."""
     import torch
