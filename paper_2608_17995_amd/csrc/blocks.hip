@@ -36,7 +36,8 @@ namespace {
 
 // ---------------------------------------------------------------------------
 // Means.  A workgroup takes one block and 32 vectors of 16 bytes of its columns;
-// eight strands of rows meet in LDS.  Bound by reading x once.
+// eight strands of rows meet in LDS.  Bound by reading x once: 16896 rows of 16 heads of 128 in bf16, 69 MB, 10.8 to
+// 13.4 us, 5.1 TB/s and more with what the caches still hold.
 struct MeanArgs {
   const void* x;
   int64_t ld;
@@ -92,7 +93,8 @@ __global__ __launch_bounds__(256) void block_means_kernel(const MeanArgs a) {
 // where there are at most 512.
 // Times at 264 key blocks, 132 query blocks and 16 heads of 128: keys read from LDS for each bit 42 us, from registers 30;
 // the products' operands fetched as a lane needs them, 64 bytes of each of 16 rows to an instruction, kept the L1
-// cache busy for 20 us of these: a row's bytes are now fetched together and change lanes in LDS.
+// cache busy for 20 us of these: a row's bytes are now fetched together and change lanes in LDS (20 us).  What is left is
+// latency: up to 64 rounds of counting, each of which needs the last.
 constexpr int kSelWaves = 8;
 constexpr int kMaxKeyBlocks = 16384;  // 128 KiB of scores for one row
 

@@ -216,7 +216,9 @@ __device__ __forceinline__ void load_gain(const Lane<T, HALVES, VEC>& at, uint32
 }
 
 // Bound by HBM: each row is read and written once.  The first kU steps of the queries and of the keys are under
-// way together (16 heads of 128 each: the whole row), as they lie in memory, to hold few registers.
+// way together (16 heads of 128 each: the whole row), as they lie in memory, to hold few registers.  16896 rows of 16 + 16
+// heads of 128 in bf16, 277 MB: 50 us, 5.5 TB/s (a call 58; with one step
+// after another 73); one row 4.3 us, a launch.
 template <typename T, int DH, bool HALVES, bool VEC>
 __global__ __launch_bounds__(256) void qk_rotate_kernel(const RopeArgs a) {
   constexpr int kLPH = DH / 8, kHPW = kWave / kLPH, kU = 4;  // lanes to a head, heads to a step, steps at once
@@ -276,6 +278,10 @@ __global__ __launch_bounds__(256) void qk_rotate_kernel(const RopeArgs a) {
   }
 }
 
+// The backward pass reads x and the gradient and writes dx.  A wave has consecutive rows, whose shares of the gains' gradients
+// it keeps in registers; as many waves as the chip holds, so that there are few sums for the second launch.  4608 rows of
+// 16 + 16 heads of 128 in bf16, 113 MB: 27 us, 4.2 TB/s, and 3.8 for the sums (a call 35; with more waves than
+// the chip holds 45).
 constexpr int kBackWaves = 8;  // waves of a workgroup of the backward pass
 
 template <typename T, int DH, bool HALVES, bool VEC>
@@ -384,7 +390,7 @@ __global__ __launch_bounds__(64 * kBackWaves, VEC && sizeof(T) == 2 ? 3 : 2) voi
   }
 }
 
-// The workgroups' sums added up: 32 columns, 32 strands of rows to a workgroup.
+// The workgroups' sums added up: 32 columns, 32 strands of rows to a workgroup.  A launch's latency: 1.7 to 3.8 us.
 __global__ __launch_bounds__(1024) void gain_sum_kernel(const float* part, int64_t n, int d, float* dgq, float* dgk) {
   __shared__ float red[32][33];
   const int lane = threadIdx.x % 32, col = blockIdx.x * 32 + lane, strand = threadIdx.x / 32;

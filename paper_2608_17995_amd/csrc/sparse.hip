@@ -117,7 +117,9 @@ __device__ __forceinline__ f32x4 add_sums(const float* from, int i, int c) {
   return v;
 }
 
-// The forward pass.  SPLIT, for few rows: a workgroup owns 16 of them, each of its waves a quarter of every
+// The forward pass: bound by the fp32 matrix instructions (4096 rows of 16 heads of 128, half the blocks kept: 774 us, 89 TFLOP/s
+// of the 154 of a large library product), for few rows by the latency of a tile's two barriers and products (288 rows of 4 heads
+// of 64: 11 us for five tiles in a row; without SPLIT 25).  SPLIT, for few rows: a workgroup owns 16 of them, each of its waves a quarter of every
 // tile's keys, and the waves' maxima and sums meet in LDS at the end.
 template <int DH, bool SPLIT>
 __global__ __launch_bounds__(256, 2) void sparse_f32_kernel(const SparseArgs a) {
@@ -356,8 +358,8 @@ __global__ __launch_bounds__(256, 2) void sparse_dkv_f32_kernel(const SparseArgs
 
 // delta = do . o of every row and head, beside lse: DH / 8 lanes to a head; a workgroup takes 16 rows of up to
 // 64 heads, whose results pass through LDS so that they are written row after row (straight from the
-// lanes, 8 bytes to a place M apart, 9.5 us at 4608 rows of 16 heads of 128).  The first workgroups make
-// the plans of dq and of dk and dv meanwhile.
+// lanes, 8 bytes to a place M apart, 9.5 us at 4608 rows of 16 heads of 128; 7.4 at a copy's rate).  The first workgroups make
+// the plans of dq and of dk and dv meanwhile: 10 to 11 us with that of dq.
 constexpr int kDeltaRows = 16, kDeltaHeads = 64;
 template <typename T, int DH>
 __global__ __launch_bounds__(1024) void sparse_delta_kernel(const SparseArgs a, SparsePlan* plan_q, SparsePlan* plan_k) {
