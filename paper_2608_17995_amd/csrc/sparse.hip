@@ -248,6 +248,7 @@ __global__ __launch_bounds__(256, 2) void sparse_dq_f32_kernel(const SparseArgs 
       columns_product<DH>(kt, key0 + 16 * t, ds, dq);
     }
   }
+  const float scale = grad_scale(a, s);
   if constexpr (SPLIT) {
     __syncthreads();
     put_sums<DH>(kt, wave, dq);
@@ -255,13 +256,13 @@ __global__ __launch_bounds__(256, 2) void sparse_dq_f32_kernel(const SparseArgs 
     for (int e = threadIdx.x; e < 16 * kQ; e += 256) {
       const int i = e / kQ, c = 4 * (e % kQ);
       if (first + i >= s.q_hi) return;
-      store4(static_cast<float*>(a.dq) + int64_t(first + i) * a.dq_ld + int64_t(h) * DH + c, add_sums<DH>(kt, i, c) * a.scale);
+      store4(static_cast<float*>(a.dq) + int64_t(first + i) * a.dq_ld + int64_t(h) * DH + c, add_sums<DH>(kt, i, c) * scale);
     }
   } else {
     if (row >= s.q_hi) return;
     float* dst = static_cast<float*>(a.dq) + int64_t(row) * a.dq_ld + int64_t(h) * DH + 4 * (lane / 16);
 #pragma unroll
-    for (int d = 0; d < kD; ++d) store4(dst + 16 * d, dq[d] * a.scale);
+    for (int d = 0; d < kD; ++d) store4(dst + 16 * d, dq[d] * scale);
   }
 }
 
@@ -334,6 +335,7 @@ __global__ __launch_bounds__(256, 2) void sparse_dkv_f32_kernel(const SparseArgs
   }
   float* pk = static_cast<float*>(a.dk) + int64_t(hk) * DH;
   float* pv = static_cast<float*>(a.dv) + int64_t(hk) * DH;
+  const float scale = grad_scale(a, s);
   if constexpr (SPLIT) {
     __syncthreads();
     put_sums<DH>(qt, wave, dk);
@@ -342,7 +344,7 @@ __global__ __launch_bounds__(256, 2) void sparse_dkv_f32_kernel(const SparseArgs
     for (int e = threadIdx.x; e < 16 * kQ; e += 256) {
       const int r = e / kQ, c = 4 * (e % kQ);
       if (first + r >= s.k_hi) return;
-      store4(pk + int64_t(first + r) * a.dk_ld + c, add_sums<DH>(qt, r, c) * a.scale);
+      store4(pk + int64_t(first + r) * a.dk_ld + c, add_sums<DH>(qt, r, c) * scale);
       store4(pv + int64_t(first + r) * a.dv_ld + c, add_sums<DH>(gt, r, c));
     }
   } else {
@@ -350,7 +352,7 @@ __global__ __launch_bounds__(256, 2) void sparse_dkv_f32_kernel(const SparseArgs
     if (to >= s.k_hi) return;
 #pragma unroll
     for (int d = 0; d < kD; ++d) {
-      store4(pk + int64_t(to) * a.dk_ld + c + 16 * d, dk[d] * a.scale);
+      store4(pk + int64_t(to) * a.dk_ld + c + 16 * d, dk[d] * scale);
       store4(pv + int64_t(to) * a.dv_ld + c + 16 * d, dv[d]);
     }
   }

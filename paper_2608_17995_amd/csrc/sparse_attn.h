@@ -81,6 +81,10 @@ __device__ __forceinline__ u32x2 lds_read_tr(const char* p) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p)));
 }
 
+// The factor of a sequence's sums for dq and dk.  Over one key the probability is 1 whatever q and k are, so these
+// are zero: the sums hold what dout . v and dout . o differ by in the order of their additions.
+__device__ __forceinline__ float grad_scale(const SparseArgs& a, const Seq& s) { return s.k_hi - s.k_lo == 1 ? 0.f : a.scale; }
+
 // Whether query block blk of head h keeps its sequence's key block j.
 __device__ __forceinline__ bool kept(const SparseArgs& a, int h, int blk, int j) {
   return !a.mask || (a.mask[(int64_t(h) * a.seq.q_blk[kMaxSeqs] + blk) * a.words + j / 64] >> (j % 64) & 1);

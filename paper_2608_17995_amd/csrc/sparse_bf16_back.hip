@@ -272,7 +272,7 @@ __global__ __launch_bounds__(256, 2) void sparse_dq_bf16_kernel(const SparseArgs
     return;
   }
   bf16_t* dst = static_cast<bf16_t*>(a.dq) + int64_t(row) * a.dq_ld + h * DH + 4 * hi;
-  store_sums<DH>(dst, acc, a.scale);
+  store_sums<DH>(dst, acc, grad_scale(a, s));
 }
 
 // ---------------------------------------------------------------------------
@@ -508,7 +508,7 @@ __global__ __launch_bounds__(512, 2) void sparse_dkv_bf16_kernel(const SparseArg
     return;
   }
   if (wq == 2) store_sums<DH>(static_cast<bf16_t*>(a.dv) + int64_t(row) * a.dv_ld + int64_t(hk) * DH + 4 * hi, dv, 1.f);
-  else store_sums<DH>(static_cast<bf16_t*>(a.dk) + int64_t(row) * a.dk_ld + int64_t(hk) * DH + 4 * hi, dk, a.scale);
+  else store_sums<DH>(static_cast<bf16_t*>(a.dk) + int64_t(row) * a.dk_ld + int64_t(hk) * DH + 4 * hi, dk, grad_scale(a, s));
 }
 
 // The pieces of cut lists added up in order: eight columns to a thread.  dq: 128 rows to a unit; dk, dv: 64 of each.  5 us
@@ -532,7 +532,8 @@ __global__ __launch_bounds__(256) void sparse_sum_kernel(const SparseArgs a) {
     x += *reinterpret_cast<const f32x4*>(p + i * step);
     y += *reinterpret_cast<const f32x4*>(p + i * step + 4);
   }
-  if (!is_dv) x *= a.scale, y *= a.scale;
+  const float f = is_dv ? 1.f : grad_scale(a, s);
+  x *= f, y *= f;
   bf16_t* out = static_cast<bf16_t*>(KEYS ? (is_dv ? a.dv : a.dk) : a.dq);
   const int64_t ld = KEYS ? (is_dv ? a.dv_ld : a.dk_ld) : a.dq_ld;
   *reinterpret_cast<u32x4*>(out + int64_t(row) * ld + int64_t(h) * DH + c) =
