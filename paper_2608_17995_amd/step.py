@@ -820,7 +820,7 @@ class SparseAttention:
     the calls only enqueue, and may be captured.  The constructor waits for the current stream, so that the
     calls may use any; it may not be captured.  One object's calls belong on one stream at a time, and
     backward() belongs to the forward() before it; the object has to live until its work on a stream other
-    than the constructor's is done.
+    than the constructor's is done.  run() may come between forward() and backward().
     """
 
     def __init__(self, rows: int, H: int, d: int, keep: int, dims=(16, 56, 56), Hk=None, lead=0, g_q=None, g_k=None, theta=10000.0,
@@ -841,9 +841,14 @@ class SparseAttention:
 
         # Each sequence ends with a shorter block.
         nq, nk = -(-rows // B.Q_BLOCK) + batch, -(-rows // B.K_BLOCK) + batch
-        self._q, self._k = new(rows, H, d), new(rows, Hk, d)
+
+        def buffers():
+            return new(rows, H, d), new(rows, Hk, d), new(H * nq * -(-nk // 64), dtype=torch.int64)
+
+        self._q, self._k, self._mask = buffers()
+        # With tune, run() leaves what backward() takes from forward() alone.
+        self._run_buffers = buffers() if tune else (self._q, self._k, self._mask)
         self._qm, self._km = new(nq, H, d, dtype=torch.float64), new(nk, Hk, d, dtype=torch.float64)
-        self._mask = new(H * nq * -(-nk // 64), dtype=torch.int64)
         code = B._dtype_code(self._q)
         nbytes = [16, B.avits_sparse_attention_workspace_bytes(rows, rows, batch, H, d, code)]
         if tune:
@@ -866,7 +871,7 @@ class SparseAttention:
         rope = {} if self.dims is None else dict(pos=pos[:m], freq=self._freq, dims=self.dims, pos_scale=pos_scale)
         return dict(g_q=self.g_q, g_k=self.g_k, eps=self.eps, layout=self.layout, **rope)
 
-    def _attend(self, qkv, pos, out, off, pos_scale, stream, keep_lse=False):
+    def _attend(self, qkv, pos, out, off, pos_scale, stream, tuned=False):
         q, k, v = self._heads(qkv)
         M = q.shape[0]
         host = [0, M] if off is None else [int(o) for o in off]
@@ -877,9 +882,10 @@ class SparseAttention:
         m = host[-1]
         nq, nk = B._block_count(host, B.Q_BLOCK), B._block_count(host, B.K_BLOCK)
         words = max(1, max(-(-(b - a) // (64 * B.K_BLOCK)) for a, b in zip(host, host[1:])))
-        qn, kn, qm, km = self._q[:M], self._k[:M], self._qm[:nq], self._km[:nk]
-        mask = self._mask[:self.H * nq * words].view(self.H, nq, words)
-        lse = self._lse[:self.H * M].view(self.H, M) if keep_lse else None
+        q_buf, k_buf, mask_buf = (self._q, self._k, self._mask) if tuned else self._run_buffers
+        qn, kn, qm, km = q_buf[:M], k_buf[:M], self._qm[:nq], self._km[:nk]
+        mask = mask_buf[:self.H * nq * words].view(self.H, nq, words)
+        lse = self._lse[:self.H * M].view(self.H, M) if tuned else None
         B.avits_qk_norm_rope(q[:m], k[:m], qn[:m], kn[:m], stream=stream, **self._turns(pos, pos_scale, m))
         B.avits_block_means(qn, B.Q_BLOCK, qm, off=host, stream=stream)
         B.avits_block_means(kn, B.K_BLOCK, km, off=host, stream=stream)
