@@ -827,8 +827,11 @@ class SparseAttention:
                  layout=B.ROPE_PAIRS, eps=1e-6, batch=1, tune=False, dtype=None, device="cuda"):
         import torch
         Hk = H if Hk is None else Hk
-        if rows < 1 or batch < 1 or H < 1 or Hk < 1 or H % Hk != 0 or d not in (64, 128):
-            raise ValueError(f"SparseAttention: rows = {rows}, batch = {batch}, H = {H}, Hk = {Hk}, d = {d}")
+        # The limits of the calls that the object will make.
+        if (not 1 <= rows < 2 ** 31 - 4096 or not 1 <= batch <= 16 or not 1 <= Hk <= H <= 1024 or H % Hk != 0 or d not in (64, 128) or
+                keep < 0 or lead < 0 or (dims is not None and sum(dims) > d)):
+            raise ValueError(f"SparseAttention: rows = {rows}, batch = {batch} (at most 16), H = {H}, Hk = {Hk}, d = {d}, keep = {keep}, "
+                             f"lead = {lead}, dims = {dims}")
         if torch.cuda.is_current_stream_capturing():
             raise ValueError("SparseAttention: made in a capture")
         self.rows, self.H, self.Hk, self.d, self.keep, self.lead, self.batch = rows, H, Hk, d, keep, lead, batch
