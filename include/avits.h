@@ -855,7 +855,8 @@ int avits_qk_norm_rope_backward(const void* dq_out, int64_t dqo_ld, const void* 
  * first k_lead rows (the text), and the `keep` others (all if fewer) with the largest
  * q_means . k_means; a query block that holds one of its sequence's first q_lead rows keeps all.
  * Scores are in 64 bits; among equal ones the lowest block wins; NaN ranks below every
- * number.  Bits past a sequence's last key block are 0.  At most 16384 key blocks to a sequence.
+ * number.  Bits past a sequence's last key block are 0.  At most 16384 key blocks to a sequence (else
+ * AVITS_ERR_UNSUPPORTED; so are 2^31 query blocks x heads or more).
  * ---------------------------------------------------------------------- */
 #define AVITS_Q_BLOCK 128
 #define AVITS_K_BLOCK 64
@@ -882,7 +883,8 @@ int avits_block_select(const double* q_means, const double* k_means, int64_t M, 
  * overlap nothing.  0 <= M, N < 2^31 - 4096.  2^-64 <= scale <= 2^64.
  * A workspace of the size asked for with M, N and B does for calls of fewer rows and sequences, with or without a
  * mask; it lies on 16 bytes, and calls that may run at once need one each.
- * Errors: AVITS_ERR_INVALID_ARG, AVITS_ERR_UNSUPPORTED (dtype, d, key blocks),
+ * Errors: AVITS_ERR_INVALID_ARG, AVITS_ERR_UNSUPPORTED (dtype, d; bf16: 2^24 query blocks x heads, backward
+ * 2^23 key blocks x key heads, or more; fp32: 2^23 query blocks, backward 2^24 key blocks, or more),
  * AVITS_ERR_WORKSPACE.
  * ---------------------------------------------------------------------- */
 typedef struct avits_rows {

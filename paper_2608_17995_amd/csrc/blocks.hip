@@ -42,7 +42,7 @@ struct MeanArgs {
   const void* x;
   int64_t ld;
   double* out;
-  int32_t B, block, cols;
+  int32_t B, block, blocks, cols;
   int32_t row[kMaxSeqs + 1], blk[kMaxSeqs + 1];
 };
 
@@ -50,13 +50,14 @@ template <typename T>
 __global__ __launch_bounds__(256) void block_means_kernel(const MeanArgs a) {
   constexpr int kV = 16 / sizeof(T);  // columns to a thread
   __shared__ double red[8][kV][33];
-  const int vec = threadIdx.x % 32, strand = threadIdx.x / 32;
-  const int col = (blockIdx.y * 32 + vec) * kV;
+  const int vec = threadIdx.x % 32, strand = threadIdx.x / 32, blk = int(wide_block());
+  const int col = (blockIdx.z * 32 + vec) * kV;
+  if (blk >= a.blocks) return;
   int lo = a.row[0], hi = a.row[1], b0 = 0;
 #pragma unroll
   for (int b = 1; b < kMaxSeqs; ++b)
-    if (b < a.B && int(blockIdx.x) >= a.blk[b]) lo = a.row[b], hi = a.row[b + 1], b0 = a.blk[b];
-  lo += (int(blockIdx.x) - b0) * a.block;
+    if (b < a.B && blk >= a.blk[b]) lo = a.row[b], hi = a.row[b + 1], b0 = a.blk[b];
+  lo += (blk - b0) * a.block;
   const int n = std::min(a.block, hi - lo);
   double acc[kV];
 #pragma unroll
@@ -82,8 +83,8 @@ __global__ __launch_bounds__(256) void block_means_kernel(const MeanArgs a) {
   double sum = 0.0;
 #pragma unroll
   for (int s = 0; s < 8; ++s) sum += red[s][e][v];
-  const int c = (blockIdx.y * 32 + v) * kV + e;
-  if (c < a.cols) a.out[int64_t(blockIdx.x) * a.cols + c] = sum / n;
+  const int c = (blockIdx.z * 32 + v) * kV + e;
+  if (c < a.cols) a.out[int64_t(blk) * a.cols + c] = sum / n;
 }
 
 // ---------------------------------------------------------------------------
@@ -105,7 +106,7 @@ struct SelectArgs {
   int64_t words;
   int H, Hk, d, rows;   // rows: query blocks to a workgroup
   int q_lead, k_lead, keep;
-  int groups[kMaxSeqs + 1];  // workgroups (of a head) before each sequence
+  int groups[kMaxSeqs + 1];  // workgroups (of a head) before each sequence; all of them in the last entry
 };
 
 typedef double f64x2 __attribute__((ext_vector_type(2)));
@@ -168,8 +169,10 @@ __global__ __launch_bounds__(64 * kSelWaves) void block_select_kernel(const Sele
   extern __shared__ __attribute__((aligned(16))) uint64_t keys[];
   // Heads vary fastest over the workgroups: a head's stay on one XCD (for multiples of eight), whose L2 then reads its
   // keys' means once.
-  const int h = blockIdx.x % a.H, group = blockIdx.x / a.H, hk = h / (a.H / a.Hk), lane = threadIdx.x % kWave, l16 = lane % 16, g = lane / 16;
+  const unsigned wg = unsigned(wide_block());
+  const int h = int(wg % unsigned(a.H)), group = int(wg / unsigned(a.H)), hk = h / (a.H / a.Hk), lane = threadIdx.x % kWave, l16 = lane % 16, g = lane / 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  if (group >= a.groups[kMaxSeqs]) return;
   int q_blk = a.seq.q_blk[0], q_end = a.seq.q_blk[1], k_blk = a.seq.k_blk[0], nk = a.seq.k_blk[1] - k_blk, g0 = 0;
 #pragma unroll
   for (int b = 1; b < kMaxSeqs; ++b)
@@ -264,11 +267,12 @@ extern "C" int avits_block_means(const void* x, int64_t ld, int64_t M, int32_t H
   a.out = means;
   a.B = B;
   a.block = block;
+  a.blocks = n;
   a.cols = int(cols);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   TimedLaunch timed("block_means", s);
   const int per = 32 * int(16 / elem);
-  const dim3 grid(static_cast<unsigned>(n), static_cast<unsigned>((cols + per - 1) / per));
+  const dim3 grid = wide_grid(n, static_cast<unsigned>((cols + per - 1) / per));
   if (dtype == AVITS_BF16) hipLaunchKernelGGL((block_means_kernel<bf16_t>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((block_means_kernel<float>), grid, dim3(256), 0, s, a);
   return launch_status("block_means");
@@ -306,6 +310,9 @@ extern "C" int avits_block_select(const double* q_means, const double* k_means, 
   // As many query blocks to a workgroup as a product has rows, fewer where their scores would not fit.
   a.rows = std::max(1, std::min(16, kMaxKeyBlocks / std::max(nk, 1)));
   for (int b = 0; b < B; ++b) a.groups[b + 1] = a.groups[b] + (a.seq.q_blk[b + 1] - a.seq.q_blk[b] + a.rows - 1) / a.rows;
+  a.groups[kMaxSeqs] = a.groups[B];
+  if (int64_t(a.groups[B]) * H >= int64_t(1) << 31)
+    return set_error(AVITS_ERR_UNSUPPORTED, "block_select: %d query blocks of %d heads", nq, H);
   a.seq.q_blk[kMaxSeqs] = nq;
   const size_t lds = size_t(a.rows) * nk * sizeof(uint64_t) + kSelWaves * 4096;
   const hipStream_t s = static_cast<hipStream_t>(stream);
@@ -314,6 +321,6 @@ extern "C" int avits_block_select(const double* q_means, const double* k_means, 
                                              kMaxKeyBlocks * int(sizeof(uint64_t)) + kSelWaves * 4096) != hipSuccess)
     return set_error(AVITS_ERR_HIP, "block_select: no %zu bytes of LDS", lds);
   TimedLaunch timed("block_select", s);
-  hipLaunchKernelGGL(kernel, dim3(unsigned(a.groups[B]) * unsigned(H)), dim3(64 * kSelWaves), lds, s, a);
+  hipLaunchKernelGGL(kernel, wide_grid(int64_t(a.groups[B]) * H), dim3(64 * kSelWaves), lds, s, a);
   return launch_status("block_select");
 }

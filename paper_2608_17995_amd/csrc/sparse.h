@@ -33,6 +33,16 @@ __device__ __forceinline__ Seq seq_of(const SeqBlocks& a, int blk) {
   return s;
 }
 
+// A launch has fewer than 2^32 threads along x (it drops the rest without an error): n workgroups, in rows of 2^20 along
+// y where they are more, the last row not whole.
+inline dim3 wide_grid(int64_t n, unsigned z = 1) {
+  const int64_t x = std::min<int64_t>(n, int64_t(1) << 20);
+  return dim3(unsigned(x), unsigned(ceil_div64(n, std::max<int64_t>(x, 1))), z);
+}
+__device__ __forceinline__ int64_t wide_block() { return int64_t(blockIdx.y) * gridDim.x + blockIdx.x; }
+// Whether n workgroups fit along x alone.
+inline bool fits_x(int64_t n, int threads) { return n * threads < int64_t(1) << 32; }
+
 // Host: checks the offsets (null: one sequence of all rows) and cuts the blocks.
 int seq_blocks(SeqBlocks& s, const char* what, int32_t B, const int64_t* q_off, int64_t M, const int64_t* k_off, int64_t N);
 int seq_rows(const char* what, int32_t B, const int64_t* off, int64_t rows, int block, int32_t* row, int32_t* blk);

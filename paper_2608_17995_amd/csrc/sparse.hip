@@ -369,7 +369,7 @@ __global__ __launch_bounds__(1024) void sparse_delta_kernel(const SparseArgs a, 
   __shared__ int counts[kMaxUnits];
   __shared__ uint64_t sums[1024];
   __shared__ float out[kDeltaHeads][kDeltaRows + 1];
-  int64_t wg = blockIdx.x;
+  int64_t wg = wide_block();
   if (plan_q && wg-- == 0) return sparse_plan<false, 1024>(a, plan_q, counts, sums);
   if (plan_k && wg-- == 0) return sparse_plan<true, 1024>(a, plan_k, counts, sums);
   const int chunks = (a.H + kDeltaHeads - 1) / kDeltaHeads, h0 = int(wg % chunks) * kDeltaHeads, nh = std::min(kDeltaHeads, a.H - h0);
@@ -437,6 +437,9 @@ int fill(SparseArgs& a, const char* what, const avits_rows* q, const avits_rows*
                 (long long)words, nk);
   AVITS_REQUIRE(reinterpret_cast<uintptr_t>(mask) % 8 == 0, "%s: the mask is not aligned to its words", what);
   AVITS_REQUIRE(q && k && v, "%s: null rows", what);
+  // A workgroup of 256 to each query block of a head; fp32: two to each query block, heads along y.
+  if (!fits_x(dtype == AVITS_BF16 ? int64_t(a.seq.q_blk[B]) * H : 2 * int64_t(a.seq.q_blk[B]), 256))
+    return set_error(AVITS_ERR_UNSUPPORTED, "%s: %d query blocks of %d heads", what, a.seq.q_blk[B], H);
   a.q = q->p, a.k = k->p, a.v = v->p;
   a.q_ld = q->ld, a.k_ld = k->ld, a.v_ld = v->ld;
   a.mask = mask;
@@ -590,6 +593,9 @@ extern "C" int avits_sparse_attention_backward(const avits_rows* dout, const avi
   AVITS_ROWS(dv, n, Hk);
   if (m == 0 && n == 0) return AVITS_OK;
   AVITS_REQUIRE(lse || m == 0, "%s: null lse", what);
+  // A workgroup of 512 to each key block of a head; fp32: of 256 to each key block, heads along y.
+  if (!(dtype == AVITS_BF16 ? fits_x(int64_t(a.seq.k_blk[B]) * Hk, 512) : fits_x(a.seq.k_blk[B], 256)))
+    return set_error(AVITS_ERR_UNSUPPORTED, "%s: %d key blocks of %d heads", what, a.seq.k_blk[B], Hk);
   const size_t need = avits_sparse_attention_backward_workspace_bytes(M, N, B, H, Hk, d, dtype);
   if (need > 0 && (!workspace || workspace_bytes < need))
     return set_error(AVITS_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", what, workspace ? workspace_bytes : size_t(0), need);
@@ -631,7 +637,7 @@ extern "C" int avits_sparse_attention_backward(const avits_rows* dout, const avi
   const hipStream_t s = static_cast<hipStream_t>(stream);
   TimedLaunch timed(what, s);
   if (m > 0) {
-    const dim3 grid(unsigned(ceil_div64(m, kDeltaRows) * ceil_div64(H, kDeltaHeads) + (plan_q != nullptr) + (plan_k != nullptr)));
+    const dim3 grid = wide_grid(ceil_div64(m, kDeltaRows) * ceil_div64(H, kDeltaHeads) + (plan_q != nullptr) + (plan_k != nullptr));
     if (dtype == AVITS_BF16) {
       if (d == 128) hipLaunchKernelGGL((sparse_delta_kernel<bf16_t, 128>), grid, dim3(1024), 0, s, a, plan_q, plan_k);
       else hipLaunchKernelGGL((sparse_delta_kernel<bf16_t, 64>), grid, dim3(1024), 0, s, a, plan_q, plan_k);
