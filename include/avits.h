@@ -877,8 +877,10 @@ int avits_block_select(const double* q_means, const double* k_means, int64_t M, 
  * avits_sparse_attention_backward — from dout, the forward's inputs, o and lse:
  *   p_ij = exp(s_ij - lse_i),  ds_ij = p_ij (dout_i . v_j - dout_i . o_i)
  *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i
- * (zeros where nothing is kept; dq and dk of a sequence of one key are zero, exactly).  bf16: probabilities, and ds for dk, are rounded to
- * bf16 before they are multiplied by v, q or dout; ds for dq to two bf16 parts.  A masked block is never read.
+ * (zeros where nothing is kept; dq and dk of a sequence of one key are zero, exactly).  bf16: probabilities, and ds for
+ * dk, are rounded to bf16 before they are multiplied by v, q or dout; ds for dq to two bf16 parts.  A masked block is
+ * never read.  Logits: of up to 2^30 in size in bf16 (a row with larger ones may come out as NaN); in either type the backward
+ * pass's p are as exact as lse is in fp32, within a factor of exp(2^-24 |lse|).
  * Rows on 16 bytes with strides of whole 16 bytes, from heads * d to 2^24 elements; outputs
  * overlap nothing.  0 <= M, N < 2^31 - 4096.  2^-64 <= scale <= 2^64.
  * A workspace of the size asked for with M, N and B does for calls of fewer rows and sequences, with or without a

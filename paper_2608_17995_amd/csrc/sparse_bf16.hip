@@ -13,7 +13,9 @@
 // operand holds V's keys in that order: four keys at a time of one column, which is what
 // ds_read_b64_tr_b16 makes of four rows of V as they lie in memory.
 // Probabilities are rounded to bf16 for the product with V, which the matrix
-// instruction takes; maxima, sums and outputs are fp32.
+// instruction takes; maxima, sums and outputs are fp32.  An exponent is fma(s, scale log2 e, -maximum), whose product is exact but whose
+// maximum was rounded: all of a row's probabilities carry 2 to the power of that rounding, which their sum takes away
+// again.  From logits of 2^31 on it could leave fp32.
 //
 // Bound by the matrix instructions and, at heads of 64, the exponentials: 16896 rows of 16 heads of 128, a quarter kept, 600 us,
 // 1.04 PFLOP/s (a large library product 1.2); 5171 rows of 16 heads of 64, 40 us, 0.52 (three workgroups
@@ -30,7 +32,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kNone = -3e38f;  // a running maximum below every finite logit
+constexpr float kNone = -3e38f;  // a running maximum below every logit
 
 __device__ __forceinline__ f32x16 mfma32(const bf16x8& a, const bf16x8& b, const f32x16& c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
