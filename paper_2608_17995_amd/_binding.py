@@ -832,6 +832,8 @@ def avits_mxfp4_linear_backward(dy, wq, ws, dx, workspace=None, stream=None):
 def _heads(t, name, dtype, dev, rows=None, heads=None, d=None):
     """Pointer and row stride of heads [rows, heads, d] that lie side by side in
     rows any number of elements apart (columns of a projection's rows, say)."""
+    if t is None:
+        raise ValueError(f"{name} is missing")
     shape = t.shape
     if len(shape) != 3 or (rows is not None and shape != (rows, heads, d)):
         raise ValueError(f"{name}: expected {'[rows, heads, d]' if rows is None else (rows, heads, d)}, got {tuple(shape)}")
