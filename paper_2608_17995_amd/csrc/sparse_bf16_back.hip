@@ -10,6 +10,9 @@
 // ds add up to zero, so dq has nothing of what all keys have in common, but the roundings' errors do (with keys of which a
 // third is shared by their neighbours, 110 rows: dq off by 0.0026 of its size, with the rest by 0.0017, its own rounding's;
 // it costs 25 of 136 us at 4608 rows, 16 heads of 128, 30 % kept).  dk and dv are off by 0.0024.
+// All this is against the formula with o as it is stored, in bf16.  What o lost reaches delta, and through it every ds of a row
+// alike, so that dq takes it times the mean key: against the exact gradient of the inputs dq is off by 0.0017 where keys have little in
+// common (110 rows and more, 4 heads), by 0.014 to 0.027 where they share eight times what they differ by.
 #include <utility>
 
 #include "sparse_plan.h"
