@@ -65,7 +65,8 @@ struct BlockWalk {
   }
 };
 
-// The forward pass's pieces of every list where there are few units: two workgroups to each of 256 CUs, each with two blocks at least.
+// The forward pass's pieces of every list where there are few units: two workgroups to each of 256 CUs, each with two blocks at
+// least where the mask keeps everything.  (What it keeps is not known here: pieces of a list of few blocks may have none.)
 constexpr int kMaxPieces = 64, kFewUnits = 64;
 inline int sparse_pieces(int64_t units, int64_t most_list) {
   if (units > kFewUnits || units == 0) return 1;

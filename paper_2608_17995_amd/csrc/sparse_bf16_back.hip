@@ -521,14 +521,14 @@ __global__ __launch_bounds__(256) void sparse_sum_kernel(const SparseArgs a) {
   constexpr int kL = DH / 8, kR = 256 / kL, kPer = kQB / kR;
   const int4 cut = sparse_cut(a, blockIdx.x / kPer);
   if (cut.x < 0) return;
-  const int Hu = KEYS ? a.H / a.group : a.H, units = a.seq.q_blk[kMaxSeqs] * Hu;
+  const int Hu = KEYS ? a.H / a.group : a.H;
   const int blk = cut.x / Hu, h = cut.x % Hu, r = blockIdx.x % kPer * kR + threadIdx.x / kL, c = threadIdx.x % kL * 8;
   const Seq s = seq_of<KEYS>(a.seq, blk);
   const bool is_dv = KEYS && r >= kKB;
   const int row = KEYS ? s.k_lo + (blk - s.kb) * kKB + r % kKB : s.q_lo + (blk - s.qb) * kQB + r;
   if (row >= (KEYS ? s.k_hi : s.q_hi)) return;
   const float* p = a.part + (cut.z * int64_t(kQB) + r) * DH + c;
-  const int64_t step = (sparse_slot(a, units, cut.z, 1) - cut.z) * kQB * DH;
+  constexpr int64_t step = int64_t(kQB) * DH;  // a plan's pieces (no lists are cut without one here) have consecutive slots
   f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
 #pragma unroll 4
   for (int i = 0; i < cut.y; ++i) {
