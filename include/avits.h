@@ -777,8 +777,9 @@ int avits_mxfp4_linear_backward(const void* dy, int64_t M, int64_t N, const uint
 /* ------------------------------------------------------------------------
  * The attention half of a block by its parts: norm and rotation of queries and
  * keys, a choice of key blocks by a cheap score, attention over the chosen
- * blocks, and the backward passes.  With the block's own formulas (the block
- * of avits_block_forward) these are its attention where every key block is kept.
+ * blocks, and the backward passes.  With the formulas of avits_block_forward's block (its gains, pairs, dims d / 8, 7 d / 16,
+ * 7 d / 16) these are its attention where every key block is kept; a double block's text rows, which have gains of their own, take
+ * a call of their own of the norm and rotation.
  *
  * Rows hold heads side by side: element e of head h of row r lies at
  * p + r * ld + h * d + e, so that queries, keys and values may be columns of

@@ -816,6 +816,10 @@ class SparseAttention:
     at).  The rows are one sequence, or up to `batch` packed ones at the host offsets off; the first `lead`
     rows of each are text.  Rows behind the last sequence are neither read nor written.
 
+    With the projection of a single-stream block, its gains and every block kept this is that block's attention.  A double-stream
+    block has gains of its own for its text rows: g_q_text, g_k_text take the first `lead` rows then, g_q and g_k the others (one
+    sequence only, batch = 1).
+
     All buffers for up to `rows` rows are allocated here (the ones of the backward pass with tune=True);
     the calls only enqueue, and may be captured.  The constructor waits for the current stream, so that the
     calls may use any; it may not be captured.  One object's calls belong on one stream at a time, and
@@ -824,7 +828,7 @@ class SparseAttention:
     """
 
     def __init__(self, rows: int, H: int, d: int, keep: int, dims=(16, 56, 56), Hk=None, lead=0, g_q=None, g_k=None, theta=10000.0,
-                 layout=B.ROPE_PAIRS, eps=1e-6, batch=1, tune=False, dtype=None, device="cuda"):
+                 layout=B.ROPE_PAIRS, eps=1e-6, batch=1, tune=False, dtype=None, device="cuda", g_q_text=None, g_k_text=None):
         import torch
         Hk = H if Hk is None else Hk
         # The limits of the calls that the object will make.
@@ -832,6 +836,9 @@ class SparseAttention:
                 keep < 0 or lead < 0 or (dims is not None and sum(dims) > d)):
             raise ValueError(f"SparseAttention: rows = {rows}, batch = {batch} (at most 16), H = {H}, Hk = {Hk}, d = {d}, keep = {keep}, "
                              f"lead = {lead}, dims = {dims}")
+        self._text_gains = None if g_q_text is None and g_k_text is None else (g_q_text, g_k_text)
+        if self._text_gains is not None and batch != 1:
+            raise ValueError("SparseAttention: gains of the text rows need batch = 1")
         if torch.cuda.is_current_stream_capturing():
             raise ValueError("SparseAttention: made in a capture")
         self.rows, self.H, self.Hk, self.d, self.keep, self.lead, self.batch = rows, H, Hk, d, keep, lead, batch
@@ -871,8 +878,14 @@ class SparseAttention:
         return qkv.split([self.H, self.Hk, self.Hk], 1)
 
     def _turns(self, pos, pos_scale, m):
-        rope = {} if self.dims is None else dict(pos=pos[:m], freq=self._freq, dims=self.dims, pos_scale=pos_scale)
-        return dict(g_q=self.g_q, g_k=self.g_k, eps=self.eps, layout=self.layout, **rope)
+        """The rows that share their gains, and how the norm and rotation calls take them: all, or text and image."""
+        cuts = [(0, m, self.g_q, self.g_k)]
+        if self._text_gains is not None:
+            text = min(self.lead, m)
+            cuts = [(0, text, *self._text_gains), (text, m, self.g_q, self.g_k)]
+        for lo, hi, g_q, g_k in cuts:
+            rope = {} if self.dims is None else dict(pos=pos[lo:hi], freq=self._freq, dims=self.dims, pos_scale=pos_scale)
+            yield slice(lo, hi), dict(g_q=g_q, g_k=g_k, eps=self.eps, layout=self.layout, **rope)
 
     def _attend(self, qkv, pos, out, off, pos_scale, stream, tuned=False):
         q, k, v = self._heads(qkv)
@@ -889,7 +902,8 @@ class SparseAttention:
         qn, kn, qm, km = q_buf[:M], k_buf[:M], self._qm[:nq], self._km[:nk]
         mask = mask_buf[:self.H * nq * words].view(self.H, nq, words)
         lse = self._lse[:self.H * M].view(self.H, M) if tuned else None
-        B.avits_qk_norm_rope(q[:m], k[:m], qn[:m], kn[:m], stream=stream, **self._turns(pos, pos_scale, m))
+        for r, turn in self._turns(pos, pos_scale, m):
+            B.avits_qk_norm_rope(q[r], k[r], qn[r], kn[r], stream=stream, **turn)
         B.avits_block_means(qn, B.Q_BLOCK, qm, off=host, stream=stream)
         B.avits_block_means(kn, B.K_BLOCK, km, off=host, stream=stream)
         B.avits_block_select(qm, km, self.keep, mask, q_lead=self.lead, k_lead=self.lead, q_off=host, k_off=host, stream=stream)
@@ -910,9 +924,12 @@ class SparseAttention:
         self._pos_scale = pos_scale
         return out
 
-    def backward(self, dout, qkv, pos, out, dqkv, dg_q=None, dg_k=None, stream=None):
-        """dqkv, shaped as qkv, and dg_q, dg_k [d] fp32 where asked for, of the last
+    def backward(self, dout, qkv, pos, out, dqkv, dg_q=None, dg_k=None, stream=None, dg_q_text=None, dg_k_text=None):
+        """dqkv, shaped as qkv, and dg_q, dg_k (and those of the text rows' gains) [d] fp32 where asked for, of the last
         forward(), whose qkv, pos and out these are, from dout [M, H, d]."""
+        gains = [(dg_q, dg_k)] if self._text_gains is None else [(dg_q_text, dg_k_text), (dg_q, dg_k)]
+        if self._text_gains is None and (dg_q_text is not None or dg_k_text is not None):
+            raise ValueError("SparseAttention: built without gains of the text rows")
         if self._n is None:
             raise ValueError("SparseAttention: backward() without a forward()")
         q, k, v = self._heads(qkv)
@@ -923,6 +940,6 @@ class SparseAttention:
         m = off[-1]
         B.avits_sparse_attention_backward(dout, self._q[:M], self._k[:M], v, out, self._row_lse, dq, dk, dv, self._kept, q_off=off,
                                           k_off=off, workspace=self._ws, stream=stream)
-        B.avits_qk_norm_rope_backward(dq[:m], dk[:m], q[:m], k[:m], dq[:m], dk[:m], dg_q, dg_k, workspace=self._ws, stream=stream,
-                                      **self._turns(pos, self._pos_scale, m))
+        for (r, turn), dg in zip(self._turns(pos, self._pos_scale, m), gains):
+            B.avits_qk_norm_rope_backward(dq[r], dk[r], q[r], k[r], dq[r], dk[r], *dg, workspace=self._ws, stream=stream, **turn)
         return dqkv
