@@ -94,8 +94,9 @@ __global__ __launch_bounds__(256) void block_means_kernel(const MeanArgs a) {
 // where there are at most 512.
 // Times at 264 key blocks, 132 query blocks and 16 heads of 128: keys read from LDS for each bit 42 us, from registers 30;
 // the products' operands fetched as a lane needs them, 64 bytes of each of 16 rows to an instruction, kept the L1
-// cache busy for 20 us of these: a row's bytes are now fetched together and change lanes in LDS (20 us).  What is left is
-// latency: up to 64 rounds of counting, each of which needs the last.
+// cache busy for 20 us of these: a row's bytes are now fetched together and change lanes in LDS (20 us).  Of these the
+// counting takes 6 (up to 64 rounds, each of which needs the last), the products 4, the fetch of the keys' means 2; the other 8 are
+// the start, the queries' means and the mask's words.
 constexpr int kSelWaves = 8;
 constexpr int kMaxKeyBlocks = 16384;  // 128 KiB of scores for one row
 

@@ -280,7 +280,7 @@ __global__ __launch_bounds__(256) void qk_rotate_kernel(const RopeArgs a) {
 
 // The backward pass reads x and the gradient and writes dx.  A wave has consecutive rows, whose shares of the gains' gradients
 // it keeps in registers; as many waves as the chip holds, so that there are few sums for the second launch.  4608 rows of
-// 16 + 16 heads of 128 in bf16, 113 MB: 27 us, 4.2 TB/s, and 3.8 for the sums (a call 35; with more waves than
+// 16 + 16 heads of 128 in bf16, 113 MB: 25 to 27 us, 4.2 to 4.5 TB/s, and 3.9 for the sums (a call 35; with more waves than
 // the chip holds 45).
 constexpr int kBackWaves = 8;  // waves of a workgroup of the backward pass
 
