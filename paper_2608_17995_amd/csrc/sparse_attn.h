@@ -75,6 +75,19 @@ inline int sparse_pieces(int64_t units, int64_t most_list) {
 void launch_sparse_bf16(const SparseArgs& a, hipStream_t s);
 void launch_sparse_back_bf16(const SparseArgs& q, const SparseArgs& k, hipStream_t s);  // one plan for each
 
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ f32x16 mfma32(const bf16x8& a, const bf16x8& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// Position of 16-byte chunk c of row r of an LDS tile is c ^ swz(r): reads of one chunk of 16 rows, and
+// of four chunks of four rows (the transposed ones), touch every bank once.
+template <int DH>
+__device__ __forceinline__ int swz(int r) {
+  return DH == 128 ? (r & 3) << 2 | ((r >> 2) & 3) : ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
+}
+
 // Transposing read: of 16 lanes, lane i gives the address of four 16-bit elements of row i / 4,
 // columns 4 (i % 4) .., and receives column i of the four rows.
 __device__ __forceinline__ u32x2 lds_read_tr(const char* p) {

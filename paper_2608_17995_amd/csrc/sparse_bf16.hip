@@ -30,13 +30,8 @@
 namespace avits {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNone = -3e38f;  // a running maximum below every logit
-
-__device__ __forceinline__ f32x16 mfma32(const bf16x8& a, const bf16x8& b, const f32x16& c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-}
 
 template <int DH>
 __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a) {
@@ -48,7 +43,7 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
   constexpr int kRows = kWave / kCH;       // rows to a load instruction
   constexpr int kTB = kKT * DH * 2;        // bytes of a tile
   constexpr int kL = kTB / 1024 / NW;      // load instructions to a wave and tile
-  // Two K tiles, then two V tiles, unpadded: chunk c of row r lies at c ^ swz(r), so that the fragment
+  // Two K tiles, then two V tiles, unpadded: chunk c of row r lies at c ^ swz_k(r) (K) or c ^ swz(r) (V), so that the fragment
   // reads (16 rows of one chunk; four rows of four chunks) touch every bank once.
   __shared__ __attribute__((aligned(16))) char smem[4 * kTB];
 
@@ -86,13 +81,12 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
     }
     const float scale2 = kLog2e * a.scale;
     auto swz_k = [](int r) { return DH == 128 ? r & 15 : (r >> 1) & 7; };
-    auto swz_v = [](int r) { return DH == 128 ? (r & 3) << 2 | ((r >> 2) & 3) : ((r >> 1) & 1) << 2 | ((r >> 2) & 3); };
     uint32_t k_off[kL], v_off[kL];
 #pragma unroll
     for (int j = 0; j < kL; ++j) {
       const int r = kRows * (wave + NW * j) + lane / kCH;
       k_off[j] = uint32_t(r) * uint32_t(a.k_ld * 2) + uint32_t(((lane % kCH) ^ swz_k(r)) * 16);
-      v_off[j] = uint32_t(r) * uint32_t(a.v_ld * 2) + uint32_t(((lane % kCH) ^ swz_v(r)) * 16);
+      v_off[j] = uint32_t(r) * uint32_t(a.v_ld * 2) + uint32_t(((lane % kCH) ^ swz<DH>(r)) * 16);
     }
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(
         uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)(&smem[0]))));
@@ -124,7 +118,7 @@ __global__ __launch_bounds__(256, 2) void sparse_bf16_kernel(const SparseArgs a)
     // This lane's address for the transposed reads of V: row (l % 16) / 4 + 4 hi, column
     // 16 ((l / 16) % 2) + 4 (l % 4), less the tile and the 32-column group.
     const int vr = (lane % 16) / 4 + 4 * hi;
-    const int va = vr * (DH * 2) + ((2 * ((lane / 16) % 2) + (lane % 4) / 2) ^ swz_v(vr)) * 16 + (lane % 2) * 8;
+    const int va = vr * (DH * 2) + ((2 * ((lane / 16) % 2) + (lane % 4) / 2) ^ swz<DH>(vr)) * 16 + (lane % 2) * 8;
     typedef f32x16 STile[kKT / 32];
     typedef bf16x8 PTile[kKT / 16];
     constexpr int kQK = kC * (kKT / 32), kPV = kDT * (kKT / 16);

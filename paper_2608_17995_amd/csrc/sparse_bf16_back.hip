@@ -32,19 +32,6 @@ __device__ __forceinline__ void each(F&& f) {
 template <int N> using Int = std::integral_constant<int, N>;
 #define AVITS_INLINE __attribute__((always_inline))
 
-constexpr float kLog2e = 1.4426950408889634f;
-
-__device__ __forceinline__ f32x16 mfma32(const bf16x8& a, const bf16x8& b, const f32x16& c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-}
-
-// Position of 16-byte chunk c of row r of an LDS tile is c ^ swz(r): reads of one chunk of 16 rows, and
-// of four chunks of four rows (the transposed ones), touch every bank once.
-template <int DH>
-__device__ __forceinline__ int swz(int r) {
-  return DH == 128 ? (r & 3) << 2 | ((r >> 2) & 3) : ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
-}
-
 // Byte address within a tile of the fragment of rows row0 + l % 32, elements 16 c + 8 (l / 32) ..
 template <int DH>
 struct Frag {
