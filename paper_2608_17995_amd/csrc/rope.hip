@@ -427,7 +427,7 @@ void plan_forward(RopeArgs& a, int d) {
 // Backward: each wave ends with a sum over its lanes and its workgroup's, so there are no more than the chip holds
 // at once, with as many (row, part) pairs each; parts of two steps of the queries and two of the keys, which
 // are under way together.
-constexpr int64_t kBackwardWaves = 3072;
+constexpr int64_t kBackwardWaves = 12 * 256;  // twelve to a CU
 void plan_backward(RopeArgs& a, int d) {
   a.parts = std::max(1, most_parts(a, d) / 2);
   if (a.M * a.parts < kBackwardWaves) a.parts = int(std::min<int64_t>(most_parts(a, d), ceil_div64(kBackwardWaves, a.M)));
